@@ -216,7 +216,7 @@ def _plain_slots(s):
     rank = (need_end - need)[:, None] + col - old[:, None]
     tables_out = torch.where(fresh, stack((count + R - 1 - rank).clamp(min=0)), tables)
     i = torch.arange(len(ids), device=dev)
-    ids_out = torch.where((i >= count) & (i < free_out), stack(i), ids)
+    ids_out = torch.where((i >= count) & (i < count + R), stack(i), ids)   # what was popped again stays above the new top
     t = torch.arange(len(s["slots"]), device=dev)
     row = torch.searchsorted(tok_end, t, right=True).clamp(max=len(ctx) - 1)
     p = ctx[row] + t - (tok_end - add)[row]
