@@ -345,6 +345,140 @@ int32_t ps_decode_attn_static(const void* kpool, const void* vpool, const void* 
                               int32_t block_size, int32_t num_gpu_blocks, int32_t kv_split_tokens,
                               int32_t* status_word, void* stream, char* err_buf, int32_t err_cap);
 
+/* ---- a decode step whose lengths stay on the device ----------------------------------------- */
+
+/* The paper has no counterpart to the calls of this section.  ps_decode_attn and ps_decode_attn_static take the
+ * context lengths from the host, and the key and value of the new token are the caller's business.  An engine that
+ * keeps its request lengths on the device (a captured step, lengths that sampling decides) needs the rest of the
+ * step there as well:
+ *
+ *   ps_build_slots   lengths -> block tables, positions and slots of the new tokens (and the free stack)
+ *   ps_rope_append   rotates queries and keys and writes keys and values to their slots
+ *   ps_paged_attn    attention of the new tokens over the pools, from the same tables and lengths
+ *
+ * None of them needs a context, allocates, synchronises or reads device memory on the host, and their launches depend
+ * on sizes only, so that a captured call may be replayed with other contents.  Everything is enqueued on `stream`
+ * (cudaStream_t) of the current device.  Argument errors are returned (PS_ERR_INVALID) before anything is enqueued,
+ * with a text in err_buf (host, err_cap bytes, or NULL).  What only the device sees is reported through status_word
+ * (device int32, or NULL), which is written on an error and left alone otherwise: 1 = ps_rope_append met a slot
+ * outside the pool (that token is not appended), 2 = a block id outside [0, num_gpu_blocks) (its tokens are skipped;
+ * ps_build_slots gives them slot -1), 4 = ps_build_slots found too few free blocks, 5 = a length out of range.
+ * The launches are programmatically dependent on the kernel before them on the stream and wait for its completion
+ * before they read or write anything, like ps_decode_attn's.
+ * Pools are [num_gpu_blocks][block_size][num_kv_heads][head_dim] as everywhere; here their blocks may lie any
+ * *_block_stride elements apart (at least a block), e.g. when one buffer holds K and V of a block side by side.  The
+ * pools of a context are a dense case of it.  Strides are counted in elements. */
+
+enum ps_dtype { PS_DTYPE_BF16 = 0, PS_DTYPE_FP16 = 1 };
+
+/* new_lens[b]: the row ends (see ps_build_slots) */
+#define PS_SLOTS_END (-1)
+
+typedef struct ps_slots_args {
+    const int32_t* ctx_lens;    /* device [batch]: tokens of every row before the call */
+    const int32_t* new_lens;    /* device [batch]: tokens that the row gets, 0 or more, or PS_SLOTS_END */
+    int32_t* block_tables;      /* device [batch][table_stride]; entries below ceil(ctx / block_size) are read, those
+                                   that the row gets are written */
+    int32_t* free_ids;          /* device [num_gpu_blocks]: free stack, top at free_count - 1; or NULL */
+    const int32_t* free_count;  /* device [1] */
+    int32_t* free_count_out;    /* device [1]; may be free_count */
+    int64_t* slots;             /* device [max_tokens]: out */
+    int32_t* positions;         /* device [max_tokens]: out, or NULL */
+    int32_t* token_start;       /* device [batch + 1]: out */
+    int32_t* ctx_lens_out;      /* device [batch]: out; may be ctx_lens */
+    int32_t* status_word;
+    int32_t batch, table_stride, block_size, num_gpu_blocks, max_tokens, reserved0;
+} ps_slots_args;
+
+/* Block tables, slots and positions of a batch's new tokens.  Row b goes from ctx_lens[b] to ctx_lens[b] + new_lens[b]
+ * tokens; its new tokens are numbered token_start[b] .. token_start[b + 1] - 1 and get
+ *   positions[t] = ctx_lens[b] + t - token_start[b],
+ *   slots[t]     = block_tables[b][positions[t] / block_size] * block_size + positions[t] % block_size.
+ * slots behind the last token (up to max_tokens) are -1, positions there 0.
+ * With a free stack the blocks that a row is short of are taken from it: first every row with PS_SLOTS_END gives its
+ * blocks back (rows in order, each table in order, every id on top of the stack) and has ctx_lens_out 0, then the
+ * growing rows take one id at a time from the top, in order.  That is what ps_kv_free of the former and ps_kv_alloc
+ * of the latter do on the host.  Ids handed out stay in free_ids' entries above the new top.  A block that several
+ * rows share must not be given back by more than one of them.
+ * Without one (free_ids NULL) the tables hold the blocks already, e.g. from ps_kv_alloc; PS_SLOTS_END only sets
+ * ctx_lens_out to 0.
+ * All or nothing: if a length is negative or does not fit into table_stride blocks, the new tokens are more than
+ * max_tokens, the stack would overflow (status 5) or lacks blocks (status 4), then tables, stack and lengths keep
+ * their contents (ctx_lens_out and free_count_out are copies), every slot is -1 and token_start is all zeros.
+ * The outputs must not overlap the inputs except as said.  Two calls that change one free stack or table must be
+ * ordered by the caller.  Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_build_slots(const ps_slots_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+enum ps_rope_flags {
+    PS_ROPE_NEIGHBOURS = 1, /* pairs are (x[2i], x[2i + 1]); default: (x[i], x[i + rot_dim / 2]) */
+    PS_ROPE_INVERSE = 2     /* turns by the negative angle: undoes a rotation, and takes its gradient back */
+};
+
+typedef struct ps_rope_args {
+    const void* q;            /* device [tokens][num_q_heads][head_dim], rows q_stride apart, or NULL */
+    const void* k;            /* device [tokens][num_kv_heads][head_dim], or NULL */
+    const void* v;            /* device, as k; needed with pools */
+    void* q_out;              /* as q; may be q itself (same stride) */
+    void* k_out;              /* as k, or NULL; may be k itself */
+    void* kpool;              /* pools the keys and values are appended to, or both NULL */
+    void* vpool;
+    const int64_t* slots;     /* device [tokens]: row of the pools, block * block_size + place; negative = padding */
+    const int32_t* positions; /* device: axis a of token t at positions[a * axis_stride + t] */
+    const float* inv_freq;    /* device [rot_dim / 2]: radians per unit of position, taken as exact */
+    const int32_t* freq_axis; /* HOST [rot_dim / 2]: the axis of every frequency, or NULL for axis 0 */
+    int32_t* status_word;
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+    int64_t k_block_stride, v_block_stride, axis_stride;
+    int32_t tokens, num_q_heads, num_kv_heads, head_dim, rot_dim, num_axes, block_size, num_gpu_blocks;
+    int32_t dtype, flags;     /* ps_dtype; OR of ps_rope_flags */
+} ps_rope_args;
+
+/* Rotary positions on q and k, and the append of the rotated k and of v to the paged pools.  For i < rot_dim / 2 the
+ * pair i of every query and key head is turned by positions[freq_axis[i]][t] * inv_freq[i]; dims from rot_dim on are
+ * copied.  With several axes (time, height, width) every frequency follows the axis that freq_axis gives it; with
+ * axis_stride 0 all axes read one row of positions (text).  rot_dim 0 only copies.  The angle is reduced in 64 bits
+ * (far positions keep their phase), values are rotated in 32 bits and rounded once.
+ * A token whose slot is negative is padding: nothing of it is written, neither its rows of q_out and k_out nor the
+ * pools.  slots NULL: every token is rotated, which needs pools NULL.  slots without pools only marks padding.  No
+ * two tokens of a call may have the same slot: which of them the pool then holds is not defined.  In training the gradient of
+ * q and k is the same call on the outputs' gradients with PS_ROPE_INVERSE added.
+ * head_dim up to 512, rot_dim even, up to 8 axes.  Rows on 16-byte boundaries with rot_dim a multiple of 16 (8 with
+ * PS_ROPE_NEIGHBOURS) and head_dim of 8 are read 16 bytes at a time, everything else element by element.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+typedef struct ps_paged_attn_args {
+    const void* kpool;           /* device pools of one layer, on 32-byte boundaries */
+    const void* vpool;
+    const void* q;               /* device [batch][num_q_heads][head_dim], rows q_stride apart, 16-byte boundaries */
+    void* out;                   /* as q, rows out_stride apart */
+    float* lse;                  /* device [batch][num_q_heads], natural log, or NULL */
+    const int32_t* block_tables; /* device [batch][table_stride] */
+    const int32_t* ctx_lens;     /* device [batch]: tokens of every row, the new one included */
+    int32_t* status_word;
+    void* workspace;             /* device, 256-byte boundary, contents do not matter before or after the call */
+    int64_t workspace_bytes;     /* at least what ps_paged_attn_workspace says */
+    int64_t k_block_stride, v_block_stride, q_stride, out_stride;
+    int32_t batch, table_stride, num_kv_heads, num_q_heads, head_dim, block_size, num_gpu_blocks;
+    int32_t window;              /* > 0: only the last `window` tokens are attended; 0: all */
+    float scale;                 /* factor on q . k; 0 = 1 / sqrt(head_dim) */
+    int32_t dtype;               /* ps_dtype of pools, q and out */
+} ps_paged_attn_args;
+
+/* Decode attention as ps_decode_attn computes it, from lengths and tables on the device:
+ *   out[b][h] = softmax_t(scale * q[b][h] . K[t][h / G]) . V[t][h / G],   max(0, ctx - window) <= t < ctx,
+ * bf16 or fp16 inputs and outputs, 32-bit scores, softmax statistics and accumulators; the softmax weights are rounded
+ * to the inputs' type for the product with V.  A row with ctx_lens 0 gives zeros (lse = -inf).  A length that is
+ * negative counts as 0, one beyond table_stride * block_size as that many (status 5).  Blocks may be shared by rows,
+ * and nothing outside the attended tokens is read into a result, whatever the pools hold there.
+ * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, any batch.
+ * One workspace serves calls in order; calls that may overlap on the device need one each.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+/* Bytes of workspace that ps_paged_attn needs on the current device for these heads, whatever the batch. */
+int32_t ps_paged_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes);
+
 /* ---- one engine step under the copy budget (Section 4.3 "Put it Together"; Alg. 1) -------- */
 
 /* In order: reaps finished offloads; turns copy_budget_bytes into blocks (floor(bytes /

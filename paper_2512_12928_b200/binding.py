@@ -24,6 +24,9 @@ PS_ERR_STATE, PS_ERR_BUSY, PS_ERR_TIMEOUT, PS_ERR_CUDA, PS_ERR_BOUNDS = -4, -5, 
 PS_REQ_NONE, PS_REQ_RESIDENT, PS_REQ_SWAPPING_OUT, PS_REQ_HOST, PS_REQ_SWAPPING_IN = 0, 1, 2, 3, 4
 PS_FLAG_BOOKKEEPING_ONLY, PS_FLAG_PROFILE, PS_FLAG_SYNC_RELOAD, PS_FLAG_ATTN_PLAIN_LAUNCH = 1, 2, 4, 8
 PS_ATTN_AUTO, PS_ATTN_SIMT, PS_ATTN_MMA, PS_ATTN_MMA_ROWS = 0, 1, 2, 3
+PS_DTYPE_BF16, PS_DTYPE_FP16 = 0, 1
+PS_SLOTS_END = -1
+PS_ROPE_NEIGHBOURS, PS_ROPE_INVERSE = 1, 2
 
 EXPORTS = [
     "ps_create", "ps_destroy", "ps_last_error", "ps_kv_alloc", "ps_kv_free", "ps_block_table",
@@ -33,6 +36,7 @@ EXPORTS = [
     "ps_decode_attn_static", "ps_copy_budget", "ps_offload_progress", "ps_host_blocks", "ps_host_segment",
     "ps_select_victims", "ps_copy_condition", "ps_order_queue", "ps_estimate_batch", "ps_resume_cost",
     "ps_reload_fence", "ps_offload_sweep", "ps_step_ruled", "ps_step_host", "ps_inject_status", "ps_hbm_probe", "ps_reload_backlog",
+    "ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace",
 ]
 
 
@@ -93,6 +97,30 @@ class PsLatencyModel(C.Structure):
 
 class PsTraceSpan(C.Structure):
     _fields_ = [("kind", C.c_int32), ("tag", C.c_int32), ("start_us", C.c_float), ("end_us", C.c_float)]
+
+
+def _fields(pointers: str, i64s: str, i32s: str):
+    return ([(n, C.c_void_p) for n in pointers.split()] + [(n, C.c_int64) for n in i64s.split()]
+            + [(n, C.c_int32) for n in i32s.split()])
+
+
+class PsSlotsArgs(C.Structure):
+    _fields_ = _fields("ctx_lens new_lens block_tables free_ids free_count free_count_out slots positions token_start "
+                       "ctx_lens_out status_word", "",
+                       "batch table_stride block_size num_gpu_blocks max_tokens reserved0")
+
+
+class PsRopeArgs(C.Structure):
+    _fields_ = _fields("q k v q_out k_out kpool vpool slots positions inv_freq freq_axis status_word",
+                       "q_stride k_stride v_stride q_out_stride k_out_stride k_block_stride v_block_stride axis_stride",
+                       "tokens num_q_heads num_kv_heads head_dim rot_dim num_axes block_size num_gpu_blocks dtype flags")
+
+
+class PsPagedAttnArgs(C.Structure):
+    _fields_ = (_fields("kpool vpool q out lse block_tables ctx_lens status_word workspace",
+                        "workspace_bytes k_block_stride v_block_stride q_stride out_stride",
+                        "batch table_stride num_kv_heads num_q_heads head_dim block_size num_gpu_blocks window")
+                + [("scale", C.c_float), ("dtype", C.c_int32)])
 
 
 TRACE_KINDS = ["attn", "merge", "gather", "scatter", "d2h", "h2d"]
@@ -163,6 +191,10 @@ def load() -> C.CDLL:
                                  C.POINTER(C.c_double)]),
         "ps_decode_attn_static": (i32, [vp, vp, vp, vp, vp, vp, i32, p32, i32, i32, i32, i32, i32, i32, i32, vp, vp,
                                         C.c_char_p, i32]),
+        "ps_build_slots": (i32, [C.POINTER(PsSlotsArgs), vp, C.c_char_p, i32]),
+        "ps_rope_append": (i32, [C.POINTER(PsRopeArgs), vp, C.c_char_p, i32]),
+        "ps_paged_attn": (i32, [C.POINTER(PsPagedAttnArgs), vp, C.c_char_p, i32]),
+        "ps_paged_attn_workspace": (i32, [i32, i32, i32, p64]),
     }
     for name, (res, args) in proto.items():
         fn = getattr(lib, name)
@@ -214,6 +246,224 @@ def ps_decode_attn_static(kpool, vpool, q, out, block_tables, ctx_lens: Sequence
                                       arr, batch, num_kv_heads, num_q_heads, head_dim, block_size, num_gpu_blocks,
                                       kv_split_tokens, ptr(status_word), C.c_void_p(stream or None), err, 512)
     return rc, err.value.decode()
+
+
+# ---- a decode step whose lengths stay on the device ------------------------------------------------
+#
+# Shapes, types and strides are taken from the tensors and checked here, since the library sees addresses only; what
+# does not fit comes back as (PS_ERR_INVALID, text), as from the library.  Work is enqueued on torch's current stream
+# of the tensors' device.
+
+class _BadArg(Exception):
+    pass
+
+
+def _need(ok, text: str):
+    if not ok:
+        raise _BadArg(text)
+
+
+def _vec(name: str, t, dtype, least: int, dev: int) -> int:
+    """Address of a contiguous device tensor of dtype with at least `least` elements."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev or t.numel() < least:
+        raise _BadArg(f"{name}: need a contiguous {dtype} tensor of at least {least} elements on device {dev}, "
+                      f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(name: str, t, shape, dtype, dev: int) -> int:
+    """Row stride of [rows][heads][dim] whose rows are dense; the tensor's address is t.data_ptr()."""
+    st = t.stride()
+    if (t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != dev or (shape[2] > 1 and st[2] != 1)
+            or (shape[1] > 1 and st[1] != shape[2])):
+        raise _BadArg(f"{name}: need {dtype} {shape} with dense rows on device {dev}, got {t.dtype} {tuple(t.shape)} "
+                      f"strides {st} on {t.device}")
+    return st[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _pool(name: str, t, shape, dtype, dev: int) -> int:
+    """Block stride of a pool [blocks][block_size][heads][dim] whose blocks are dense."""
+    st = t.stride()
+    _, s, h, d = shape
+    if (t.dtype is not dtype or tuple(t.shape) != tuple(shape) or t.get_device() != dev or (d > 1 and st[3] != 1)
+            or (h > 1 and st[2] != d) or (s > 1 and st[1] != h * d)):
+        raise _BadArg(f"{name}: need a {dtype} pool {tuple(shape)} with dense blocks on device {dev}, got {t.dtype} "
+                      f"{tuple(t.shape)} strides {st} on {t.device}")
+    return st[0] if shape[0] > 1 else s * h * d
+
+
+def _enqueue(fn, args, dev: int):
+    import torch
+    err = C.create_string_buffer(256)
+    if torch.cuda.current_device() == dev:
+        rc = fn(C.byref(args), torch.cuda.current_stream(dev).cuda_stream, err, 256)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(C.byref(args), torch.cuda.current_stream(dev).cuda_stream, err, 256)
+    return rc, (err.value.decode() if rc else "")
+
+
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return PS_DTYPE_BF16
+    _need(t.dtype is torch.float16, f"need bfloat16 or float16 tensors, got {t.dtype}")
+    return PS_DTYPE_FP16
+
+
+def ps_build_slots(ctx_lens, new_lens, block_tables, slots, positions, token_start, ctx_lens_out, *, block_size: int,
+                   num_gpu_blocks: int, free_ids=None, free_count=None, free_count_out=None, status_word=None):
+    """Block tables, slots and positions of a batch's new tokens, from lengths on the device: (status, error text).
+
+    ctx_lens, new_lens, ctx_lens_out int32 [batch]; block_tables int32 [batch][stride], grown in place; slots int64
+    [max_tokens]; positions int32 [max_tokens] or None; token_start int32 [batch + 1]; free_ids int32 [num_gpu_blocks]
+    with free_count and free_count_out int32 [1], or None when the tables hold the blocks already.  ctx_lens_out may
+    be ctx_lens and free_count_out may be free_count.  See ps_build_slots in the header."""
+    import torch
+    i32 = torch.int32
+    try:
+        dev, batch, room = slots.get_device(), ctx_lens.numel(), slots.numel()
+        _need(dev >= 0, "slots: not a device tensor")
+        _need(block_tables.dim() == 2 and block_tables.shape[1] > 0, "block_tables: need [batch][stride]")
+        stride = block_tables.shape[1]
+        args = PsSlotsArgs(
+            _vec("ctx_lens", ctx_lens, i32, batch, dev), _vec("new_lens", new_lens, i32, batch, dev),
+            _vec("block_tables", block_tables, i32, batch * stride, dev),
+            None if free_ids is None else _vec("free_ids", free_ids, i32, num_gpu_blocks, dev),
+            None if free_count is None else _vec("free_count", free_count, i32, 1, dev),
+            None if free_count_out is None else _vec("free_count_out", free_count_out, i32, 1, dev),
+            _vec("slots", slots, torch.int64, 0, dev),
+            None if positions is None else _vec("positions", positions, i32, room, dev),
+            _vec("token_start", token_start, i32, batch + 1, dev), _vec("ctx_lens_out", ctx_lens_out, i32, batch, dev),
+            None if status_word is None else _vec("status_word", status_word, i32, 1, dev),
+            batch, stride, block_size, num_gpu_blocks, room, 0)
+    except _BadArg as e:
+        return PS_ERR_INVALID, f"ps_build_slots: {e}"
+    return _enqueue(load().ps_build_slots, args, dev)
+
+
+def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=None, vpool=None, slots=None, freq_axis=None,
+                   neighbours: bool = False, inverse: bool = False, status_word=None):
+    """Rotary positions on q and k and the append of k and v to the paged pools: (status, error text).
+
+    q, q_out [tokens][q heads][dim], k, v, k_out [tokens][kv heads][dim] (any of q, k, k_out may be None; q_out may be
+    q, k_out may be k; rows may be strided); positions int32 [tokens] or [axes][tokens] (an axis stride of 0 is fine);
+    inv_freq float32 [rot_dim / 2], or None for no rotation; freq_axis: the axis of every frequency, or None for axis
+    0; kpool, vpool [blocks][block_size][kv heads][dim] with slots int64 [tokens].  See ps_rope_append in the header."""
+    import torch
+    i32 = torch.int32
+    try:
+        ref = q if q is not None else k
+        _need(ref is not None and ref.dim() == 3 and ref.get_device() >= 0, "need q or k, a device tensor [tokens][heads][dim]")
+        dev, dt, T, D = ref.get_device(), ref.dtype, ref.shape[0], ref.shape[2]
+        code = _dtype_code(ref)
+        hq, hkv = (0 if q is None else q.shape[1]), 0
+        q_st = qo_st = k_st = v_st = ko_st = kb = vb = ax_st = 0
+        if q is not None:
+            q_st = _rows("q", q, (T, hq, D), dt, dev)
+            _need(q_out is not None, "q needs q_out")
+            qo_st = _rows("q_out", q_out, (T, hq, D), dt, dev)
+            _need(T < 2 or qo_st >= hq * D, "q_out: rows overlap")
+        if k is not None:
+            _need(k.dim() == 3, "k: need [tokens][heads][dim]")
+            hkv = k.shape[1]
+            k_st = _rows("k", k, (T, hkv, D), dt, dev)
+            if k_out is not None:
+                ko_st = _rows("k_out", k_out, (T, hkv, D), dt, dev)
+                _need(T < 2 or ko_st >= hkv * D, "k_out: rows overlap")
+        else:
+            _need(k_out is None and kpool is None, "k_out and pools need k")
+        nb = bs = 0
+        if kpool is not None or vpool is not None:
+            _need(kpool is not None and vpool is not None and v is not None and slots is not None,
+                  "an append needs k, v, both pools and slots")
+            _need(kpool.dim() == 4, "kpool: need [blocks][block_size][heads][dim]")
+            nb, bs = kpool.shape[0], kpool.shape[1]
+            kb = _pool("kpool", kpool, (nb, bs, hkv, D), dt, dev)
+            vb = _pool("vpool", vpool, (nb, bs, hkv, D), dt, dev)
+            v_st = _rows("v", v, (T, hkv, D), dt, dev)
+        half = axes = 0
+        if inv_freq is not None:
+            half = inv_freq.numel()
+            _need(positions is not None and positions.dim() in (1, 2) and positions.dtype is i32
+                  and positions.get_device() == dev and positions.shape[-1] == T and (T < 2 or positions.stride(-1) == 1),
+                  "positions: need int32 [tokens] or [axes][tokens] on the tensors' device")
+            axes = 1 if positions.dim() == 1 else positions.shape[0]
+            ax_st = 0 if axes == 1 else positions.stride(0)
+            _need(freq_axis is None or len(freq_axis) == half, "freq_axis: need one axis per frequency")
+        args = PsRopeArgs(
+            None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
+            None if kpool is None else v.data_ptr(), None if q is None else q_out.data_ptr(),
+            None if k_out is None else k_out.data_ptr(), None if kpool is None else kpool.data_ptr(),
+            None if kpool is None else vpool.data_ptr(),
+            None if slots is None else _vec("slots", slots, torch.int64, T, dev),
+            positions.data_ptr() if half else None,
+            _vec("inv_freq", inv_freq, torch.float32, half, dev) if half else None,
+            C.cast((C.c_int32 * half)(*freq_axis), C.c_void_p) if half and freq_axis is not None else None,
+            None if status_word is None else _vec("status_word", status_word, i32, 1, dev),
+            q_st, k_st, v_st, qo_st, ko_st, kb, vb, ax_st,
+            T, hq, hkv, D, 2 * half, axes, bs, nb, code,
+            (PS_ROPE_NEIGHBOURS if neighbours else 0) | (PS_ROPE_INVERSE if inverse else 0))
+    except _BadArg as e:
+        return PS_ERR_INVALID, f"ps_rope_append: {e}"
+    return _enqueue(load().ps_rope_append, args, dev)
+
+
+_workspace_bytes = {}
+
+
+def ps_paged_attn_workspace(num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int] = None) -> int:
+    """Bytes of workspace that ps_paged_attn needs for these heads on a device (default: the current one)."""
+    import torch
+    dev = torch.cuda.current_device() if device is None else device
+    key = (dev, num_kv_heads, num_q_heads, head_dim)
+    n = _workspace_bytes.get(key)
+    if n is None:
+        out = C.c_int64()
+        with torch.cuda.device(dev):
+            rc = load().ps_paged_attn_workspace(num_kv_heads, num_q_heads, head_dim, C.byref(out))
+        if rc != PS_OK:
+            raise PsError(rc, "ps_paged_attn_workspace", "unsupported heads, or no device")
+        n = _workspace_bytes[key] = out.value
+    return n
+
+
+def ps_paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, *, lse=None, window: int = 0, scale: Optional[float] = None,
+                  status_word=None, workspace=None):
+    """Decode attention from lengths and block tables on the device: (status, error text).
+
+    kpool, vpool [blocks][block_size][kv heads][dim], blocks may be strided; q, out [batch][q heads][dim], rows may be
+    strided; block_tables int32 [at least batch][stride]; ctx_lens int32 [batch]; lse float32 [batch][q heads] or
+    None; scale None = 1 / sqrt(dim).  workspace: a uint8 tensor of ps_paged_attn_workspace bytes; by default one is
+    taken from torch's allocator on the current stream for the duration of the call.  See ps_paged_attn in the header."""
+    import torch
+    try:
+        _need(q.dim() == 3 and q.get_device() >= 0, "q: need a device tensor [batch][heads][dim]")
+        dev, dt, (batch, hq, D) = q.get_device(), q.dtype, q.shape
+        code = _dtype_code(q)
+        _need(kpool.dim() == 4 and block_tables.dim() == 2, "need kpool [blocks][block_size][heads][dim] and block_tables [batch][stride]")
+        nb, bs, hkv, _ = kpool.shape
+        kb = _pool("kpool", kpool, (nb, bs, hkv, D), dt, dev)
+        vb = _pool("vpool", vpool, (nb, bs, hkv, D), dt, dev)
+        q_st, o_st = _rows("q", q, (batch, hq, D), dt, dev), _rows("out", out, (batch, hq, D), dt, dev)
+        stride = block_tables.shape[1]
+        _need(hkv > 0 and D in (64, 128) and hq > 0 and hq % hkv == 0 and hq // hkv <= 64 and hkv <= 1024,
+              "head_dim must be 64 or 128, with 1 to 64 query heads per KV head")
+        need = ps_paged_attn_workspace(hkv, hq, D, dev)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _need(scale is None or scale != 0, "scale: 0 is not a factor")
+        args = PsPagedAttnArgs(
+            kpool.data_ptr(), vpool.data_ptr(), q.data_ptr(), out.data_ptr(),
+            None if lse is None else _vec("lse", lse, torch.float32, batch * hq, dev),
+            _vec("block_tables", block_tables, torch.int32, batch * stride, dev),
+            _vec("ctx_lens", ctx_lens, torch.int32, batch, dev),
+            None if status_word is None else _vec("status_word", status_word, torch.int32, 1, dev),
+            _vec("workspace", workspace, torch.uint8, need, dev), workspace.numel(), kb, vb, q_st, o_st,
+            batch, stride, hkv, hq, D, bs, nb, window, scale or 0.0, code)
+    except _BadArg as e:
+        return PS_ERR_INVALID, f"ps_paged_attn: {e}"
+    return _enqueue(load().ps_paged_attn, args, dev)
 
 
 def ps_order_queue(exec_us, remain_us, weight, *, eta: float, gamma: float, t_c: float, waited_us=None, tau: float = 0.0):

@@ -3,8 +3,39 @@
 
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <stdio.h>
 
 namespace ps {
+
+// ---- entry points without a context: error text, launches ---------------------------------------
+
+inline int32_t arg_fail(char* err_buf, int32_t err_cap, int32_t code, const char* msg) {
+    if (err_buf && err_cap > 0) snprintf(err_buf, (size_t)err_cap, "%s", msg);
+    return code;
+}
+
+inline int32_t launch_fail(char* err_buf, int32_t err_cap, const char* where, cudaError_t e) {
+    cudaGetLastError();
+    if (err_buf && err_cap > 0) snprintf(err_buf, (size_t)err_cap, "%s: %s", where, cudaGetErrorString(e));
+    return -7;   // PS_ERR_CUDA
+}
+
+// A launch that may be scheduled and set up under the tail of the kernel before it on the stream.  The kernel has to
+// execute griddepcontrol.wait, in every thread, before it touches memory.
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 
 // ---- block gather / scatter (swap-out and swap-in kernels) -----------------------------------
 

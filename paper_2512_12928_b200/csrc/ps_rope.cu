@@ -1,0 +1,314 @@
+// ps_rope_append: rotary positions with several axes on queries and keys, and the append of keys and values to the
+// paged pools.
+//
+//   angle_i = positions[axis_i][t] * inv_freq_i,   i < R / 2
+//   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin)      PS_ROPE_INVERSE turns by -angle: the transpose, the gradient
+//
+// on the pairs (x_i, x_{i + R/2}), or (x_{2i}, x_{2i+1}) with PS_ROPE_NEIGHBOURS; dims from R on pass unchanged.
+//
+// Bound: memory (every element is read once and written once, 3 flops for 4 bytes).  So the rotation shares its pass
+// with the append: the rotated key goes from registers into its slot of the pool instead of to memory and back.
+//
+// Angles: a position of 10^6 times a frequency of 1 in 32 bits is off by up to 0.03 radians, so the product and its
+// reduction to a fraction of a turn are done in 64 bits, once per token and frequency, and sine and cosine (of the
+// fraction, 32 bits) are kept in shared memory for all heads of the token.
+//
+// Inputs are rotated in 32 bits and rounded once, at the store.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ps_internal.h"
+#include "ps_kvswap.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxHeadDim = 512;
+constexpr int kTokensPerCta = 4;      // most tokens whose sines a CTA keeps: 4 * 256 * 8 bytes
+constexpr int kStatusBadSlot = 1;
+
+struct FreqAxes {
+    uint8_t v[kMaxHeadDim / 2];
+};
+
+struct RopeParams {
+    const void *q, *k, *v;
+    void *q_out, *k_out, *kpool, *vpool;
+    const int64_t* slots;
+    const int32_t* positions;
+    const float* inv_freq;
+    int32_t* status;
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, axis_stride, k_block_stride, v_block_stride;
+    int64_t num_slots;
+    int32_t tokens, hq, hkv, dim, rot, block_size, tok_per_cta;
+    float sign;
+};
+
+struct TokenPlace {   // of one token of the CTA
+    int64_t k_off, v_off;   // element offset of its row in the pools; -1: not appended
+    int32_t live;           // 0: padding, nothing of it is written
+    int32_t pad;
+};
+
+template <typename T> __device__ __forceinline__ float to_f(T x);
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f(float x) { return __float2half_rn(x); }
+
+template <typename T>
+struct alignas(16) Vec8 {
+    T e[8];
+};
+template <typename T>
+__device__ __forceinline__ Vec8<T> ld8(const T* p) {
+    Vec8<T> r;
+    *reinterpret_cast<uint4*>(&r) = *reinterpret_cast<const uint4*>(p);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void st8(T* p, const Vec8<T>& v) {
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&v);
+}
+
+// Places and sines of the CTA's tokens.
+__device__ __forceinline__ void token_setup(const RopeParams& p, const FreqAxes& axes, int32_t t0, int n, float2* cs,
+                                            TokenPlace* place) {
+    const int half = p.rot >> 1;
+    for (int i = threadIdx.x; i < n * half; i += kThreads) {
+        const int k = i / half, f = i - k * half;
+        const double turns = (double)p.positions[axes.v[f] * p.axis_stride + t0 + k] * (double)p.inv_freq[f] *
+                             0.15915494309189533577;   // 1 / (2 pi)
+        const float frac = (float)(turns - rint(turns));
+        float s, c;
+        sincospif(2.0f * frac, &s, &c);
+        cs[k * half + f] = make_float2(c, p.sign * s);
+    }
+    for (int k = threadIdx.x; k < n; k += kThreads) {
+        TokenPlace pl{-1, -1, 1, 0};
+        if (p.slots != nullptr) {
+            const int64_t slot = p.slots[t0 + k];
+            if (slot < 0) {
+                pl.live = 0;
+            } else if (slot >= p.num_slots) {
+                if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+            } else if (p.kpool != nullptr) {
+                const int64_t blk = slot / p.block_size;
+                const int64_t in_block = (slot - blk * p.block_size) * (int64_t)p.hkv * p.dim;
+                pl.k_off = blk * p.k_block_stride + in_block;
+                pl.v_off = blk * p.v_block_stride + in_block;
+            }
+        }
+        place[k] = pl;
+    }
+}
+
+// Where head `head` of a token is read and written: heads 0 .. hq-1 are queries, then keys, then values.
+template <typename T>
+struct HeadAt {
+    const T* src;
+    T *dst, *dst2;   // dst2: a key that goes to k_out and into the pool
+    bool rotate;
+};
+template <typename T>
+__device__ __forceinline__ HeadAt<T> head_at(const RopeParams& p, int64_t t, int head, const TokenPlace& pl) {
+    HeadAt<T> h{nullptr, nullptr, nullptr, true};
+    if (head < p.hq) {
+        h.src = (const T*)p.q + t * p.q_stride + (int64_t)head * p.dim;
+        h.dst = (T*)p.q_out + t * p.q_out_stride + (int64_t)head * p.dim;
+    } else if (head < p.hq + p.hkv) {
+        const int64_t o = (int64_t)(head - p.hq) * p.dim;
+        h.src = (const T*)p.k + t * p.k_stride + o;
+        if (p.k_out) h.dst = (T*)p.k_out + t * p.k_out_stride + o;
+        if (pl.k_off >= 0) (h.dst ? h.dst2 : h.dst) = (T*)p.kpool + pl.k_off + o;
+    } else {
+        const int64_t o = (int64_t)(head - p.hq - p.hkv) * p.dim;
+        h.rotate = false;
+        h.src = (const T*)p.v + t * p.v_stride + o;
+        if (pl.v_off >= 0) h.dst = (T*)p.vpool + pl.v_off + o;
+    }
+    if (!pl.live) h.dst = h.dst2 = nullptr;
+    return h;
+}
+
+// 16 bytes per access: every address and row is 16-byte aligned, and a pair's partners lie in whole vectors.
+// A head is worked on by `lanes` neighbouring threads (a power of two).
+template <typename T, bool kNeighbours>
+__global__ void __launch_bounds__(kThreads)
+rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads,
+                   int32_t lanes_log2) {
+    extern __shared__ float2 cs[];
+    __shared__ TokenPlace place[kTokensPerCta];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t t0 = blockIdx.x * p.tok_per_cta;
+    const int n = min(p.tok_per_cta, p.tokens - t0);
+    token_setup(p, axes, t0, n, cs, place);
+    __syncthreads();
+    const int half = p.rot >> 1;
+    const int lane = threadIdx.x & ((1 << lanes_log2) - 1);
+    const int vecs = p.dim >> 3;
+    const int pair_vecs = kNeighbours ? p.rot >> 3 : half >> 3;   // units of the rotated part
+    for (int u = threadIdx.x >> lanes_log2; u < n * heads; u += kThreads >> lanes_log2) {
+        const int k = u / heads, head = u - k * heads;
+        const HeadAt<T> h = head_at<T>(p, t0 + k, head, place[k]);
+        if (!h.dst) continue;
+        int first = 0;
+        if (h.rotate) {
+            const float2* c = cs + k * half;
+            for (int i = lane; i < pair_vecs; i += 1 << lanes_log2) {
+                if (kNeighbours) {
+                    Vec8<T> x = ld8(h.src + 8 * i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 w = c[4 * i + j];
+                        const float x1 = to_f(x.e[2 * j]), x2 = to_f(x.e[2 * j + 1]);
+                        x.e[2 * j] = from_f<T>(fmaf(x1, w.x, -x2 * w.y));
+                        x.e[2 * j + 1] = from_f<T>(fmaf(x2, w.x, x1 * w.y));
+                    }
+                    st8(h.dst + 8 * i, x);
+                    if (h.dst2) st8(h.dst2 + 8 * i, x);
+                } else {
+                    Vec8<T> a = ld8(h.src + 8 * i), b = ld8(h.src + half + 8 * i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2 w = c[8 * i + j];
+                        const float x1 = to_f(a.e[j]), x2 = to_f(b.e[j]);
+                        a.e[j] = from_f<T>(fmaf(x1, w.x, -x2 * w.y));
+                        b.e[j] = from_f<T>(fmaf(x2, w.x, x1 * w.y));
+                    }
+                    st8(h.dst + 8 * i, a);
+                    st8(h.dst + half + 8 * i, b);
+                    if (h.dst2) {
+                        st8(h.dst2 + 8 * i, a);
+                        st8(h.dst2 + half + 8 * i, b);
+                    }
+                }
+            }
+            first = p.rot >> 3;
+        }
+        for (int i = first + lane; i < vecs; i += 1 << lanes_log2) {
+            const Vec8<T> x = ld8(h.src + 8 * i);
+            if (h.dst != h.src) st8(h.dst + 8 * i, x);
+            if (h.dst2) st8(h.dst2 + 8 * i, x);
+        }
+    }
+}
+
+// Element by element, for rows or pairs that are not on 16-byte boundaries.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads,
+                            bool neighbours) {
+    extern __shared__ float2 cs[];
+    __shared__ TokenPlace place[kTokensPerCta];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t t0 = blockIdx.x * p.tok_per_cta;
+    const int n = min(p.tok_per_cta, p.tokens - t0);
+    token_setup(p, axes, t0, n, cs, place);
+    __syncthreads();
+    const int half = p.rot >> 1;
+    const int units = p.dim - half;   // of a rotated head: its pairs, then the dims that pass
+    for (int u = threadIdx.x >> 5; u < n * heads; u += kThreads >> 5) {
+        const int k = u / heads, head = u - k * heads;
+        const HeadAt<T> h = head_at<T>(p, t0 + k, head, place[k]);
+        if (!h.dst) continue;
+        for (int i = threadIdx.x & 31; i < (h.rotate ? units : p.dim); i += 32) {
+            if (h.rotate && i < half) {
+                const float2 w = cs[k * half + i];
+                const int d1 = neighbours ? 2 * i : i, d2 = neighbours ? 2 * i + 1 : i + half;
+                const float x1 = to_f(h.src[d1]), x2 = to_f(h.src[d2]);
+                const T y1 = from_f<T>(fmaf(x1, w.x, -x2 * w.y)), y2 = from_f<T>(fmaf(x2, w.x, x1 * w.y));
+                h.dst[d1] = y1;
+                h.dst[d2] = y2;
+                if (h.dst2) {
+                    h.dst2[d1] = y1;
+                    h.dst2[d2] = y2;
+                }
+            } else {
+                const int d = h.rotate ? i + half : i;
+                const T x = h.src[d];
+                h.dst[d] = x;
+                if (h.dst2) h.dst2[d] = x;
+            }
+        }
+    }
+}
+
+bool on16(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
+
+template <typename T>
+cudaError_t launch_rope(const RopeParams& p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
+    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
+    const size_t smem = (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2);
+    if (!vec) return ps::launch_dependent(rope_append_elements_kernel<T>, grid, dim3(kThreads), smem, s, p, axes, heads, neighbours);
+    // threads per head: one per unit of the longer of "pairs" and "all vectors of a value head / 2"
+    const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
+    int log2 = 0;
+    while ((1 << log2) < units && log2 < 5) ++log2;
+    return neighbours ? ps::launch_dependent(rope_append_kernel<T, true>, grid, dim3(kThreads), smem, s, p, axes, heads, log2)
+                      : ps::launch_dependent(rope_append_kernel<T, false>, grid, dim3(kThreads), smem, s, p, axes, heads, log2);
+}
+
+}  // namespace
+
+extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* err_buf, int32_t err_cap) {
+    using ps::arg_fail;
+    if (err_buf && err_cap > 0) err_buf[0] = 0;
+    auto bad = [&](const char* m) { return arg_fail(err_buf, err_cap, PS_ERR_INVALID, m); };
+    if (!args) return bad("ps_rope_append: null arguments");
+    const ps_rope_args a = *args;
+    if (a.tokens < 0 || a.num_q_heads < 0 || a.num_kv_heads < 0 || a.head_dim <= 0 || a.rot_dim < 0 || a.num_axes < 0)
+        return bad("ps_rope_append: negative count or non-positive size");
+    if (a.head_dim > kMaxHeadDim || a.rot_dim > a.head_dim || a.rot_dim % 2)
+        return bad("ps_rope_append: head_dim is at most 512, rot_dim an even number up to head_dim");
+    if (a.dtype != PS_DTYPE_BF16 && a.dtype != PS_DTYPE_FP16) return bad("ps_rope_append: dtype must be PS_DTYPE_BF16 or PS_DTYPE_FP16");
+    if (a.flags & ~(PS_ROPE_NEIGHBOURS | PS_ROPE_INVERSE)) return bad("ps_rope_append: unknown flag");
+    const bool append = a.kpool || a.vpool;
+    const bool do_q = a.q != nullptr && a.num_q_heads > 0, do_k = a.k != nullptr && a.num_kv_heads > 0;
+    if (do_q && !a.q_out) return bad("ps_rope_append: q without q_out");
+    if (append && (!a.kpool || !a.vpool || !a.k || !a.v || !a.slots || a.num_kv_heads == 0))
+        return bad("ps_rope_append: an append needs k, v, both pools and slots");
+    if (append && (a.block_size <= 0 || a.num_gpu_blocks <= 0)) return bad("ps_rope_append: non-positive block size or pool");
+    const int64_t block_elems = append ? (int64_t)a.block_size * a.num_kv_heads * a.head_dim : 0;
+    if (append && ((a.num_gpu_blocks > 1 && (a.k_block_stride < block_elems || a.v_block_stride < block_elems))))
+        return bad("ps_rope_append: a pool's block stride is smaller than a block");
+    if (do_k && !append && !a.k_out) return bad("ps_rope_append: k without k_out or pools");
+    FreqAxes axes{};
+    if (a.rot_dim > 0) {
+        if (!a.inv_freq || a.num_axes < 1 || a.num_axes > 8) return bad("ps_rope_append: a rotation needs positions, inv_freq and 1 to 8 axes");
+        if (a.freq_axis)
+            for (int i = 0; i < a.rot_dim / 2; ++i) {
+                if (a.freq_axis[i] < 0 || a.freq_axis[i] >= a.num_axes) return bad("ps_rope_append: freq_axis names an axis that is not there");
+                axes.v[i] = (uint8_t)a.freq_axis[i];
+            }
+    }
+    if (a.tokens == 0 || (!do_q && !do_k)) return PS_OK;
+    if (a.rot_dim > 0 && !a.positions) return bad("ps_rope_append: a rotation needs positions, inv_freq and 1 to 8 axes");
+    RopeParams p{};
+    p.q = a.q, p.k = a.k, p.v = a.v, p.q_out = a.q_out, p.k_out = a.k_out, p.kpool = a.kpool, p.vpool = a.vpool;
+    p.slots = a.slots, p.positions = a.positions, p.inv_freq = a.inv_freq, p.status = a.status_word;
+    p.q_stride = a.q_stride, p.k_stride = a.k_stride, p.v_stride = a.v_stride;
+    p.q_out_stride = a.q_out_stride, p.k_out_stride = a.k_out_stride, p.axis_stride = a.axis_stride;
+    p.k_block_stride = a.k_block_stride, p.v_block_stride = a.v_block_stride;
+    p.tokens = a.tokens, p.dim = a.head_dim, p.rot = a.rot_dim, p.block_size = append ? a.block_size : 1;
+    p.hq = do_q ? a.num_q_heads : 0;
+    p.hkv = do_k ? a.num_kv_heads : 0;
+    // slots without pools only mark the padding: none of them is out of range
+    p.num_slots = append ? (int64_t)a.num_gpu_blocks * a.block_size : INT64_MAX;
+    p.sign = a.flags & PS_ROPE_INVERSE ? -1.f : 1.f;
+    const int32_t heads = p.hq + p.hkv + (append ? p.hkv : 0);
+    const bool neighbours = a.flags & PS_ROPE_NEIGHBOURS;
+    bool vec = a.head_dim % 8 == 0 && a.rot_dim % (neighbours ? 8 : 16) == 0;
+    if (do_q) vec = vec && on16(a.q, a.q_stride) && on16(a.q_out, a.q_out_stride);
+    if (do_k) vec = vec && on16(a.k, a.k_stride) && on16(a.k_out, a.k_out ? a.k_out_stride : 0);
+    if (append) vec = vec && on16(a.v, a.v_stride) && on16(a.kpool, a.k_block_stride) && on16(a.vpool, a.v_block_stride);
+    // few tokens: one per CTA, so that they spread over the chip; many: several, which share the barrier's wait
+    p.tok_per_cta = a.tokens <= 1024 ? 1 : kTokensPerCta;
+    cudaError_t e = a.dtype == PS_DTYPE_BF16 ? launch_rope<__nv_bfloat16>(p, axes, heads, neighbours, vec, (cudaStream_t)stream)
+                                             : launch_rope<__half>(p, axes, heads, neighbours, vec, (cudaStream_t)stream);
+    if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_rope_append", e);
+    return PS_OK;
+}
