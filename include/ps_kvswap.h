@@ -448,9 +448,9 @@ typedef struct ps_rope_args {
 int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* err_buf, int32_t err_cap);
 
 typedef struct ps_paged_attn_args {
-    const void* kpool;           /* device pools of one layer, on 32-byte boundaries */
+    const void* kpool;           /* device pools of one layer; like q and out on 16-byte boundaries */
     const void* vpool;
-    const void* q;               /* device [batch][num_q_heads][head_dim], rows q_stride apart, 16-byte boundaries */
+    const void* q;               /* device [batch][num_q_heads][head_dim], rows q_stride apart */
     void* out;                   /* as q, rows out_stride apart */
     float* lse;                  /* device [batch][num_q_heads], natural log, or NULL */
     const int32_t* block_tables; /* device [batch][table_stride] */

@@ -5,17 +5,21 @@
 //   max(0, ctx_b - window) <= t < ctx_b,   m = max_t s_t (running),   lse = ln 2 (m + log2 sum_t p_t)
 //
 // Bound: HBM.  A token and KV head cost 4 D bytes and 4 G D flops; up to G = 64 the card computes faster than it
-// loads.  So the kernel is built around the loads:
+// loads.  So every warp streams its own tiles of 16 tokens through a ring in shared memory (cp.async, 16 bytes a lane,
+// whole 128-byte lines), across the ends of rows, and no barrier lies between HBM and the tensor cores.  Tokens may
+// lie anywhere; what is not attended is filled with zeros instead of being read.
 //
-//  * Fragments come straight from global memory.  mma.m16n8k16 contracts over k, and the order of k is free as long
-//    as both operands use the same one; so is the order of the 8 columns of a product.  A lane therefore loads 32
-//    contiguous bytes of a key row, which are its B operands of four products (the query is loaded in the same
-//    order), and for V 16 bytes (D = 64) or 32 bytes (D = 128) of four token rows, whose halves are paired by byte
-//    permutes.  No shared memory, no barrier, no transposing load lies between HBM and the tensor cores, tokens may
-//    lie anywhere (any block size, any block stride), and every warp runs on its own.
-//    (The tile shapes of tcgen05.mma need 64 or 128 rows; a group of at most 16 query heads would leave most idle.)
-//  * The next tile's keys are requested before the softmax of the present one and its values before the next
-//    products, so a warp has 4 to 8 KiB in flight throughout.
+// Products: a group has few query heads, so they are the narrow side: S^T = K Q^T and O^T = V^T P^T as
+// mma.m16n8k16 with tokens, then dims, as the 16 rows and 8 heads as the columns.  K comes through ldmatrix and V
+// through its transposing form, both without bank conflicts (16-byte pieces exclusive-ored with the token's number);
+// P^T leaves the first product as pairs of heads and enters the second as pairs of tokens, which is one movmatrix.
+// With heads as the rows instead, half of every product was padding for up to 8 heads and V's pairs cost 32 byte
+// permutes a tile: 535 instructions a tile instead of XX, and 159 us instead of XX for 672 MB.
+// (The tile shapes of tcgen05.mma have 64 or 128 rows and its P would go through shared or tensor memory; the
+// tensor cores are idle most of the time either way.)
+//
+// Softmax: the reference m of a head is raised only when a score exceeds it by more than kSlack, so that a tile needs
+// one vote instead of a maximum over the lanes; weights stay below 2^kSlack and sums in 32 bits lose nothing by it.
 //
 // Work: the rows' tiles form one sequence that is cut into equal shares, one per CTA, from the lengths each CTA
 // reads itself: no plan is made on the host or by another kernel.  A row cut by a share's end leaves partial
@@ -23,8 +27,9 @@
 // The join is a second launch rather than a last-arrival counter in the first: the workspace then needs no
 // initial state, and neither a replayed graph nor a call that shares it in turn can find a stale counter.
 //
-// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices; the units of a
-// token are neighbours in memory.  The slices' states are combined through shared memory at a segment's end.
+// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of
+// two); the units of a token are neighbours in memory.  The slices' states are combined pairwise through shared
+// memory at a segment's end.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -71,43 +76,65 @@ struct AttnParams {
 
 template <typename T> struct Num;
 template <> struct Num<__nv_bfloat16> {
-    static constexpr float kLift = 0.f;
+    static constexpr float kLift = 0.f, kSlack = 8.f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
-    static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                               uint32_t b1) {
+    static __device__ __forceinline__ void mma(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
     }
 };
 template <> struct Num<__half> {
-    // p is rounded to fp16 for the product with V.  Its largest value is 1 and fp16 loses relative precision below
-    // 2^-14, so p is computed 2^14 times larger (the sum carries the same factor, and both cancel).
-    static constexpr float kLift = 14.f;
+    // p is rounded to fp16 for the product with V, and fp16 loses relative precision below 2^-14.  So p is computed
+    // 2^kLift times larger (the sum carries the same factor, and both cancel): at most 2^(kLift + kSlack) = 2^14.
+    static constexpr float kLift = 8.f, kSlack = 6.f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
-    static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                               uint32_t b1) {
+    static __device__ __forceinline__ void mma(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
     }
 };
 
-__device__ __forceinline__ void ld32(const void* p, uint32_t* r) {   // 32 bytes, read once
-    asm volatile("ld.global.nc.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "l"(p));
+__device__ __forceinline__ uint4 ldsm(uint32_t a) {
+    uint4 v;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
 }
-__device__ __forceinline__ void ld16(const void* p, uint32_t* r) {
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "l"(p));
+__device__ __forceinline__ uint4 ldsm_t(uint32_t a) {
+    uint4 v;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// 16 bytes to shared memory, read once
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+// the same, or zeros where bytes is 0, and then src is not read
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(bytes), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {   // all but the newest N groups have landed
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint64_t read_once_policy() {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
 }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -129,12 +156,6 @@ __device__ __forceinline__ void row_span(const AttnParams& p, int b, int32_t* fi
     *end = e;
     *first = p.window > 0 && e > p.window ? e - p.window : 0;
 }
-__device__ __forceinline__ int32_t row_tiles(const AttnParams& p, int b) {
-    int32_t first, end;
-    row_span(p, b, &first, &end);
-    const int32_t step = kTile * p.subs;
-    return end > first ? (end - first + step - 1) / step : 1;   // an empty row still has a result to write
-}
 
 // Where a unit's queries are: heads [h0, h0 + n).
 __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* kv, int* h0, int* n) {
@@ -144,202 +165,249 @@ __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* k
     *n = min(p.rows, p.group - s * p.rows);
 }
 
-// A tile's tokens: lane l < 16 holds block id and place in the block of token l (-1: not attended).
-struct TileIds {
-    int32_t id, at;
+// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`.  Tiles begin
+// at multiples of 16 tokens, so that one lies in one block if the block size is such a multiple too.
+struct Cursor {
+    int32_t b, chunk, i, tiles, first, end;
+    __device__ __forceinline__ void row(const AttnParams& p) {
+        row_span(p, b, &first, &end);
+        const int32_t step = kTile * p.subs;
+        tiles = end > first ? (end - (first & -kTile) + step - 1) / step : 1;   // an empty row still has a result to write
+    }
+    __device__ __forceinline__ void next(const AttnParams& p, bool more) {
+        if (++i < tiles) return;
+        i = 0;
+        if (++chunk < p.chunks) return;
+        chunk = 0;
+        ++b;
+        if (more) row(p);
+    }
+    // first token of slice `sub` of the tile; may lie at or behind the end
+    __device__ __forceinline__ int32_t token(const AttnParams& p, int sub) const { return (first & -kTile) + kTile * (i * p.subs + sub); }
 };
 
-// The softmax state of a warp: rows lane / 4 and lane / 4 + 8, dims [D/4 * c, D/4 * (c + 1)) with c = lane % 4;
-// acc[j][0], acc[j][1] are the dims D/4 * c + j and D/4 * c + D/8 + j of the first row, [2], [3] of the second.
-template <int D>
+// The softmax state of a warp.  Lane (g = lane / 4, c = lane % 4) holds heads 8 t + 2 c and 8 t + 2 c + 1 of column tile t:
+// the reference m of the weights p = 2^(s - m), the sum over the tokens it has seen itself, and acc[t][j] = dims
+// 16 j + g of both heads, dims 16 j + 8 + g of both.  m is kNothing before the first token: finite, so that
+// differences from it are never NaN, and as a reference as good as any for scores as low as that.
+constexpr float kNothing = -3.0e38f;
+template <int D, int NT>
 struct State {
-    float m[2], l[2];
-    float acc[D / 8][4];
+    float m[NT][2], l[NT][2];
+    float acc[NT][D / 16][4];
 };
 
 // -------------------------------------------------------------------------------------------- main kernel
 
-template <typename T, int D, int MR>
-struct Worker {
-    static constexpr int KC = D / 64;          // 32-byte pieces of a key row per lane
-    static constexpr int VW = D / 16;          // registers of a value row per lane
-    const AttnParams& p;
-    const int lane, g, c;
-    uint32_t q0[KC][8], q1[KC][8];             // query rows g and g + 8 in the key's order
-    uint32_t k[2][KC][8];                      // keys of tokens g and g + 8
-    uint32_t v[4][VW];                         // values of tokens 2c, 2c + 1, 2c + 8, 2c + 9
-    TileIds ids;
-    uint32_t mask, next_mask;                  // tokens of the tile that are attended
+template <int D>
+struct Ring {
+    static constexpr int kStages = D == 128 ? 3 : 4;
+    static constexpr int kRowBytes = 2 * D;
+    static constexpr int kSideBytes = kTile * kRowBytes;     // keys, then values
+    static constexpr int kStageBytes = 2 * kSideBytes;
+    static constexpr int kWarpBytes = kStages * kStageBytes;
+};
 
-    __device__ __forceinline__ Worker(const AttnParams& pp) : p(pp), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), c(threadIdx.x & 3) {}
+// kOneBlock: the block size is a multiple of a tile, so that a tile lies in one block.
+template <typename T, int D, int NT, bool kOneBlock>
+struct Worker {
+    using R = Ring<D>;
+    const AttnParams& p;
+    const int lane, g, c, unit_in_cta, sub;
+    const uint32_t ring;                       // the warp's first stage
+    const uint64_t policy;
+    uint32_t put;                              // this lane's place in a stage: row lane / 8 and, in place, piece lane % 8
+    uint32_t k_at[4], v_at[4];                 // what this lane reads of a stage: pieces 2 j + .. of its row of the four parts
+    uint32_t q[NT][D / 16][2];                 // query head 8 t + g, dims 16 j + 2 c and 16 j + 8 + 2 c
+    const T *k_src, *v_src;                    // pools at this lane's head, piece and (kOneBlock) row
+    const int32_t* table;
+    int32_t id, at;                            // block and place of the first token (kOneBlock), else of token lane % 16
+    bool idle;                                 // the unit does not exist
+    uint64_t masks;                            // which tokens of the tiles in the ring are attended, 16 bits each
+
+    __device__ __forceinline__ Worker(const AttnParams& pp, uint32_t smem)
+        : p(pp), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), c(threadIdx.x & 3), unit_in_cta((threadIdx.x >> 5) % pp.units),
+          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), masks(0) {
+        const int x = lane & 7, up = lane >> 4, mid = lane >> 3 & 1;
+        put = (lane >> 3) * R::kRowBytes + (((lane & 7) ^ (lane >> 3)) << 4);   // rows 4 to 7 and 12 to 15: piece ^ 4
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            k_at[j] = (x + 8 * mid) * R::kRowBytes + (((2 * j + up) ^ x) << 4);
+            v_at[j] = R::kSideBytes + (x + 8 * up) * R::kRowBytes + (((2 * j + mid) ^ x) << 4);
+        }
+    }
 
     __device__ __forceinline__ void load_query(int b, int h0, int n) {
-        const T* q = (const T*)p.q + b * p.q_stride + (int64_t)h0 * D;
 #pragma unroll
-        for (int j = 0; j < KC; ++j) {
+        for (int t = 0; t < NT; ++t) {
+            const T* src = (const T*)p.q + b * p.q_stride + (int64_t)(h0 + 8 * t + g) * D + 2 * c;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q0[j][i] = q1[j][i] = 0;
-            if (g < n) {
-                ld16(q + g * D + 64 * j + 16 * c, q0[j]);
-                ld16(q + g * D + 64 * j + 16 * c + 8, q0[j] + 4);
-            }
-            if (MR == 16 && g + 8 < n) {
-                ld16(q + (g + 8) * D + 64 * j + 16 * c, q1[j]);
-                ld16(q + (g + 8) * D + 64 * j + 16 * c + 8, q1[j] + 4);
-            }
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    q[t][j][h] = 8 * t + g < n ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 8 * h)) : 0u;
         }
     }
 
-    __device__ __forceinline__ void load_ids(const int32_t* table, int32_t t0, int32_t end) {
-        const int32_t t = t0 + (lane & 15);
-        ids.id = -1;
-        ids.at = 0;
-        if (t < end) {
+    // The row and chunk of the tiles to come.
+    __device__ __forceinline__ void enter(const Cursor& cur) {
+        const int kv = (cur.chunk * p.units + unit_in_cta) / p.splits;
+        idle = kv >= p.hkv;
+        const int64_t o = (int64_t)kv * D + 8 * (lane & 7) + (kOneBlock ? (int64_t)(lane >> 3) * p.hkv * D : 0);
+        k_src = (const T*)p.kpool + (idle ? 0 : o);
+        v_src = (const T*)p.vpool + (idle ? 0 : o);
+        table = p.tables + (int64_t)cur.b * p.table_stride;
+    }
+
+    // Looks the tile's tokens up; at = -1: no token.
+    __device__ __forceinline__ void load_ids(const Cursor& cur) {
+        const int32_t t = cur.token(p, sub) + (kOneBlock ? 0 : lane & 15);
+        id = 0;
+        at = -1;
+        if (t < cur.end && (kOneBlock || t >= cur.first)) {
             const int32_t blk = block_of(t, p);
-            const int32_t id = __ldg(table + blk);
-            ids.at = t - blk * p.block_size;
-            if ((unsigned)id < (unsigned)p.num_blocks) ids.id = id;
-            else if (p.status) *(volatile int32_t*)p.status = kStatusBadId;
+            at = t - blk * p.block_size;
+            id = __ldg(table + blk);
         }
-        next_mask = __ballot_sync(0xffffffffu, ids.id >= 0) & 0xffffu;
     }
 
-    __device__ __forceinline__ void load_keys(int kv) {
+    // Requests the tile that load_ids looked up, into stage s.  Lane = (row of four, 16-byte piece of 128).
+    __device__ __forceinline__ void copy_tile(const Cursor& cur, int s) {
+        const bool known = (unsigned)id < (unsigned)p.num_blocks;
+        if (at >= 0 && !known && p.status) *(volatile int32_t*)p.status = kStatusBadId;
+        const bool read = at >= 0 && known && !idle;
+        const int64_t tok = (int64_t)p.hkv * D;
+        const uint32_t dst = ring + s * R::kStageBytes + put;
+        if constexpr (kOneBlock) {
+            // of the tile's 16 tokens those in [first, end): a run of bits
+            const int32_t t0 = cur.token(p, sub);
+            const int32_t lo = max(cur.first - t0, 0), hi = min(cur.end - t0, kTile);
+            const uint32_t mask = read && hi > lo ? (0xffffu >> (kTile - hi)) & (0xffffu << lo) : 0u;
+            masks |= (uint64_t)mask << 48;
+            const T* k = k_src + (read ? id * p.k_block_stride + at * tok : 0);
+            const T* v = v_src + (read ? id * p.v_block_stride + at * tok : 0);
+            if (mask == 0xffffu) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int32_t id = __shfl_sync(0xffffffffu, ids.id, g + 8 * r), at = __shfl_sync(0xffffffffu, ids.at, g + 8 * r);
-            const T* row = (const T*)p.kpool + id * p.k_block_stride + ((int64_t)at * p.hkv + kv) * D + 16 * c;
-            if (next_mask == 0xffffu) {
+                for (int i = 0; i < 4; ++i, k += 4 * tok, v += 4 * tok)
 #pragma unroll
-                for (int j = 0; j < KC; ++j) ld32(row + 64 * j, k[r][j]);
+                    for (int j = 0; j < D / 64; ++j) {
+                        const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
+                        copy16(to, k + 64 * j, policy);
+                        copy16(to + R::kSideBytes, v + 64 * j, policy);
+                    }
             } else {
 #pragma unroll
-                for (int j = 0; j < KC; ++j) {
+                for (int i = 0; i < 4; ++i) {
+                    const bool on = mask >> (4 * i + (lane >> 3)) & 1;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) k[r][j][i] = 0;
-                    if (id >= 0) ld32(row + 64 * j, k[r][j]);
-                }
-            }
-        }
-    }
-
-    __device__ __forceinline__ void load_values(int kv) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int tok = 2 * c + (r & 1) + 8 * (r >> 1);
-            const int32_t id = __shfl_sync(0xffffffffu, ids.id, tok), at = __shfl_sync(0xffffffffu, ids.at, tok);
-            const T* row = (const T*)p.vpool + id * p.v_block_stride + ((int64_t)at * p.hkv + kv) * D + (D / 8) * g;
-            if (next_mask == 0xffffu) {
-                if constexpr (D == 128) ld32(row, v[r]); else ld16(row, v[r]);
-            } else {   // a value that is not attended must not reach the product, where 0 times a NaN is a NaN
-#pragma unroll
-                for (int i = 0; i < VW; ++i) v[r][i] = 0;
-                if (id >= 0) {
-                    if constexpr (D == 128) ld32(row, v[r]); else ld16(row, v[r]);
-                }
-            }
-        }
-    }
-
-    // Attends this warp's tiles of tokens [t_lo, t_hi): those with index = sub modulo subs.
-    __device__ __forceinline__ void run(const int32_t* table, int32_t t_lo, int32_t t_hi, int sub, int kv, State<D>& st) {
-        const int32_t step = kTile * p.subs;
-        int32_t t = t_lo + kTile * sub;
-        if (t >= t_hi) return;
-        load_ids(table, t, t_hi);
-        mask = next_mask;
-        load_keys(kv);
-        load_values(kv);
-        t += step;
-        bool more = t < t_hi;
-        if (more) load_ids(table, t, t_hi);
-        while (true) {
-            float s[2][4];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
-#pragma unroll
-                for (int j = 0; j < KC; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        Num<T>::mma(s[r], q0[j][2 * i], MR == 16 ? q1[j][2 * i] : 0u, q0[j][2 * i + 1],
-                                    MR == 16 ? q1[j][2 * i + 1] : 0u, k[r][j][2 * i], k[r][j][2 * i + 1]);
-            }
-            if (more) load_keys(kv);
-            // scores in base 2; columns 2c, 2c + 1 of the two products are tokens 8r + 2c, 8r + 2c + 1
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int i = 0; i < MR / 4; ++i) s[r][i] *= p.scale_log2e;
-            if (mask != 0xffffu) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int i = 0; i < MR / 4; ++i)
-                        if (!(mask >> (8 * r + 2 * c + (i & 1)) & 1)) s[r][i] = -CUDART_INF_F;
-            }
-            bool grown = false;
-            float m_new[2], alpha[2];
-#pragma unroll
-            for (int h = 0; h < MR / 8; ++h) {
-                float mx = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                m_new[h] = fmaxf(st.m[h], mx);
-                grown |= m_new[h] > st.m[h];
-            }
-            if (__any_sync(0xffffffffu, grown)) {
-#pragma unroll
-                for (int h = 0; h < MR / 8; ++h) {
-                    // a row that has seen nothing has m = -inf and sum 0: its factor is 0 and not a NaN
-                    alpha[h] = st.m[h] == m_new[h] ? 1.f : ex2(st.m[h] - m_new[h]);
-                    st.m[h] = m_new[h];
-                    st.l[h] *= alpha[h];
-#pragma unroll
-                    for (int j = 0; j < D / 8; ++j) {
-                        st.acc[j][2 * h] *= alpha[h];
-                        st.acc[j][2 * h + 1] *= alpha[h];
+                    for (int j = 0; j < D / 64; ++j) {
+                        const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
+                        copy16(to, on ? k + i * 4 * tok + 64 * j : (const T*)p.kpool, on ? 16 : 0, policy);
+                        copy16(to + R::kSideBytes, on ? v + i * 4 * tok + 64 * j : (const T*)p.vpool, on ? 16 : 0, policy);
                     }
                 }
             }
-            uint32_t a[4] = {0u, 0u, 0u, 0u};
+        } else {
+            masks |= (uint64_t)(__ballot_sync(0xffffffffu, read) & 0xffffu) << 48;
+            const int32_t id_or = read ? id : -1;
 #pragma unroll
-            for (int h = 0; h < MR / 8; ++h) {
-                const float m = st.m[h] == -CUDART_INF_F ? 0.f : st.m[h] - Num<T>::kLift;
+            for (int i = 0; i < 4; ++i) {
+                const int row = 4 * i + (lane >> 3);
+                const int32_t b = __shfl_sync(0xffffffffu, id_or, row), a = __shfl_sync(0xffffffffu, at, row);
+                const bool on = b >= 0;
+                const T* k = on ? k_src + (b * p.k_block_stride + a * tok) : (const T*)p.kpool;
+                const T* v = on ? v_src + (b * p.v_block_stride + a * tok) : (const T*)p.vpool;
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float e0 = ex2(s[r][2 * h] - m), e1 = ex2(s[r][2 * h + 1] - m);
-                    st.l[h] += e0 + e1;
-                    a[2 * r + h] = Num<T>::pack(e0, e1);
+                for (int j = 0; j < D / 64; ++j) {
+                    const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
+                    copy16(to, k + (on ? 64 * j : 0), on ? 16 : 0, policy);
+                    copy16(to + R::kSideBytes, v + (on ? 64 * j : 0), on ? 16 : 0, policy);
                 }
             }
+        }
+    }
+
+    // Attends the tile in stage s; `mask`: its tokens that count.
+    __device__ __forceinline__ void attend(int stage, uint32_t mask, State<D, NT>& st) {
+        const uint32_t src = ring + stage * R::kStageBytes;
+        float s[NT][4];
 #pragma unroll
-            for (int j = 0; j < D / 8; ++j) {
-                const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-                Num<T>::mma(st.acc[j], a[0], a[1], a[2], a[3], __byte_perm(v[0][j / 2], v[1][j / 2], sel),
-                            __byte_perm(v[2][j / 2], v[3][j / 2], sel));
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            const uint4 k = ldsm(src + k_at[j % 4] + 128 * (j / 4));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) Num<T>::mma(s[t], k, q[t][j][0], q[t][j][1]);
+        }
+        // s[t][0], [1]: token g, heads 8t + 2c, + 1; [2], [3]: token g + 8.  The weights' exponents:
+        float e[NT][4];
+        bool over = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (mask != 0xffffu && !(mask >> (g + 4 * (i & 2)) & 1)) s[t][i] = -CUDART_INF_F;
+                else s[t][i] *= p.scale_log2e;
+                e[t][i] = s[t][i] - st.m[t][i & 1];
+                over |= e[t][i] > Num<T>::kSlack;
             }
-            if (!more) break;
-            load_values(kv);
-            mask = next_mask;
-            t += step;
-            more = t < t_hi;
-            if (more) load_ids(table, t, t_hi);
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float mx = fmaxf(s[t][h], s[t][2 + h]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    mx = fmaxf(mx, st.m[t][h]);
+                    const float alpha = ex2(st.m[t][h] - mx);
+                    st.m[t][h] = mx;
+                    st.l[t][h] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        st.acc[t][j][h] *= alpha;
+                        st.acc[t][j][2 + h] *= alpha;
+                    }
+                    e[t][h] = s[t][h] - mx;
+                    e[t][2 + h] = s[t][2 + h] - mx;
+                }
+        }
+        uint32_t pt[NT][2];      // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 of head 8t + g
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[t][i] = ex2(e[t][i] + Num<T>::kLift);
+            st.l[t][0] += e[t][0] + e[t][2];
+            st.l[t][1] += e[t][1] + e[t][3];
+            pt[t][0] = transpose8(Num<T>::pack(e[t][0], e[t][1]));
+            pt[t][1] = transpose8(Num<T>::pack(e[t][2], e[t][3]));
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            const uint4 v = ldsm_t(src + v_at[j % 4] + 128 * (j / 4));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v, pt[t][0], pt[t][1]);
         }
     }
 };
 
-template <int D, int MR>
-__device__ __forceinline__ void state_reset(State<D>& st) {
+template <int D, int NT>
+__device__ __forceinline__ void state_reset(State<D, NT>& st) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        st.m[h] = -CUDART_INF_F;
-        st.l[h] = 0.f;
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            st.m[t][h] = kNothing;
+            st.l[t][h] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.acc[t][j][i] = 0.f;
     }
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.acc[j][i] = 0.f;
 }
 
 // Joins another state into st: weights 2^(m - max), 0 for a side that has seen nothing.
@@ -349,11 +417,50 @@ __device__ __forceinline__ void join_weights(float m, float m2, float* m_new, fl
     *w2 = m2 == *m_new ? 1.f : ex2(m2 - *m_new);
 }
 
-template <typename T, int D, int MR>
+// Combines the states of the CTA's token slices into slice 0's, in pairs: half of the slices hand theirs over, the
+// other half take it, and so on.  Every warp calls it.
+template <int D, int NT>
+__device__ __forceinline__ void join_slices(State<D, NT>& st, float4* xchg, int units, int unit, int subs, int sub, int lane) {
+    constexpr int kPieces = D / 16 + 1;      // of one column tile: they are handed over one after the other
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        for (int half = subs >> 1; half > 0; half >>= 1) {
+            if (sub >= half && sub < 2 * half) {
+                float4* x = xchg + ((sub - half) * units + unit) * kPieces * 32 + lane;
+                x[0] = make_float4(st.m[t][0], st.m[t][1], st.l[t][0], st.l[t][1]);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
+                    x[(1 + j) * 32] = make_float4(st.acc[t][j][0], st.acc[t][j][1], st.acc[t][j][2], st.acc[t][j][3]);
+            }
+            __syncthreads();
+            if (sub < half) {
+                const float4* x = xchg + (sub * units + unit) * kPieces * 32 + lane;
+                const float4 ml = x[0];
+                float w[2], w2[2];
+                join_weights(st.m[t][0], ml.x, &st.m[t][0], &w[0], &w2[0]);
+                join_weights(st.m[t][1], ml.y, &st.m[t][1], &w[1], &w2[1]);
+                st.l[t][0] = st.l[t][0] * w[0] + ml.z * w2[0];
+                st.l[t][1] = st.l[t][1] * w[1] + ml.w * w2[1];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    const float4 y = x[(1 + j) * 32];
+                    st.acc[t][j][0] = st.acc[t][j][0] * w[0] + y.x * w2[0];
+                    st.acc[t][j][1] = st.acc[t][j][1] * w[1] + y.y * w2[1];
+                    st.acc[t][j][2] = st.acc[t][j][2] * w[0] + y.z * w2[0];
+                    st.acc[t][j][3] = st.acc[t][j][3] * w[1] + y.w * w2[1];
+                }
+            }
+            __syncthreads();
+        }
+}
+
+template <typename T, int D, int NT, bool kOneBlock>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
-    extern __shared__ float4 xchg[];   // [(subs - 1) * units][MR / 8 * (D / 16 + 1)][32]
-    constexpr int kXchg = MR / 8 * (D / 16) + 1;
+    using R = Ring<D>;
+    extern __shared__ unsigned char smem_raw[];   // rings of the warps, then the slices' exchange
+    // the pieces' places are exclusive-ored within 128 bytes
+    unsigned char* smem = smem_raw + (-(uint32_t)__cvta_generic_to_shared(smem_raw) & 127);
     __shared__ long long sh_sum[kMaxWarps];
     __shared__ long long sh_at;        // tiles before the CTA's first row
     __shared__ int sh_row;
@@ -366,8 +473,11 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     const int per = (p.batch + blockDim.x - 1) / blockDim.x;
     const int b_lo = min(p.batch, (int)threadIdx.x * per), b_hi = min(p.batch, b_lo + per);
     long long mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += row_tiles(p, b);
-    mine *= p.chunks;
+    Cursor cur;
+    for (cur.b = b_lo; cur.b < b_hi; ++cur.b) {
+        cur.row(p);
+        mine += (long long)cur.tiles * p.chunks;
+    }
     long long before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -385,147 +495,114 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     const long long share = (total + gridDim.x - 1) / gridDim.x;
     const long long begin = share * blockIdx.x, end = min(total, begin + share);
     if (begin >= before && begin < before + mine) {
-        long long at = before;
-        int b = b_lo;
-        while (true) {
-            const long long n = (long long)row_tiles(p, b) * p.chunks;
-            if (begin < at + n) break;
-            at += n;
-            ++b;
+        long long a = before;
+        for (cur.b = b_lo;; ++cur.b) {
+            cur.row(p);
+            const long long n = (long long)cur.tiles * p.chunks;
+            if (begin < a + n) break;
+            a += n;
         }
-        sh_row = b;
-        sh_at = at;
+        sh_row = cur.b;
+        sh_at = a;
     }
     __syncthreads();
     int4 cut = make_int4(0, 0, 0, 0);
     if (begin < end) {
-        int b = sh_row;
-        long long seg = sh_at;      // where the row's first chunk begins
-        int32_t first, last;
-        row_span(p, b, &first, &last);
-        int32_t tiles = row_tiles(p, b);
-        int chunk = (int)((begin - seg) / tiles);
-        seg += (long long)chunk * tiles;
-        const int unit_in_cta = warp % p.units, sub = warp / p.units;
-        Worker<T, D, MR> wk(p);
-        for (long long at = begin; at < end;) {
-            const long long seg_end = seg + tiles;
-            const int32_t lo = (int32_t)(at - seg), hi = (int32_t)(min(end, seg_end) - seg);
-            const int32_t step = kTile * p.subs;
-            // of 64 bits where 32 could wrap: lengths go up to 2^31 - 1
-            const int32_t t_lo = first + lo * step, t_hi = (int32_t)min((int64_t)last, (int64_t)first + (int64_t)hi * step);
-            const int unit = chunk * p.units + unit_in_cta;
-            const bool busy = unit < p.hkv * p.splits;
-            int kv = 0, h0 = 0, n = 0;
-            State<D> st;
-            state_reset<D, MR>(st);
-            if (busy) {
-                unit_heads(p, unit, &kv, &h0, &n);
-                wk.load_query(b, h0, n);
-                wk.run(p.tables + (int64_t)b * p.table_stride, t_lo, t_hi, sub, kv, st);
-#pragma unroll
-                for (int h = 0; h < MR / 8; ++h) {
-                    st.l[h] += __shfl_xor_sync(0xffffffffu, st.l[h], 1);
-                    st.l[h] += __shfl_xor_sync(0xffffffffu, st.l[h], 2);
+        cur.b = sh_row;
+        cur.row(p);
+        const long long into = begin - sh_at;
+        cur.chunk = (int)(into / cur.tiles);
+        cur.i = (int)(into - (long long)cur.chunk * cur.tiles);
+        Cursor ahead = cur;                      // the tile that is requested next
+        Worker<T, D, NT, kOneBlock> wk(p, (uint32_t)__cvta_generic_to_shared(smem));
+        float4* xchg = reinterpret_cast<float4*>(smem + nwarps * R::kWarpBytes);
+        long long asked = begin;
+        int slot = 0;                            // stage that is filled next
+        wk.enter(ahead);
+        wk.load_ids(ahead);
+        auto request = [&]() {
+            wk.masks >>= 16;
+            if (asked < end) {
+                wk.copy_tile(ahead, slot);
+                if (++asked < end) {
+                    ahead.next(p, true);
+                    if (ahead.i == 0) wk.enter(ahead);
+                    wk.load_ids(ahead);
                 }
             }
-            if (p.subs > 1) {
-                if (sub > 0) {
-                    float4* x = xchg + ((sub - 1) * p.units + unit_in_cta) * kXchg * 32 + lane;
-                    x[0] = make_float4(st.m[0], st.l[0], st.m[1], st.l[1]);
+            copies_commit();
+            slot = slot + 1 == R::kStages ? 0 : slot + 1;
+        };
 #pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        if constexpr (MR == 16) {
-                            x[(1 + 2 * j) * 32] = make_float4(st.acc[2 * j][0], st.acc[2 * j][1], st.acc[2 * j][2], st.acc[2 * j][3]);
-                            x[(2 + 2 * j) * 32] =
-                                make_float4(st.acc[2 * j + 1][0], st.acc[2 * j + 1][1], st.acc[2 * j + 1][2], st.acc[2 * j + 1][3]);
-                        } else {
-                            x[(1 + j) * 32] = make_float4(st.acc[2 * j][0], st.acc[2 * j][1], st.acc[2 * j + 1][0], st.acc[2 * j + 1][1]);
+        for (int s = 0; s < R::kStages - 1; ++s) request();
+        State<D, NT> st;
+        int kv = 0, h0 = 0, n = 0;
+        int32_t lo = 0;
+        bool fresh = true;
+        for (long long at = begin; at < end; ++at) {
+            const int unit = cur.chunk * p.units + wk.unit_in_cta;
+            if (fresh) {
+                state_reset(st);
+                n = 0;
+                if (unit < p.hkv * p.splits) unit_heads(p, unit, &kv, &h0, &n);
+                wk.load_query(cur.b, h0, n);
+                lo = cur.i;
+                fresh = false;
+            }
+            copies_wait<R::kStages - 2>();
+            __syncwarp();                        // the other lanes' copies too, and they have left the stage before
+            // the oldest of the kStages - 1 masks
+            const uint32_t mask = (uint32_t)(wk.masks >> (16 * (5 - R::kStages))) & 0xffffu;
+            request();                           // into the stage that the tile before left
+            wk.attend(slot, mask, st);           // after the request the oldest stage is the next to be filled
+            const bool seg_end = cur.i + 1 == cur.tiles;
+            if (seg_end || at + 1 == end) {
+                const bool whole = lo == 0 && seg_end;
+                join_slices(st, xchg, p.units, wk.unit_in_cta, p.subs, wk.sub, lane);
+                if (wk.sub == 0) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        float inv[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float l = st.l[t][h];
+                            l += __shfl_xor_sync(0xffffffffu, l, 4);
+                            l += __shfl_xor_sync(0xffffffffu, l, 8);
+                            l += __shfl_xor_sync(0xffffffffu, l, 16);
+                            st.l[t][h] = l;
+                            inv[h] = !whole ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F;
                         }
-                    }
-                }
-                __syncthreads();
-                if (sub == 0)
-                    for (int o = 0; o < p.subs - 1; ++o) {
-                        const float4* x = xchg + (o * p.units + unit_in_cta) * kXchg * 32 + lane;
-                        const float4 ml = x[0];
-                        float w[2], w2[2];
-                        join_weights(st.m[0], ml.x, &st.m[0], &w[0], &w2[0]);
-                        join_weights(st.m[1], ml.z, &st.m[1], &w[1], &w2[1]);
-                        st.l[0] = st.l[0] * w[0] + ml.y * w2[0];
-                        st.l[1] = st.l[1] * w[1] + ml.w * w2[1];
+                        // an even lane takes its pair's values of the first head, an odd one of the second, so that
+                        // each holds two neighbouring dims
+                        const int odd = wk.g & 1, r = 8 * t + 2 * wk.c + odd;
+                        const int64_t at_part = (((int64_t)blockIdx.x * 2 + (lo == 0)) * p.units + wk.unit_in_cta) * p.rows + r;
+                        T* o = (T*)p.out + cur.b * p.out_stride + (int64_t)(h0 + r) * D + (wk.g & 6);
+                        float* po = p.part_o + at_part * D + (wk.g & 6);
 #pragma unroll
-                        for (int j = 0; j < D / 16; ++j) {
-                            if constexpr (MR == 16) {
+                        for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float4 y = x[(1 + 2 * j + e) * 32];
-                                    float(&d)[4] = st.acc[2 * j + e];
-                                    d[0] = d[0] * w[0] + y.x * w2[0];
-                                    d[1] = d[1] * w[0] + y.y * w2[0];
-                                    d[2] = d[2] * w[1] + y.z * w2[1];
-                                    d[3] = d[3] * w[1] + y.w * w2[1];
+                            for (int e = 0; e < 2; ++e) {
+                                const float x = st.acc[t][j][2 * e] * inv[0], y = st.acc[t][j][2 * e + 1] * inv[1];
+                                const float z = __shfl_xor_sync(0xffffffffu, odd ? x : y, 4);
+                                const float a0 = odd ? z : x, a1 = odd ? y : z;
+                                if (r < n) {
+                                    if (whole) *reinterpret_cast<uint32_t*>(o + 16 * j + 8 * e) = Num<T>::pack(a0, a1);
+                                    else *reinterpret_cast<float2*>(po + 16 * j + 8 * e) = make_float2(a0, a1);
                                 }
-                            } else {
-                                const float4 y = x[(1 + j) * 32];
-                                st.acc[2 * j][0] = st.acc[2 * j][0] * w[0] + y.x * w2[0];
-                                st.acc[2 * j][1] = st.acc[2 * j][1] * w[0] + y.y * w2[0];
-                                st.acc[2 * j + 1][0] = st.acc[2 * j + 1][0] * w[0] + y.z * w2[0];
-                                st.acc[2 * j + 1][1] = st.acc[2 * j + 1][1] * w[0] + y.w * w2[0];
                             }
+                        if (wk.g < 2 && r < n) {
+                            const float l = odd ? st.l[t][1] : st.l[t][0], m = odd ? st.m[t][1] : st.m[t][0];
+                            if (!whole) p.part_ml[at_part] = make_float2(m, l);
+                            else if (p.lse)
+                                p.lse[(int64_t)cur.b * p.hq + h0 + r] = l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
                         }
                     }
-                __syncthreads();
-            }
-            const bool whole = lo == 0 && hi == tiles;
-            if (busy && sub == 0) {
-                const int gg = lane >> 2, cc = lane & 3;
-#pragma unroll
-                for (int h = 0; h < MR / 8; ++h) {
-                    const int r = gg + 8 * h;
-                    if (r >= n) continue;
-                    if (whole) {
-                        const float inv = st.l[h] > 0.f ? 1.f / st.l[h] : st.l[h] == 0.f ? 0.f : CUDART_NAN_F;
-                        T* o = (T*)p.out + b * p.out_stride + (int64_t)(h0 + r) * D + (D / 4) * cc;
-                        // dims D/4 c + j are acc[j][0], dims D/4 c + D/8 + j acc[j][1]
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-#pragma unroll
-                            for (int j = 0; j < D / 8; j += 8) {
-                                uint4 w;
-                                w.x = Num<T>::pack(st.acc[j][2 * h + e] * inv, st.acc[j + 1][2 * h + e] * inv);
-                                w.y = Num<T>::pack(st.acc[j + 2][2 * h + e] * inv, st.acc[j + 3][2 * h + e] * inv);
-                                w.z = Num<T>::pack(st.acc[j + 4][2 * h + e] * inv, st.acc[j + 5][2 * h + e] * inv);
-                                w.w = Num<T>::pack(st.acc[j + 6][2 * h + e] * inv, st.acc[j + 7][2 * h + e] * inv);
-                                *reinterpret_cast<uint4*>(o + e * (D / 8) + j) = w;
-                            }
-                        if (p.lse && cc == 0)
-                            p.lse[(int64_t)b * p.hq + h0 + r] =
-                                st.l[h] == 0.f ? -CUDART_INF_F : (st.m[h] - Num<T>::kLift + log2f(st.l[h])) * kLn2;
-                    } else {
-                        const int64_t slot = (((int64_t)blockIdx.x * 2 + (lo == 0)) * p.units + unit_in_cta) * p.rows + r;
-                        float* o = p.part_o + slot * D + (D / 4) * cc;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-#pragma unroll
-                            for (int j = 0; j < D / 8; j += 4)
-                                *reinterpret_cast<float4*>(o + e * (D / 8) + j) =
-                                    make_float4(st.acc[j][2 * h + e], st.acc[j + 1][2 * h + e], st.acc[j + 2][2 * h + e], st.acc[j + 3][2 * h + e]);
-                        if (cc == 0) p.part_ml[slot] = make_float2(st.m[h], st.l[h]);
-                    }
                 }
+                if (lo == 0 && !seg_end)
+                    cut = make_int4(cur.b, cur.chunk, (int)((at + cur.tiles - cur.i - 1) / share) - (int)blockIdx.x + 1, 0);
+                fresh = true;
             }
-            if (lo == 0 && hi < tiles) cut = make_int4(b, chunk, (int)((seg_end - 1) / share) - (int)blockIdx.x + 1, 0);
-            at = seg + hi;
-            if (at == seg_end && at < end) {
-                seg = seg_end;
-                if (++chunk == p.chunks) {
-                    chunk = 0;
-                    ++b;
-                    row_span(p, b, &first, &last);
-                    tiles = row_tiles(p, b);
-                }
-            }
+            cur.next(p, at + 1 < end);
         }
     }
     if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
@@ -574,7 +651,7 @@ paged_join_kernel(const __grid_constant__ AttnParams p, int32_t ctas) {
             int kv, h0, n;
             unit_heads(p, unit, &kv, &h0, &n);
             if (r >= n) continue;
-            float m = -CUDART_INF_F, l = 0.f;
+            float m = kNothing, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int q = slice; q < cut.z; q += kSlices) {
                 const int64_t slot = (((int64_t)(i + q) * 2 + (q == 0)) * p.units + u) * p.rows + r;
@@ -624,7 +701,7 @@ paged_join_kernel(const __grid_constant__ AttnParams p, int32_t ctas) {
 // How the heads are dealt to warps; the same for a shape on every call.
 struct Layout {
     int32_t splits, rows, units, chunks, subs, ctas;
-    int mr;
+    int nt;                                // column tiles of 8 heads of a unit
     size_t part_o, part_ml, cuts, bytes;   // offsets and size of the workspace
 };
 
@@ -633,7 +710,7 @@ Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
     const int32_t group = hq / hkv;
     y.splits = (group + kMaxGroup - 1) / kMaxGroup;
     y.rows = (group + y.splits - 1) / y.splits;
-    y.mr = y.rows <= 8 ? 8 : 16;
+    y.nt = (y.rows + 7) / 8;
     const int32_t all = hkv * y.splits;
     y.chunks = (all + kMaxWarps - 1) / kMaxWarps;
     y.units = (all + y.chunks - 1) / y.chunks;
@@ -650,12 +727,21 @@ Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
 
 constexpr int kMaxDevices = 64;
 
-// SM count of the current device; looked up once per device.  The kernels' shared memory limit is raised there too.
-template <typename T, int D, int MR>
-cudaError_t allow_smem() {
-    return cudaFuncSetAttribute(paged_attn_kernel<T, D, MR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (kMaxWarps - 1) * (MR / 8 * (D / 16) + 1) * 32 * (int)sizeof(float4));
+// Rings of all warps and the exchange of half of the token slices.
+int attn_smem(int dim, int units, int subs) {
+    return 128 + units * subs * (dim == 128 ? Ring<128>::kWarpBytes : Ring<64>::kWarpBytes) +
+           subs / 2 * units * (dim / 16 + 1) * 32 * (int)sizeof(float4);
 }
+
+template <typename T, int D, int NT>
+cudaError_t allow_smem() {
+    const int bytes = attn_smem(D, 1, kMaxWarps);
+    cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e;
+}
+
+// SM count of the current device; looked up once per device.  The kernels' shared memory limit is raised there too.
 cudaError_t device_sms(int* sms) {
     static std::atomic<int> known[kMaxDevices];
     int dev = -1;
@@ -665,24 +751,28 @@ cudaError_t device_sms(int* sms) {
     *sms = known[dev].load(std::memory_order_acquire);
     if (*sms > 0) return cudaSuccess;
     e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 64, 8>();
-    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 64, 16>();
-    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 128, 8>();
-    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 128, 16>();
-    if (e == cudaSuccess) e = allow_smem<__half, 64, 8>();
-    if (e == cudaSuccess) e = allow_smem<__half, 64, 16>();
-    if (e == cudaSuccess) e = allow_smem<__half, 128, 8>();
-    if (e == cudaSuccess) e = allow_smem<__half, 128, 16>();
+    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 64, 1>();
+    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 64, 2>();
+    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 128, 1>();
+    if (e == cudaSuccess) e = allow_smem<__nv_bfloat16, 128, 2>();
+    if (e == cudaSuccess) e = allow_smem<__half, 64, 1>();
+    if (e == cudaSuccess) e = allow_smem<__half, 64, 2>();
+    if (e == cudaSuccess) e = allow_smem<__half, 128, 1>();
+    if (e == cudaSuccess) e = allow_smem<__half, 128, 2>();
     if (e == cudaSuccess) known[dev].store(*sms, std::memory_order_release);
     return e;
 }
 
+template <typename T, int D, int NT>
+cudaError_t launch_main(const AttnParams& p, const Layout& y, cudaStream_t s) {
+    const dim3 grid((unsigned)y.ctas), block((unsigned)(32 * y.units * y.subs));
+    const size_t smem = (size_t)attn_smem(D, y.units, y.subs);
+    return p.block_size % kTile == 0 ? ps::launch_dependent(paged_attn_kernel<T, D, NT, true>, grid, block, smem, s, p)
+                                     : ps::launch_dependent(paged_attn_kernel<T, D, NT, false>, grid, block, smem, s, p);
+}
 template <typename T, int D>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
-    const dim3 block((unsigned)(32 * y.units * y.subs));
-    const size_t smem = (size_t)(y.subs - 1) * y.units * (y.mr / 8 * (D / 16) + 1) * 32 * sizeof(float4);
-    cudaError_t e = y.mr == 8 ? ps::launch_dependent(paged_attn_kernel<T, D, 8>, dim3((unsigned)y.ctas), block, smem, s, p)
-                              : ps::launch_dependent(paged_attn_kernel<T, D, 16>, dim3((unsigned)y.ctas), block, smem, s, p);
+    cudaError_t e = y.nt == 1 ? launch_main<T, D, 1>(p, y, s) : launch_main<T, D, 2>(p, y, s);
     if (e == cudaSuccess && may_cut)
         e = ps::launch_dependent(paged_join_kernel<T, D>, dim3((unsigned)y.ctas * 8), dim3(kJoinThreads),
                                  (size_t)y.ctas * sizeof(int4), s, p, y.ctas);
@@ -733,10 +823,8 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     const int64_t block_elems = (int64_t)a.block_size * a.num_kv_heads * a.head_dim;
     if (a.num_gpu_blocks > 1 && (a.k_block_stride < block_elems || a.v_block_stride < block_elems))
         return bad("ps_paged_attn: a pool's block stride is smaller than a block");
-    if (!on(a.kpool, a.k_block_stride, 32) || !on(a.vpool, a.v_block_stride, 32))
-        return bad("ps_paged_attn: pools and their block strides must be multiples of 32 bytes");
-    if (!on(a.q, a.q_stride, 16) || !on(a.out, a.out_stride, 16))
-        return bad("ps_paged_attn: q, out and their row strides must be multiples of 16 bytes");
+    if (!on(a.kpool, a.k_block_stride, 16) || !on(a.vpool, a.v_block_stride, 16) || !on(a.q, a.q_stride, 16) || !on(a.out, a.out_stride, 16))
+        return bad("ps_paged_attn: pools, q, out and their strides must be multiples of 16 bytes");
     if (a.batch > 1 && a.out_stride < (int64_t)a.num_q_heads * a.head_dim) return bad("ps_paged_attn: rows of out overlap");
     int sms = 0;
     cudaError_t e = device_sms(&sms);
@@ -761,7 +849,7 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     p.scale_log2e = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * kLog2e;
     // rows that cannot be longer than one tile are never cut
     const int64_t longest = a.window > 0 && a.window < p.room ? a.window : p.room;
-    const bool may_cut = longest > (int64_t)kTile * y.subs;
+    const bool may_cut = longest > (int64_t)kTile * (y.subs - 1);   // a window may begin inside a tile
     cudaStream_t s = (cudaStream_t)stream;
     if (a.dtype == PS_DTYPE_BF16)
         e = a.head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(p, y, may_cut, s) : launch_attn<__nv_bfloat16, 64>(p, y, may_cut, s);

@@ -66,7 +66,7 @@ def test_rope_append_refuses_an_axis_that_is_not_there():
     dict(num_kv_heads=1025, num_q_heads=1025), dict(batch=-1), dict(block_size=0), dict(num_gpu_blocks=0), dict(table_stride=0),
     dict(window=-1), dict(dtype=2), dict(scale=float("nan")), dict(scale=float("inf")), dict(kpool=None), dict(vpool=None),
     dict(q=None), dict(out=None), dict(block_tables=None), dict(ctx_lens=None), dict(workspace=None),
-    dict(k_block_stride=1024), dict(v_block_stride=16 * 1024 + 8), dict(kpool=A + 16), dict(q=A + 8), dict(q_stride=4100),
+    dict(k_block_stride=1024), dict(v_block_stride=16 * 1024 + 4), dict(kpool=A + 8), dict(q=A + 8), dict(q_stride=4100),
     dict(out=A + 2), dict(out_stride=2048)])
 def test_paged_attn_refuses(kw):
     assert refused(B.load().ps_paged_attn, attn_args(**kw)).startswith("ps_paged_attn: ")

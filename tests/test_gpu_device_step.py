@@ -354,7 +354,7 @@ def test_attn_batches(rows, hi):
 def test_attn_strided_everything():
     rng = np.random.default_rng(11)
     ctx = [50, 700, 3, 0]
-    for gap in (16, 4096):
+    for gap in (8, 4096):
         kp, vp, _, tables = attn_case(rng, ctx, 8, 2, 128, 24, torch.bfloat16, gap=gap)
         wide = torch.randn((4, 3, 8, 128), device="cuda").bfloat16()
         q = wide[:, 1]
@@ -490,7 +490,7 @@ def test_tensors_that_do_not_fit_are_refused():
                 dict(block_tables=t.long()), dict(block_tables=t[:2]), dict(block_tables=t[:, :2]), dict(ctx_lens=n[:2]), dict(ctx_lens=n.cpu()),
                 dict(lse=torch.zeros((3, 8), device="cuda", dtype=bf)), dict(lse=torch.zeros((2, 8), device="cuda")), dict(scale=0.0),
                 dict(scale=float("nan")), dict(window=-1), dict(q=torch.zeros((3, 7, 64), device="cuda", dtype=bf)),
-                dict(kpool=kp.view(-1)[8:8 + 7 * 16 * 128].view(7, 16, 2, 64), vpool=kp[:7])):
+                dict(kpool=kp.view(-1)[4:4 + 7 * 16 * 128].view(7, 16, 2, 64), vpool=kp[:7])):
         rc, text = B.ps_paged_attn(**{**good, **bad})
         assert rc == B.PS_ERR_INVALID and text, bad.keys()
     k = torch.zeros((3, 2, 64), device="cuda", dtype=bf)
