@@ -34,6 +34,7 @@
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -46,7 +47,8 @@ constexpr int kMaxWarps = 8;
 constexpr int kTile = 16;             // tokens of a warp's tile
 constexpr int kMaxGroup = 16;         // query heads of a unit
 constexpr int kCtaFactor = 1;         // CTAs per SM
-constexpr int kJoinThreads = 128;
+constexpr int kJoinThreads = 256;
+constexpr int kFewParts = 16;          // up to so many are a warp's work in the join
 constexpr int32_t kMaxTokens = INT32_MAX - 1024;   // of a row, so that a tile's end cannot wrap
 constexpr int kStatusBadId = 2, kStatusLength = 5;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -610,89 +612,181 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 
 // Combines the parts of the rows that a share's end cut: CTA i of the main kernel names in cuts[i] the segment that
 // begins in it and goes on, whose parts are slot 1 of CTA i and slot 0 of the CTAs that follow.  Work items are
-// (segment, unit, query head), dealt to the CTAs in turn; a CTA's slices of D / 4 threads take every fourth or eighth
-// part each, and the slices are combined in order, so a result does not depend on timing.
+// (segment, unit, query head).  What an item costs is latency, so its loads do not wait for one another: parts are
+// requested while the weights are made from all parts' m.  A segment of few parts (the rows of a batch) is a warp's
+// item, one of many (a long row on much of the chip) a CTA's, whose slices of D / 4 threads take every eighth or
+// sixteenth part.  Sums are taken in a fixed order, so a result does not depend on timing.
+template <typename T, int D>
+struct Joiner {
+    static constexpr int kLanes = D / 4;     // a lane owns 4 dims
+    static constexpr int kAhead = 4;         // parts that a thread requests at a time
+    const AttnParams& p;
+    int4 cut;                                // row, chunk, parts, first CTA
+    int64_t slot0, step;
+    int h0, r, per;
+
+    __device__ __forceinline__ Joiner(const AttnParams& pp) : p(pp), per(pp.units * pp.rows) {}
+
+    // Item k of a segment; false if that unit or head does not exist.
+    __device__ __forceinline__ bool set(const int4& segment, int k) {
+        cut = segment;
+        const int u = k / p.rows, unit = cut.y * p.units + u;
+        int kv, n;
+        unit_heads(p, unit, &kv, &h0, &n);
+        r = k - u * p.rows;
+        step = 2 * (int64_t)per;             // from one CTA's slots to the next's
+        slot0 = (int64_t)cut.w * step + k;
+        return kv < p.hkv && r < n;
+    }
+    __device__ __forceinline__ int64_t slot(int q) const { return slot0 + q * step + (q == 0 ? per : 0); }
+    __device__ __forceinline__ float4 load(int q, int lane) const {
+        return __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(q) * D) + lane);
+    }
+    // The slice's sum of weight_of(q) times part q over q = slice, slice + slices, ...; the first parts are in x already.
+    template <typename W>
+    __device__ __forceinline__ float4 sum(float4 (&x)[kAhead], int slice, int slices, int rounds, int lane, W weight_of) const {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int q0 = slice; rounds > 0; --rounds, q0 += kAhead * slices)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int q = q0 + i * slices;
+                const float w = weight_of(q);
+                o.x += x[i].x * w;
+                o.y += x[i].y * w;
+                o.z += x[i].z * w;
+                o.w += x[i].w * w;
+                const int next = q + kAhead * slices;
+                if (next < cut.z) x[i] = load(next, lane);
+            }
+        return o;
+    }
+    __device__ __forceinline__ void request(float4 (&x)[kAhead], int slice, int slices, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int q = slice + i * slices;
+            x[i] = q < cut.z ? load(q, lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+    __device__ __forceinline__ void store(const float4& o, float m, float l, int lane) const {
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F;
+        uint2 w;
+        w.x = Num<T>::pack(o.x * inv, o.y * inv);
+        w.y = Num<T>::pack(o.z * inv, o.w * inv);
+        *reinterpret_cast<uint2*>((T*)p.out + cut.x * p.out_stride + (int64_t)(h0 + r) * D + 4 * lane) = w;
+        if (p.lse && lane == 0)
+            p.lse[(int64_t)cut.x * p.hq + h0 + r] = l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
+    }
+};
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float weight_for(float m, float top) { return m == top ? 1.f : ex2(m - top); }
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const __grid_constant__ AttnParams p, int32_t ctas) {
-    constexpr int kLanes = D / 4;            // a lane owns 4 dims
-    constexpr int kSlices = kJoinThreads / kLanes;
-    extern __shared__ int4 list[];           // [ctas]: the cuts; .w is the CTA that a segment begins in
-    __shared__ float sm_m[kSlices], sm_l[kSlices];
-    __shared__ float4 sm_o[kSlices][kLanes];
-    __shared__ int sm_count[kJoinThreads / 32];
-    const int lane = threadIdx.x % kLanes, slice = threadIdx.x / kLanes;
+    using J = Joiner<T, D>;
+    constexpr int kLanes = J::kLanes, kWarps = kJoinThreads / 32;
+    extern __shared__ int4 list[];           // [ctas]: segments of few parts from the front, of many from the back; [ctas] weights
+    float* weight = reinterpret_cast<float*>(list + ctas);
+    __shared__ float4 sm_o[kJoinThreads / kLanes][kLanes];
+    __shared__ float sm_l[kWarps];
+    __shared__ int sm_count[2][kWarps];
+    const int tid = threadIdx.x, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    int count = 0;
+    int few = 0, many = 0;
     for (int i0 = 0; i0 < ctas; i0 += kJoinThreads) {
-        const int i = i0 + threadIdx.x;
+        const int i = i0 + tid;
         const int4 cut = i < ctas ? __ldcg(p.cuts + i) : make_int4(0, 0, 0, 0);
-        const unsigned some = __ballot_sync(0xffffffffu, cut.z != 0);
-        if ((threadIdx.x & 31) == 0) sm_count[threadIdx.x >> 5] = __popc(some);
-        __syncthreads();
-        int at = count + __popc(some & ((1u << (threadIdx.x & 31)) - 1));
-        for (int w = 0; w < kJoinThreads / 32; ++w) {
-            if (w < (int)(threadIdx.x >> 5)) at += sm_count[w];
-            count += sm_count[w];
+        const bool is_few = cut.z > 0 && cut.z <= kFewParts, is_many = cut.z > kFewParts;
+        const unsigned a = __ballot_sync(0xffffffffu, is_few), b = __ballot_sync(0xffffffffu, is_many);
+        const unsigned below = (1u << (tid & 31)) - 1;
+        if ((tid & 31) == 0) {
+            sm_count[0][warp] = __popc(a);
+            sm_count[1][warp] = __popc(b);
         }
-        if (cut.z != 0) list[at] = make_int4(cut.x, cut.y, cut.z, i);
+        __syncthreads();
+        int at_few = few + __popc(a & below), at_many = many + __popc(b & below);
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) {
+                at_few += sm_count[0][w];
+                at_many += sm_count[1][w];
+            }
+            few += sm_count[0][w];
+            many += sm_count[1][w];
+        }
+        if (is_few) list[at_few] = make_int4(cut.x, cut.y, cut.z, i);
+        if (is_many) list[ctas - 1 - at_many] = make_int4(cut.x, cut.y, cut.z, i);
         __syncthreads();
     }
-    const int per = p.units * p.rows;
-    for (int item = blockIdx.x; item < count * per; item += gridDim.x) {
-        {
-            const int seg = item / per, k = item - seg * per;
-            const int4 cut = list[seg];
-            const int i = cut.w;
-            const int u = k / p.rows, r = k - u * p.rows;
-            const int unit = cut.y * p.units + u;
-            if (unit >= p.hkv * p.splits) continue;
-            int kv, h0, n;
-            unit_heads(p, unit, &kv, &h0, &n);
-            if (r >= n) continue;
-            float m = kNothing, l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int q = slice; q < cut.z; q += kSlices) {
-                const int64_t slot = (((int64_t)(i + q) * 2 + (q == 0)) * p.units + u) * p.rows + r;
-                const float2 ml = __ldcg(p.part_ml + slot);
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + slot * D) + lane);
-                float w, w2;
-                join_weights(m, ml.x, &m, &w, &w2);
-                l = l * w + ml.y * w2;
-                o.x = o.x * w + x.x * w2;
-                o.y = o.y * w + x.y * w2;
-                o.z = o.z * w + x.z * w2;
-                o.w = o.w * w + x.w * w2;
-            }
-            __syncthreads();
-            if (lane == 0) {
-                sm_m[slice] = m;
-                sm_l[slice] = l;
-            }
-            sm_o[slice][lane] = o;
-            __syncthreads();
-            if (slice == 0) {
-#pragma unroll
-                for (int q = 1; q < kSlices; ++q) {
-                    float w, w2;
-                    join_weights(m, sm_m[q], &m, &w, &w2);
-                    const float4 x = sm_o[q][lane];
-                    l = l * w + sm_l[q] * w2;
-                    o.x = o.x * w + x.x * w2;
-                    o.y = o.y * w + x.y * w2;
-                    o.z = o.z * w + x.z * w2;
-                    o.w = o.w * w + x.w * w2;
-                }
-                const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F;
-                uint2 w;
-                w.x = Num<T>::pack(o.x * inv, o.y * inv);
-                w.y = Num<T>::pack(o.z * inv, o.w * inv);
-                *reinterpret_cast<uint2*>((T*)p.out + cut.x * p.out_stride + (int64_t)(h0 + r) * D + 4 * lane) = w;
-                if (p.lse && lane == 0)
-                    p.lse[(int64_t)cut.x * p.hq + h0 + r] = l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
-            }
+    J j(p);
+    float4 x[J::kAhead];
+    for (int item = blockIdx.x; item < many * j.per; item += gridDim.x) {
+        const int seg = item / j.per;
+        if (!j.set(list[ctas - 1 - seg], item - seg * j.per)) continue;
+        constexpr int kSlices = kJoinThreads / kLanes;
+        const int lane = tid % kLanes, slice = tid / kLanes, parts = j.cut.z;
+        j.request(x, slice, kSlices, lane);
+        float m = kNothing, l = 0.f;         // every warp finds the largest m for itself
+        for (int q = tid & 31; q < parts; q += 32) m = fmaxf(m, __ldcg(&p.part_ml[j.slot(q)].x));
+        m = warp_max(m);
+        for (int q = tid; q < parts; q += kJoinThreads) {
+            const float2 ml = __ldcg(p.part_ml + j.slot(q));
+            weight[q] = weight_for(ml.x, m);
+            l += ml.y * weight[q];
         }
+        l = warp_sum(l);
+        if ((tid & 31) == 0) sm_l[warp] = l;
+        __syncthreads();
+        const int rounds = (parts + J::kAhead * kSlices - 1) / (J::kAhead * kSlices);
+        float4 o = j.sum(x, slice, kSlices, rounds, lane, [&](int q) { return q < parts ? weight[q] : 0.f; });
+        sm_o[slice][lane] = o;
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int q = 1; q < kSlices; ++q) {
+                const float4 y = sm_o[q][lane];
+                o.x += y.x;
+                o.y += y.y;
+                o.z += y.z;
+                o.w += y.w;
+            }
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) l += sm_l[w];
+            j.store(o, m, l, lane);
+        }
+        __syncthreads();                     // weight, sm_l and sm_o are free again
+    }
+    for (int item = blockIdx.x * kWarps + warp; item < few * j.per; item += gridDim.x * kWarps) {
+        const int seg = item / j.per;
+        if (!j.set(list[seg], item - seg * j.per)) continue;
+        constexpr int kSlices = 32 / kLanes;
+        const int lane = (tid & 31) % kLanes, slice = (tid & 31) / kLanes, parts = j.cut.z;
+        j.request(x, slice, kSlices, lane);
+        const float2 ml = (tid & 31) < parts ? __ldcg(p.part_ml + j.slot(tid & 31)) : make_float2(kNothing, 0.f);
+        const float m = warp_max(ml.x), w = weight_for(ml.x, m), l = warp_sum(ml.y * w);
+        const int rounds = (parts + J::kAhead * kSlices - 1) / (J::kAhead * kSlices);
+        float4 o = j.sum(x, slice, kSlices, rounds, lane, [&](int q) {
+            const float v = __shfl_sync(0xffffffffu, w, q & 31);
+            return q < parts ? v : 0.f;
+        });
+        if (kSlices == 2) {
+            o.x += __shfl_xor_sync(0xffffffffu, o.x, 16);
+            o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+            o.z += __shfl_xor_sync(0xffffffffu, o.z, 16);
+            o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+        }
+        if (slice == 0) j.store(o, m, l, lane);
     }
 }
 
@@ -773,9 +867,12 @@ cudaError_t launch_main(const AttnParams& p, const Layout& y, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
     cudaError_t e = y.nt == 1 ? launch_main<T, D, 1>(p, y, s) : launch_main<T, D, 2>(p, y, s);
-    if (e == cudaSuccess && may_cut)
-        e = ps::launch_dependent(paged_join_kernel<T, D>, dim3((unsigned)y.ctas * 8), dim3(kJoinThreads),
-                                 (size_t)y.ctas * sizeof(int4), s, p, y.ctas);
+    if (e == cudaSuccess && may_cut) {
+        // at most one cut segment per CTA, and per chunk of a row
+        const int64_t items = std::min<int64_t>(y.ctas - 1, (int64_t)p.batch * y.chunks) * y.units * y.rows;
+        e = ps::launch_dependent(paged_join_kernel<T, D>, dim3((unsigned)std::min<int64_t>(items, 4 * y.ctas)), dim3(kJoinThreads),
+                                 (size_t)y.ctas * (sizeof(int4) + sizeof(float)), s, p, y.ctas);
+    }
     return e;
 }
 
