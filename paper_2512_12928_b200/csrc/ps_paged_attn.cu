@@ -63,7 +63,7 @@ struct AttnParams {
     int32_t* status;
     float* part_o;       // [cta][2][unit][row][D]
     float2* part_ml;     // [cta][2][unit][row]
-    int4* cuts;          // [cta]: a segment that begins in this CTA and ends in a later one: {row, chunk, parts, 0}
+    int4* cuts;          // [cta]: the segment that this CTA did not finish: {row, chunk, parts, first CTA}; parts 0: none
     int64_t k_block_stride, v_block_stride, q_stride, out_stride;
     int64_t room;        // tokens a table row has room for
     uint64_t block_magic;
@@ -144,14 +144,17 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// Of non-negative numbers.  A division of 64 bits takes a few hundred cycles, and nearly always 32 do.
+__device__ __forceinline__ long long divide(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // t / block_size for 0 <= t < 2^31: magic is 2^64 / block_size rounded up (block_size > 1)
 __device__ __forceinline__ int32_t block_of(int32_t t, const AttnParams& p) {
     return p.block_size == 1 ? t : (int32_t)__umul64hi((uint64_t)(uint32_t)t, p.block_magic);
 }
 
-// Tokens of row b that are attended: [first, end).
-__device__ __forceinline__ void row_span(const AttnParams& p, int b, int32_t* first, int32_t* end) {
-    const int32_t n = p.ctx[b];
+// Tokens that are attended of a row of n: [first, end).
+__device__ __forceinline__ void row_span(const AttnParams& p, int32_t n, int32_t* first, int32_t* end) {
     int32_t e = n < 0 ? 0 : n;
     if ((int64_t)e > p.room) e = (int32_t)p.room;
     if (e != n && p.status) *(volatile int32_t*)p.status = kStatusLength;
@@ -171,8 +174,9 @@ __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* k
 // at multiples of 16 tokens, so that one lies in one block if the block size is such a multiple too.
 struct Cursor {
     int32_t b, chunk, i, tiles, first, end;
-    __device__ __forceinline__ void row(const AttnParams& p) {
-        row_span(p, b, &first, &end);
+    int32_t next_len;                        // of row b + 1, asked for while row b is worked on
+    __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
+        row_span(p, len, &first, &end);
         const int32_t step = kTile * p.subs;
         tiles = end > first ? (end - (first & -kTile) + step - 1) / step : 1;   // an empty row still has a result to write
     }
@@ -182,8 +186,10 @@ struct Cursor {
         if (++chunk < p.chunks) return;
         chunk = 0;
         ++b;
-        if (more) row(p);
+        if (more) row(p, next_len);
+        look_ahead(p);
     }
+    __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? __ldg(p.ctx + b + 1) : 0; }
     // first token of slice `sub` of the tile; may lie at or behind the end
     __device__ __forceinline__ int32_t token(const AttnParams& p, int sub) const { return (first & -kTile) + kTile * (i * p.subs + sub); }
 };
@@ -259,6 +265,13 @@ struct Worker {
         k_src = (const T*)p.kpool + (idle ? 0 : o);
         v_src = (const T*)p.vpool + (idle ? 0 : o);
         table = p.tables + (int64_t)cur.b * p.table_stride;
+        // the unit's queries, into L1: they are loaded when its tiles have come, and then nothing hides their latency
+        const int n = min(p.rows, p.group) * D / 64, h0 = (cur.chunk * p.units + unit_in_cta) / p.splits * p.group +
+                                                         (cur.chunk * p.units + unit_in_cta) % p.splits * p.rows;
+        if (!idle && lane < n && h0 * D + lane * 64 < p.hq * D) {
+            uint32_t unused;
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + cur.b * p.q_stride + (int64_t)h0 * D + lane * 64));
+        }
     }
 
     // Looks the tile's tokens up; at = -1: no token.
@@ -477,7 +490,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     long long mine = 0;
     Cursor cur;
     for (cur.b = b_lo; cur.b < b_hi; ++cur.b) {
-        cur.row(p);
+        cur.row(p, __ldg(p.ctx + cur.b));
         mine += (long long)cur.tiles * p.chunks;
     }
     long long before = mine;
@@ -494,12 +507,12 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         if (w < warp) before += sh_sum[w];
         total += sh_sum[w];
     }
-    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    const long long share = divide(total + gridDim.x - 1, gridDim.x);
     const long long begin = share * blockIdx.x, end = min(total, begin + share);
     if (begin >= before && begin < before + mine) {
         long long a = before;
         for (cur.b = b_lo;; ++cur.b) {
-            cur.row(p);
+            cur.row(p, __ldg(p.ctx + cur.b));
             const long long n = (long long)cur.tiles * p.chunks;
             if (begin < a + n) break;
             a += n;
@@ -511,9 +524,10 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     int4 cut = make_int4(0, 0, 0, 0);
     if (begin < end) {
         cur.b = sh_row;
-        cur.row(p);
+        cur.row(p, __ldg(p.ctx + cur.b));
+        cur.look_ahead(p);
         const long long into = begin - sh_at;
-        cur.chunk = (int)(into / cur.tiles);
+        cur.chunk = (int)divide(into, cur.tiles);
         cur.i = (int)(into - (long long)cur.chunk * cur.tiles);
         Cursor ahead = cur;                      // the tile that is requested next
         Worker<T, D, NT, kOneBlock> wk(p, (uint32_t)__cvta_generic_to_shared(smem));
@@ -600,8 +614,10 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                         }
                     }
                 }
-                if (lo == 0 && !seg_end)
-                    cut = make_int4(cur.b, cur.chunk, (int)((at + cur.tiles - cur.i - 1) / share) - (int)blockIdx.x + 1, 0);
+                if (!seg_end) {
+                    const int from = (int)divide(at - cur.i, share);
+                    cut = make_int4(cur.b, cur.chunk, (int)divide(at + cur.tiles - cur.i - 1, share) - from + 1, from);
+                }
                 fresh = true;
             }
             cur.next(p, at + 1 < end);
@@ -610,12 +626,13 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
 }
 
-// Combines the parts of the rows that a share's end cut: CTA i of the main kernel names in cuts[i] the segment that
-// begins in it and goes on, whose parts are slot 1 of CTA i and slot 0 of the CTAs that follow.  Work items are
-// (segment, unit, query head).  What an item costs is latency, so its loads do not wait for one another: parts are
-// requested while the weights are made from all parts' m.  A segment of few parts (the rows of a batch) is a warp's
-// item, one of many (a long row on much of the chip) a CTA's, whose slices of D / 4 threads take every eighth or
-// sixteenth part.  Sums are taken in a fixed order, so a result does not depend on timing.
+// Combines the parts of the rows that a share's end cut.  cuts[i] names the segment that CTA i of the main kernel did
+// not finish: its row and chunk, its number of parts and the CTA that it begins in.  The parts are slot 1 of that CTA
+// and slot 0 of those that follow.  The CTAs of all cuts of a segment share its work items, (unit, query head) pairs:
+// nothing has to be counted or listed first.  What an item costs is latency, so its loads do not wait for one
+// another: parts are requested while the weights are made from all parts' m.  A segment of few parts (the rows of a
+// batch) is warps' work, one of many (a long row on much of the chip) CTAs', whose slices of D / 4 threads take every
+// eighth or sixteenth part.  Sums are taken in a fixed order, so a result does not depend on timing.
 template <typename T, int D>
 struct Joiner {
     static constexpr int kLanes = D / 4;     // a lane owns 4 dims
@@ -692,47 +709,23 @@ __device__ __forceinline__ float weight_for(float m, float top) { return m == to
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads)
-paged_join_kernel(const __grid_constant__ AttnParams p, int32_t ctas) {
+paged_join_kernel(const __grid_constant__ AttnParams p) {
     using J = Joiner<T, D>;
     constexpr int kLanes = J::kLanes, kWarps = kJoinThreads / 32;
-    extern __shared__ int4 list[];           // [ctas]: segments of few parts from the front, of many from the back; [ctas] weights
-    float* weight = reinterpret_cast<float*>(list + ctas);
+    extern __shared__ float weight[];        // [ctas]
     __shared__ float4 sm_o[kJoinThreads / kLanes][kLanes];
     __shared__ float sm_l[kWarps];
-    __shared__ int sm_count[2][kWarps];
     const int tid = threadIdx.x, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    int few = 0, many = 0;
-    for (int i0 = 0; i0 < ctas; i0 += kJoinThreads) {
-        const int i = i0 + tid;
-        const int4 cut = i < ctas ? __ldcg(p.cuts + i) : make_int4(0, 0, 0, 0);
-        const bool is_few = cut.z > 0 && cut.z <= kFewParts, is_many = cut.z > kFewParts;
-        const unsigned a = __ballot_sync(0xffffffffu, is_few), b = __ballot_sync(0xffffffffu, is_many);
-        const unsigned below = (1u << (tid & 31)) - 1;
-        if ((tid & 31) == 0) {
-            sm_count[0][warp] = __popc(a);
-            sm_count[1][warp] = __popc(b);
-        }
-        __syncthreads();
-        int at_few = few + __popc(a & below), at_many = many + __popc(b & below);
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) {
-                at_few += sm_count[0][w];
-                at_many += sm_count[1][w];
-            }
-            few += sm_count[0][w];
-            many += sm_count[1][w];
-        }
-        if (is_few) list[at_few] = make_int4(cut.x, cut.y, cut.z, i);
-        if (is_many) list[ctas - 1 - at_many] = make_int4(cut.x, cut.y, cut.z, i);
-        __syncthreads();
-    }
+    // grid: (CTAs per cut, cuts)
+    const int4 cut = __ldcg(p.cuts + blockIdx.y);
+    if (cut.z == 0) return;
+    const int first = (blockIdx.y - cut.w) * gridDim.x + blockIdx.x, sharers = (cut.z - 1) * gridDim.x;
     J j(p);
     float4 x[J::kAhead];
-    for (int item = blockIdx.x; item < many * j.per; item += gridDim.x) {
-        const int seg = item / j.per;
-        if (!j.set(list[ctas - 1 - seg], item - seg * j.per)) continue;
+    for (int item = first; cut.z > kFewParts && item < j.per; item += sharers) {
+        if (!j.set(cut, item)) continue;
         constexpr int kSlices = kJoinThreads / kLanes;
         const int lane = tid % kLanes, slice = tid / kLanes, parts = j.cut.z;
         j.request(x, slice, kSlices, lane);
@@ -767,9 +760,8 @@ paged_join_kernel(const __grid_constant__ AttnParams p, int32_t ctas) {
         }
         __syncthreads();                     // weight, sm_l and sm_o are free again
     }
-    for (int item = blockIdx.x * kWarps + warp; item < few * j.per; item += gridDim.x * kWarps) {
-        const int seg = item / j.per;
-        if (!j.set(list[seg], item - seg * j.per)) continue;
+    for (int item = first * kWarps + warp; cut.z <= kFewParts && item < j.per; item += sharers * kWarps) {
+        if (!j.set(cut, item)) continue;
         constexpr int kSlices = 32 / kLanes;
         const int lane = (tid & 31) % kLanes, slice = (tid & 31) / kLanes, parts = j.cut.z;
         j.request(x, slice, kSlices, lane);
@@ -868,10 +860,8 @@ template <typename T, int D>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
     cudaError_t e = y.nt == 1 ? launch_main<T, D, 1>(p, y, s) : launch_main<T, D, 2>(p, y, s);
     if (e == cudaSuccess && may_cut) {
-        // at most one cut segment per CTA, and per chunk of a row
-        const int64_t items = std::min<int64_t>(y.ctas - 1, (int64_t)p.batch * y.chunks) * y.units * y.rows;
-        e = ps::launch_dependent(paged_join_kernel<T, D>, dim3((unsigned)std::min<int64_t>(items, 4 * y.ctas)), dim3(kJoinThreads),
-                                 (size_t)y.ctas * (sizeof(int4) + sizeof(float)), s, p, y.ctas);
+        const dim3 grid((unsigned)((y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
+        e = ps::launch_dependent(paged_join_kernel<T, D>, grid, dim3(kJoinThreads), (size_t)y.ctas * sizeof(float), s, p);
     }
     return e;
 }
