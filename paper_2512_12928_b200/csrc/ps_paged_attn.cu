@@ -27,9 +27,9 @@
 // The join is a second launch rather than a last-arrival counter in the first: the workspace then needs no
 // initial state, and neither a replayed graph nor a call that shares it in turn can find a stale counter.
 //
-// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of
-// two); the units of a token are neighbours in memory.  The slices' states are combined pairwise through shared
-// memory at a segment's end.
+// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of two); the
+// units of a token are neighbours in memory.  The slices' states are combined through shared memory at a
+// segment's end.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -71,6 +71,8 @@ struct AttnParams {
     int32_t hkv, hq, group;          // group: query heads per KV head
     int32_t splits, rows;            // a KV head's query heads are cut into `splits` units of `rows` heads
     int32_t units, chunks, subs;     // units per CTA, CTAs' worth of units per row, token slices
+    int32_t ctas;                    // of the main kernel
+    int32_t step_log2;               // tokens of a tile of all slices
     float scale_log2e;
 };
 
@@ -119,11 +121,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// 16 bytes to shared memory, read once
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t policy) {
-    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
-}
-// the same, or zeros where bytes is 0, and then src is not read
+// 16 bytes to shared memory, read once; zeros where bytes is 0, and then src is not read
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(bytes), "l"(policy)
                  : "memory");
@@ -144,10 +142,6 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// Of non-negative numbers.  A division of 64 bits takes a few hundred cycles, and nearly always 32 do.
-__device__ __forceinline__ long long divide(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
 // t / block_size for 0 <= t < 2^31: magic is 2^64 / block_size rounded up (block_size > 1)
 __device__ __forceinline__ int32_t block_of(int32_t t, const AttnParams& p) {
     return p.block_size == 1 ? t : (int32_t)__umul64hi((uint64_t)(uint32_t)t, p.block_magic);
@@ -177,8 +171,8 @@ struct Cursor {
     int32_t next_len;                        // of row b + 1, asked for while row b is worked on
     __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
         row_span(p, len, &first, &end);
-        const int32_t step = kTile * p.subs;
-        tiles = end > first ? (end - (first & -kTile) + step - 1) / step : 1;   // an empty row still has a result to write
+        // an empty row still has a result to write
+        tiles = end > first ? (end - (first & -kTile) + (1 << p.step_log2) - 1) >> p.step_log2 : 1;
     }
     __device__ __forceinline__ void next(const AttnParams& p, bool more) {
         if (++i < tiles) return;
@@ -299,27 +293,17 @@ struct Worker {
             const int32_t lo = max(cur.first - t0, 0), hi = min(cur.end - t0, kTile);
             const uint32_t mask = read && hi > lo ? (0xffffu >> (kTile - hi)) & (0xffffu << lo) : 0u;
             masks |= (uint64_t)mask << 48;
+            // rows that are not read lie in the pool all the same: in this block, or in the first
             const T* k = k_src + (read ? id * p.k_block_stride + at * tok : 0);
             const T* v = v_src + (read ? id * p.v_block_stride + at * tok : 0);
-            if (mask == 0xffffu) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i, k += 4 * tok, v += 4 * tok)
+            for (int i = 0; i < 4; ++i, k += 4 * tok, v += 4 * tok) {
+                const uint32_t bytes = (mask >> (4 * i + (lane >> 3)) & 1) << 4;
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) {
-                        const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
-                        copy16(to, k + 64 * j, policy);
-                        copy16(to + R::kSideBytes, v + 64 * j, policy);
-                    }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool on = mask >> (4 * i + (lane >> 3)) & 1;
-#pragma unroll
-                    for (int j = 0; j < D / 64; ++j) {
-                        const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
-                        copy16(to, on ? k + i * 4 * tok + 64 * j : (const T*)p.kpool, on ? 16 : 0, policy);
-                        copy16(to + R::kSideBytes, on ? v + i * 4 * tok + 64 * j : (const T*)p.vpool, on ? 16 : 0, policy);
-                    }
+                for (int j = 0; j < D / 64; ++j) {
+                    const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
+                    copy16(to, k + 64 * j, bytes, policy);
+                    copy16(to + R::kSideBytes, v + 64 * j, bytes, policy);
                 }
             }
         } else {
@@ -329,33 +313,42 @@ struct Worker {
             for (int i = 0; i < 4; ++i) {
                 const int row = 4 * i + (lane >> 3);
                 const int32_t b = __shfl_sync(0xffffffffu, id_or, row), a = __shfl_sync(0xffffffffu, at, row);
-                const bool on = b >= 0;
-                const T* k = on ? k_src + (b * p.k_block_stride + a * tok) : (const T*)p.kpool;
-                const T* v = on ? v_src + (b * p.v_block_stride + a * tok) : (const T*)p.vpool;
+                const uint32_t bytes = b >= 0 ? 16 : 0;
+                const T* k = k_src + (b >= 0 ? b * p.k_block_stride + a * tok : 0);
+                const T* v = v_src + (b >= 0 ? b * p.v_block_stride + a * tok : 0);
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
                     const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
-                    copy16(to, k + (on ? 64 * j : 0), on ? 16 : 0, policy);
-                    copy16(to + R::kSideBytes, v + (on ? 64 * j : 0), on ? 16 : 0, policy);
+                    copy16(to, k + 64 * j, bytes, policy);
+                    copy16(to + R::kSideBytes, v + 64 * j, bytes, policy);
                 }
             }
         }
     }
 
-    // Attends the tile in stage s; `mask`: its tokens that count.
-    __device__ __forceinline__ void attend(int stage, uint32_t mask, State<D, NT>& st) {
+    // The keys of the tile in a stage.
+    __device__ __forceinline__ void read_keys(int stage, uint4 (&k)[D / 16]) const {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) k[j] = ldsm(ring + stage * R::kStageBytes + k_at[j % 4] + 128 * (j / 4));
+    }
+    // Attends that tile; `mask`: its tokens that count.
+    __device__ __forceinline__ void attend(int stage, const uint4 (&k)[D / 16], uint32_t mask, State<D, NT>& st) {
         const uint32_t src = ring + stage * R::kStageBytes;
-        float s[NT][4];
+        float s[NT][4], s2[NT][4];               // two chains of products
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
+            for (int i = 0; i < 4; ++i) s[t][i] = s2[t][i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-            const uint4 k = ldsm(src + k_at[j % 4] + 128 * (j / 4));
+        for (int j = 0; j < D / 16; j += 2)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) Num<T>::mma(s[t], k, q[t][j][0], q[t][j][1]);
-        }
+            for (int t = 0; t < NT; ++t) {
+                Num<T>::mma(s[t], k[j], q[t][j][0], q[t][j][1]);
+                Num<T>::mma(s2[t], k[j + 1], q[t][j + 1][0], q[t][j + 1][1]);
+            }
+        uint4 v[D / 16];                         // asked for before the softmax
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) v[j] = ldsm_t(src + v_at[j % 4] + 128 * (j / 4));
         // s[t][0], [1]: token g, heads 8t + 2c, + 1; [2], [3]: token g + 8.  The weights' exponents:
         float e[NT][4];
         bool over = false;
@@ -363,8 +356,7 @@ struct Worker {
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (mask != 0xffffu && !(mask >> (g + 4 * (i & 2)) & 1)) s[t][i] = -CUDART_INF_F;
-                else s[t][i] *= p.scale_log2e;
+                s[t][i] = mask >> (g + 4 * (i & 2)) & 1 ? (s[t][i] + s2[t][i]) * p.scale_log2e : -CUDART_INF_F;
                 e[t][i] = s[t][i] - st.m[t][i & 1];
                 over |= e[t][i] > Num<T>::kSlack;
             }
@@ -401,11 +393,9 @@ struct Worker {
             pt[t][1] = transpose8(Num<T>::pack(e[t][2], e[t][3]));
         }
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-            const uint4 v = ldsm_t(src + v_at[j % 4] + 128 * (j / 4));
+        for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v, pt[t][0], pt[t][1]);
-        }
+            for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v[j], pt[t][0], pt[t][1]);
     }
 };
 
@@ -425,60 +415,30 @@ __device__ __forceinline__ void state_reset(State<D, NT>& st) {
     }
 }
 
-// Joins another state into st: weights 2^(m - max), 0 for a side that has seen nothing.
-__device__ __forceinline__ void join_weights(float m, float m2, float* m_new, float* w, float* w2) {
-    *m_new = fmaxf(m, m2);
-    *w = m == *m_new ? 1.f : ex2(m - *m_new);
-    *w2 = m2 == *m_new ? 1.f : ex2(m2 - *m_new);
+__device__ __forceinline__ float weight_for(float m, float top) { return m == top ? 1.f : ex2(m - top); }
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F; }
+template <typename T>
+__device__ __forceinline__ float natural_log_sum(float m, float l) {
+    return l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
 }
-
-// Combines the states of the CTA's token slices into slice 0's, in pairs: half of the slices hand theirs over, the
-// other half take it, and so on.  Every warp calls it.
-template <int D, int NT>
-__device__ __forceinline__ void join_slices(State<D, NT>& st, float4* xchg, int units, int unit, int subs, int sub, int lane) {
-    constexpr int kPieces = D / 16 + 1;      // of one column tile: they are handed over one after the other
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-        for (int half = subs >> 1; half > 0; half >>= 1) {
-            if (sub >= half && sub < 2 * half) {
-                float4* x = xchg + ((sub - half) * units + unit) * kPieces * 32 + lane;
-                x[0] = make_float4(st.m[t][0], st.m[t][1], st.l[t][0], st.l[t][1]);
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j)
-                    x[(1 + j) * 32] = make_float4(st.acc[t][j][0], st.acc[t][j][1], st.acc[t][j][2], st.acc[t][j][3]);
-            }
-            __syncthreads();
-            if (sub < half) {
-                const float4* x = xchg + (sub * units + unit) * kPieces * 32 + lane;
-                const float4 ml = x[0];
-                float w[2], w2[2];
-                join_weights(st.m[t][0], ml.x, &st.m[t][0], &w[0], &w2[0]);
-                join_weights(st.m[t][1], ml.y, &st.m[t][1], &w[1], &w2[1]);
-                st.l[t][0] = st.l[t][0] * w[0] + ml.z * w2[0];
-                st.l[t][1] = st.l[t][1] * w[1] + ml.w * w2[1];
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
-                    const float4 y = x[(1 + j) * 32];
-                    st.acc[t][j][0] = st.acc[t][j][0] * w[0] + y.x * w2[0];
-                    st.acc[t][j][1] = st.acc[t][j][1] * w[1] + y.y * w2[1];
-                    st.acc[t][j][2] = st.acc[t][j][2] * w[0] + y.z * w2[0];
-                    st.acc[t][j][3] = st.acc[t][j][3] * w[1] + y.w * w2[1];
-                }
-            }
-            __syncthreads();
-        }
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, const float4& o, float f) {
+    uint2 w;
+    w.x = Num<T>::pack(o.x * f, o.y * f);
+    w.y = Num<T>::pack(o.z * f, o.w * f);
+    *reinterpret_cast<uint2*>(dst) = w;
 }
 
 template <typename T, int D, int NT, bool kOneBlock>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
     using R = Ring<D>;
-    extern __shared__ unsigned char smem_raw[];   // rings of the warps, then the slices' exchange
+    extern __shared__ unsigned char smem_raw[];   // rings of the warps
     // the pieces' places are exclusive-ored within 128 bytes
     unsigned char* smem = smem_raw + (-(uint32_t)__cvta_generic_to_shared(smem_raw) & 127);
-    __shared__ long long sh_sum[kMaxWarps];
-    __shared__ long long sh_at;        // tiles before the CTA's first row
-    __shared__ int sh_row;
+    __shared__ float2 sh_ml[kMaxWarps][8 * NT];
+    __shared__ int sh_sum[kMaxWarps];
+    __shared__ int3 sh_begin;          // the row that the share begins in, the tiles before it, its length
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nwarps = blockDim.x >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -487,59 +447,82 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     // This CTA's share of the sequence row 0 chunk 0, row 0 chunk 1, ..., row 1 chunk 0, ...
     const int per = (p.batch + blockDim.x - 1) / blockDim.x;
     const int b_lo = min(p.batch, (int)threadIdx.x * per), b_hi = min(p.batch, b_lo + per);
-    long long mine = 0;
+    int mine = 0, len = 0;
     Cursor cur;
+#pragma unroll 1
     for (cur.b = b_lo; cur.b < b_hi; ++cur.b) {
-        cur.row(p, __ldg(p.ctx + cur.b));
-        mine += (long long)cur.tiles * p.chunks;
+        len = __ldg(p.ctx + cur.b);
+        cur.row(p, len);
+        mine += cur.tiles * p.chunks;
     }
-    long long before = mine;
+    int before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long n = __shfl_up_sync(0xffffffffu, before, o);
+        const int n = __shfl_up_sync(0xffffffffu, before, o);
         if (lane >= o) before += n;
     }
     if (lane == 31) sh_sum[warp] = before;
     __syncthreads();
-    long long total = 0;
-    before -= mine;
-    for (int w = 0; w < nwarps; ++w) {
-        if (w < warp) before += sh_sum[w];
-        total += sh_sum[w];
+    int sums = lane < nwarps ? sh_sum[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < kMaxWarps; o <<= 1) {
+        const int n = __shfl_up_sync(0xffffffffu, sums, o);
+        if (lane >= o) sums += n;
     }
-    const long long share = divide(total + gridDim.x - 1, gridDim.x);
-    const long long begin = share * blockIdx.x, end = min(total, begin + share);
+    const int total = __shfl_sync(0xffffffffu, sums, kMaxWarps - 1);
+    const int earlier = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+    before += (warp > 0 ? earlier : 0) - mine;
+    const int share = (total + gridDim.x - 1) / gridDim.x;
+    const int begin = share * blockIdx.x, end = min(total, begin + share);
     if (begin >= before && begin < before + mine) {
-        long long a = before;
-        for (cur.b = b_lo;; ++cur.b) {
-            cur.row(p, __ldg(p.ctx + cur.b));
-            const long long n = (long long)cur.tiles * p.chunks;
-            if (begin < a + n) break;
-            a += n;
-        }
-        sh_row = cur.b;
-        sh_at = a;
+        int a = before;
+        if (per == 1) cur.b = b_lo;              // and the length is still there
+        else
+#pragma unroll 1
+            for (cur.b = b_lo;; ++cur.b) {
+                len = __ldg(p.ctx + cur.b);
+                cur.row(p, len);
+                const int n = cur.tiles * p.chunks;
+                if (begin < a + n) break;
+                a += n;
+            }
+        sh_begin = make_int3(cur.b, a, len);
     }
     __syncthreads();
     int4 cut = make_int4(0, 0, 0, 0);
     if (begin < end) {
-        cur.b = sh_row;
-        cur.row(p, __ldg(p.ctx + cur.b));
+        cur.b = sh_begin.x;
         cur.look_ahead(p);
-        const long long into = begin - sh_at;
-        cur.chunk = (int)divide(into, cur.tiles);
-        cur.i = (int)(into - (long long)cur.chunk * cur.tiles);
+        cur.row(p, sh_begin.z);
+        cur.i = begin - sh_begin.y;
+        cur.chunk = 0;
+        if (p.chunks > 1) {
+            cur.chunk = cur.i / cur.tiles;
+            cur.i -= cur.chunk * cur.tiles;
+        }
         Cursor ahead = cur;                      // the tile that is requested next
         Worker<T, D, NT, kOneBlock> wk(p, (uint32_t)__cvta_generic_to_shared(smem));
-        float4* xchg = reinterpret_cast<float4*>(smem + nwarps * R::kWarpBytes);
-        long long asked = begin;
+        int asked = begin;
         int slot = 0;                            // stage that is filled next
         wk.enter(ahead);
         wk.load_ids(ahead);
-        auto request = [&]() {
+        State<D, NT> st;
+        int kv = 0, h0 = 0, n = 0;
+        int32_t lo = 0;
+        bool fresh = true;
+#pragma unroll 1
+        for (int at = begin - (R::kStages - 1); at < end; ++at) {   // the first rounds only fill the ring
+            copies_wait<R::kStages - 2>();
+            __syncwarp();                        // the other lanes' copies too, and they have left the stage before
+            // the oldest of the kStages - 1 masks
+            const uint32_t mask = (uint32_t)(wk.masks >> (16 * (5 - R::kStages))) & 0xffffu;
             wk.masks >>= 16;
+            const int filled = slot;             // the stage that the tile before left
+            slot = slot + 1 == R::kStages ? 0 : slot + 1;       // the oldest
+            uint4 k[D / 16];
+            wk.read_keys(slot, k);               // in the first rounds what it reads is not used
             if (asked < end) {
-                wk.copy_tile(ahead, slot);
+                wk.copy_tile(ahead, filled);
                 if (++asked < end) {
                     ahead.next(p, true);
                     if (ahead.i == 0) wk.enter(ahead);
@@ -547,15 +530,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 }
             }
             copies_commit();
-            slot = slot + 1 == R::kStages ? 0 : slot + 1;
-        };
-#pragma unroll
-        for (int s = 0; s < R::kStages - 1; ++s) request();
-        State<D, NT> st;
-        int kv = 0, h0 = 0, n = 0;
-        int32_t lo = 0;
-        bool fresh = true;
-        for (long long at = begin; at < end; ++at) {
+            if (at < begin) continue;
             const int unit = cur.chunk * p.units + wk.unit_in_cta;
             if (fresh) {
                 state_reset(st);
@@ -565,58 +540,73 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 lo = cur.i;
                 fresh = false;
             }
-            copies_wait<R::kStages - 2>();
-            __syncwarp();                        // the other lanes' copies too, and they have left the stage before
-            // the oldest of the kStages - 1 masks
-            const uint32_t mask = (uint32_t)(wk.masks >> (16 * (5 - R::kStages))) & 0xffffu;
-            request();                           // into the stage that the tile before left
-            wk.attend(slot, mask, st);           // after the request the oldest stage is the next to be filled
+            wk.attend(slot, k, mask, st);
             const bool seg_end = cur.i + 1 == cur.tiles;
             if (seg_end || at + 1 == end) {
                 const bool whole = lo == 0 && seg_end;
-                join_slices(st, xchg, p.units, wk.unit_in_cta, p.subs, wk.sub, lane);
-                if (wk.sub == 0) {
+                // The states of the slices go through the stage that has just been read, heads as rows, and come
+                // back as rows of four dims a lane.  (The places' exclusive or keeps the writes free of conflicts.)
+                float* own = reinterpret_cast<float*>(smem + warp * R::kWarpBytes + slot * R::kStageBytes);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        float inv[2];
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float l = st.l[t][h];
-                            l += __shfl_xor_sync(0xffffffffu, l, 4);
-                            l += __shfl_xor_sync(0xffffffffu, l, 8);
-                            l += __shfl_xor_sync(0xffffffffu, l, 16);
-                            st.l[t][h] = l;
-                            inv[h] = !whole ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F;
-                        }
-                        // an even lane takes its pair's values of the first head, an odd one of the second, so that
-                        // each holds two neighbouring dims
-                        const int odd = wk.g & 1, r = 8 * t + 2 * wk.c + odd;
-                        const int64_t at_part = (((int64_t)blockIdx.x * 2 + (lo == 0)) * p.units + wk.unit_in_cta) * p.rows + r;
-                        T* o = (T*)p.out + cur.b * p.out_stride + (int64_t)(h0 + r) * D + (wk.g & 6);
-                        float* po = p.part_o + at_part * D + (wk.g & 6);
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = 8 * t + 2 * wk.c + h;
 #pragma unroll
                         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float x = st.acc[t][j][2 * e] * inv[0], y = st.acc[t][j][2 * e + 1] * inv[1];
-                                const float z = __shfl_xor_sync(0xffffffffu, odd ? x : y, 4);
-                                const float a0 = odd ? z : x, a1 = odd ? y : z;
-                                if (r < n) {
-                                    if (whole) *reinterpret_cast<uint32_t*>(o + 16 * j + 8 * e) = Num<T>::pack(a0, a1);
-                                    else *reinterpret_cast<float2*>(po + 16 * j + 8 * e) = make_float2(a0, a1);
-                                }
-                            }
-                        if (wk.g < 2 && r < n) {
-                            const float l = odd ? st.l[t][1] : st.l[t][0], m = odd ? st.m[t][1] : st.m[t][0];
-                            if (!whole) p.part_ml[at_part] = make_float2(m, l);
-                            else if (p.lse)
-                                p.lse[(int64_t)cur.b * p.hq + h0 + r] = l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
+                            for (int e = 0; e < 2; ++e) own[r * D + ((16 * j + 8 * e + wk.g) ^ (8 * wk.c))] = st.acc[t][j][2 * e + h];
+                        float l = st.l[t][h];
+                        l += __shfl_xor_sync(0xffffffffu, l, 4);
+                        l += __shfl_xor_sync(0xffffffffu, l, 8);
+                        l += __shfl_xor_sync(0xffffffffu, l, 16);
+                        if (wk.g == 0) sh_ml[warp][r] = make_float2(st.m[t][h], l);
+                    }
+                if (p.subs > 1) __syncthreads(); else __syncwarp();
+                constexpr int kLanes = D / 4, kHeads = 32 / kLanes;      // heads that a warp works on at a time
+                const int dim = 4 * (lane % kLanes);
+                auto put = [&](int r, const float4& o, float m, float l) {
+                    if (whole) {
+                        store4((T*)p.out + cur.b * p.out_stride + (int64_t)(h0 + r) * D + dim, o, inverse_sum(l));
+                        if (p.lse && dim == 0) p.lse[(int64_t)cur.b * p.hq + h0 + r] = natural_log_sum<T>(m, l);
+                    } else {
+                        const int64_t part = (((int64_t)blockIdx.x * 2 + (lo == 0)) * p.units + wk.unit_in_cta) * p.rows + r;
+                        *reinterpret_cast<float4*>(p.part_o + part * D + dim) = o;
+                        if (dim == 0) p.part_ml[part] = make_float2(m, l);
+                    }
+                };
+                auto get = [&](int w, int r) {
+                    return *reinterpret_cast<const float4*>(smem + w * R::kWarpBytes + slot * R::kStageBytes +
+                                                            4 * (r * D + (dim ^ (8 * (r >> 1 & 3)))));
+                };
+                if (p.subs == 1) {
+#pragma unroll 4
+                    for (int r = lane / kLanes; r < n; r += kHeads) put(r, get(warp, r), sh_ml[warp][r].x, sh_ml[warp][r].y);
+                } else {
+#pragma unroll 1
+                    for (int r = wk.sub * kHeads + lane / kLanes; r < n; r += p.subs * kHeads) {
+                        float m = kNothing, l = 0.f;
+                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units) m = fmaxf(m, sh_ml[w][r].x);
+#pragma unroll 2
+                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units) {
+                            const float2 ml = sh_ml[w][r];
+                            const float4 x = get(w, r);
+                            const float f = weight_for(ml.x, m);
+                            l += ml.y * f;
+                            o.x += x.x * f;
+                            o.y += x.y * f;
+                            o.z += x.z * f;
+                            o.w += x.w * f;
                         }
+                        put(r, o, m, l);
                     }
                 }
+                if (p.subs > 1) __syncthreads(); else __syncwarp();      // the stage is free again
                 if (!seg_end) {
-                    const int from = (int)divide(at - cur.i, share);
-                    cut = make_int4(cur.b, cur.chunk, (int)divide(at + cur.tiles - cur.i - 1, share) - from + 1, from);
+                    const int from = (at - cur.i) / share;
+                    cut = make_int4(cur.b, cur.chunk, (at + cur.tiles - cur.i - 1) / share - from + 1, from);
                 }
                 fresh = true;
             }
@@ -636,7 +626,6 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 template <typename T, int D>
 struct Joiner {
     static constexpr int kLanes = D / 4;     // a lane owns 4 dims
-    static constexpr int kAhead = 4;         // parts that a thread requests at a time
     const AttnParams& p;
     int4 cut;                                // row, chunk, parts, first CTA
     int64_t slot0, step;
@@ -660,9 +649,10 @@ struct Joiner {
         return __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(q) * D) + lane);
     }
     // The slice's sum of weight_of(q) times part q over q = slice, slice + slices, ...; the first parts are in x already.
-    template <typename W>
+    template <int kAhead, typename W>
     __device__ __forceinline__ float4 sum(float4 (&x)[kAhead], int slice, int slices, int rounds, int lane, W weight_of) const {
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
         for (int q0 = slice; rounds > 0; --rounds, q0 += kAhead * slices)
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -677,6 +667,7 @@ struct Joiner {
             }
         return o;
     }
+    template <int kAhead>
     __device__ __forceinline__ void request(float4 (&x)[kAhead], int slice, int slices, int lane) const {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -685,13 +676,8 @@ struct Joiner {
         }
     }
     __device__ __forceinline__ void store(const float4& o, float m, float l, int lane) const {
-        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : CUDART_NAN_F;
-        uint2 w;
-        w.x = Num<T>::pack(o.x * inv, o.y * inv);
-        w.y = Num<T>::pack(o.z * inv, o.w * inv);
-        *reinterpret_cast<uint2*>((T*)p.out + cut.x * p.out_stride + (int64_t)(h0 + r) * D + 4 * lane) = w;
-        if (p.lse && lane == 0)
-            p.lse[(int64_t)cut.x * p.hq + h0 + r] = l == 0.f ? -CUDART_INF_F : (m - Num<T>::kLift + log2f(l)) * kLn2;
+        store4((T*)p.out + cut.x * p.out_stride + (int64_t)(h0 + r) * D + 4 * lane, o, inverse_sum(l));
+        if (p.lse && lane == 0) p.lse[(int64_t)cut.x * p.hq + h0 + r] = natural_log_sum<T>(m, l);
     }
 };
 
@@ -705,16 +691,15 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ float weight_for(float m, float top) { return m == top ? 1.f : ex2(m - top); }
-
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 4)
 paged_join_kernel(const __grid_constant__ AttnParams p) {
     using J = Joiner<T, D>;
     constexpr int kLanes = J::kLanes, kWarps = kJoinThreads / 32;
-    extern __shared__ float weight[];        // [ctas]
+    extern __shared__ float weight[];        // [ctas], then [ctas] sums
+    float* sums = weight + p.ctas;
     __shared__ float4 sm_o[kJoinThreads / kLanes][kLanes];
-    __shared__ float sm_l[kWarps];
+    __shared__ float sm_m[kWarps], sm_l[kWarps];
     const int tid = threadIdx.x, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -723,29 +708,40 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
     if (cut.z == 0) return;
     const int first = (blockIdx.y - cut.w) * gridDim.x + blockIdx.x, sharers = (cut.z - 1) * gridDim.x;
     J j(p);
-    float4 x[J::kAhead];
+#pragma unroll 1
     for (int item = first; cut.z > kFewParts && item < j.per; item += sharers) {
         if (!j.set(cut, item)) continue;
-        constexpr int kSlices = kJoinThreads / kLanes;
+        constexpr int kSlices = kJoinThreads / kLanes, kAhead = 6;
         const int lane = tid % kLanes, slice = tid / kLanes, parts = j.cut.z;
+        float4 x[kAhead];
         j.request(x, slice, kSlices, lane);
-        float m = kNothing, l = 0.f;         // every warp finds the largest m for itself
-        for (int q = tid & 31; q < parts; q += 32) m = fmaxf(m, __ldcg(&p.part_ml[j.slot(q)].x));
-        m = warp_max(m);
+        float m = kNothing, l = 0.f;
+#pragma unroll 1
         for (int q = tid; q < parts; q += kJoinThreads) {
             const float2 ml = __ldcg(p.part_ml + j.slot(q));
-            weight[q] = weight_for(ml.x, m);
-            l += ml.y * weight[q];
+            weight[q] = ml.x;
+            sums[q] = ml.y;
+            m = fmaxf(m, ml.x);
+        }
+        m = warp_max(m);
+        if ((tid & 31) == 0) sm_m[warp] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm_m[w]);
+#pragma unroll 1
+        for (int q = tid; q < parts; q += kJoinThreads) {
+            weight[q] = weight_for(weight[q], m);
+            l += sums[q] * weight[q];
         }
         l = warp_sum(l);
         if ((tid & 31) == 0) sm_l[warp] = l;
         __syncthreads();
-        const int rounds = (parts + J::kAhead * kSlices - 1) / (J::kAhead * kSlices);
+        const int rounds = (parts + kAhead * kSlices - 1) / (kAhead * kSlices);
         float4 o = j.sum(x, slice, kSlices, rounds, lane, [&](int q) { return q < parts ? weight[q] : 0.f; });
         sm_o[slice][lane] = o;
         __syncthreads();
         if (slice == 0) {
-#pragma unroll
+#pragma unroll 4
             for (int q = 1; q < kSlices; ++q) {
                 const float4 y = sm_o[q][lane];
                 o.x += y.x;
@@ -758,16 +754,18 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
             for (int w = 0; w < kWarps; ++w) l += sm_l[w];
             j.store(o, m, l, lane);
         }
-        __syncthreads();                     // weight, sm_l and sm_o are free again
+        __syncthreads();                     // what is shared is free again
     }
+#pragma unroll 1
     for (int item = first * kWarps + warp; cut.z <= kFewParts && item < j.per; item += sharers * kWarps) {
         if (!j.set(cut, item)) continue;
-        constexpr int kSlices = 32 / kLanes;
+        constexpr int kSlices = 32 / kLanes, kAhead = 4;
         const int lane = (tid & 31) % kLanes, slice = (tid & 31) / kLanes, parts = j.cut.z;
+        float4 x[kAhead];
         j.request(x, slice, kSlices, lane);
         const float2 ml = (tid & 31) < parts ? __ldcg(p.part_ml + j.slot(tid & 31)) : make_float2(kNothing, 0.f);
         const float m = warp_max(ml.x), w = weight_for(ml.x, m), l = warp_sum(ml.y * w);
-        const int rounds = (parts + J::kAhead * kSlices - 1) / (J::kAhead * kSlices);
+        const int rounds = (parts + kAhead * kSlices - 1) / (kAhead * kSlices);
         float4 o = j.sum(x, slice, kSlices, rounds, lane, [&](int q) {
             const float v = __shfl_sync(0xffffffffu, w, q & 31);
             return q < parts ? v : 0.f;
@@ -800,7 +798,7 @@ Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
     const int32_t all = hkv * y.splits;
     y.chunks = (all + kMaxWarps - 1) / kMaxWarps;
     y.units = (all + y.chunks - 1) / y.chunks;
-    y.subs = kMaxWarps / y.units;
+    for (y.subs = 1; 2 * y.subs * y.units <= kMaxWarps; y.subs *= 2) {}
     y.ctas = sms * kCtaFactor;
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
@@ -813,15 +811,12 @@ Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
 
 constexpr int kMaxDevices = 64;
 
-// Rings of all warps and the exchange of half of the token slices.
-int attn_smem(int dim, int units, int subs) {
-    return 128 + units * subs * (dim == 128 ? Ring<128>::kWarpBytes : Ring<64>::kWarpBytes) +
-           subs / 2 * units * (dim / 16 + 1) * 32 * (int)sizeof(float4);
-}
+// Rings of all warps, and room to begin on a 128-byte boundary.
+int attn_smem(int dim, int warps) { return 128 + warps * (dim == 128 ? Ring<128>::kWarpBytes : Ring<64>::kWarpBytes); }
 
 template <typename T, int D, int NT>
 cudaError_t allow_smem() {
-    const int bytes = attn_smem(D, 1, kMaxWarps);
+    const int bytes = attn_smem(D, kMaxWarps);
     cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     return e;
@@ -852,7 +847,7 @@ cudaError_t device_sms(int* sms) {
 template <typename T, int D, int NT>
 cudaError_t launch_main(const AttnParams& p, const Layout& y, cudaStream_t s) {
     const dim3 grid((unsigned)y.ctas), block((unsigned)(32 * y.units * y.subs));
-    const size_t smem = (size_t)attn_smem(D, y.units, y.subs);
+    const size_t smem = (size_t)attn_smem(D, y.units * y.subs);
     return p.block_size % kTile == 0 ? ps::launch_dependent(paged_attn_kernel<T, D, NT, true>, grid, block, smem, s, p)
                                      : ps::launch_dependent(paged_attn_kernel<T, D, NT, false>, grid, block, smem, s, p);
 }
@@ -861,7 +856,7 @@ cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cuda
     cudaError_t e = y.nt == 1 ? launch_main<T, D, 1>(p, y, s) : launch_main<T, D, 2>(p, y, s);
     if (e == cudaSuccess && may_cut) {
         const dim3 grid((unsigned)((y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
-        e = ps::launch_dependent(paged_join_kernel<T, D>, grid, dim3(kJoinThreads), (size_t)y.ctas * sizeof(float), s, p);
+        e = ps::launch_dependent(paged_join_kernel<T, D>, grid, dim3(kJoinThreads), (size_t)y.ctas * 2 * sizeof(float), s, p);
     }
     return e;
 }
@@ -932,8 +927,11 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     p.block_magic = a.block_size > 1 ? ~0ull / (uint64_t)a.block_size + 1 : 0;
     p.batch = a.batch, p.table_stride = a.table_stride, p.num_blocks = a.num_gpu_blocks, p.block_size = a.block_size, p.window = a.window;
     p.hkv = a.num_kv_heads, p.hq = a.num_q_heads, p.group = a.num_q_heads / a.num_kv_heads;
-    p.splits = y.splits, p.rows = y.rows, p.units = y.units, p.chunks = y.chunks, p.subs = y.subs;
+    p.splits = y.splits, p.rows = y.rows, p.units = y.units, p.chunks = y.chunks, p.subs = y.subs, p.ctas = y.ctas;
+    for (p.step_log2 = 0; (1 << p.step_log2) < kTile * y.subs; ++p.step_log2) {}
     p.scale_log2e = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * kLog2e;
+    if (p.room / (kTile * y.subs) + 2 > (1 << 30) / ((int64_t)a.batch * y.chunks))
+        return bad("ps_paged_attn: the tables of the batch have room for more than 2^30 tiles of tokens");
     // rows that cannot be longer than one tile are never cut
     const int64_t longest = a.window > 0 && a.window < p.room ? a.window : p.room;
     const bool may_cut = longest > (int64_t)kTile * (y.subs - 1);   // a window may begin inside a tile
