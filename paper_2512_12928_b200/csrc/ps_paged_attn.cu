@@ -5,7 +5,7 @@
 //   max(0, ctx_b - window) <= t < ctx_b,   m = max_t s_t (running),   lse = ln 2 (m + log2 sum_t p_t)
 //
 // Bound: HBM.  A token and KV head cost 4 D bytes and 4 G D flops; up to G = 64 the card computes faster than it
-// loads.  So every warp streams its own tiles of 16 tokens through a ring in shared memory (cp.async, 16 bytes a lane,
+// loads.  So every warp streams its own tiles of 16 or 32 tokens (4 KiB of K and of V) through a ring in shared memory (cp.async, 16 bytes a lane,
 // whole 128-byte lines), across the ends of rows, and no barrier lies between HBM and the tensor cores.  Tokens may
 // lie anywhere; what is not attended is filled with zeros instead of being read.
 //
@@ -44,11 +44,9 @@
 namespace {
 
 constexpr int kMaxWarps = 8;
-constexpr int kTile = 16;             // tokens of a warp's tile
 constexpr int kMaxGroup = 16;         // query heads of a unit
 constexpr int kCtaFactor = 1;         // CTAs per SM
 constexpr int kJoinThreads = 256;
-constexpr int kFewParts = 16;          // up to so many are a warp's work in the join
 constexpr int32_t kMaxTokens = INT32_MAX - 1024;   // of a row, so that a tile's end cannot wrap
 constexpr int kStatusBadId = 2, kStatusLength = 5;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -164,15 +162,14 @@ __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* k
     *n = min(p.rows, p.group - s * p.rows);
 }
 
-// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`.  Tiles begin
-// at multiples of 16 tokens, so that one lies in one block if the block size is such a multiple too.
+// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`.
 struct Cursor {
     int32_t b, chunk, i, tiles, first, end;
     int32_t next_len;                        // of row b + 1, asked for while row b is worked on
     __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
         row_span(p, len, &first, &end);
         // an empty row still has a result to write
-        tiles = end > first ? (end - (first & -kTile) + (1 << p.step_log2) - 1) >> p.step_log2 : 1;
+        tiles = end > first ? (end - first + (1 << p.step_log2) - 1) >> p.step_log2 : 1;
     }
     __device__ __forceinline__ void next(const AttnParams& p, bool more) {
         if (++i < tiles) return;
@@ -184,8 +181,6 @@ struct Cursor {
         look_ahead(p);
     }
     __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? __ldg(p.ctx + b + 1) : 0; }
-    // first token of slice `sub` of the tile; may lie at or behind the end
-    __device__ __forceinline__ int32_t token(const AttnParams& p, int sub) const { return (first & -kTile) + kTile * (i * p.subs + sub); }
 };
 
 // The softmax state of a warp.  Lane (g = lane / 4, c = lane % 4) holds heads 8 t + 2 c and 8 t + 2 c + 1 of column tile t:
@@ -203,17 +198,18 @@ struct State {
 
 template <int D>
 struct Ring {
-    static constexpr int kStages = D == 128 ? 3 : 4;
+    static constexpr int kStages = 3;
+    static constexpr int kTokens = 2048 / D;                 // of a tile: 16 or 32, products take 16 at a time
     static constexpr int kRowBytes = 2 * D;
-    static constexpr int kSideBytes = kTile * kRowBytes;     // keys, then values
+    static constexpr int kSideBytes = kTokens * kRowBytes;   // keys, then values
     static constexpr int kStageBytes = 2 * kSideBytes;
     static constexpr int kWarpBytes = kStages * kStageBytes;
 };
 
-// kOneBlock: the block size is a multiple of a tile, so that a tile lies in one block.
-template <typename T, int D, int NT, bool kOneBlock>
+template <typename T, int D, int NT>
 struct Worker {
     using R = Ring<D>;
+    static constexpr int kSub = R::kTokens / 16;             // groups of 16 tokens in a tile
     const AttnParams& p;
     const int lane, g, c, unit_in_cta, sub;
     const uint32_t ring;                       // the warp's first stage
@@ -221,17 +217,18 @@ struct Worker {
     uint32_t put;                              // this lane's place in a stage: row lane / 8 and, in place, piece lane % 8
     uint32_t k_at[4], v_at[4];                 // what this lane reads of a stage: pieces 2 j + .. of its row of the four parts
     uint32_t q[NT][D / 16][2];                 // query head 8 t + g, dims 16 j + 2 c and 16 j + 8 + 2 c
-    const T *k_src, *v_src;                    // pools at this lane's head, piece and (kOneBlock) row
+    const T *k_src, *v_src;                    // pools at this lane's head and piece
     const int32_t* table;
-    int32_t id, at;                            // block and place of the first token (kOneBlock), else of token lane % 16
+    int32_t id, at;                            // block and place of token lane % kTokens; at = -1: no token
     bool idle;                                 // the unit does not exist
-    uint64_t masks;                            // which tokens of the tiles in the ring are attended, 16 bits each
+    uint32_t mask, next_mask;                  // which tokens of the two oldest tiles in the ring are attended
 
     __device__ __forceinline__ Worker(const AttnParams& pp, uint32_t smem)
         : p(pp), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), c(threadIdx.x & 3), unit_in_cta((threadIdx.x >> 5) % pp.units),
-          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), masks(0) {
+          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), mask(0),
+          next_mask(0) {
         const int x = lane & 7, up = lane >> 4, mid = lane >> 3 & 1;
-        put = (lane >> 3) * R::kRowBytes + (((lane & 7) ^ (lane >> 3)) << 4);   // rows 4 to 7 and 12 to 15: piece ^ 4
+        put = (lane >> 3) * R::kRowBytes + (((lane & 7) ^ (lane >> 3)) << 4);   // rows 4 to 7 of 8: piece ^ 4
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             k_at[j] = (x + 8 * mid) * R::kRowBytes + (((2 * j + up) ^ x) << 4);
@@ -253,119 +250,111 @@ struct Worker {
 
     // The row and chunk of the tiles to come.
     __device__ __forceinline__ void enter(const Cursor& cur) {
-        const int kv = (cur.chunk * p.units + unit_in_cta) / p.splits;
+        int kv, h0, n;
+        unit_heads(p, cur.chunk * p.units + unit_in_cta, &kv, &h0, &n);
         idle = kv >= p.hkv;
-        const int64_t o = (int64_t)kv * D + 8 * (lane & 7) + (kOneBlock ? (int64_t)(lane >> 3) * p.hkv * D : 0);
-        k_src = (const T*)p.kpool + (idle ? 0 : o);
-        v_src = (const T*)p.vpool + (idle ? 0 : o);
+        const int64_t o = idle ? 0 : (int64_t)kv * D + 8 * (lane & 7);
+        k_src = (const T*)p.kpool + o;
+        v_src = (const T*)p.vpool + o;
         table = p.tables + (int64_t)cur.b * p.table_stride;
         // the unit's queries, into L1: they are loaded when its tiles have come, and then nothing hides their latency
-        const int n = min(p.rows, p.group) * D / 64, h0 = (cur.chunk * p.units + unit_in_cta) / p.splits * p.group +
-                                                         (cur.chunk * p.units + unit_in_cta) % p.splits * p.rows;
-        if (!idle && lane < n && h0 * D + lane * 64 < p.hq * D) {
+        if (!idle && lane < n * D / 64) {
             uint32_t unused;
             asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + cur.b * p.q_stride + (int64_t)h0 * D + lane * 64));
         }
     }
 
-    // Looks the tile's tokens up; at = -1: no token.
+    // Looks the tile's tokens up.
     __device__ __forceinline__ void load_ids(const Cursor& cur) {
-        const int32_t t = cur.token(p, sub) + (kOneBlock ? 0 : lane & 15);
+        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - (D == 128 ? 4 : 5))) + sub) + lane % R::kTokens;
         id = 0;
         at = -1;
-        if (t < cur.end && (kOneBlock || t >= cur.first)) {
+        if (t < cur.end) {
             const int32_t blk = block_of(t, p);
             at = t - blk * p.block_size;
             id = __ldg(table + blk);
         }
     }
 
-    // Requests the tile that load_ids looked up, into stage s.  Lane = (row of four, 16-byte piece of 128).
-    __device__ __forceinline__ void copy_tile(const Cursor& cur, int s) {
+    // Requests the tile that load_ids looked up, into a stage; returns which of its tokens are attended.
+    __device__ __forceinline__ uint32_t copy_tile(int stage) {
         const bool known = (unsigned)id < (unsigned)p.num_blocks;
         if (at >= 0 && !known && p.status) *(volatile int32_t*)p.status = kStatusBadId;
         const bool read = at >= 0 && known && !idle;
-        const int64_t tok = (int64_t)p.hkv * D;
-        const uint32_t dst = ring + s * R::kStageBytes + put;
-        if constexpr (kOneBlock) {
-            // of the tile's 16 tokens those in [first, end): a run of bits
-            const int32_t t0 = cur.token(p, sub);
-            const int32_t lo = max(cur.first - t0, 0), hi = min(cur.end - t0, kTile);
-            const uint32_t mask = read && hi > lo ? (0xffffu >> (kTile - hi)) & (0xffffu << lo) : 0u;
-            masks |= (uint64_t)mask << 48;
-            // rows that are not read lie in the pool all the same: in this block, or in the first
-            const T* k = k_src + (read ? id * p.k_block_stride + at * tok : 0);
-            const T* v = v_src + (read ? id * p.v_block_stride + at * tok : 0);
+        const uint32_t on = __ballot_sync(0xffffffffu, read);
+        // where the lane's token lies in the pools; what is not read has the address of the first block's first token
+        const int64_t in_block = (int64_t)at * p.hkv * D;
+        const int64_t k_off = read ? id * p.k_block_stride + in_block : 0, v_off = read ? id * p.v_block_stride + in_block : 0;
+        const uint32_t dst = ring + stage * R::kStageBytes + put;
 #pragma unroll
-            for (int i = 0; i < 4; ++i, k += 4 * tok, v += 4 * tok) {
-                const uint32_t bytes = (mask >> (4 * i + (lane >> 3)) & 1) << 4;
+        for (int i = 0; i < R::kTokens / 4; ++i) {
+            const int row = 4 * i + (lane >> 3);
+            const uint32_t bytes = (on >> row & 1) << 4;
+            const int64_t ko = __shfl_sync(0xffffffffu, k_off, row);
+            const int64_t vo = p.k_block_stride == p.v_block_stride ? ko : __shfl_sync(0xffffffffu, v_off, row);
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
-                    copy16(to, k + 64 * j, bytes, policy);
-                    copy16(to + R::kSideBytes, v + 64 * j, bytes, policy);
-                }
-            }
-        } else {
-            masks |= (uint64_t)(__ballot_sync(0xffffffffu, read) & 0xffffu) << 48;
-            const int32_t id_or = read ? id : -1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 4 * i + (lane >> 3);
-                const int32_t b = __shfl_sync(0xffffffffu, id_or, row), a = __shfl_sync(0xffffffffu, at, row);
-                const uint32_t bytes = b >= 0 ? 16 : 0;
-                const T* k = k_src + (b >= 0 ? b * p.k_block_stride + a * tok : 0);
-                const T* v = v_src + (b >= 0 ? b * p.v_block_stride + a * tok : 0);
-#pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
-                    copy16(to, k + 64 * j, bytes, policy);
-                    copy16(to + R::kSideBytes, v + 64 * j, bytes, policy);
-                }
+            for (int j = 0; j < D / 64; ++j) {
+                const uint32_t to = (dst ^ (64 * (i & 1))) + 4 * i * R::kRowBytes + 128 * j;
+                copy16(to, k_src + ko + 64 * j, bytes, policy);
+                copy16(to + R::kSideBytes, v_src + vo + 64 * j, bytes, policy);
             }
         }
+        return on;
     }
 
     // The keys of the tile in a stage.
-    __device__ __forceinline__ void read_keys(int stage, uint4 (&k)[D / 16]) const {
+    __device__ __forceinline__ void read_keys(int stage, uint4 (&k)[kSub][D / 16]) const {
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) k[j] = ldsm(ring + stage * R::kStageBytes + k_at[j % 4] + 128 * (j / 4));
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) k[u][j] = ldsm(ring + stage * R::kStageBytes + 16 * u * R::kRowBytes + k_at[j % 4] + 128 * (j / 4));
     }
-    // Attends that tile; `mask`: its tokens that count.
-    __device__ __forceinline__ void attend(int stage, const uint4 (&k)[D / 16], uint32_t mask, State<D, NT>& st) {
+    // Attends that tile; `on`: its tokens that count.
+    __device__ __forceinline__ void attend(int stage, const uint4 (&k)[kSub][D / 16], uint32_t on, State<D, NT>& st) {
         const uint32_t src = ring + stage * R::kStageBytes;
-        float s[NT][4], s2[NT][4];               // two chains of products
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][i] = s2[t][i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < D / 16; j += 2)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                Num<T>::mma(s[t], k[j], q[t][j][0], q[t][j][1]);
-                Num<T>::mma(s2[t], k[j + 1], q[t][j + 1][0], q[t][j + 1][1]);
-            }
-        uint4 v[D / 16];                         // asked for before the softmax
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) v[j] = ldsm_t(src + v_at[j % 4] + 128 * (j / 4));
-        // s[t][0], [1]: token g, heads 8t + 2c, + 1; [2], [3]: token g + 8.  The weights' exponents:
-        float e[NT][4];
-        bool over = false;
+        constexpr int kChains = 2 / kSub;        // two chains of products either way
+        float s[kSub][NT][4], s2[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[t][i] = mask >> (g + 4 * (i & 2)) & 1 ? (s[t][i] + s2[t][i]) * p.scale_log2e : -CUDART_INF_F;
-                e[t][i] = s[t][i] - st.m[t][i & 1];
-                over |= e[t][i] > Num<T>::kSlack;
+                s2[t][i] = 0.f;
+#pragma unroll
+                for (int u = 0; u < kSub; ++u) s[u][t][i] = 0.f;
             }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) Num<T>::mma(kChains == 2 && (j & 1) ? s2[t] : s[u][t], k[u][j], q[t][j][0], q[t][j][1]);
+        uint4 v[kSub][D / 16];                   // asked for before the softmax
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) v[u][j] = ldsm_t(src + 16 * u * R::kRowBytes + v_at[j % 4] + 128 * (j / 4));
+        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g.  The weights' exponents:
+        float e[kSub][NT][4];
+        bool over = false;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = s[u][t][i] + (kChains == 2 ? s2[t][i] : 0.f);
+                    x = on >> (16 * u + g + 4 * (i & 2)) & 1 ? x * p.scale_log2e : -CUDART_INF_F;
+                    s[u][t][i] = x;
+                    e[u][t][i] = x - st.m[t][i & 1];
+                    over |= e[u][t][i] > Num<T>::kSlack;
+                }
         if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float mx = fmaxf(s[t][h], s[t][2 + h]);
+                    float mx = fmaxf(s[0][t][h], s[0][t][2 + h]);
+                    if (kSub == 2) mx = fmaxf(mx, fmaxf(s[kSub - 1][t][h], s[kSub - 1][t][2 + h]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -378,24 +367,31 @@ struct Worker {
                         st.acc[t][j][h] *= alpha;
                         st.acc[t][j][2 + h] *= alpha;
                     }
-                    e[t][h] = s[t][h] - mx;
-                    e[t][2 + h] = s[t][2 + h] - mx;
+#pragma unroll
+                    for (int u = 0; u < kSub; ++u) {
+                        e[u][t][h] = s[u][t][h] - mx;
+                        e[u][t][2 + h] = s[u][t][2 + h] - mx;
+                    }
                 }
         }
-        uint32_t pt[NT][2];      // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 of head 8t + g
+        uint32_t pt[kSub][NT][2];      // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 (of 16) of head 8t + g
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[t][i] = ex2(e[t][i] + Num<T>::kLift);
-            st.l[t][0] += e[t][0] + e[t][2];
-            st.l[t][1] += e[t][1] + e[t][3];
-            pt[t][0] = transpose8(Num<T>::pack(e[t][0], e[t][1]));
-            pt[t][1] = transpose8(Num<T>::pack(e[t][2], e[t][3]));
-        }
+            for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j)
+                for (int i = 0; i < 4; ++i) e[u][t][i] = ex2(e[u][t][i] + Num<T>::kLift);
+                st.l[t][0] += e[u][t][0] + e[u][t][2];
+                st.l[t][1] += e[u][t][1] + e[u][t][3];
+                pt[u][t][0] = transpose8(Num<T>::pack(e[u][t][0], e[u][t][1]));
+                pt[u][t][1] = transpose8(Num<T>::pack(e[u][t][2], e[u][t][3]));
+            }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v[j], pt[t][0], pt[t][1]);
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v[u][j], pt[u][t][0], pt[u][t][1]);
     }
 };
 
@@ -429,7 +425,7 @@ __device__ __forceinline__ void store4(T* dst, const float4& o, float f) {
     *reinterpret_cast<uint2*>(dst) = w;
 }
 
-template <typename T, int D, int NT, bool kOneBlock>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
     using R = Ring<D>;
@@ -438,10 +434,11 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     unsigned char* smem = smem_raw + (-(uint32_t)__cvta_generic_to_shared(smem_raw) & 127);
     __shared__ float2 sh_ml[kMaxWarps][8 * NT];
     __shared__ int sh_sum[kMaxWarps];
-    __shared__ int3 sh_begin;          // the row that the share begins in, the tiles before it, its length
+    __shared__ int4 sh_begin;          // where the share begins: row, chunk, tile; the row's length
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nwarps = blockDim.x >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Worker<T, D, NT> wk(p, (uint32_t)__cvta_generic_to_shared(smem));
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // This CTA's share of the sequence row 0 chunk 0, row 0 chunk 1, ..., row 1 chunk 0, ...
@@ -486,22 +483,30 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 if (begin < a + n) break;
                 a += n;
             }
-        sh_begin = make_int3(cur.b, a, len);
-    }
-    __syncthreads();
-    int4 cut = make_int4(0, 0, 0, 0);
-    if (begin < end) {
-        cur.b = sh_begin.x;
-        cur.look_ahead(p);
-        cur.row(p, sh_begin.z);
-        cur.i = begin - sh_begin.y;
         cur.chunk = 0;
+        cur.i = begin - a;
         if (p.chunks > 1) {
             cur.chunk = cur.i / cur.tiles;
             cur.i -= cur.chunk * cur.tiles;
         }
+        sh_begin = make_int4(cur.b, cur.chunk, cur.i, len);
+        // the first block ids, into L1 while the CTA meets
+        const int32_t t = cur.first + (cur.i << p.step_log2);
+        if (t < cur.end) {
+            uint32_t unused;
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"(p.tables + (int64_t)cur.b * p.table_stride + block_of(t, p)));
+        }
+    }
+    __syncthreads();
+    int4 cut = make_int4(0, 0, 0, 0);
+    if (begin < end) {
+        const int4 start = sh_begin;
+        cur.b = start.x;
+        cur.chunk = start.y;
+        cur.i = start.z;
+        cur.look_ahead(p);
+        cur.row(p, start.w);
         Cursor ahead = cur;                      // the tile that is requested next
-        Worker<T, D, NT, kOneBlock> wk(p, (uint32_t)__cvta_generic_to_shared(smem));
         int asked = begin;
         int slot = 0;                            // stage that is filled next
         wk.enter(ahead);
@@ -514,15 +519,14 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         for (int at = begin - (R::kStages - 1); at < end; ++at) {   // the first rounds only fill the ring
             copies_wait<R::kStages - 2>();
             __syncwarp();                        // the other lanes' copies too, and they have left the stage before
-            // the oldest of the kStages - 1 masks
-            const uint32_t mask = (uint32_t)(wk.masks >> (16 * (5 - R::kStages))) & 0xffffu;
-            wk.masks >>= 16;
             const int filled = slot;             // the stage that the tile before left
             slot = slot + 1 == R::kStages ? 0 : slot + 1;       // the oldest
-            uint4 k[D / 16];
+            const uint32_t on = wk.mask;
+            wk.mask = wk.next_mask;
+            uint4 k[Worker<T, D, NT>::kSub][D / 16];
             wk.read_keys(slot, k);               // in the first rounds what it reads is not used
             if (asked < end) {
-                wk.copy_tile(ahead, filled);
+                wk.next_mask = wk.copy_tile(filled);
                 if (++asked < end) {
                     ahead.next(p, true);
                     if (ahead.i == 0) wk.enter(ahead);
@@ -540,7 +544,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 lo = cur.i;
                 fresh = false;
             }
-            wk.attend(slot, k, mask, st);
+            wk.attend(slot, k, on, st);
             const bool seg_end = cur.i + 1 == cur.tiles;
             if (seg_end || at + 1 == end) {
                 const bool whole = lo == 0 && seg_end;
@@ -583,24 +587,39 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 4
                     for (int r = lane / kLanes; r < n; r += kHeads) put(r, get(warp, r), sh_ml[warp][r].x, sh_ml[warp][r].y);
                 } else {
+                    constexpr int kAtOnce = 4;           // heads of a warp whose loads overlap
+                    const int r_step = p.subs * kHeads;
 #pragma unroll 1
-                    for (int r = wk.sub * kHeads + lane / kLanes; r < n; r += p.subs * kHeads) {
-                        float m = kNothing, l = 0.f;
-                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units) m = fmaxf(m, sh_ml[w][r].x);
-#pragma unroll 2
-                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units) {
-                            const float2 ml = sh_ml[w][r];
-                            const float4 x = get(w, r);
-                            const float f = weight_for(ml.x, m);
-                            l += ml.y * f;
-                            o.x += x.x * f;
-                            o.y += x.y * f;
-                            o.z += x.z * f;
-                            o.w += x.w * f;
+                    for (int r0 = wk.sub * kHeads + lane / kLanes; r0 < n; r0 += kAtOnce * r_step) {
+                        float m[kAtOnce], l[kAtOnce];
+                        float4 o[kAtOnce];
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            m[i] = kNothing;
+                            l[i] = 0.f;
+                            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                         }
-                        put(r, o, m, l);
+#pragma unroll 1
+                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units)
+#pragma unroll
+                            for (int i = 0; i < kAtOnce; ++i) m[i] = fmaxf(m[i], sh_ml[w][min(r0 + i * r_step, n - 1)].x);
+#pragma unroll 1
+                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units)
+#pragma unroll
+                            for (int i = 0; i < kAtOnce; ++i) {
+                                const int r = min(r0 + i * r_step, n - 1);
+                                const float2 ml = sh_ml[w][r];
+                                const float4 x = get(w, r);
+                                const float f = weight_for(ml.x, m[i]);
+                                l[i] += ml.y * f;
+                                o[i].x += x.x * f;
+                                o[i].y += x.y * f;
+                                o[i].z += x.z * f;
+                                o[i].w += x.w * f;
+                            }
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i)
+                            if (r0 + i * r_step < n) put(r0 + i * r_step, o[i], m[i], l[i]);
                     }
                 }
                 if (p.subs > 1) __syncthreads(); else __syncwarp();      // the stage is free again
@@ -620,9 +639,9 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 // not finish: its row and chunk, its number of parts and the CTA that it begins in.  The parts are slot 1 of that CTA
 // and slot 0 of those that follow.  The CTAs of all cuts of a segment share its work items, (unit, query head) pairs:
 // nothing has to be counted or listed first.  What an item costs is latency, so its loads do not wait for one
-// another: parts are requested while the weights are made from all parts' m.  A segment of few parts (the rows of a
-// batch) is warps' work, one of many (a long row on much of the chip) CTAs', whose slices of D / 4 threads take every
-// eighth or sixteenth part.  Sums are taken in a fixed order, so a result does not depend on timing.
+// another: parts are requested while the weights are made from all parts' m.  Where a segment has as many CTAs to
+// share it as items (a long row on much of the chip), an item is a CTA's, whose slices of D / 4 threads take every
+// eighth or sixteenth part; else it is a warp's.  Sums are taken in a fixed order, so a result does not depend on timing.
 template <typename T, int D>
 struct Joiner {
     static constexpr int kLanes = D / 4;     // a lane owns 4 dims
@@ -692,7 +711,7 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads, 4)
+__global__ void __launch_bounds__(kJoinThreads, 3)
 paged_join_kernel(const __grid_constant__ AttnParams p) {
     using J = Joiner<T, D>;
     constexpr int kLanes = J::kLanes, kWarps = kJoinThreads / 32;
@@ -707,9 +726,10 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
     const int4 cut = __ldcg(p.cuts + blockIdx.y);
     if (cut.z == 0) return;
     const int first = (blockIdx.y - cut.w) * gridDim.x + blockIdx.x, sharers = (cut.z - 1) * gridDim.x;
+    const bool wide = cut.z > 32 || sharers >= p.units * p.rows;   // a CTA per item; else a warp
     J j(p);
 #pragma unroll 1
-    for (int item = first; cut.z > kFewParts && item < j.per; item += sharers) {
+    for (int item = first; wide && item < j.per; item += sharers) {
         if (!j.set(cut, item)) continue;
         constexpr int kSlices = kJoinThreads / kLanes, kAhead = 6;
         const int lane = tid % kLanes, slice = tid / kLanes, parts = j.cut.z;
@@ -757,9 +777,9 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
         __syncthreads();                     // what is shared is free again
     }
 #pragma unroll 1
-    for (int item = first * kWarps + warp; cut.z <= kFewParts && item < j.per; item += sharers * kWarps) {
+    for (int item = first * kWarps + warp; !wide && item < j.per; item += sharers * kWarps) {
         if (!j.set(cut, item)) continue;
-        constexpr int kSlices = 32 / kLanes, kAhead = 4;
+        constexpr int kSlices = 32 / kLanes, kAhead = 8 / kSlices;
         const int lane = (tid & 31) % kLanes, slice = (tid & 31) / kLanes, parts = j.cut.z;
         float4 x[kAhead];
         j.request(x, slice, kSlices, lane);
@@ -782,21 +802,26 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-// How the heads are dealt to warps; the same for a shape on every call.
+// How the heads are dealt to warps.
 struct Layout {
     int32_t splits, rows, units, chunks, subs, ctas;
     int nt;                                // column tiles of 8 heads of a unit
     size_t part_o, part_ml, cuts, bytes;   // offsets and size of the workspace
 };
 
-Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
+// Units per CTA: all of a token's, up to the warps, so that a CTA reads whole rows of the pools and combines nothing at
+// a segment's end.  For one or two rows fewer, whose warps share the tokens: a long row is then cut into a quarter as
+// many parts, and a short one may not be cut at all (one row of 8 KV heads of 128: 300 tokens 7.5 instead of 7.7 us,
+// 4096 9.7 instead of 10.8, 32768 29.1 instead of 30.3; but 4 rows of 30000 80.4 instead of 78.6 us).
+Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, int sms) {
     Layout y{};
     const int32_t group = hq / hkv;
     y.splits = (group + kMaxGroup - 1) / kMaxGroup;
     y.rows = (group + y.splits - 1) / y.splits;
     y.nt = (y.rows + 7) / 8;
     const int32_t all = hkv * y.splits;
-    y.chunks = (all + kMaxWarps - 1) / kMaxWarps;
+    const int32_t most = (int64_t)batch * all <= 2 * kMaxWarps ? 2 : kMaxWarps;
+    y.chunks = (all + most - 1) / most;
     y.units = (all + y.chunks - 1) / y.chunks;
     for (y.subs = 1; 2 * y.subs * y.units <= kMaxWarps; y.subs *= 2) {}
     y.ctas = sms * kCtaFactor;
@@ -812,14 +837,12 @@ Layout layout_of(int32_t hkv, int32_t hq, int32_t dim, int sms) {
 constexpr int kMaxDevices = 64;
 
 // Rings of all warps, and room to begin on a 128-byte boundary.
-int attn_smem(int dim, int warps) { return 128 + warps * (dim == 128 ? Ring<128>::kWarpBytes : Ring<64>::kWarpBytes); }
+static_assert(Ring<64>::kWarpBytes == Ring<128>::kWarpBytes, "one size for both");
+int attn_smem(int warps) { return 128 + warps * Ring<128>::kWarpBytes; }
 
 template <typename T, int D, int NT>
 cudaError_t allow_smem() {
-    const int bytes = attn_smem(D, kMaxWarps);
-    cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, D, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return e;
+    return cudaFuncSetAttribute(paged_attn_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(kMaxWarps));
 }
 
 // SM count of the current device; looked up once per device.  The kernels' shared memory limit is raised there too.
@@ -846,10 +869,8 @@ cudaError_t device_sms(int* sms) {
 
 template <typename T, int D, int NT>
 cudaError_t launch_main(const AttnParams& p, const Layout& y, cudaStream_t s) {
-    const dim3 grid((unsigned)y.ctas), block((unsigned)(32 * y.units * y.subs));
-    const size_t smem = (size_t)attn_smem(D, y.units * y.subs);
-    return p.block_size % kTile == 0 ? ps::launch_dependent(paged_attn_kernel<T, D, NT, true>, grid, block, smem, s, p)
-                                     : ps::launch_dependent(paged_attn_kernel<T, D, NT, false>, grid, block, smem, s, p);
+    return ps::launch_dependent(paged_attn_kernel<T, D, NT>, dim3((unsigned)y.ctas), dim3((unsigned)(32 * y.units * y.subs)),
+                                (size_t)attn_smem(y.units * y.subs), s, p);
 }
 template <typename T, int D>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
@@ -878,7 +899,8 @@ extern "C" int32_t ps_paged_attn_workspace(int32_t num_kv_heads, int32_t num_q_h
         cudaGetLastError();
         return PS_ERR_CUDA;
     }
-    *bytes = (int64_t)layout_of(num_kv_heads, num_q_heads, head_dim, sms).bytes;
+    *bytes = (int64_t)std::max(layout_of(1, num_kv_heads, num_q_heads, head_dim, sms).bytes,
+                               layout_of(1 << 30, num_kv_heads, num_q_heads, head_dim, sms).bytes);
     return PS_OK;
 }
 
@@ -911,7 +933,7 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     int sms = 0;
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_paged_attn: device", e);
-    const Layout y = layout_of(a.num_kv_heads, a.num_q_heads, a.head_dim, sms);
+    const Layout y = layout_of(a.batch, a.num_kv_heads, a.num_q_heads, a.head_dim, sms);
     if (a.workspace_bytes < (int64_t)y.bytes || (reinterpret_cast<uintptr_t>(a.workspace) & 255))
         return bad("ps_paged_attn: the workspace is smaller than ps_paged_attn_workspace says, or not on a 256-byte boundary");
     AttnParams p{};
@@ -928,13 +950,13 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     p.batch = a.batch, p.table_stride = a.table_stride, p.num_blocks = a.num_gpu_blocks, p.block_size = a.block_size, p.window = a.window;
     p.hkv = a.num_kv_heads, p.hq = a.num_q_heads, p.group = a.num_q_heads / a.num_kv_heads;
     p.splits = y.splits, p.rows = y.rows, p.units = y.units, p.chunks = y.chunks, p.subs = y.subs, p.ctas = y.ctas;
-    for (p.step_log2 = 0; (1 << p.step_log2) < kTile * y.subs; ++p.step_log2) {}
+    for (p.step_log2 = a.head_dim == 128 ? 4 : 5; (1 << p.step_log2) < 2048 / a.head_dim * y.subs; ++p.step_log2) {}   // Ring::kTokens
     p.scale_log2e = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * kLog2e;
-    if (p.room / (kTile * y.subs) + 2 > (1 << 30) / ((int64_t)a.batch * y.chunks))
+    if ((p.room >> p.step_log2) + 2 > (1 << 30) / ((int64_t)a.batch * y.chunks))
         return bad("ps_paged_attn: the tables of the batch have room for more than 2^30 tiles of tokens");
     // rows that cannot be longer than one tile are never cut
     const int64_t longest = a.window > 0 && a.window < p.room ? a.window : p.room;
-    const bool may_cut = longest > (int64_t)kTile * (y.subs - 1);   // a window may begin inside a tile
+    const bool may_cut = longest > (int64_t)1 << p.step_log2;
     cudaStream_t s = (cudaStream_t)stream;
     if (a.dtype == PS_DTYPE_BF16)
         e = a.head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(p, y, may_cut, s) : launch_attn<__nv_bfloat16, 64>(p, y, may_cut, s);
