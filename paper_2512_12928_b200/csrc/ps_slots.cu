@@ -8,10 +8,16 @@
 // a time in row order: the free stack and the tables come out as from ps_kv_free and ps_kv_alloc in those orders.
 //
 // The work is a few words per row and token; what bounds it is latency: the chain "load lengths, scan, load a free
-// id, store".  One CTA does all of it (slots_plan_kernel): a scan over the rows needs no second launch, and because
-// one CTA both pushes and pops, a barrier orders them.  Work on blocks and tokens is dealt to threads by the scanned
-// prefix (binary search in shared memory), so one long prompt costs the same as many short ones.  With room for
-// many tokens the map itself is filled by a second kernel over the whole chip (slots_fill_kernel).
+// id, store".  Two ways, chosen by the room for tokens:
+//   - slots_one_cta_kernel: one CTA scans, pushes, pops and maps; barriers order its steps and one launch does all.
+//     Up to 4096 tokens (a decode batch: XX us).
+//   - slots_wide_kernel: every CTA scans all rows for itself (cheaper than another launch) and takes its part of
+//     pushes, pops and tokens.  A popped id is found without waiting for the pushes: an index above the old top
+//     belongs to the table of a row that ended, which a search in the scanned counts names.  Where lengths or count are
+//     updated in place, a second kernel of one CTA does that when nobody reads them any more.
+// Work on blocks and tokens is dealt to threads by the scanned counts (binary search in shared memory), so one long
+// prompt costs the same as many short ones.
+#include <algorithm>
 #include <cstdio>
 
 #include "ps_internal.h"
@@ -24,17 +30,19 @@ constexpr int kStatusLength = 5;    // a length, a total or the free count is ou
 constexpr int kStatusBadId = 2;     // a block id outside the pool
 
 constexpr int kMaxThreads = 1024;
-constexpr int kFillThreads = 256;
-constexpr int32_t kFillInPlan = 4096;  // room for at most so many tokens: the plan kernel writes the map itself
-
-struct Plan {
-    int64_t total, need, back;
-    int ok;
-};
+constexpr int kWideThreads = 1024;
+constexpr int32_t kOneCtaTokens = 4096;  // room for at most so many tokens: one CTA
+constexpr int kWideCtas = 148;          // one per SM: each scans all rows
+constexpr int32_t kWideRows = 4096;      // the scanned counts of so many rows fit into shared memory
 
 struct Row {
     int32_t ctx, add, old_blocks, need, back;
 };
+
+// Blocks of n >= 0 tokens; in 32 bits, where a division takes a tenth of one in 64.
+__device__ __forceinline__ int32_t blocks_of(const ps_slots_args& a, int32_t n) {
+    return (int32_t)(((uint32_t)n + (uint32_t)a.block_size - 1u) / (uint32_t)a.block_size);
+}
 
 // Row b's figures; *bad is raised when a length does not fit.
 __device__ __forceinline__ Row load_row(const ps_slots_args& a, int b, bool* bad) {
@@ -46,43 +54,57 @@ __device__ __forceinline__ Row load_row(const ps_slots_args& a, int b, bool* bad
         return r;
     }
     r.ctx = ctx;
-    r.old_blocks = (int32_t)(((int64_t)ctx + a.block_size - 1) / a.block_size);
+    r.old_blocks = blocks_of(a, ctx);
     if (nw == PS_SLOTS_END) {
         r.back = r.old_blocks;
     } else {
         r.add = nw;
-        r.need = (int32_t)(((int64_t)ctx + nw + a.block_size - 1) / a.block_size) - r.old_blocks;
+        r.need = blocks_of(a, ctx + nw) - r.old_blocks;
     }
     return r;
 }
 
-__device__ __forceinline__ int warp_scan(int v) {   // inclusive
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int n = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += n;
-    }
-    return v;
+// What keeps a call with these totals from being carried out; 0: nothing.
+__device__ __forceinline__ int refusal(const ps_slots_args& a, bool bad, int64_t add, int64_t need, int64_t back, int32_t count) {
+    if (bad || add > a.max_tokens) return kStatusLength;
+    if (!a.free_ids) return 0;
+    if (count < 0 || count + back > a.num_gpu_blocks) return kStatusLength;
+    return count + back - need < 0 ? kStatusNoMem : 0;
 }
 
-// Exclusive scans of three values over the CTA; the totals come back in tot.  Every thread calls it.
-__device__ void block_scan3(int (&v)[3], int (&tot)[3], int (*warp_sums)[32]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
-    int inc[3];
+// Three counts; in 64 bits, so that no sum of valid or invalid lengths wraps.
+struct Counts {
+    long long v[3];
+};
+__device__ __forceinline__ void warp_scan3(Counts& c) {   // inclusive
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) inc[k] = warp_scan(v[k]);
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const long long n = __shfl_up_sync(0xffffffffu, c.v[k], o);
+            if (lane >= o) c.v[k] += n;
+        }
+}
+// Exclusive scan over the CTA; the totals come back in all.  Every thread calls it.
+__device__ void cta_scan3(Counts& c, Counts& all, long long (*warp_sums)[32]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+    Counts inc = c;
+    warp_scan3(inc);
     __syncthreads();   // the sums of an earlier call have been read
     if (lane == 31)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) warp_sums[k][warp] = inc[k];
+        for (int k = 0; k < 3; ++k) warp_sums[k][warp] = inc.v[k];
     __syncthreads();
+    Counts w;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) w.v[k] = lane < nwarps ? warp_sums[k][lane] : 0;
+    warp_scan3(w);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        const int s = warp_scan(lane < nwarps ? warp_sums[k][lane] : 0);
-        const int before = __shfl_sync(0xffffffffu, s, warp > 0 ? warp - 1 : 0);
-        tot[k] = __shfl_sync(0xffffffffu, s, 31);
-        v[k] = inc[k] - v[k] + (warp > 0 ? before : 0);
+        all.v[k] = __shfl_sync(0xffffffffu, w.v[k], 31);
+        const long long before = __shfl_sync(0xffffffffu, w.v[k], warp > 0 ? warp - 1 : 0);
+        c.v[k] = inc.v[k] - c.v[k] + (warp > 0 ? before : 0);
     }
 }
 
@@ -99,174 +121,222 @@ __device__ __forceinline__ int row_of(P pfx, int n, int e) {
 }
 
 __global__ void __launch_bounds__(kMaxThreads)
-slots_plan_kernel(const ps_slots_args a, int32_t fill) {
-    __shared__ int warp_sums[3][32];
-    __shared__ int pfx[kMaxThreads + 1], pfx_need[kMaxThreads + 1];
+slots_one_cta_kernel(const ps_slots_args a) {
+    __shared__ long long warp_sums[3][32];
+    __shared__ int pfx[kMaxThreads], pfx_need[kMaxThreads];
     __shared__ int32_t row_ctx[kMaxThreads], row_old[kMaxThreads];
-    __shared__ unsigned long long sum_add, sum_need, sum_back;
-    __shared__ int sh_bad;
     const int tid = threadIdx.x, nt = blockDim.x;
     const bool pool = a.free_ids != nullptr;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (tid == 0) {
-        sum_add = sum_need = sum_back = 0;
-        sh_bad = 0;
-    }
-    __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // totals first: a call that does not fit changes nothing
-    {
-        const int32_t count = pool ? *a.free_count : 0;
-        bool bad = false;
-        long long add = 0, need = 0, back = 0;
-        for (int b = tid; b < a.batch; b += nt) {
-            const Row r = load_row(a, b, &bad);
-            add += r.add;
-            need += r.need;
-            back += r.back;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            add += __shfl_xor_sync(0xffffffffu, add, o);
-            need += __shfl_xor_sync(0xffffffffu, need, o);
-            back += __shfl_xor_sync(0xffffffffu, back, o);
-        }
-        if ((tid & 31) == 0) {
-            if (add) atomicAdd(&sum_add, (unsigned long long)add);
-            if (need) atomicAdd(&sum_need, (unsigned long long)need);
-            if (back) atomicAdd(&sum_back, (unsigned long long)back);
-        }
-        if (bad) sh_bad = kStatusLength;
-        __syncthreads();
-        if (tid == 0) {
-            int code = sh_bad;
-            if (!code && (int64_t)sum_add > a.max_tokens) code = kStatusLength;
-            if (!code && pool) {
-                if (count < 0 || count + (int64_t)sum_back > a.num_gpu_blocks) code = kStatusLength;
-                else if (count + (int64_t)sum_back - (int64_t)sum_need < 0) code = kStatusNoMem;
-            }
-            sh_bad = code;
-            if (code && a.status_word) *(volatile int32_t*)a.status_word = code;
-            if (pool) *a.free_count_out = code ? count : (int32_t)(count + (int64_t)sum_back - (int64_t)sum_need);
-            if (a.batch == 0) a.token_start[0] = 0;
-            sum_need = (unsigned long long)(count + (int64_t)sum_back);   // top of the stack after the pushes
-        }
-        __syncthreads();
+    const int32_t count = pool ? *a.free_count : 0;
+    bool bad = false;
+    Row r{0, 0, 0, 0, 0};
+    Counts c{{0, 0, 0}}, all;
+    for (int b = tid; b < a.batch; b += nt) {
+        r = load_row(a, b, &bad);
+        c.v[0] += r.add;
+        c.v[1] += r.need;
+        c.v[2] += r.back;
     }
-    const bool failed = sh_bad != 0;
-    const int32_t count_after = (int32_t)(int64_t)sum_need;                // valid unless failed
-    const int32_t count = count_after - (int32_t)(int64_t)sum_back;
-    const int32_t total = failed ? 0 : (int32_t)(int64_t)sum_add;
-    if (failed) {
+    cta_scan3(c, all, warp_sums);
+    const int code = refusal(a, __syncthreads_or(bad), all.v[0], all.v[1], all.v[2], count);
+    const int32_t total = code ? 0 : (int32_t)all.v[0];
+    const int32_t top = count + (int32_t)all.v[2];      // of the stack after the pushes
+    if (tid == 0) {
+        if (code && a.status_word) *(volatile int32_t*)a.status_word = code;
+        if (pool) *a.free_count_out = code ? count : (int32_t)(top - all.v[1]);
+        a.token_start[a.batch] = total;
+    }
+    if (code) {
         for (int b = tid; b < a.batch; b += nt) {
             a.ctx_lens_out[b] = a.ctx_lens[b];
-            a.token_start[b + 1] = 0;
+            a.token_start[b] = 0;
         }
-        if (tid == 0) a.token_start[0] = 0;
     } else {
+        const bool once = a.batch <= nt;                 // the scan above is the one that is needed
         // blocks of the rows that end go onto the stack
-        if (pool && sum_back > 0) {
+        if (pool && all.v[2] > 0) {
             int carry = 0;
             for (int c0 = 0; c0 < a.batch; c0 += nt) {
-                bool bad = false;
-                Row r{0, 0, 0, 0, 0};
-                if (c0 + tid < a.batch) r = load_row(a, c0 + tid, &bad);
-                int v[3] = {r.back, 0, 0}, tot[3];
-                block_scan3(v, tot, warp_sums);
-                pfx[tid] = v[0];
+                Counts v = c, tot = all;
+                if (!once) {
+                    r = c0 + tid < a.batch ? load_row(a, c0 + tid, &bad) : Row{0, 0, 0, 0, 0};
+                    v = Counts{{0, 0, r.back}};
+                    cta_scan3(v, tot, warp_sums);
+                }
+                pfx[tid] = (int)v.v[2];
                 __syncthreads();
-                for (int e = tid; e < tot[0]; e += nt) {
+                for (int e = tid; e < (int)tot.v[2]; e += nt) {
                     const int k = row_of(pfx, min(nt, a.batch - c0), e);
                     a.free_ids[count + carry + e] = a.block_tables[(int64_t)(c0 + k) * a.table_stride + (e - pfx[k])];
                 }
-                carry += tot[0];
+                carry += (int)tot.v[2];
                 __syncthreads();
             }
         }
         // growing rows take theirs from the top, and the tokens get their slots
         int carry_tok = 0, carry_need = 0;
         for (int c0 = 0; c0 < a.batch; c0 += nt) {
-            bool bad = false;
-            Row r{0, 0, 0, 0, 0};
-            const int b = c0 + tid;
-            const int rows = min(nt, a.batch - c0);
-            if (b < a.batch) r = load_row(a, b, &bad);
-            int v[3] = {r.add, r.need, 0}, tot[3];
-            block_scan3(v, tot, warp_sums);
-            pfx[tid] = v[0];
-            pfx_need[tid] = v[1];
+            const int b = c0 + tid, rows = min(nt, a.batch - c0);
+            Counts v = c, tot = all;
+            if (!once) {
+                r = b < a.batch ? load_row(a, b, &bad) : Row{0, 0, 0, 0, 0};
+                v = Counts{{r.add, r.need, 0}};
+                cta_scan3(v, tot, warp_sums);
+            }
+            pfx[tid] = (int)v.v[0];
+            pfx_need[tid] = (int)v.v[1];
             row_ctx[tid] = r.ctx;
             row_old[tid] = r.old_blocks;
             if (b < a.batch) {
-                a.ctx_lens_out[b] = r.back > 0 || a.new_lens[b] == PS_SLOTS_END ? 0 : r.ctx + r.add;
-                a.token_start[b] = carry_tok + v[0];
-                if (b == a.batch - 1) a.token_start[a.batch] = carry_tok + v[0] + r.add;
+                a.ctx_lens_out[b] = a.new_lens[b] == PS_SLOTS_END ? 0 : r.ctx + r.add;
+                a.token_start[b] = carry_tok + (int)v.v[0];
             }
             __syncthreads();
             if (pool)
-                for (int e = tid; e < tot[1]; e += nt) {
+                for (int e = tid; e < (int)tot.v[1]; e += nt) {
                     const int k = row_of(pfx_need, rows, e);
                     a.block_tables[(int64_t)(c0 + k) * a.table_stride + row_old[k] + (e - pfx_need[k])] =
-                        __ldcg(a.free_ids + (count_after - 1 - carry_need - e));
+                        __ldcg(a.free_ids + (top - 1 - carry_need - e));
                 }
-            if (fill)
-                for (int e = tid; e < tot[0]; e += nt) {
-                    const int k = row_of(pfx, rows, e);
-                    const int32_t p = row_ctx[k] + (e - pfx[k]);
-                    const int32_t blk = p / a.block_size;
-                    // a block taken in this call is read from the stack, so that no barrier has to order the
-                    // table's store before this load
-                    const int32_t id = pool && blk >= row_old[k]
-                                           ? __ldcg(a.free_ids + (count_after - 1 - carry_need - pfx_need[k] - (blk - row_old[k])))
-                                           : __ldcg(a.block_tables + (int64_t)(c0 + k) * a.table_stride + blk);
-                    const bool in_pool = (unsigned)id < (unsigned)a.num_gpu_blocks;
-                    if (!in_pool && a.status_word) *(volatile int32_t*)a.status_word = kStatusBadId;
-                    a.slots[carry_tok + e] = in_pool ? (int64_t)id * a.block_size + (p - blk * a.block_size) : -1;
-                    if (a.positions) a.positions[carry_tok + e] = p;
-                }
-            carry_tok += tot[0];
-            carry_need += tot[1];
+            for (int e = tid; e < (int)tot.v[0]; e += nt) {
+                const int k = row_of(pfx, rows, e);
+                const int32_t p = row_ctx[k] + (e - pfx[k]);
+                const int32_t blk = (int32_t)((uint32_t)p / (uint32_t)a.block_size);
+                // a block taken in this call is read from the stack, so that no barrier has to order the table's
+                // store before this load
+                const int32_t id = pool && blk >= row_old[k]
+                                       ? __ldcg(a.free_ids + (top - 1 - carry_need - pfx_need[k] - (blk - row_old[k])))
+                                       : __ldcg(a.block_tables + (int64_t)(c0 + k) * a.table_stride + blk);
+                const bool in_pool = (unsigned)id < (unsigned)a.num_gpu_blocks;
+                if (!in_pool && a.status_word) *(volatile int32_t*)a.status_word = kStatusBadId;
+                a.slots[carry_tok + e] = in_pool ? (int64_t)id * a.block_size + (p - blk * a.block_size) : -1;
+                if (a.positions) a.positions[carry_tok + e] = p;
+            }
+            carry_tok += (int)tot.v[0];
+            carry_need += (int)tot.v[1];
             __syncthreads();
         }
     }
-    if (fill)
-        for (int t = total + tid; t < a.max_tokens; t += nt) {
-            a.slots[t] = -1;
-            if (a.positions) a.positions[t] = 0;
-        }
+    for (int t = total + tid; t < a.max_tokens; t += nt) {
+        a.slots[t] = -1;
+        if (a.positions) a.positions[t] = 0;
+    }
 }
 
-// The slot map for many tokens: one thread per token.  The CTA's first and last token are located in the row starts
-// first, so that the threads search a few rows instead of all.
-__global__ void __launch_bounds__(kFillThreads)
-slots_fill_kernel(const ps_slots_args a) {
-    __shared__ int range[2];
+__device__ __forceinline__ void update_row(const ps_slots_args& a, int b, int code) {
+    const int32_t n = a.ctx_lens[b], m = a.new_lens[b];
+    a.ctx_lens_out[b] = code ? n : m == PS_SLOTS_END ? 0 : n + m;
+}
+__device__ __forceinline__ void update_count(const ps_slots_args& a, int code, int32_t count, const Counts& all) {
+    if (a.free_ids) *a.free_count_out = code ? count : (int32_t)(count + all.v[2] - all.v[1]);
+    if (code && a.status_word) *(volatile int32_t*)a.status_word = code;
+}
+
+// Every CTA knows all rows; the CTAs share pushes, pops and tokens.  Reads what it does not write: table entries of
+// blocks that rows have, and the stack below its top.  apart: lengths and count have places of their own to go to.
+__global__ void __launch_bounds__(kWideThreads)
+slots_wide_kernel(const ps_slots_args a, bool apart) {
+    extern __shared__ int32_t rows_smem[];     // [batch] each: tokens, needs, returns before the row; its length
+    int32_t *tok = rows_smem, *need = tok + a.batch, *back = need + a.batch, *ctx = back + a.batch;
+    __shared__ long long warp_sums[3][32];
+    const int tid = threadIdx.x;
+    const bool pool = a.free_ids != nullptr;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int32_t total = __ldcg(a.token_start + a.batch);
-    const int64_t t0 = (int64_t)blockIdx.x * kFillThreads;
-    const int64_t t = t0 + threadIdx.x;
-    if (t0 < total && threadIdx.x < 2)
-        range[threadIdx.x] = row_of(a.token_start, a.batch, threadIdx.x ? (int)min((int64_t)total - 1, t0 + kFillThreads - 1) : (int)t0);
-    __syncthreads();
-    if (t >= a.max_tokens) return;
-    int64_t slot = -1;
-    int32_t p = 0;
-    if (t < total) {
-        const int first = range[0];
-        const int b = first + row_of(a.token_start + first, range[1] - first + 1, (int)t);
-        p = a.ctx_lens_out[b] - (a.token_start[b + 1] - (int32_t)t);
-        const int32_t blk = p / a.block_size;
-        const int32_t id = a.block_tables[(int64_t)b * a.table_stride + blk];
-        if ((unsigned)id < (unsigned)a.num_gpu_blocks)
-            slot = (int64_t)id * a.block_size + (p - blk * a.block_size);
-        else if (a.status_word)
-            *(volatile int32_t*)a.status_word = kStatusBadId;
+    const int32_t count = pool ? *a.free_count : 0;
+    const int per = (a.batch + kWideThreads - 1) / kWideThreads;
+    const int b_lo = min(a.batch, tid * per), b_hi = min(a.batch, b_lo + per);
+    bool bad = false;
+    Row r{0, 0, 0, 0, 0};
+    Counts c{{0, 0, 0}}, all;
+    for (int b = b_lo; b < b_hi; ++b) {
+        r = load_row(a, b, &bad);
+        c.v[0] += r.add;
+        c.v[1] += r.need;
+        c.v[2] += r.back;
     }
-    a.slots[t] = slot;
-    if (a.positions) a.positions[t] = p;
+    cta_scan3(c, all, warp_sums);
+    const int code = refusal(a, __syncthreads_or(bad), all.v[0], all.v[1], all.v[2], count);
+    const bool failed = code != 0;
+    if (apart && blockIdx.x == 0) {
+        for (int b = tid; b < a.batch; b += kWideThreads) update_row(a, b, code);
+        if (tid == 0) update_count(a, code, count, all);
+    }
+    const int32_t total = failed ? 0 : (int32_t)all.v[0];
+    const int32_t top = count + (int32_t)(failed ? 0 : all.v[2]);    // of the stack after the pushes
+    if (!failed) {                              // every total that is used fits 32 bits
+        int at[3] = {(int)c.v[0], (int)c.v[1], (int)c.v[2]};
+        for (int b = b_lo; b < b_hi; ++b) {
+            if (per > 1) r = load_row(a, b, &bad);
+            tok[b] = at[0];
+            need[b] = at[1];
+            back[b] = at[2];
+            ctx[b] = r.ctx;
+            at[0] += r.add;
+            at[1] += r.need;
+            at[2] += r.back;
+        }
+        __syncthreads();
+    }
+    const int64_t me = (int64_t)blockIdx.x * kWideThreads + tid, everyone = (int64_t)gridDim.x * kWideThreads;
+    for (int64_t b = me; b <= a.batch; b += everyone) a.token_start[b] = failed ? 0 : b < a.batch ? tok[b] : total;
+    auto returned = [&](int e) {                // the e-th id that goes back
+        const int k = row_of(back, a.batch, e);
+        return __ldg(a.block_tables + (int64_t)k * a.table_stride + (e - back[k]));
+    };
+    auto popped = [&](int e) {                  // the e-th id that is taken
+        const int at = top - 1 - e;
+        return at < count ? __ldg(a.free_ids + at) : returned(at - count);
+    };
+    if (!failed && pool) {
+        for (int64_t e = me; e < all.v[2]; e += everyone) a.free_ids[count + e] = returned((int)e);
+        for (int64_t e = me; e < all.v[1]; e += everyone) {
+            const int k = row_of(need, a.batch, (int)e);
+            a.block_tables[(int64_t)k * a.table_stride + blocks_of(a, ctx[k]) + ((int)e - need[k])] = popped((int)e);
+        }
+    }
+    for (int64_t t = me; t < a.max_tokens; t += everyone) {
+        int64_t slot = -1;
+        int32_t p = 0;
+        if (t < total) {
+            const int k = row_of(tok, a.batch, (int)t);
+            p = ctx[k] + ((int)t - tok[k]);
+            const int32_t blk = (int32_t)((uint32_t)p / (uint32_t)a.block_size), old_blocks = blocks_of(a, ctx[k]);
+            const int32_t id = pool && blk >= old_blocks ? popped(need[k] + (blk - old_blocks))
+                                                         : __ldg(a.block_tables + (int64_t)k * a.table_stride + blk);
+            if ((unsigned)id < (unsigned)a.num_gpu_blocks) slot = (int64_t)id * a.block_size + (p - blk * a.block_size);
+            else if (a.status_word) *(volatile int32_t*)a.status_word = kStatusBadId;
+        }
+        a.slots[t] = slot;
+        if (a.positions) a.positions[t] = p;
+    }
+}
+
+// Behind slots_wide_kernel: what it read and may be updated in place.
+__global__ void __launch_bounds__(kMaxThreads)
+slots_update_kernel(const ps_slots_args a) {
+    __shared__ long long warp_sums[3][32];
+    const int tid = threadIdx.x;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t count = a.free_ids ? *a.free_count : 0;
+    bool bad = false;
+    Counts c{{0, 0, 0}}, all;
+    for (int b = tid; b < a.batch; b += kMaxThreads) {
+        const Row r = load_row(a, b, &bad);
+        c.v[0] += r.add;
+        c.v[1] += r.need;
+        c.v[2] += r.back;
+    }
+    cta_scan3(c, all, warp_sums);
+    const int code = refusal(a, __syncthreads_or(bad), all.v[0], all.v[1], all.v[2], count);
+    for (int b = tid; b < a.batch; b += kMaxThreads) update_row(a, b, code);
+    if (tid == 0) update_count(a, code, count, all);
 }
 
 }  // namespace
@@ -284,13 +354,21 @@ extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char*
     if (a.free_ids && (!a.free_count || !a.free_count_out))
         return arg_fail(err_buf, err_cap, PS_ERR_INVALID, "ps_build_slots: a free stack needs free_count and free_count_out");
     cudaStream_t s = (cudaStream_t)stream;
-    const bool fill = a.max_tokens <= kFillInPlan;
-    // few rows and tokens: fewer warps make the barriers of the scan cheaper
-    const int threads = a.batch <= 256 && (!fill || a.max_tokens <= 1024) ? 256 : kMaxThreads;
-    cudaError_t e = ps::launch_dependent(slots_plan_kernel, dim3(1), dim3(threads), 0, s, a, (int32_t)fill);
-    if (e == cudaSuccess && !fill)
-        e = ps::launch_dependent(slots_fill_kernel, dim3((unsigned)((a.max_tokens + (int64_t)kFillThreads - 1) / kFillThreads)),
-                                 dim3(kFillThreads), 0, s, a);
+    cudaError_t e;
+    if (a.max_tokens <= kOneCtaTokens || a.batch > kWideRows) {
+        // few rows and tokens: fewer warps make the barriers of the scan cheaper
+        const int threads = a.batch <= 256 && a.max_tokens <= 1024 ? 256 : kMaxThreads;
+        e = ps::launch_dependent(slots_one_cta_kernel, dim3(1), dim3(threads), 0, s, a);
+    } else {
+        // a token a thread, at most a CTA per SM
+        const int ctas = (int)std::min<int64_t>(((int64_t)a.max_tokens + kWideThreads - 1) / kWideThreads, kWideCtas);
+        const size_t smem = (size_t)a.batch * 4 * sizeof(int32_t);
+        const bool apart = a.ctx_lens_out != a.ctx_lens && (!a.free_ids || a.free_count_out != a.free_count);
+        e = smem > 48 << 10 ? cudaFuncSetAttribute(slots_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kWideRows * 4 * sizeof(int32_t)))
+                            : cudaSuccess;
+        if (e == cudaSuccess) e = ps::launch_dependent(slots_wide_kernel, dim3(ctas), dim3(kWideThreads), smem, s, a, apart);
+        if (e == cudaSuccess && !apart) e = ps::launch_dependent(slots_update_kernel, dim3(1), dim3(kMaxThreads), 0, s, a);
+    }
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_build_slots", e);
     return PS_OK;
 }
