@@ -24,7 +24,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHeadDim = 512;
-constexpr int kTokensPerCta = 4;      // most tokens whose sines a CTA keeps: 4 * 256 * 8 bytes
+constexpr int kTokensPerCta = 8;      // most tokens of a CTA
+constexpr int kTwoRounds = 2 * 4 * 148;
 constexpr int kStatusBadSlot = 1;
 
 struct FreqAxes {
@@ -108,91 +109,124 @@ __device__ __forceinline__ void token_setup(const RopeParams& p, const FreqAxes&
 template <typename T>
 struct HeadAt {
     const T* src;
-    T *dst, *dst2;   // dst2: a key that goes to k_out and into the pool
+    T *dst, *dst2;   // dst2: a key that goes to k_out and into the pool; no dst: nothing of the head is written
     bool rotate;
 };
 template <typename T>
-__device__ __forceinline__ HeadAt<T> head_at(const RopeParams& p, int64_t t, int head, const TokenPlace& pl) {
+__device__ __forceinline__ HeadAt<T> head_source(const RopeParams& p, int64_t t, int head) {
     HeadAt<T> h{nullptr, nullptr, nullptr, true};
     if (head < p.hq) {
         h.src = (const T*)p.q + t * p.q_stride + (int64_t)head * p.dim;
+    } else if (head < p.hq + p.hkv) {
+        h.src = (const T*)p.k + t * p.k_stride + (int64_t)(head - p.hq) * p.dim;
+    } else {
+        h.rotate = false;
+        h.src = (const T*)p.v + t * p.v_stride + (int64_t)(head - p.hq - p.hkv) * p.dim;
+    }
+    return h;
+}
+template <typename T>
+__device__ __forceinline__ void head_target(const RopeParams& p, int64_t t, int head, const TokenPlace& pl, HeadAt<T>& h) {
+    if (!pl.live) return;
+    if (head < p.hq) {
         h.dst = (T*)p.q_out + t * p.q_out_stride + (int64_t)head * p.dim;
     } else if (head < p.hq + p.hkv) {
         const int64_t o = (int64_t)(head - p.hq) * p.dim;
-        h.src = (const T*)p.k + t * p.k_stride + o;
         if (p.k_out) h.dst = (T*)p.k_out + t * p.k_out_stride + o;
         if (pl.k_off >= 0) (h.dst ? h.dst2 : h.dst) = (T*)p.kpool + pl.k_off + o;
-    } else {
-        const int64_t o = (int64_t)(head - p.hq - p.hkv) * p.dim;
-        h.rotate = false;
-        h.src = (const T*)p.v + t * p.v_stride + o;
-        if (pl.v_off >= 0) h.dst = (T*)p.vpool + pl.v_off + o;
+    } else if (pl.v_off >= 0) {
+        h.dst = (T*)p.vpool + pl.v_off + (int64_t)(head - p.hq - p.hkv) * p.dim;
     }
-    if (!pl.live) h.dst = h.dst2 = nullptr;
-    return h;
 }
 
 // 16 bytes per access: every address and row is 16-byte aligned, and a pair's partners lie in whole vectors.
-// A head is worked on by `lanes` neighbouring threads (a power of two).
+//
+// A CTA's threads are dealt evenly to its tokens.  A head has `units`: vectors of pairs (two vectors each where the
+// partners lie half a rotation apart) and vectors that pass; a thread has one unit of every `slots`-th head of its
+// token, so its sines stay in registers.  kAtOnce heads are loaded at a time, and the first of them before the sines
+// are made, whose latency hides behind the loads'.
 template <typename T, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads)
-rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads,
-                   int32_t lanes_log2) {
+__global__ void __launch_bounds__(kThreads, 4)
+rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads, int32_t units, int32_t slots) {
     extern __shared__ float2 cs[];
     __shared__ TokenPlace place[kTokensPerCta];
+    constexpr int kPairs = kNeighbours ? 4 : 8, kAtOnce = kNeighbours ? 3 : 2;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     const int n = min(p.tok_per_cta, p.tokens - t0);
+    const int threads = kThreads / p.tok_per_cta;          // of a token
+    const int k = threadIdx.x / threads, me = threadIdx.x - k * threads;
+    const int slot = me / units, lane = me - slot * units;
+    const int64_t t = t0 + k;
+    const int half = p.rot >> 1, turned = kNeighbours ? p.rot >> 3 : half >> 3;
+    // this thread's vectors of a query or key head, and of a value head; -1: none
+    const bool pairs = lane < turned;
+    const int first = pairs || kNeighbours ? 8 * lane : 8 * (turned + lane);      // what passes lies behind both halves
+    const int second = pairs && !kNeighbours ? half + 8 * lane : -1;
+    const int v_first = 8 * lane, v_second = units + lane < (p.dim >> 3) ? 8 * (units + lane) : -1;
+    Vec8<T> a[kAtOnce], b[kAtOnce];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int h = h0 + i * slots;
+            if (h >= heads) continue;
+            const bool value = h >= p.hq + p.hkv;
+            const T* src = h < p.hq ? (const T*)p.q + t * p.q_stride + (int64_t)h * p.dim
+                           : !value ? (const T*)p.k + t * p.k_stride + (int64_t)(h - p.hq) * p.dim
+                                    : (const T*)p.v + t * p.v_stride + (int64_t)(h - p.hq - p.hkv) * p.dim;
+            a[i] = ld8(src + (value ? v_first : first));
+            const int s = value ? v_second : second;
+            if (s >= 0) b[i] = ld8(src + s);
+        }
+    };
+    const bool busy = k < n && slot < slots;
+    if (busy) load(slot);
     token_setup(p, axes, t0, n, cs, place);
     __syncthreads();
-    const int half = p.rot >> 1;
-    const int lane = threadIdx.x & ((1 << lanes_log2) - 1);
-    const int vecs = p.dim >> 3;
-    const int pair_vecs = kNeighbours ? p.rot >> 3 : half >> 3;   // units of the rotated part
-    for (int u = threadIdx.x >> lanes_log2; u < n * heads; u += kThreads >> lanes_log2) {
-        const int k = u / heads, head = u - k * heads;
-        const HeadAt<T> h = head_at<T>(p, t0 + k, head, place[k]);
-        if (!h.dst) continue;
-        int first = 0;
-        if (h.rotate) {
-            const float2* c = cs + k * half;
-            for (int i = lane; i < pair_vecs; i += 1 << lanes_log2) {
-                if (kNeighbours) {
-                    Vec8<T> x = ld8(h.src + 8 * i);
+    if (!busy) return;
+    const TokenPlace pl = place[k];
+    if (!pl.live) return;
+    float2 w[kPairs];
+    if (pairs)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 w = c[4 * i + j];
-                        const float x1 = to_f(x.e[2 * j]), x2 = to_f(x.e[2 * j + 1]);
-                        x.e[2 * j] = from_f<T>(fmaf(x1, w.x, -x2 * w.y));
-                        x.e[2 * j + 1] = from_f<T>(fmaf(x2, w.x, x1 * w.y));
-                    }
-                    st8(h.dst + 8 * i, x);
-                    if (h.dst2) st8(h.dst2 + 8 * i, x);
-                } else {
-                    Vec8<T> a = ld8(h.src + 8 * i), b = ld8(h.src + half + 8 * i);
+        for (int j = 0; j < kPairs; ++j) w[j] = cs[k * half + kPairs * lane + j];
+    for (int h0 = slot; h0 < heads;) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float2 w = c[8 * i + j];
-                        const float x1 = to_f(a.e[j]), x2 = to_f(b.e[j]);
-                        a.e[j] = from_f<T>(fmaf(x1, w.x, -x2 * w.y));
-                        b.e[j] = from_f<T>(fmaf(x2, w.x, x1 * w.y));
-                    }
-                    st8(h.dst + 8 * i, a);
-                    st8(h.dst + half + 8 * i, b);
-                    if (h.dst2) {
-                        st8(h.dst2 + 8 * i, a);
-                        st8(h.dst2 + half + 8 * i, b);
-                    }
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int h = h0 + i * slots;
+            if (h >= heads) continue;
+            const bool value = h >= p.hq + p.hkv;
+            if (pairs && !value)
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    T& e1 = kNeighbours ? a[i].e[(2 * j) & 7] : a[i].e[j];
+                    T& e2 = kNeighbours ? a[i].e[(2 * j + 1) & 7] : b[i].e[j];
+                    const float x1 = to_f(e1), x2 = to_f(e2);
+                    e1 = from_f<T>(fmaf(x1, w[j].x, -x2 * w[j].y));
+                    e2 = from_f<T>(fmaf(x2, w[j].x, x1 * w[j].y));
                 }
+            const int f = value ? v_first : first, s = value ? v_second : second;
+            T *dst = nullptr, *dst2 = nullptr;             // dst2: a key that goes to k_out and into the pool
+            if (h < p.hq) {
+                dst = (T*)p.q_out + t * p.q_out_stride + (int64_t)h * p.dim;
+            } else if (!value) {
+                if (p.k_out) dst = (T*)p.k_out + t * p.k_out_stride + (int64_t)(h - p.hq) * p.dim;
+                if (pl.k_off >= 0) dst2 = (T*)p.kpool + pl.k_off + (int64_t)(h - p.hq) * p.dim;
+            } else if (pl.v_off >= 0) {
+                dst = (T*)p.vpool + pl.v_off + (int64_t)(h - p.hq - p.hkv) * p.dim;
             }
-            first = p.rot >> 3;
+            if (dst) {
+                st8(dst + f, a[i]);
+                if (s >= 0) st8(dst + s, b[i]);
+            }
+            if (dst2) {
+                st8(dst2 + f, a[i]);
+                if (s >= 0) st8(dst2 + s, b[i]);
+            }
         }
-        for (int i = first + lane; i < vecs; i += 1 << lanes_log2) {
-            const Vec8<T> x = ld8(h.src + 8 * i);
-            if (h.dst != h.src) st8(h.dst + 8 * i, x);
-            if (h.dst2) st8(h.dst2 + 8 * i, x);
-        }
+        h0 += kAtOnce * slots;
+        if (h0 < heads) load(h0);
     }
 }
 
@@ -213,7 +247,8 @@ rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_c
     const int units = p.dim - half;   // of a rotated head: its pairs, then the dims that pass
     for (int u = threadIdx.x >> 5; u < n * heads; u += kThreads >> 5) {
         const int k = u / heads, head = u - k * heads;
-        const HeadAt<T> h = head_at<T>(p, t0 + k, head, place[k]);
+        HeadAt<T> h = head_source<T>(p, t0 + k, head);
+        head_target(p, t0 + k, head, place[k], h);
         if (!h.dst) continue;
         for (int i = threadIdx.x & 31; i < (h.rotate ? units : p.dim); i += 32) {
             if (h.rotate && i < half) {
@@ -240,16 +275,18 @@ rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_c
 bool on16(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
 
 template <typename T>
-cudaError_t launch_rope(const RopeParams& p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
+cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
+    const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
+    // few tokens: one per CTA, so that they spread over the chip; many: as many as make a sine per thread, while at
+    // least two rounds of four CTAs per SM are left
+    for (p.tok_per_cta = 1; p.tok_per_cta < kTokensPerCta; p.tok_per_cta *= 2)
+        if (p.tok_per_cta * p.rot > kThreads || 2 * p.tok_per_cta * units > kThreads || p.tokens / (2 * p.tok_per_cta) < kTwoRounds) break;
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
     const size_t smem = (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2);
     if (!vec) return ps::launch_dependent(rope_append_elements_kernel<T>, grid, dim3(kThreads), smem, s, p, axes, heads, neighbours);
-    // threads per head: one per unit of the longer of "pairs" and "all vectors of a value head / 2"
-    const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
-    int log2 = 0;
-    while ((1 << log2) < units && log2 < 5) ++log2;
-    return neighbours ? ps::launch_dependent(rope_append_kernel<T, true>, grid, dim3(kThreads), smem, s, p, axes, heads, log2)
-                      : ps::launch_dependent(rope_append_kernel<T, false>, grid, dim3(kThreads), smem, s, p, axes, heads, log2);
+    const int slots = kThreads / p.tok_per_cta / units;
+    return neighbours ? ps::launch_dependent(rope_append_kernel<T, true>, grid, dim3(kThreads), smem, s, p, axes, heads, units, slots)
+                      : ps::launch_dependent(rope_append_kernel<T, false>, grid, dim3(kThreads), smem, s, p, axes, heads, units, slots);
 }
 
 }  // namespace
@@ -305,8 +342,6 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
     if (do_q) vec = vec && on16(a.q, a.q_stride) && on16(a.q_out, a.q_out_stride);
     if (do_k) vec = vec && on16(a.k, a.k_stride) && on16(a.k_out, a.k_out ? a.k_out_stride : 0);
     if (append) vec = vec && on16(a.v, a.v_stride) && on16(a.kpool, a.k_block_stride) && on16(a.vpool, a.v_block_stride);
-    // few tokens: one per CTA, so that they spread over the chip; many: several, which share the barrier's wait
-    p.tok_per_cta = a.tokens <= 1024 ? 1 : kTokensPerCta;
     cudaError_t e = a.dtype == PS_DTYPE_BF16 ? launch_rope<__nv_bfloat16>(p, axes, heads, neighbours, vec, (cudaStream_t)stream)
                                              : launch_rope<__half>(p, axes, heads, neighbours, vec, (cudaStream_t)stream);
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_rope_append", e);
