@@ -425,12 +425,12 @@ typedef struct ps_rope_args {
     const int64_t* slots;     /* device [tokens]: row of the pools, block * block_size + place; negative = padding */
     const int32_t* positions; /* device: axis a of token t at positions[a * axis_stride + t] */
     const float* inv_freq;    /* device [rot_dim / 2]: radians per unit of position, taken as exact */
-    const int32_t* freq_axis; /* HOST [rot_dim / 2]: the axis of every frequency, or NULL for axis 0 */
     int32_t* status_word;
     int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
     int64_t k_block_stride, v_block_stride, axis_stride;
     int32_t tokens, num_q_heads, num_kv_heads, head_dim, rot_dim, num_axes, block_size, num_gpu_blocks;
     int32_t dtype, flags;     /* ps_dtype; OR of ps_rope_flags */
+    uint8_t freq_axis[256];   /* the axis of every frequency, [rot_dim / 2] of them; zeros: axis 0 */
 } ps_rope_args;
 
 /* Rotary positions on q and k, and the append of the rotated k and of v to the paged pools.  For i < rot_dim / 2 the

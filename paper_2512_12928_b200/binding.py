@@ -12,6 +12,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 from typing import List, Optional, Sequence, Tuple
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -111,9 +113,10 @@ class PsSlotsArgs(C.Structure):
 
 
 class PsRopeArgs(C.Structure):
-    _fields_ = _fields("q k v q_out k_out kpool vpool slots positions inv_freq freq_axis status_word",
-                       "q_stride k_stride v_stride q_out_stride k_out_stride k_block_stride v_block_stride axis_stride",
-                       "tokens num_q_heads num_kv_heads head_dim rot_dim num_axes block_size num_gpu_blocks dtype flags")
+    _fields_ = (_fields("q k v q_out k_out kpool vpool slots positions inv_freq status_word",
+                        "q_stride k_stride v_stride q_out_stride k_out_stride k_block_stride v_block_stride axis_stride",
+                        "tokens num_q_heads num_kv_heads head_dim rot_dim num_axes block_size num_gpu_blocks dtype flags")
+                + [("freq_axis", C.c_uint8 * 256)])
 
 
 class PsPagedAttnArgs(C.Structure):
@@ -191,9 +194,10 @@ def load() -> C.CDLL:
                                  C.POINTER(C.c_double)]),
         "ps_decode_attn_static": (i32, [vp, vp, vp, vp, vp, vp, i32, p32, i32, i32, i32, i32, i32, i32, i32, vp, vp,
                                         C.c_char_p, i32]),
-        "ps_build_slots": (i32, [C.POINTER(PsSlotsArgs), vp, C.c_char_p, i32]),
-        "ps_rope_append": (i32, [C.POINTER(PsRopeArgs), vp, C.c_char_p, i32]),
-        "ps_paged_attn": (i32, [C.POINTER(PsPagedAttnArgs), vp, C.c_char_p, i32]),
+        # the argument structures also come as their bytes (see _packer)
+        "ps_build_slots": (i32, [vp, vp, C.c_char_p, i32]),
+        "ps_rope_append": (i32, [vp, vp, C.c_char_p, i32]),
+        "ps_paged_attn": (i32, [vp, vp, C.c_char_p, i32]),
         "ps_paged_attn_workspace": (i32, [i32, i32, i32, p64]),
     }
     for name, (res, args) in proto.items():
@@ -254,8 +258,39 @@ def ps_decode_attn_static(kpool, vpool, q, out, block_tables, ctx_lens: Sequence
 # does not fit comes back as (PS_ERR_INVALID, text), as from the library.  Work is enqueued on torch's current stream
 # of the tensors' device.
 
+# The calls are made once per layer and step, and a small one takes 3 us on the device: so arguments are packed into the
+# structures' bytes (a ctypes structure of 30 fields takes four times as long to fill) and torch is asked little.
+
 class _BadArg(Exception):
     pass
+
+
+class _ErrorText(threading.local):
+    def __init__(self):
+        self.buf = C.create_string_buffer(256)
+
+
+_error_text = _ErrorText()
+_torch = None
+
+
+def _import_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _packer(cls):
+    """struct.Struct that packs cls's fields in order; None is not accepted, 0 is the null pointer."""
+    codes = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f", C.c_uint8 * 256: "256s"}
+    s = struct.Struct("@" + "".join(codes[f[1]] for f in cls._fields_))
+    assert s.size == C.sizeof(cls)
+    return s.pack
+
+
+_pack_slots, _pack_rope, _pack_attn = _packer(PsSlotsArgs), _packer(PsRopeArgs), _packer(PsPagedAttnArgs)
 
 
 def _need(ok, text: str):
@@ -264,50 +299,49 @@ def _need(ok, text: str):
 
 
 def _vec(name: str, t, dtype, least: int, dev: int) -> int:
-    """Address of a contiguous device tensor of dtype with at least `least` elements."""
-    if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev or t.numel() < least:
+    """Address of a contiguous device tensor of dtype with at least `least` elements; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < least or not t.is_contiguous():
         raise _BadArg(f"{name}: need a contiguous {dtype} tensor of at least {least} elements on device {dev}, "
                       f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(name: str, t, shape, dtype, dev: int) -> int:
+def _rows(name: str, t, rows: int, heads: int, dim: int, dtype, dev: int) -> int:
     """Row stride of [rows][heads][dim] whose rows are dense; the tensor's address is t.data_ptr()."""
     st = t.stride()
-    if (t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != dev or (shape[2] > 1 and st[2] != 1)
-            or (shape[1] > 1 and st[1] != shape[2])):
-        raise _BadArg(f"{name}: need {dtype} {shape} with dense rows on device {dev}, got {t.dtype} {tuple(t.shape)} "
-                      f"strides {st} on {t.device}")
-    return st[0] if shape[0] > 1 else shape[1] * shape[2]
+    if (t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, heads, dim) or (st[2] != 1 and dim > 1)
+            or (st[1] != dim and heads > 1)):
+        raise _BadArg(f"{name}: need {dtype} {(rows, heads, dim)} with dense rows on device {dev}, got {t.dtype} "
+                      f"{tuple(t.shape)} strides {st} on {t.device}")
+    return st[0] if rows > 1 else heads * dim
 
 
-def _pool(name: str, t, shape, dtype, dev: int) -> int:
+def _pool(name: str, t, nb: int, s: int, h: int, d: int, dtype, dev: int) -> int:
     """Block stride of a pool [blocks][block_size][heads][dim] whose blocks are dense."""
     st = t.stride()
-    _, s, h, d = shape
-    if (t.dtype is not dtype or tuple(t.shape) != tuple(shape) or t.get_device() != dev or (d > 1 and st[3] != 1)
-            or (h > 1 and st[2] != d) or (s > 1 and st[1] != h * d)):
-        raise _BadArg(f"{name}: need a {dtype} pool {tuple(shape)} with dense blocks on device {dev}, got {t.dtype} "
+    if (t.dtype is not dtype or t.get_device() != dev or t.shape != (nb, s, h, d) or (st[3] != 1 and d > 1)
+            or (st[2] != d and h > 1) or (st[1] != h * d and s > 1)):
+        raise _BadArg(f"{name}: need a {dtype} pool {(nb, s, h, d)} with dense blocks on device {dev}, got {t.dtype} "
                       f"{tuple(t.shape)} strides {st} on {t.device}")
-    return st[0] if shape[0] > 1 else s * h * d
+    return st[0] if nb > 1 else s * h * d
 
 
-def _enqueue(fn, args, dev: int):
-    import torch
-    err = C.create_string_buffer(256)
+def _enqueue(fn, packed: bytes, dev: int):
+    torch, err = _torch, _error_text.buf
     if torch.cuda.current_device() == dev:
-        rc = fn(C.byref(args), torch.cuda.current_stream(dev).cuda_stream, err, 256)
+        rc = fn(packed, torch._C._cuda_getCurrentRawStream(dev), err, 256)
     else:
         with torch.cuda.device(dev):
-            rc = fn(C.byref(args), torch.cuda.current_stream(dev).cuda_stream, err, 256)
-    return rc, (err.value.decode() if rc else "")
+            rc = fn(packed, torch._C._cuda_getCurrentRawStream(dev), err, 256)
+    return (rc, err.value.decode()) if rc else (0, "")
 
 
-def _dtype_code(t) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
+def _dtype_code(dt) -> int:
+    if dt is _torch.bfloat16:
         return PS_DTYPE_BF16
-    _need(t.dtype is torch.float16, f"need bfloat16 or float16 tensors, got {t.dtype}")
+    _need(dt is _torch.float16, f"need bfloat16 or float16 tensors, got {dt}")
     return PS_DTYPE_FP16
 
 
@@ -319,25 +353,21 @@ def ps_build_slots(ctx_lens, new_lens, block_tables, slots, positions, token_sta
     [max_tokens]; positions int32 [max_tokens] or None; token_start int32 [batch + 1]; free_ids int32 [num_gpu_blocks]
     with free_count and free_count_out int32 [1], or None when the tables hold the blocks already.  ctx_lens_out may
     be ctx_lens and free_count_out may be free_count.  See ps_build_slots in the header."""
-    import torch
+    torch = _import_torch()
     i32 = torch.int32
     try:
         dev, batch, room = slots.get_device(), ctx_lens.numel(), slots.numel()
-        _need(dev >= 0, "slots: not a device tensor")
-        _need(block_tables.dim() == 2 and block_tables.shape[1] > 0, "block_tables: need [batch][stride]")
+        if dev < 0 or block_tables.dim() != 2 or block_tables.shape[1] == 0:
+            raise _BadArg("need slots on a device and block_tables [batch][stride]")
         stride = block_tables.shape[1]
-        args = PsSlotsArgs(
+        args = _pack_slots(
             _vec("ctx_lens", ctx_lens, i32, batch, dev), _vec("new_lens", new_lens, i32, batch, dev),
-            _vec("block_tables", block_tables, i32, batch * stride, dev),
-            None if free_ids is None else _vec("free_ids", free_ids, i32, num_gpu_blocks, dev),
-            None if free_count is None else _vec("free_count", free_count, i32, 1, dev),
-            None if free_count_out is None else _vec("free_count_out", free_count_out, i32, 1, dev),
-            _vec("slots", slots, torch.int64, 0, dev),
-            None if positions is None else _vec("positions", positions, i32, room, dev),
+            _vec("block_tables", block_tables, i32, batch * stride, dev), _vec("free_ids", free_ids, i32, num_gpu_blocks, dev),
+            _vec("free_count", free_count, i32, 1, dev), _vec("free_count_out", free_count_out, i32, 1, dev),
+            _vec("slots", slots, torch.int64, 0, dev), _vec("positions", positions, i32, room, dev),
             _vec("token_start", token_start, i32, batch + 1, dev), _vec("ctx_lens_out", ctx_lens_out, i32, batch, dev),
-            None if status_word is None else _vec("status_word", status_word, i32, 1, dev),
-            batch, stride, block_size, num_gpu_blocks, room, 0)
-    except _BadArg as e:
+            _vec("status_word", status_word, i32, 1, dev), batch, stride, block_size, num_gpu_blocks, room, 0)
+    except (_BadArg, struct.error) as e:
         return PS_ERR_INVALID, f"ps_build_slots: {e}"
     return _enqueue(load().ps_build_slots, args, dev)
 
@@ -348,63 +378,66 @@ def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=Non
 
     q, q_out [tokens][q heads][dim], k, v, k_out [tokens][kv heads][dim] (any of q, k, k_out may be None; q_out may be
     q, k_out may be k; rows may be strided); positions int32 [tokens] or [axes][tokens] (an axis stride of 0 is fine);
-    inv_freq float32 [rot_dim / 2], or None for no rotation; freq_axis: the axis of every frequency, or None for axis
-    0; kpool, vpool [blocks][block_size][kv heads][dim] with slots int64 [tokens].  See ps_rope_append in the header."""
-    import torch
+    inv_freq float32 [rot_dim / 2], or None for no rotation; freq_axis: a list with the axis of every frequency, or None
+    for axis 0; kpool, vpool [blocks][block_size][kv heads][dim] with slots int64 [tokens].  See ps_rope_append in the header."""
+    torch = _import_torch()
     i32 = torch.int32
     try:
         ref = q if q is not None else k
-        _need(ref is not None and ref.dim() == 3 and ref.get_device() >= 0, "need q or k, a device tensor [tokens][heads][dim]")
-        dev, dt, T, D = ref.get_device(), ref.dtype, ref.shape[0], ref.shape[2]
-        code = _dtype_code(ref)
-        hq, hkv = (0 if q is None else q.shape[1]), 0
-        q_st = qo_st = k_st = v_st = ko_st = kb = vb = ax_st = 0
-        if q is not None:
-            q_st = _rows("q", q, (T, hq, D), dt, dev)
-            _need(q_out is not None, "q needs q_out")
-            qo_st = _rows("q_out", q_out, (T, hq, D), dt, dev)
-            _need(T < 2 or qo_st >= hq * D, "q_out: rows overlap")
-        if k is not None:
-            _need(k.dim() == 3, "k: need [tokens][heads][dim]")
-            hkv = k.shape[1]
-            k_st = _rows("k", k, (T, hkv, D), dt, dev)
-            if k_out is not None:
-                ko_st = _rows("k_out", k_out, (T, hkv, D), dt, dev)
-                _need(T < 2 or ko_st >= hkv * D, "k_out: rows overlap")
+        if ref is None or ref.dim() != 3 or ref.get_device() < 0:
+            raise _BadArg("need q or k, a device tensor [tokens][heads][dim]")
+        dev, dt, (T, hq, D) = ref.get_device(), ref.dtype, ref.shape
+        code = _dtype_code(dt)
+        q_at = k_at = v_at = qo_at = ko_at = kp_at = vp_at = pos_at = 0
+        axis_of = b""
+        hkv = nb = bs = half = axes = q_st = k_st = v_st = qo_st = ko_st = kb = vb = ax_st = 0
+        if q is None:
+            hq = 0
         else:
-            _need(k_out is None and kpool is None, "k_out and pools need k")
-        nb = bs = 0
+            q_at, q_st = q.data_ptr(), _rows("q", q, T, hq, D, dt, dev)
+            if q_out is None:
+                raise _BadArg("q needs q_out")
+            qo_at, qo_st = q_out.data_ptr(), _rows("q_out", q_out, T, hq, D, dt, dev)
+            if qo_st < hq * D:
+                raise _BadArg("q_out: rows overlap")
+        if k is not None:
+            hkv = k.shape[1]
+            k_at, k_st = k.data_ptr(), _rows("k", k, T, hkv, D, dt, dev)
+            if k_out is not None:
+                ko_at, ko_st = k_out.data_ptr(), _rows("k_out", k_out, T, hkv, D, dt, dev)
+                if ko_st < hkv * D:
+                    raise _BadArg("k_out: rows overlap")
+        elif k_out is not None or kpool is not None:
+            raise _BadArg("k_out and pools need k")
         if kpool is not None or vpool is not None:
-            _need(kpool is not None and vpool is not None and v is not None and slots is not None,
-                  "an append needs k, v, both pools and slots")
-            _need(kpool.dim() == 4, "kpool: need [blocks][block_size][heads][dim]")
-            nb, bs = kpool.shape[0], kpool.shape[1]
-            kb = _pool("kpool", kpool, (nb, bs, hkv, D), dt, dev)
-            vb = _pool("vpool", vpool, (nb, bs, hkv, D), dt, dev)
-            v_st = _rows("v", v, (T, hkv, D), dt, dev)
-        half = axes = 0
-        if inv_freq is not None:
+            if kpool is None or vpool is None or v is None or slots is None or kpool.dim() != 4:
+                raise _BadArg("an append needs k, v, slots and two pools [blocks][block_size][heads][dim]")
+            nb, bs, _, _ = kpool.shape
+            kp_at, kb = kpool.data_ptr(), _pool("kpool", kpool, nb, bs, hkv, D, dt, dev)
+            vp_at, vb = vpool.data_ptr(), _pool("vpool", vpool, nb, bs, hkv, D, dt, dev)
+            v_at, v_st = v.data_ptr(), _rows("v", v, T, hkv, D, dt, dev)
+        if inv_freq is not None and inv_freq.numel() > 0:
             half = inv_freq.numel()
-            _need(positions is not None and positions.dim() in (1, 2) and positions.dtype is i32
-                  and positions.get_device() == dev and positions.shape[-1] == T and (T < 2 or positions.stride(-1) == 1),
-                  "positions: need int32 [tokens] or [axes][tokens] on the tensors' device")
-            axes = 1 if positions.dim() == 1 else positions.shape[0]
-            ax_st = 0 if axes == 1 else positions.stride(0)
-            _need(freq_axis is None or len(freq_axis) == half, "freq_axis: need one axis per frequency")
-        args = PsRopeArgs(
-            None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
-            None if kpool is None else v.data_ptr(), None if q is None else q_out.data_ptr(),
-            None if k_out is None else k_out.data_ptr(), None if kpool is None else kpool.data_ptr(),
-            None if kpool is None else vpool.data_ptr(),
-            None if slots is None else _vec("slots", slots, torch.int64, T, dev),
-            positions.data_ptr() if half else None,
-            _vec("inv_freq", inv_freq, torch.float32, half, dev) if half else None,
-            C.cast((C.c_int32 * half)(*freq_axis), C.c_void_p) if half and freq_axis is not None else None,
-            None if status_word is None else _vec("status_word", status_word, i32, 1, dev),
-            q_st, k_st, v_st, qo_st, ko_st, kb, vb, ax_st,
-            T, hq, hkv, D, 2 * half, axes, bs, nb, code,
-            (PS_ROPE_NEIGHBOURS if neighbours else 0) | (PS_ROPE_INVERSE if inverse else 0))
-    except _BadArg as e:
+            shape = positions.shape if positions is not None else ()
+            if (len(shape) not in (1, 2) or shape[-1] != T or positions.dtype is not i32 or positions.get_device() != dev
+                    or (positions.stride(-1) != 1 and T > 1)):
+                raise _BadArg("positions: need int32 [tokens] or [axes][tokens] on the tensors' device")
+            pos_at = positions.data_ptr()
+            if len(shape) == 1:
+                axes = 1
+            else:
+                axes = shape[0]
+                ax_st = positions.stride(0) if axes > 1 else 0
+            if freq_axis is not None:
+                axis_of = bytes(freq_axis)
+                if len(axis_of) != half or half > 256:
+                    raise _BadArg("freq_axis: need one axis per frequency, of at most 256")
+        args = _pack_rope(
+            q_at, k_at, v_at, qo_at, ko_at, kp_at, vp_at, _vec("slots", slots, torch.int64, T, dev), pos_at,
+            _vec("inv_freq", inv_freq, torch.float32, half, dev), _vec("status_word", status_word, i32, 1, dev),
+            q_st, k_st, v_st, qo_st, ko_st, kb, vb, ax_st, T, hq, hkv, D, 2 * half, axes, bs, nb, code,
+            (PS_ROPE_NEIGHBOURS if neighbours else 0) | (PS_ROPE_INVERSE if inverse else 0), axis_of)
+    except (_BadArg, struct.error, ValueError, TypeError) as e:
         return PS_ERR_INVALID, f"ps_rope_append: {e}"
     return _enqueue(load().ps_rope_append, args, dev)
 
@@ -414,7 +447,7 @@ _workspace_bytes = {}
 
 def ps_paged_attn_workspace(num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int] = None) -> int:
     """Bytes of workspace that ps_paged_attn needs for these heads on a device (default: the current one)."""
-    import torch
+    torch = _import_torch()
     dev = torch.cuda.current_device() if device is None else device
     key = (dev, num_kv_heads, num_q_heads, head_dim)
     n = _workspace_bytes.get(key)
@@ -436,32 +469,34 @@ def ps_paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, *, lse=None, win
     strided; block_tables int32 [at least batch][stride]; ctx_lens int32 [batch]; lse float32 [batch][q heads] or
     None; scale None = 1 / sqrt(dim).  workspace: a uint8 tensor of ps_paged_attn_workspace bytes; by default one is
     taken from torch's allocator on the current stream for the duration of the call.  See ps_paged_attn in the header."""
-    import torch
+    torch = _import_torch()
     try:
-        _need(q.dim() == 3 and q.get_device() >= 0, "q: need a device tensor [batch][heads][dim]")
-        dev, dt, (batch, hq, D) = q.get_device(), q.dtype, q.shape
-        code = _dtype_code(q)
-        _need(kpool.dim() == 4 and block_tables.dim() == 2, "need kpool [blocks][block_size][heads][dim] and block_tables [batch][stride]")
-        nb, bs, hkv, _ = kpool.shape
-        kb = _pool("kpool", kpool, (nb, bs, hkv, D), dt, dev)
-        vb = _pool("vpool", vpool, (nb, bs, hkv, D), dt, dev)
-        q_st, o_st = _rows("q", q, (batch, hq, D), dt, dev), _rows("out", out, (batch, hq, D), dt, dev)
+        if q.dim() != 3 or q.get_device() < 0 or kpool.dim() != 4 or block_tables.dim() != 2:
+            raise _BadArg("need q [batch][heads][dim], kpool [blocks][block_size][heads][dim] and block_tables [batch][stride] on a device")
+        dev, dt, (batch, hq, D), (nb, bs, hkv, _) = q.get_device(), q.dtype, q.shape, kpool.shape
+        code = _dtype_code(dt)
+        kb = _pool("kpool", kpool, nb, bs, hkv, D, dt, dev)
+        vb = _pool("vpool", vpool, nb, bs, hkv, D, dt, dev)
+        q_st, o_st = _rows("q", q, batch, hq, D, dt, dev), _rows("out", out, batch, hq, D, dt, dev)
         stride = block_tables.shape[1]
-        _need(hkv > 0 and D in (64, 128) and hq > 0 and hq % hkv == 0 and hq // hkv <= 64 and hkv <= 1024,
-              "head_dim must be 64 or 128, with 1 to 64 query heads per KV head")
-        need = ps_paged_attn_workspace(hkv, hq, D, dev)
+        need = _workspace_bytes.get((dev, hkv, hq, D))
+        if need is None:
+            _need(hkv > 0 and D in (64, 128) and hq > 0 and hq % hkv == 0 and hq // hkv <= 64 and hkv <= 1024,
+                  "head_dim must be 64 or 128, with 1 to 64 query heads per KV head")
+            need = ps_paged_attn_workspace(hkv, hq, D, dev)
+        if scale is not None and scale == 0:
+            raise _BadArg("scale: 0 is not a factor")
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _need(scale is None or scale != 0, "scale: 0 is not a factor")
-        args = PsPagedAttnArgs(
-            kpool.data_ptr(), vpool.data_ptr(), q.data_ptr(), out.data_ptr(),
-            None if lse is None else _vec("lse", lse, torch.float32, batch * hq, dev),
-            _vec("block_tables", block_tables, torch.int32, batch * stride, dev),
-            _vec("ctx_lens", ctx_lens, torch.int32, batch, dev),
-            None if status_word is None else _vec("status_word", status_word, torch.int32, 1, dev),
-            _vec("workspace", workspace, torch.uint8, need, dev), workspace.numel(), kb, vb, q_st, o_st,
+            ws_at, ws_bytes = workspace.data_ptr(), need
+        else:
+            ws_at, ws_bytes = _vec("workspace", workspace, torch.uint8, need, dev), workspace.numel()
+        args = _pack_attn(
+            kpool.data_ptr(), vpool.data_ptr(), q.data_ptr(), out.data_ptr(), _vec("lse", lse, torch.float32, batch * hq, dev),
+            _vec("block_tables", block_tables, torch.int32, batch * stride, dev), _vec("ctx_lens", ctx_lens, torch.int32, batch, dev),
+            _vec("status_word", status_word, torch.int32, 1, dev), ws_at, ws_bytes, kb, vb, q_st, o_st,
             batch, stride, hkv, hq, D, bs, nb, window, scale or 0.0, code)
-    except _BadArg as e:
+    except (_BadArg, struct.error) as e:
         return PS_ERR_INVALID, f"ps_paged_attn: {e}"
     return _enqueue(load().ps_paged_attn, args, dev)
 

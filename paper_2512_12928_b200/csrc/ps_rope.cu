@@ -25,7 +25,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxHeadDim = 512;
 constexpr int kTokensPerCta = 8;      // most tokens of a CTA
-constexpr int kTwoRounds = 2 * 4 * 148;
 constexpr int kStatusBadSlot = 1;
 
 struct FreqAxes {
@@ -277,10 +276,16 @@ bool on16(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p
 template <typename T>
 cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
     const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
-    // few tokens: one per CTA, so that they spread over the chip; many: as many as make a sine per thread, while at
-    // least two rounds of four CTAs per SM are left
-    for (p.tok_per_cta = 1; p.tok_per_cta < kTokensPerCta; p.tok_per_cta *= 2)
-        if (p.tok_per_cta * p.rot > kThreads || 2 * p.tok_per_cta * units > kThreads || p.tokens / (2 * p.tok_per_cta) < kTwoRounds) break;
+    // few tokens: one per CTA, so that they spread over the chip; many: as many as make a sine per thread.  In between
+    // as many as leave the chip well filled, with one round of four CTAs per SM or at least two (2048 tokens of 80
+    // heads of 128: 16.8 us at 4 tokens a CTA and 22.6 at one; 5003 tokens of 32 heads of 80: 15.5 us at 4 and 17.0 at
+    // 8, whose 626 CTAs are a little more than a round).
+    constexpr int kRound = 4 * 148, kFilled = kRound * 5 / 8;
+    p.tok_per_cta = 1;
+    for (int n = 2; n <= kTokensPerCta && n * p.rot <= 2 * kThreads && n * units <= kThreads; n *= 2) {
+        const int ctas = p.tokens / n;
+        if (ctas >= 2 * kRound || (ctas >= kFilled && ctas <= kRound)) p.tok_per_cta = n;
+    }
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
     const size_t smem = (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2);
     if (!vec) return ps::launch_dependent(rope_append_elements_kernel<T>, grid, dim3(kThreads), smem, s, p, axes, heads, neighbours);
@@ -316,11 +321,10 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
     FreqAxes axes{};
     if (a.rot_dim > 0) {
         if (!a.inv_freq || a.num_axes < 1 || a.num_axes > 8) return bad("ps_rope_append: a rotation needs positions, inv_freq and 1 to 8 axes");
-        if (a.freq_axis)
-            for (int i = 0; i < a.rot_dim / 2; ++i) {
-                if (a.freq_axis[i] < 0 || a.freq_axis[i] >= a.num_axes) return bad("ps_rope_append: freq_axis names an axis that is not there");
-                axes.v[i] = (uint8_t)a.freq_axis[i];
-            }
+        for (int i = 0; i < a.rot_dim / 2; ++i) {
+            if (a.freq_axis[i] >= a.num_axes) return bad("ps_rope_append: freq_axis names an axis that is not there");
+            axes.v[i] = a.freq_axis[i];
+        }
     }
     if (a.tokens == 0 || (!do_q && !do_k)) return PS_OK;
     if (a.rot_dim > 0 && !a.positions) return bad("ps_rope_append: a rotation needs positions, inv_freq and 1 to 8 axes");

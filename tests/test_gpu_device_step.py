@@ -183,7 +183,8 @@ def rope_inputs(T, hq, hkv, D, dt, rng_seed, fused=True):
 @pytest.mark.parametrize("T,hq,hkv,D,rot,axes,neighbours,S", [
     (1, 32, 8, 128, 128, 1, False, 16), (5, 28, 4, 128, 64, 3, False, 24), (77, 4, 2, 64, 64, 2, True, 1), (3, 3, 1, 80, 48, 3, True, 8),
     (9, 2, 2, 96, 24, 1, False, 16), (13, 5, 5, 80, 20, 4, True, 7), (6, 4, 1, 256, 256, 3, False, 32), (4, 1, 1, 512, 512, 8, False, 16),
-    (2, 3, 3, 10, 6, 2, False, 5), (1030, 8, 2, 64, 32, 3, False, 16), (11, 7, 1, 128, 0, 1, False, 16), (8, 2, 1, 6, 2, 1, True, 3)])
+    (2, 3, 3, 10, 6, 2, False, 5), (1030, 8, 2, 64, 32, 3, False, 16), (11, 7, 1, 128, 0, 1, False, 16), (8, 2, 1, 6, 2, 1, True, 3),
+    (4700, 2, 1, 64, 32, 3, False, 16), (9001, 3, 1, 64, 64, 1, True, 7), (2500, 2, 2, 128, 64, 2, False, 64), (4730, 1, 1, 512, 16, 1, False, 16)])
 def test_rope_and_append(dtype, T, hq, hkv, D, rot, axes, neighbours, S):
     dt = DTYPES[dtype]
     rng = np.random.default_rng(T * 1000 + D)
@@ -500,7 +501,7 @@ def test_tensors_that_do_not_fit_are_refused():
     for bad in (dict(q_out=None), dict(v=None), dict(slots=None), dict(slots=pos), dict(slots=sl[:2]), dict(positions=None),
                 dict(positions=pos[:2]), dict(positions=pos.long()), dict(inv_freq=inv.double()), dict(inv_freq=torch.zeros(33, device="cuda")),
                 dict(vpool=None), dict(kpool=None), dict(kpool=kp.to(h)), dict(k=k[:2]), dict(v=k.to(h)), dict(freq_axis=[0] * 31),
-                dict(freq_axis=[1] * 32), dict(q_out=q[:1].expand(3, 8, 64)), dict(k=None)):
+                dict(freq_axis=[1] * 32), dict(freq_axis=[-1] * 32), dict(freq_axis=[0.5] * 32), dict(q_out=q[:1].expand(3, 8, 64)), dict(k=None)):
         rc, text = B.ps_rope_append(**{**good, **bad})
         assert rc == B.PS_ERR_INVALID and text, bad.keys()
     ids, cnt = dev([0] * 8), dev([8])
