@@ -467,11 +467,13 @@ typedef struct ps_paged_attn_args {
 
 /* Decode attention as ps_decode_attn computes it, from lengths and tables on the device:
  *   out[b][h] = softmax_t(scale * q[b][h] . K[t][h / G]) . V[t][h / G],   max(0, ctx - window) <= t < ctx,
- * bf16 or fp16 inputs and outputs, 32-bit scores, softmax statistics and accumulators; the softmax weights are rounded
- * to the inputs' type for the product with V.  A row with ctx_lens 0 gives zeros (lse = -inf).  A length that is
+ * bf16 or fp16 inputs and outputs, 32-bit scores, softmax statistics and accumulators; for the product with V a softmax
+ * weight is the sum of two numbers of the inputs' type, and the result is rounded once.  A row with ctx_lens 0, or with
+ * no score above -inf, gives zeros (lse = -inf).  A length that is
  * negative counts as 0, one beyond table_stride * block_size as that many (status 5).  Blocks may be shared by rows,
  * and nothing outside the attended tokens is read into a result, whatever the pools hold there.
- * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, any batch.
+ * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, any batch whose tables have room for
+ * fewer than about 2^37 tokens times KV heads.  out must not overlap the inputs.  The same inputs give the same bits.
  * One workspace serves calls in order; calls that may overlap on the device need one each.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_buf, int32_t err_cap);

@@ -83,6 +83,7 @@ template <> struct Num<__nv_bfloat16> {
         const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
+    static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
     static __device__ __forceinline__ void mma(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -97,6 +98,7 @@ template <> struct Num<__half> {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
+    static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
     static __device__ __forceinline__ void mma(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -147,11 +149,15 @@ __device__ __forceinline__ int32_t block_of(int32_t t, const AttnParams& p) {
 
 // Tokens that are attended of a row of n: [first, end).
 __device__ __forceinline__ void row_span(const AttnParams& p, int32_t n, int32_t* first, int32_t* end) {
-    int32_t e = n < 0 ? 0 : n;
-    if ((int64_t)e > p.room) e = (int32_t)p.room;
-    if (e != n && p.status) *(volatile int32_t*)p.status = kStatusLength;
+    const int32_t e = (int64_t)n > p.room ? (int32_t)p.room : max(n, 0);
     *end = e;
     *first = p.window > 0 && e > p.window ? e - p.window : 0;
+}
+// Tiles of a row of n; an empty row still has a result to write.
+__device__ __forceinline__ int32_t row_tiles(const AttnParams& p, int32_t n) {
+    int32_t first, end;
+    row_span(p, n, &first, &end);
+    return end > first ? (end - first + (1 << p.step_log2) - 1) >> p.step_log2 : 1;
 }
 
 // Where a unit's queries are: heads [h0, h0 + n).
@@ -168,8 +174,8 @@ struct Cursor {
     int32_t next_len;                        // of row b + 1, asked for while row b is worked on
     __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
         row_span(p, len, &first, &end);
-        // an empty row still has a result to write
-        tiles = end > first ? (end - first + (1 << p.step_log2) - 1) >> p.step_log2 : 1;
+        tiles = row_tiles(p, len);
+        if (end != len && p.status) *(volatile int32_t*)p.status = kStatusLength;
     }
     __device__ __forceinline__ void next(const AttnParams& p, bool more) {
         if (++i < tiles) return;
@@ -374,7 +380,8 @@ struct Worker {
                     }
                 }
         }
-        uint32_t pt[kSub][NT][2];      // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 (of 16) of head 8t + g
+        // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 (of 16) of head 8t + g, as the sum of two numbers of the inputs' type
+        uint32_t pt[kSub][NT][2], rest[kSub][NT][2];
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
 #pragma unroll
@@ -383,15 +390,23 @@ struct Worker {
                 for (int i = 0; i < 4; ++i) e[u][t][i] = ex2(e[u][t][i] + Num<T>::kLift);
                 st.l[t][0] += e[u][t][0] + e[u][t][2];
                 st.l[t][1] += e[u][t][1] + e[u][t][3];
-                pt[u][t][0] = transpose8(Num<T>::pack(e[u][t][0], e[u][t][1]));
-                pt[u][t][1] = transpose8(Num<T>::pack(e[u][t][2], e[u][t][3]));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t v = Num<T>::pack(e[u][t][2 * i], e[u][t][2 * i + 1]);
+                    const float2 f = Num<T>::unpack(v);
+                    pt[u][t][i] = transpose8(v);
+                    rest[u][t][i] = transpose8(Num<T>::pack(e[u][t][2 * i] - f.x, e[u][t][2 * i + 1] - f.y));
+                }
             }
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) Num<T>::mma(st.acc[t][j], v[u][j], pt[u][t][0], pt[u][t][1]);
+                for (int t = 0; t < NT; ++t) {
+                    Num<T>::mma(st.acc[t][j], v[u][j], pt[u][t][0], pt[u][t][1]);
+                    Num<T>::mma(st.acc[t][j], v[u][j], rest[u][t][0], rest[u][t][1]);
+                }
     }
 };
 
@@ -445,13 +460,12 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     const int per = (p.batch + blockDim.x - 1) / blockDim.x;
     const int b_lo = min(p.batch, (int)threadIdx.x * per), b_hi = min(p.batch, b_lo + per);
     int mine = 0, len = 0;
-    Cursor cur;
-#pragma unroll 1
-    for (cur.b = b_lo; cur.b < b_hi; ++cur.b) {
-        len = __ldg(p.ctx + cur.b);
-        cur.row(p, len);
-        mine += cur.tiles * p.chunks;
+#pragma unroll 4
+    for (int b = b_lo; b < b_hi; ++b) {
+        len = __ldg(p.ctx + b);
+        mine += row_tiles(p, len) * p.chunks;
     }
+    Cursor cur;
     int before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -473,16 +487,16 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     const int begin = share * blockIdx.x, end = min(total, begin + share);
     if (begin >= before && begin < before + mine) {
         int a = before;
-        if (per == 1) cur.b = b_lo;              // and the length is still there
-        else
+        cur.b = b_lo;                            // and of a single row the length is still there
+        if (per > 1)
 #pragma unroll 1
-            for (cur.b = b_lo;; ++cur.b) {
+            for (;; ++cur.b) {
                 len = __ldg(p.ctx + cur.b);
-                cur.row(p, len);
-                const int n = cur.tiles * p.chunks;
+                const int n = row_tiles(p, len) * p.chunks;
                 if (begin < a + n) break;
                 a += n;
             }
+        cur.row(p, len);
         cur.chunk = 0;
         cur.i = begin - a;
         if (p.chunks > 1) {

@@ -96,17 +96,19 @@ def check_within(got, want, tol):
                            f"{np.nanmax(np.where(bad, np.abs(got - want) / np.maximum(tol, 1e-300), 0))} times its tolerance")
 
 
-def attn_want(kpool, vpool, q, tables, ctx, window=0, scale=None):
+def attn_want(kpool, vpool, q, tables, ctx, window=0, scale=None, weight_error=None):
     """(out, lse, tolerances of both) in 64 bits.  tables: lists of block ids per row; ids outside the pool are skipped.
 
     A score is a 32-bit sum of D exact products: off by at most 2^-20 sum |q k| scale (D roundings of 2^-24, and some
     room for the tensor cores' own order).  Both sides of p / sum p carry it, 2^-20 more covers exp2, the sums and
-    the division.  A weight is rounded to the inputs' type once, and so is the result."""
+    the division.  A weight is held as the sum of two numbers of the inputs' type (a half step of a half step off), and
+    the result is rounded once.  weight_error: of a kernel that rounds its weights otherwise."""
     dt = q.dtype
     B, Hq, D = q.shape
     nb, S, Hkv, _ = kpool.shape
     G = Hq // Hkv
     scale = 1 / math.sqrt(D) if scale is None else scale
+    weight_error = HALF_STEP[dt] ** 2 if weight_error is None else weight_error
     out, lse = np.zeros((B, Hq, D)), np.full((B, Hq), -np.inf)
     tol, tol_lse = np.zeros((B, Hq, D)), np.zeros((B, Hq))
     qf = f64(q)
@@ -130,7 +132,7 @@ def attn_want(kpool, vpool, q, tables, ctx, window=0, scale=None):
             lse[b, h] = m + math.log(l)
             ds = 2.0 ** -20 * abs(scale) * float((np.abs(k) @ np.abs(qf[b, h])).max())
             A = p @ np.abs(v) / l
-            e = A * (HALF_STEP[dt] + 2 * ds + 2.0 ** -20)
+            e = A * (weight_error + 2 * ds + 2.0 ** -20)
             tol[b, h] = e + HALF_STEP[dt] * (np.abs(out[b, h]) + e) + TINY[dt]
             tol_lse[b, h] = ds + 2.0 ** -20 * (1 + abs(lse[b, h]) + abs(m))
     return out, lse, tol, tol_lse

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from device_step_util import (DTYPES, SlotModel, attn_want, check_attn, check_within, make_tables, rope_want, tables_tensor)
+from device_step_util import (DTYPES, HALF_STEP, SlotModel, attn_want, check_attn, check_within, make_tables, rope_want, tables_tensor)
 from paper_2512_12928_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -667,7 +667,7 @@ def test_attention_next_to_a_contexts_own():
     assert B.ps_paged_attn(kp[0], vp[0], q_rot, a, tables, ctx, lse=la)[0] == B.PS_OK
     assert lib.decode_attn(0, q_rot, b, reqs, lb) == B.PS_OK
     assert lib.sync() == B.PS_OK
-    want = attn_want(kp[0], vp[0], q_rot, [lib.block_table(r)[0] for r in reqs], [n + 1 for n in before])
-    check_attn(a, la, want)
-    check_attn(b, lb, want)
+    args = kp[0], vp[0], q_rot, [lib.block_table(r)[0] for r in reqs], [n + 1 for n in before]
+    check_attn(a, la, attn_want(*args))
+    check_attn(b, lb, attn_want(*args, weight_error=HALF_STEP[torch.bfloat16]))   # rounds a weight once
     lib.destroy()
