@@ -37,6 +37,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "ps_internal.h"
 #include "ps_kvswap.h"
@@ -601,40 +602,45 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 4
                     for (int r = lane / kLanes; r < n; r += kHeads) put(r, get(warp, r), sh_ml[warp][r].x, sh_ml[warp][r].y);
                 } else {
-                    constexpr int kAtOnce = 4;           // heads of a warp whose loads overlap
-                    const int r_step = p.subs * kHeads;
+                    // eight parts are loaded at a time: of all slices of one, two or four heads
+                    auto combine = [&](auto slices) {
+                        constexpr int kSlices = decltype(slices)::value, kAtOnce = kMaxWarps / kSlices;
+                        constexpr int kStep = kSlices * kHeads;
 #pragma unroll 1
-                    for (int r0 = wk.sub * kHeads + lane / kLanes; r0 < n; r0 += kAtOnce * r_step) {
-                        float m[kAtOnce], l[kAtOnce];
-                        float4 o[kAtOnce];
+                        for (int r0 = wk.sub * kHeads + lane / kLanes; r0 < n; r0 += kAtOnce * kStep) {
+                            float m[kAtOnce], l[kAtOnce];
+                            float4 o[kAtOnce];
 #pragma unroll
-                        for (int i = 0; i < kAtOnce; ++i) {
-                            m[i] = kNothing;
-                            l[i] = 0.f;
-                            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        }
-#pragma unroll 1
-                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units)
+                            for (int h = 0; h < kAtOnce; ++h) {
+                                const int r = min(r0 + h * kStep, n - 1);
+                                m[h] = kNothing;
+                                l[h] = 0.f;
+                                o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                float2 ml[kSlices];
 #pragma unroll
-                            for (int i = 0; i < kAtOnce; ++i) m[i] = fmaxf(m[i], sh_ml[w][min(r0 + i * r_step, n - 1)].x);
-#pragma unroll 1
-                        for (int w = wk.unit_in_cta; w < nwarps; w += p.units)
+                                for (int i = 0; i < kSlices; ++i) {
+                                    ml[i] = sh_ml[wk.unit_in_cta + i * p.units][r];
+                                    m[h] = fmaxf(m[h], ml[i].x);
+                                }
 #pragma unroll
-                            for (int i = 0; i < kAtOnce; ++i) {
-                                const int r = min(r0 + i * r_step, n - 1);
-                                const float2 ml = sh_ml[w][r];
-                                const float4 x = get(w, r);
-                                const float f = weight_for(ml.x, m[i]);
-                                l[i] += ml.y * f;
-                                o[i].x += x.x * f;
-                                o[i].y += x.y * f;
-                                o[i].z += x.z * f;
-                                o[i].w += x.w * f;
+                                for (int i = 0; i < kSlices; ++i) {
+                                    const float4 x = get(wk.unit_in_cta + i * p.units, r);
+                                    const float f = weight_for(ml[i].x, m[h]);
+                                    l[h] += ml[i].y * f;
+                                    o[h].x += x.x * f;
+                                    o[h].y += x.y * f;
+                                    o[h].z += x.z * f;
+                                    o[h].w += x.w * f;
+                                }
                             }
 #pragma unroll
-                        for (int i = 0; i < kAtOnce; ++i)
-                            if (r0 + i * r_step < n) put(r0 + i * r_step, o[i], m[i], l[i]);
-                    }
+                            for (int h = 0; h < kAtOnce; ++h)
+                                if (r0 + h * kStep < n) put(r0 + h * kStep, o[h], m[h], l[h]);
+                        }
+                    };
+                    if (p.subs == 2) combine(std::integral_constant<int, 2>());
+                    else if (p.subs == 4) combine(std::integral_constant<int, 4>());
+                    else combine(std::integral_constant<int, 8>());
                 }
                 if (p.subs > 1) __syncthreads(); else __syncwarp();      // the stage is free again
                 if (!seg_end) {
