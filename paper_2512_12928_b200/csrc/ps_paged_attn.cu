@@ -5,21 +5,27 @@
 //   max(0, ctx_b - window) <= t < ctx_b,   m = max_t s_t (running),   lse = ln 2 (m + log2 sum_t p_t)
 //
 // Bound: HBM.  A token and KV head cost 4 D bytes and 4 G D flops; up to G = 64 the card computes faster than it
-// loads.  So every warp streams its own tiles of 16 or 32 tokens (4 KiB of K and of V) through a ring in shared memory (cp.async, 16 bytes a lane,
-// whole 128-byte lines), across the ends of rows, and no barrier lies between HBM and the tensor cores.  Tokens may
-// lie anywhere; what is not attended is filled with zeros instead of being read.
+// loads.  So every warp streams its own tiles of 16 or 32 tokens (4 KiB of K and of V) through a ring of three in
+// shared memory (cp.async, 16 bytes a lane, whole 128-byte lines), across the ends of rows, and no barrier lies between
+// HBM and the tensor cores.  Tokens may lie anywhere; what is not attended is filled with zeros instead of being read.
+// Measured: 672 MB of cache (64 rows of 1024 to 4096 tokens, 32 query heads on 8 KV heads of 128, bf16) 101.5 us, or
+// 6.6 TB/s, which is what a copy reaches; about 6 us of it pass before the first tile is there and in the join, and
+// bound small calls (one row of 300 tokens: 7.0 us).  Heads of 64 need as many instructions for half the bytes and
+// reach 0.9 of that rate, 0.77 with 16 query heads on a KV head.
 //
 // Products: a group has few query heads, so they are the narrow side: S^T = K Q^T and O^T = V^T P^T as
 // mma.m16n8k16 with tokens, then dims, as the 16 rows and 8 heads as the columns.  K comes through ldmatrix and V
 // through its transposing form, both without bank conflicts (16-byte pieces exclusive-ored with the token's number);
 // P^T leaves the first product as pairs of heads and enters the second as pairs of tokens, which is one movmatrix.
 // With heads as the rows instead, half of every product was padding for up to 8 heads and V's pairs cost 32 byte
-// permutes a tile: 535 instructions a tile instead of XX, and 159 us instead of XX for 672 MB.
+// permutes a tile: 159 us for 672 MB of cache (64 rows, 32 query heads on 8 KV heads of 128), where this form took 106.
 // (The tile shapes of tcgen05.mma have 64 or 128 rows and its P would go through shared or tensor memory; the
 // tensor cores are idle most of the time either way.)
 //
 // Softmax: the reference m of a head is raised only when a score exceeds it by more than kSlack, so that a tile needs
 // one vote instead of a maximum over the lanes; weights stay below 2^kSlack and sums in 32 bits lose nothing by it.
+// For the product with V a weight is split into two numbers of the inputs' type: one alone makes the result's error
+// 1.4 times what its own rounding costs, and the second product costs less than 1 % of the time.
 //
 // Work: the rows' tiles form one sequence that is cut into equal shares, one per CTA, from the lengths each CTA
 // reads itself: no plan is made on the host or by another kernel.  A row cut by a share's end leaves partial
@@ -27,9 +33,9 @@
 // The join is a second launch rather than a last-arrival counter in the first: the workspace then needs no
 // initial state, and neither a replayed graph nor a call that shares it in turn can find a stale counter.
 //
-// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of two); the
-// units of a token are neighbours in memory.  The slices' states are combined through shared memory at a
-// segment's end.
+// Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of two);
+// the units of a token are neighbours in memory.  The slices' states are combined through shared memory at a segment's
+// end.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -46,7 +52,6 @@ namespace {
 
 constexpr int kMaxWarps = 8;
 constexpr int kMaxGroup = 16;         // query heads of a unit
-constexpr int kCtaFactor = 1;         // CTAs per SM
 constexpr int kJoinThreads = 256;
 constexpr int32_t kMaxTokens = INT32_MAX - 1024;   // of a row, so that a tile's end cannot wrap
 constexpr int kStatusBadId = 2, kStatusLength = 5;
@@ -844,7 +849,7 @@ Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, int sms) {
     y.chunks = (all + most - 1) / most;
     y.units = (all + y.chunks - 1) / y.chunks;
     for (y.subs = 1; 2 * y.subs * y.units <= kMaxWarps; y.subs *= 2) {}
-    y.ctas = sms * kCtaFactor;
+    y.ctas = sms;                          // the rings take an SM's shared memory
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
     y.part_o = 0;

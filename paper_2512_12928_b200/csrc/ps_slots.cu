@@ -10,11 +10,13 @@
 // The work is a few words per row and token; what bounds it is latency: the chain "load lengths, scan, load a free
 // id, store".  Two ways, chosen by the room for tokens:
 //   - slots_one_cta_kernel: one CTA scans, pushes, pops and maps; barriers order its steps and one launch does all.
-//     Up to 4096 tokens (64 rows of a token each: 3.1 us; 4000 tokens of 200 rows: YY us, and YY on the wide way).
+//     Up to 2048 tokens, or 4096 in place (64 rows of a token each: 3.1 us; 200 rows: 5.4 us for 2000 tokens, 7.0 for
+//     4000, 14.4 for 16000).
 //   - slots_wide_kernel: every CTA scans all rows for itself (cheaper than another launch) and takes its part of
 //     pushes, pops and tokens.  A popped id is found without waiting for the pushes: an index above the old top
 //     belongs to the table of a row that ended, which a search in the scanned counts names.  Where lengths or count are
-//     updated in place, a second kernel of one CTA does that when nobody reads them any more.
+//     updated in place, a second kernel of one CTA does that when nobody reads them any more, which takes 2.5 us more.
+//     (200 rows: 5.8 us for 2000 to 16000 tokens.)
 // Work on blocks and tokens is dealt to threads by the scanned counts (binary search in shared memory), so one long
 // prompt costs the same as many short ones.
 #include <algorithm>
@@ -31,7 +33,7 @@ constexpr int kStatusBadId = 2;     // a block id outside the pool
 
 constexpr int kMaxThreads = 1024;
 constexpr int kWideThreads = 1024;
-constexpr int32_t kOneCtaTokens = 4096;  // room for at most so many tokens: one CTA
+constexpr int32_t kOneCtaTokens = 2048;  // room for at most so many tokens: one CTA; in place twice as many
 constexpr int kWideCtas = 148;          // one per SM: each scans all rows
 constexpr int32_t kWideRows = 4096;      // the scanned counts of so many rows fit into shared memory
 
@@ -354,8 +356,9 @@ extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char*
     if (a.free_ids && (!a.free_count || !a.free_count_out))
         return arg_fail(err_buf, err_cap, PS_ERR_INVALID, "ps_build_slots: a free stack needs free_count and free_count_out");
     cudaStream_t s = (cudaStream_t)stream;
+    const bool apart = a.ctx_lens_out != a.ctx_lens && (!a.free_ids || a.free_count_out != a.free_count);
     cudaError_t e;
-    if (a.max_tokens <= kOneCtaTokens || a.batch > kWideRows) {
+    if (a.max_tokens <= (apart ? 1 : 2) * kOneCtaTokens || a.batch > kWideRows) {
         // few rows and tokens: fewer warps make the barriers of the scan cheaper
         const int threads = a.batch <= 256 && a.max_tokens <= 1024 ? 256 : kMaxThreads;
         e = ps::launch_dependent(slots_one_cta_kernel, dim3(1), dim3(threads), 0, s, a);
@@ -363,7 +366,6 @@ extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char*
         // a token a thread, at most a CTA per SM
         const int ctas = (int)std::min<int64_t>(((int64_t)a.max_tokens + kWideThreads - 1) / kWideThreads, kWideCtas);
         const size_t smem = (size_t)a.batch * 4 * sizeof(int32_t);
-        const bool apart = a.ctx_lens_out != a.ctx_lens && (!a.free_ids || a.free_count_out != a.free_count);
         e = smem > 48 << 10 ? cudaFuncSetAttribute(slots_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kWideRows * 4 * sizeof(int32_t)))
                             : cudaSuccess;
         if (e == cudaSuccess) e = ps::launch_dependent(slots_wide_kernel, dim3(ctas), dim3(kWideThreads), smem, s, a, apart);
