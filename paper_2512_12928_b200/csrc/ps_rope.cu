@@ -276,15 +276,15 @@ bool on16(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p
 template <typename T>
 cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
     const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
-    // few tokens: one per CTA, so that they spread over the chip; many: as many as make a sine per thread.  In between
-    // as many as leave the chip well filled, with one round of four CTAs per SM or at least two (2048 tokens of 80
-    // heads of 128: 16.8 us at 4 tokens a CTA and 22.6 at one; 5003 tokens of 32 heads of 80: 15.5 us at 4 and 17.0 at
-    // 8, whose 626 CTAs are a little more than a round).
-    constexpr int kRound = 4 * 148, kFilled = kRound * 5 / 8;
+    // Few tokens: one per CTA, so that they spread over the chip.  Many: a round of four CTAs per SM costs about 2 us
+    // that its sines take, so as many as make a sine per thread and leave the chip filled, but not a little more than
+    // a round, whose rest then runs alone (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.8 / 7.6 / 8.3 us, 2048
+    // 22.7 / 18.5 / 16.9, 8192 75.9 / 61.0 / 57.9; 32 heads of 80, 1 / 2 / 4 / 8: 5003 tokens 25.2 / 18.2 / 15.8 / 17.3).
+    constexpr int kRound = 4 * 148, kFilled = 350;
     p.tok_per_cta = 1;
     for (int n = 2; n <= kTokensPerCta && n * p.rot <= 2 * kThreads && n * units <= kThreads; n *= 2) {
         const int ctas = p.tokens / n;
-        if (ctas >= 2 * kRound || (ctas >= kFilled && ctas <= kRound)) p.tok_per_cta = n;
+        if (ctas >= kFilled && (ctas <= kRound || ctas > kRound * 3 / 2)) p.tok_per_cta = n;
     }
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
     const size_t smem = (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2);

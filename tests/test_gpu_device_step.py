@@ -67,7 +67,8 @@ def slot_case(rng, rows, S, hi, stride, M, room, **kw):
 
 @pytest.mark.parametrize("in_place", [True, False])
 @pytest.mark.parametrize("rows,S,room", [(1, 16, 64), (1, 1, 64), (7, 16, 300), (33, 24, 5000), (300, 16, 4096), (257, 7, 6000),
-                                         (1024, 16, 4097), (2500, 8, 20000)])
+                                         (1024, 16, 4097), (2500, 8, 20000),
+                                         (4000, 16, 9000), (5000, 8, 6000)])
 def test_slots_over_steps_with_a_stack(rows, S, room, in_place):
     rng = np.random.default_rng(rows * 100 + S)
     hi, chunk = 60, min(40, room // (rows + 1) + 1)
