@@ -12,8 +12,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
-import threading
 from typing import List, Optional, Sequence, Tuple
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -194,10 +192,9 @@ def load() -> C.CDLL:
                                  C.POINTER(C.c_double)]),
         "ps_decode_attn_static": (i32, [vp, vp, vp, vp, vp, vp, i32, p32, i32, i32, i32, i32, i32, i32, i32, vp, vp,
                                         C.c_char_p, i32]),
-        # the argument structures also come as their bytes (see _packer)
-        "ps_build_slots": (i32, [vp, vp, C.c_char_p, i32]),
-        "ps_rope_append": (i32, [vp, vp, C.c_char_p, i32]),
-        "ps_paged_attn": (i32, [vp, vp, C.c_char_p, i32]),
+        "ps_build_slots": (i32, [C.POINTER(PsSlotsArgs), vp, C.c_char_p, i32]),
+        "ps_rope_append": (i32, [C.POINTER(PsRopeArgs), vp, C.c_char_p, i32]),
+        "ps_paged_attn": (i32, [C.POINTER(PsPagedAttnArgs), vp, C.c_char_p, i32]),
         "ps_paged_attn_workspace": (i32, [i32, i32, i32, p64]),
     }
     for name, (res, args) in proto.items():
@@ -254,95 +251,32 @@ def ps_decode_attn_static(kpool, vpool, q, out, block_tables, ctx_lens: Sequence
 
 # ---- a decode step whose lengths stay on the device ------------------------------------------------
 #
-# Shapes, types and strides are taken from the tensors and checked here, since the library sees addresses only; what
-# does not fit comes back as (PS_ERR_INVALID, text), as from the library.  Work is enqueued on torch's current stream
-# of the tensors' device.
+# Shapes, types and strides are taken from the tensors and checked by the module _ps_tensor_args (csrc/ps_tensor_args.cpp),
+# since the library sees addresses only; what does not fit comes back as (PS_ERR_INVALID, text), as from the library.
+# Work is enqueued on torch's current stream of the tensors' device.
 
-# The calls are made once per layer and step, and a small one takes 3 us on the device: so arguments are packed into the
-# structures' bytes (a ctypes structure of 30 fields takes four times as long to fill) and torch is asked little.
-
-class _BadArg(Exception):
-    pass
+TENSOR_ARGS_PATH = os.path.join(_PKG, "lib", "_ps_tensor_args.so")
+_tensor_args = None
 
 
-class _ErrorText(threading.local):
-    def __init__(self):
-        self.buf = C.create_string_buffer(256)
+def _load_tensor_args():
+    """Loads the module and gives it the library's entry points.  Raises if it is not built."""
+    global _tensor_args
+    if _tensor_args is None:
+        import importlib.machinery
+        import importlib.util
 
-
-_error_text = _ErrorText()
-_torch = None
-
-
-def _import_torch():
-    global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    return _torch
-
-
-def _packer(cls):
-    """struct.Struct that packs cls's fields in order; None is not accepted, 0 is the null pointer."""
-    codes = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f", C.c_uint8 * 256: "256s"}
-    s = struct.Struct("@" + "".join(codes[f[1]] for f in cls._fields_))
-    assert s.size == C.sizeof(cls)
-    return s.pack
-
-
-_pack_slots, _pack_rope, _pack_attn = _packer(PsSlotsArgs), _packer(PsRopeArgs), _packer(PsPagedAttnArgs)
-
-
-def _need(ok, text: str):
-    if not ok:
-        raise _BadArg(text)
-
-
-def _vec(name: str, t, dtype, least: int, dev: int) -> int:
-    """Address of a contiguous device tensor of dtype with at least `least` elements; 0 for None."""
-    if t is None:
-        return 0
-    if t.dtype is not dtype or t.get_device() != dev or t.numel() < least or not t.is_contiguous():
-        raise _BadArg(f"{name}: need a contiguous {dtype} tensor of at least {least} elements on device {dev}, "
-                      f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _rows(name: str, t, rows: int, heads: int, dim: int, dtype, dev: int) -> int:
-    """Row stride of [rows][heads][dim] whose rows are dense; the tensor's address is t.data_ptr()."""
-    st = t.stride()
-    if (t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, heads, dim) or (st[2] != 1 and dim > 1)
-            or (st[1] != dim and heads > 1)):
-        raise _BadArg(f"{name}: need {dtype} {(rows, heads, dim)} with dense rows on device {dev}, got {t.dtype} "
-                      f"{tuple(t.shape)} strides {st} on {t.device}")
-    return st[0] if rows > 1 else heads * dim
-
-
-def _pool(name: str, t, nb: int, s: int, h: int, d: int, dtype, dev: int) -> int:
-    """Block stride of a pool [blocks][block_size][heads][dim] whose blocks are dense."""
-    st = t.stride()
-    if (t.dtype is not dtype or t.get_device() != dev or t.shape != (nb, s, h, d) or (st[3] != 1 and d > 1)
-            or (st[2] != d and h > 1) or (st[1] != h * d and s > 1)):
-        raise _BadArg(f"{name}: need a {dtype} pool {(nb, s, h, d)} with dense blocks on device {dev}, got {t.dtype} "
-                      f"{tuple(t.shape)} strides {st} on {t.device}")
-    return st[0] if nb > 1 else s * h * d
-
-
-def _enqueue(fn, packed: bytes, dev: int):
-    torch, err = _torch, _error_text.buf
-    if torch.cuda.current_device() == dev:
-        rc = fn(packed, torch._C._cuda_getCurrentRawStream(dev), err, 256)
-    else:
-        with torch.cuda.device(dev):
-            rc = fn(packed, torch._C._cuda_getCurrentRawStream(dev), err, 256)
-    return (rc, err.value.decode()) if rc else (0, "")
-
-
-def _dtype_code(dt) -> int:
-    if dt is _torch.bfloat16:
-        return PS_DTYPE_BF16
-    _need(dt is _torch.float16, f"need bfloat16 or float16 tensors, got {dt}")
-    return PS_DTYPE_FP16
+        import torch  # noqa: F401  (its libraries are the module's)
+        if not os.path.exists(TENSOR_ARGS_PATH):
+            raise ImportError(f"{TENSOR_ARGS_PATH} is missing: build it with `python -m paper_2512_12928_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_ps_tensor_args", TENSOR_ARGS_PATH)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_ps_tensor_args", loader))
+        loader.exec_module(m)
+        lib = load()
+        m.bind(*[C.cast(getattr(lib, n), C.c_void_p).value
+                 for n in ("ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace")])
+        _tensor_args = m
+    return _tensor_args
 
 
 def ps_build_slots(ctx_lens, new_lens, block_tables, slots, positions, token_start, ctx_lens_out, *, block_size: int,
@@ -353,23 +287,9 @@ def ps_build_slots(ctx_lens, new_lens, block_tables, slots, positions, token_sta
     [max_tokens]; positions int32 [max_tokens] or None; token_start int32 [batch + 1]; free_ids int32 [num_gpu_blocks]
     with free_count and free_count_out int32 [1], or None when the tables hold the blocks already.  ctx_lens_out may
     be ctx_lens and free_count_out may be free_count.  See ps_build_slots in the header."""
-    torch = _import_torch()
-    i32 = torch.int32
-    try:
-        dev, batch, room = slots.get_device(), ctx_lens.numel(), slots.numel()
-        if dev < 0 or block_tables.dim() != 2 or block_tables.shape[1] == 0:
-            raise _BadArg("need slots on a device and block_tables [batch][stride]")
-        stride = block_tables.shape[1]
-        args = _pack_slots(
-            _vec("ctx_lens", ctx_lens, i32, batch, dev), _vec("new_lens", new_lens, i32, batch, dev),
-            _vec("block_tables", block_tables, i32, batch * stride, dev), _vec("free_ids", free_ids, i32, num_gpu_blocks, dev),
-            _vec("free_count", free_count, i32, 1, dev), _vec("free_count_out", free_count_out, i32, 1, dev),
-            _vec("slots", slots, torch.int64, 0, dev), _vec("positions", positions, i32, room, dev),
-            _vec("token_start", token_start, i32, batch + 1, dev), _vec("ctx_lens_out", ctx_lens_out, i32, batch, dev),
-            _vec("status_word", status_word, i32, 1, dev), batch, stride, block_size, num_gpu_blocks, room, 0)
-    except (_BadArg, struct.error) as e:
-        return PS_ERR_INVALID, f"ps_build_slots: {e}"
-    return _enqueue(load().ps_build_slots, args, dev)
+    return (_tensor_args or _load_tensor_args()).build_slots(
+        ctx_lens, new_lens, block_tables, slots, positions, token_start, ctx_lens_out, block_size, num_gpu_blocks, free_ids,
+        free_count, free_count_out, status_word)
 
 
 def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=None, vpool=None, slots=None, freq_axis=None,
@@ -380,85 +300,19 @@ def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=Non
     q, k_out may be k; rows may be strided); positions int32 [tokens] or [axes][tokens] (an axis stride of 0 is fine);
     inv_freq float32 [rot_dim / 2], or None for no rotation; freq_axis: a list with the axis of every frequency, or None
     for axis 0; kpool, vpool [blocks][block_size][kv heads][dim] with slots int64 [tokens].  See ps_rope_append in the header."""
-    torch = _import_torch()
-    i32 = torch.int32
-    try:
-        ref = q if q is not None else k
-        if ref is None or ref.dim() != 3 or ref.get_device() < 0:
-            raise _BadArg("need q or k, a device tensor [tokens][heads][dim]")
-        dev, dt, (T, hq, D) = ref.get_device(), ref.dtype, ref.shape
-        code = _dtype_code(dt)
-        q_at = k_at = v_at = qo_at = ko_at = kp_at = vp_at = pos_at = 0
-        axis_of = b""
-        hkv = nb = bs = half = axes = q_st = k_st = v_st = qo_st = ko_st = kb = vb = ax_st = 0
-        if q is None:
-            hq = 0
-        else:
-            q_at, q_st = q.data_ptr(), _rows("q", q, T, hq, D, dt, dev)
-            if q_out is None:
-                raise _BadArg("q needs q_out")
-            qo_at, qo_st = q_out.data_ptr(), _rows("q_out", q_out, T, hq, D, dt, dev)
-            if qo_st < hq * D:
-                raise _BadArg("q_out: rows overlap")
-        if k is not None:
-            hkv = k.shape[1]
-            k_at, k_st = k.data_ptr(), _rows("k", k, T, hkv, D, dt, dev)
-            if k_out is not None:
-                ko_at, ko_st = k_out.data_ptr(), _rows("k_out", k_out, T, hkv, D, dt, dev)
-                if ko_st < hkv * D:
-                    raise _BadArg("k_out: rows overlap")
-        elif k_out is not None or kpool is not None:
-            raise _BadArg("k_out and pools need k")
-        if kpool is not None or vpool is not None:
-            if kpool is None or vpool is None or v is None or slots is None or kpool.dim() != 4:
-                raise _BadArg("an append needs k, v, slots and two pools [blocks][block_size][heads][dim]")
-            nb, bs, _, _ = kpool.shape
-            kp_at, kb = kpool.data_ptr(), _pool("kpool", kpool, nb, bs, hkv, D, dt, dev)
-            vp_at, vb = vpool.data_ptr(), _pool("vpool", vpool, nb, bs, hkv, D, dt, dev)
-            v_at, v_st = v.data_ptr(), _rows("v", v, T, hkv, D, dt, dev)
-        if inv_freq is not None and inv_freq.numel() > 0:
-            half = inv_freq.numel()
-            shape = positions.shape if positions is not None else ()
-            if (len(shape) not in (1, 2) or shape[-1] != T or positions.dtype is not i32 or positions.get_device() != dev
-                    or (positions.stride(-1) != 1 and T > 1)):
-                raise _BadArg("positions: need int32 [tokens] or [axes][tokens] on the tensors' device")
-            pos_at = positions.data_ptr()
-            if len(shape) == 1:
-                axes = 1
-            else:
-                axes = shape[0]
-                ax_st = positions.stride(0) if axes > 1 else 0
-            if freq_axis is not None:
-                axis_of = bytes(freq_axis)
-                if len(axis_of) != half or half > 256:
-                    raise _BadArg("freq_axis: need one axis per frequency, of at most 256")
-        args = _pack_rope(
-            q_at, k_at, v_at, qo_at, ko_at, kp_at, vp_at, _vec("slots", slots, torch.int64, T, dev), pos_at,
-            _vec("inv_freq", inv_freq, torch.float32, half, dev), _vec("status_word", status_word, i32, 1, dev),
-            q_st, k_st, v_st, qo_st, ko_st, kb, vb, ax_st, T, hq, hkv, D, 2 * half, axes, bs, nb, code,
-            (PS_ROPE_NEIGHBOURS if neighbours else 0) | (PS_ROPE_INVERSE if inverse else 0), axis_of)
-    except (_BadArg, struct.error, ValueError, TypeError) as e:
-        return PS_ERR_INVALID, f"ps_rope_append: {e}"
-    return _enqueue(load().ps_rope_append, args, dev)
-
-
-_workspace_bytes = {}
+    return (_tensor_args or _load_tensor_args()).rope_append(
+        q, k, q_out, k_out, positions, inv_freq, v, kpool, vpool, slots, freq_axis, neighbours, inverse, status_word)
 
 
 def ps_paged_attn_workspace(num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int] = None) -> int:
     """Bytes of workspace that ps_paged_attn needs for these heads on a device (default: the current one)."""
-    torch = _import_torch()
-    dev = torch.cuda.current_device() if device is None else device
-    key = (dev, num_kv_heads, num_q_heads, head_dim)
-    n = _workspace_bytes.get(key)
-    if n is None:
-        out = C.c_int64()
-        with torch.cuda.device(dev):
-            rc = load().ps_paged_attn_workspace(num_kv_heads, num_q_heads, head_dim, C.byref(out))
-        if rc != PS_OK:
-            raise PsError(rc, "ps_paged_attn_workspace", "unsupported heads, or no device")
-        n = _workspace_bytes[key] = out.value
-    return n
+    import torch
+    out = C.c_int64()
+    with torch.cuda.device(torch.cuda.current_device() if device is None else device):
+        rc = load().ps_paged_attn_workspace(num_kv_heads, num_q_heads, head_dim, C.byref(out))
+    if rc != PS_OK:
+        raise PsError(rc, "ps_paged_attn_workspace", "unsupported heads, or no device")
+    return out.value
 
 
 def ps_paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, *, lse=None, window: int = 0, scale: Optional[float] = None,
@@ -469,36 +323,8 @@ def ps_paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, *, lse=None, win
     strided; block_tables int32 [at least batch][stride]; ctx_lens int32 [batch]; lse float32 [batch][q heads] or
     None; scale None = 1 / sqrt(dim).  workspace: a uint8 tensor of ps_paged_attn_workspace bytes; by default one is
     taken from torch's allocator on the current stream for the duration of the call.  See ps_paged_attn in the header."""
-    torch = _import_torch()
-    try:
-        if q.dim() != 3 or q.get_device() < 0 or kpool.dim() != 4 or block_tables.dim() != 2:
-            raise _BadArg("need q [batch][heads][dim], kpool [blocks][block_size][heads][dim] and block_tables [batch][stride] on a device")
-        dev, dt, (batch, hq, D), (nb, bs, hkv, _) = q.get_device(), q.dtype, q.shape, kpool.shape
-        code = _dtype_code(dt)
-        kb = _pool("kpool", kpool, nb, bs, hkv, D, dt, dev)
-        vb = _pool("vpool", vpool, nb, bs, hkv, D, dt, dev)
-        q_st, o_st = _rows("q", q, batch, hq, D, dt, dev), _rows("out", out, batch, hq, D, dt, dev)
-        stride = block_tables.shape[1]
-        need = _workspace_bytes.get((dev, hkv, hq, D))
-        if need is None:
-            _need(hkv > 0 and D in (64, 128) and hq > 0 and hq % hkv == 0 and hq // hkv <= 64 and hkv <= 1024,
-                  "head_dim must be 64 or 128, with 1 to 64 query heads per KV head")
-            need = ps_paged_attn_workspace(hkv, hq, D, dev)
-        if scale is not None and scale == 0:
-            raise _BadArg("scale: 0 is not a factor")
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            ws_at, ws_bytes = workspace.data_ptr(), need
-        else:
-            ws_at, ws_bytes = _vec("workspace", workspace, torch.uint8, need, dev), workspace.numel()
-        args = _pack_attn(
-            kpool.data_ptr(), vpool.data_ptr(), q.data_ptr(), out.data_ptr(), _vec("lse", lse, torch.float32, batch * hq, dev),
-            _vec("block_tables", block_tables, torch.int32, batch * stride, dev), _vec("ctx_lens", ctx_lens, torch.int32, batch, dev),
-            _vec("status_word", status_word, torch.int32, 1, dev), ws_at, ws_bytes, kb, vb, q_st, o_st,
-            batch, stride, hkv, hq, D, bs, nb, window, scale or 0.0, code)
-    except (_BadArg, struct.error) as e:
-        return PS_ERR_INVALID, f"ps_paged_attn: {e}"
-    return _enqueue(load().ps_paged_attn, args, dev)
+    return (_tensor_args or _load_tensor_args()).paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, lse, window, scale,
+                                                            status_word, workspace)
 
 
 def ps_order_queue(exec_us, remain_us, weight, *, eta: float, gamma: float, t_c: float, waited_us=None, tau: float = 0.0):

@@ -1,8 +1,9 @@
-"""Builds the CUDA library in-tree with nvcc for sm_100a.
+"""Builds the CUDA library in-tree with nvcc for sm_100a, and the binding's module for torch tensors with g++.
 
     python -m paper_2512_12928_b200.build [--force] [--verbose]
 
-Output: paper_2512_12928_b200/lib/libps_kvswap.so (C ABI declared in include/ps_kvswap.h).
+Output: paper_2512_12928_b200/lib/libps_kvswap.so (C ABI declared in include/ps_kvswap.h) and
+paper_2512_12928_b200/lib/_ps_tensor_args.so (where torch is installed; the library does not need it).
 """
 from __future__ import annotations
 
@@ -28,6 +29,36 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found; set NVCC or put CUDA's bin directory on PATH")
 
 
+TENSOR_ARGS_PATH = os.path.join(LIB_DIR, "_ps_tensor_args.so")
+TENSOR_ARGS_SOURCE = os.path.join(CSRC, "ps_tensor_args.cpp")
+
+
+def build_tensor_args(force: bool = False) -> str:
+    """The module that takes torch tensors apart; nothing to do where torch is not installed."""
+    import importlib.util
+    if importlib.util.find_spec("torch") is None:
+        return ""
+    deps = [TENSOR_ARGS_SOURCE, os.path.join(ROOT, "include", "ps_kvswap.h")]
+    if not force and os.path.exists(TENSOR_ARGS_PATH) and all(
+            os.path.getmtime(d) <= os.path.getmtime(TENSOR_ARGS_PATH) for d in deps):
+        return TENSOR_ARGS_PATH
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    os.makedirs(LIB_DIR, exist_ok=True)
+    cmd = [shutil.which("g++") or "g++", "-shared", "-std=c++17", "-O2", "-fPIC", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-I", os.path.join(base, "include"), "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-o", TENSOR_ARGS_PATH,
+           TENSOR_ARGS_SOURCE, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if proc.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + proc.stdout[-4000:])
+    return TENSOR_ARGS_PATH
+
+
 def needs_build() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
@@ -37,6 +68,7 @@ def needs_build() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_tensor_args(force)
     if not force and not needs_build():
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)
