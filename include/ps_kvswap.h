@@ -365,6 +365,9 @@ int32_t ps_decode_attn_static(const void* kpool, const void* vpool, const void* 
  * ps_build_slots gives them slot -1), 4 = ps_build_slots found too few free blocks, 5 = a length out of range.
  * The launches are programmatically dependent on the kernel before them on the stream and wait for its completion
  * before they read or write anything, like ps_decode_attn's.
+ * They know nothing of transfers.  Over a context's pools, call them on its compute stream: offloads are ordered behind
+ * what is enqueued there; and call ps_reload_fence before the first that touches blocks of a request that a reload
+ * has just completed.
  * Pools are [num_gpu_blocks][block_size][num_kv_heads][head_dim] as everywhere; here their blocks may lie any
  * *_block_stride elements apart (at least a block), e.g. when one buffer holds K and V of a block side by side.  The
  * pools of a context are a dense case of it.  Strides are counted in elements. */

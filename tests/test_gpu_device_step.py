@@ -491,7 +491,8 @@ def test_tensors_that_do_not_fit_are_refused():
                 dict(out=torch.zeros((3, 8, 128), device="cuda", dtype=bf)[:, :, 1:65]), dict(out=q[:1].expand(3, 8, 64)),
                 dict(block_tables=t.long()), dict(block_tables=t[:2]), dict(block_tables=t[:, :2]), dict(ctx_lens=n[:2]), dict(ctx_lens=n.cpu()),
                 dict(lse=torch.zeros((3, 8), device="cuda", dtype=bf)), dict(lse=torch.zeros((2, 8), device="cuda")), dict(scale=0.0),
-                dict(scale=float("nan")), dict(window=-1), dict(q=torch.zeros((3, 7, 64), device="cuda", dtype=bf)),
+                dict(scale=float("nan")), dict(scale="a"), dict(window=-1), dict(window=1 << 40), dict(window=1 << 70), dict(window=None),
+                dict(q=None), dict(out=None), dict(ctx_lens=None), dict(block_tables=None), dict(kpool=[1]), dict(q=torch.zeros((3, 7, 64), device="cuda", dtype=bf)),
                 dict(kpool=kp.view(-1)[4:4 + 7 * 16 * 128].view(7, 16, 2, 64), vpool=kp[:7])):
         rc, text = B.ps_paged_attn(**{**good, **bad})
         assert rc == B.PS_ERR_INVALID and text, bad.keys()
@@ -502,7 +503,7 @@ def test_tensors_that_do_not_fit_are_refused():
     for bad in (dict(q_out=None), dict(v=None), dict(slots=None), dict(slots=pos), dict(slots=sl[:2]), dict(positions=None),
                 dict(positions=pos[:2]), dict(positions=pos.long()), dict(inv_freq=inv.double()), dict(inv_freq=torch.zeros(33, device="cuda")),
                 dict(vpool=None), dict(kpool=None), dict(kpool=kp.to(h)), dict(k=k[:2]), dict(v=k.to(h)), dict(freq_axis=[0] * 31),
-                dict(freq_axis=[1] * 32), dict(freq_axis=[-1] * 32), dict(freq_axis=[0.5] * 32), dict(q_out=q[:1].expand(3, 8, 64)), dict(k=None)):
+                dict(freq_axis=[1] * 32), dict(freq_axis=[-1] * 32), dict(freq_axis=[0.5] * 32), dict(freq_axis=[1 << 80] * 32), dict(freq_axis=3), dict(q_out=q[:1].expand(3, 8, 64)), dict(k=None)):
         rc, text = B.ps_rope_append(**{**good, **bad})
         assert rc == B.PS_ERR_INVALID and text, bad.keys()
     ids, cnt = dev([0] * 8), dev([8])
@@ -511,9 +512,10 @@ def test_tensors_that_do_not_fit_are_refused():
     assert B.ps_build_slots(**good)[0] == B.PS_OK
     for bad in (dict(new_lens=n[:2]), dict(ctx_lens=n.long()), dict(block_tables=t[:2]), dict(block_tables=t[0]), dict(slots=pos),
                 dict(positions=pos[:2]), dict(token_start=n), dict(free_ids=ids[:7]), dict(free_count=None), dict(free_count_out=None),
-                dict(block_size=0), dict(ctx_lens_out=n.cpu()), dict(slots=sl.cpu())):
+                dict(block_size=0), dict(block_size=1 << 70), dict(block_size=1.5), dict(new_lens=None), dict(token_start=None), dict(ctx_lens_out=n.cpu()), dict(slots=sl.cpu())):
         rc, text = B.ps_build_slots(**{**good, **bad})
         assert rc == B.PS_ERR_INVALID and text, bad.keys()
+    assert B.ps_build_slots(**{**good, "block_size": np.int64(16)})[0] == B.PS_OK
     torch.cuda.synchronize()
 
 
@@ -671,4 +673,46 @@ def test_attention_next_to_a_contexts_own():
     args = kp[0], vp[0], q_rot, [lib.block_table(r)[0] for r in reqs], [n + 1 for n in before]
     check_attn(a, la, attn_want(*args))
     check_attn(b, lb, attn_want(*args, weight_error=HALF_STEP[torch.bfloat16]))   # rounds a weight once
+    lib.destroy()
+
+
+def test_attention_over_a_request_that_was_offloaded_and_reloaded():
+    """The context moves a request out and back; behind the fence the device-side step appends to it and attends it."""
+    rng = np.random.default_rng(24)
+    L, hkv, hq, D, S, nb = 2, 4, 8, 64, 16, 500
+    kp, vp = (torch.randn((L, nb, S, hkv, D), device="cuda").bfloat16() for _ in range(2))
+    lib = B.KVSwap(num_layers=L, num_kv_heads=hkv, num_q_heads=hq, head_dim=D, block_size=S, num_gpu_blocks=nb, max_blocks_per_req=200,
+                   max_batch=8, host_pool_bytes=256 << 20, initial_free_order=rng.permutation(nb), k_pools=[kp[l] for l in range(L)],
+                   v_pools=[vp[l] for l in range(L)])
+    ctx = [1500, 40, 900]
+    for r, n in enumerate(ctx):
+        assert lib.kv_alloc(r, n + 1) == B.PS_OK                   # with room for the token to come
+    old = lib.block_table(0)[0]
+    K, V = kp[:, torch.tensor(old, device="cuda")].clone(), vp[:, torch.tensor(old, device="cuda")].clone()
+    assert lib.swap_out(0) == B.PS_OK and lib.sync() == B.PS_OK
+    kp[:, torch.tensor(old, device="cuda")] = 0
+    vp[:, torch.tensor(old, device="cuda")] = 0
+    assert lib.swap_in_begin(0) == B.PS_OK
+    rc, _, _ = lib.step(None, None, [], -1)                        # the whole reload, asynchronously
+    assert rc == B.PS_OK and lib.reload_fence(-1) == B.PS_OK
+    ids = [lib.block_table(r)[0] for r in range(3)]
+    tables = tables_tensor(ids, 200)
+    d_ctx, start = dev(ctx), torch.zeros(4, device="cuda", dtype=I32)
+    slots, pos = torch.zeros(3, device="cuda", dtype=torch.int64), torch.zeros(3, device="cuda", dtype=I32)
+    assert B.ps_build_slots(d_ctx, dev([1] * 3), tables, slots, pos, start, d_ctx, block_size=S, num_gpu_blocks=nb) == (B.PS_OK, "")
+    outs = []
+    for l in range(L):
+        q, k, v = rope_inputs(3, hq, hkv, D, torch.bfloat16, 30 + l)
+        assert B.ps_rope_append(None, k, None, None, None, None, v=v, kpool=kp[l], vpool=vp[l], slots=slots) == (B.PS_OK, "")
+        out, lse = torch.empty((3, hq, D), device="cuda", dtype=torch.bfloat16), torch.empty((3, hq), device="cuda")
+        assert B.ps_paged_attn(kp[l], vp[l], q, out, tables, d_ctx, lse=lse) == (B.PS_OK, "")
+        outs.append((q, k, v, out, lse))
+    assert lib.sync() == B.PS_OK, lib.last_error()
+    new = torch.tensor(ids[0], device="cuda")
+    for l, (q, k, v, out, lse) in enumerate(outs):
+        for pool, was, row in ((kp, K, k), (vp, V, v)):            # the reloaded bytes, and the appended row
+            want = was[l].clone()
+            want.view(-1, hkv, D)[ctx[0]] = row[0]
+            assert torch.equal(pool[l, new], want)
+        check_attn(out, lse, attn_want(kp[l], vp[l], q, ids, [n + 1 for n in ctx]))
     lib.destroy()
