@@ -21,7 +21,8 @@ inline int32_t launch_fail(char* err_buf, int32_t err_cap, const char* where, cu
 }
 
 // A launch that may be scheduled and set up under the tail of the kernel before it on the stream.  The kernel has to
-// execute griddepcontrol.wait, in every thread, before it touches memory.
+// execute griddepcontrol.wait, in every thread, before it touches memory.  What it reads then may have been written since
+// its CTAs started, so it loads with ordinary loads and not through the read-only path.
 template <typename... P, typename... A>
 cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A... args) {
     cudaLaunchAttribute attr{};

@@ -192,7 +192,7 @@ struct Cursor {
         if (more) row(p, next_len);
         look_ahead(p);
     }
-    __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? __ldg(p.ctx + b + 1) : 0; }
+    __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? p.ctx[b + 1] : 0; }
 };
 
 // The softmax state of a warp.  Lane (g = lane / 4, c = lane % 4) holds heads 8 t + 2 c and 8 t + 2 c + 1 of column tile t:
@@ -256,7 +256,7 @@ struct Worker {
             for (int j = 0; j < D / 16; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    q[t][j][h] = 8 * t + g < n ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 8 * h)) : 0u;
+                    q[t][j][h] = 8 * t + g < n ? *reinterpret_cast<const uint32_t*>(src + 16 * j + 8 * h) : 0u;
         }
     }
 
@@ -284,7 +284,7 @@ struct Worker {
         if (t < cur.end) {
             const int32_t blk = block_of(t, p);
             at = t - blk * p.block_size;
-            id = __ldg(table + blk);
+            id = table[blk];
         }
     }
 
@@ -468,7 +468,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     int mine = 0, len = 0;
 #pragma unroll 4
     for (int b = b_lo; b < b_hi; ++b) {
-        len = __ldg(p.ctx + b);
+        len = p.ctx[b];
         mine += row_tiles(p, len) * p.chunks;
     }
     Cursor cur;
@@ -497,7 +497,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         if (per > 1)
 #pragma unroll 1
             for (;; ++cur.b) {
-                len = __ldg(p.ctx + cur.b);
+                len = p.ctx[cur.b];
                 const int n = row_tiles(p, len) * p.chunks;
                 if (begin < a + n) break;
                 a += n;

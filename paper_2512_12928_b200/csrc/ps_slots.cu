@@ -289,11 +289,11 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
     for (int64_t b = me; b <= a.batch; b += everyone) a.token_start[b] = failed ? 0 : b < a.batch ? tok[b] : total;
     auto returned = [&](int e) {                // the e-th id that goes back
         const int k = row_of(back, a.batch, e);
-        return __ldg(a.block_tables + (int64_t)k * a.table_stride + (e - back[k]));
+        return a.block_tables[(int64_t)k * a.table_stride + (e - back[k])];
     };
     auto popped = [&](int e) {                  // the e-th id that is taken
         const int at = top - 1 - e;
-        return at < count ? __ldg(a.free_ids + at) : returned(at - count);
+        return at < count ? a.free_ids[at] : returned(at - count);
     };
     if (!failed && pool) {
         for (int64_t e = me; e < all.v[2]; e += everyone) a.free_ids[count + e] = returned((int)e);
@@ -310,7 +310,7 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
             p = ctx[k] + ((int)t - tok[k]);
             const int32_t blk = (int32_t)((uint32_t)p / (uint32_t)a.block_size), old_blocks = blocks_of(a, ctx[k]);
             const int32_t id = pool && blk >= old_blocks ? popped(need[k] + (blk - old_blocks))
-                                                         : __ldg(a.block_tables + (int64_t)k * a.table_stride + blk);
+                                                         : a.block_tables[(int64_t)k * a.table_stride + blk];
             if ((unsigned)id < (unsigned)a.num_gpu_blocks) slot = (int64_t)id * a.block_size + (p - blk * a.block_size);
             else if (a.status_word) *(volatile int32_t*)a.status_word = kStatusBadId;
         }
