@@ -308,6 +308,7 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
         return bad("ps_rope_append: head_dim is at most 512, rot_dim an even number up to head_dim");
     if (a.dtype != PS_DTYPE_BF16 && a.dtype != PS_DTYPE_FP16) return bad("ps_rope_append: dtype must be PS_DTYPE_BF16 or PS_DTYPE_FP16");
     if (a.flags & ~(PS_ROPE_NEIGHBOURS | PS_ROPE_INVERSE)) return bad("ps_rope_append: unknown flag");
+    if (a.tokens == 0) return PS_OK;         // tensors without elements have no address
     const bool append = a.kpool || a.vpool;
     const bool do_q = a.q != nullptr && a.num_q_heads > 0, do_k = a.k != nullptr && a.num_kv_heads > 0;
     if (do_q && !a.q_out) return bad("ps_rope_append: q without q_out");
@@ -326,7 +327,7 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
             axes.v[i] = a.freq_axis[i];
         }
     }
-    if (a.tokens == 0 || (!do_q && !do_k)) return PS_OK;
+    if (!do_q && !do_k) return PS_OK;
     if (a.rot_dim > 0 && !a.positions) return bad("ps_rope_append: a rotation needs positions, inv_freq and 1 to 8 axes");
     RopeParams p{};
     p.q = a.q, p.k = a.k, p.v = a.v, p.q_out = a.q_out, p.k_out = a.k_out, p.kpool = a.kpool, p.vpool = a.vpool;

@@ -212,7 +212,7 @@ PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
             }
             if (kpool || vpool) {
                 const at::Tensor* v = tensor("v", a[6]);
-                if (!kpool || !vpool || !v || !p.slots || kpool->dim() != 4)
+                if (!kpool || !vpool || !v || a[9] == Py_None || kpool->dim() != 4)
                     throw BadArg{"an append needs k, v, slots and two pools [blocks][block_size][heads][dim]"};
                 const int64_t shape[4] = {kpool->size(0), kpool->size(1), heads, D};
                 p.num_gpu_blocks = int_size("blocks", shape[0]);

@@ -254,6 +254,16 @@ def test_rope_text_uses_one_row_of_positions_for_all_axes():
     assert torch.equal(a, b)
 
 
+def test_rope_of_no_tokens():
+    q, k, v = rope_inputs(0, 4, 2, 64, torch.float16, 5, fused=False)
+    pool = torch.zeros((2, 16, 2, 64), device="cuda", dtype=torch.float16)
+    inv, none = torch.rand(32, device="cuda"), dev([], torch.int64)
+    for kw in (dict(), dict(v=v, kpool=pool, vpool=pool.clone(), slots=none)):
+        assert B.ps_rope_append(q, k, torch.empty_like(q), torch.empty_like(k), dev([]), inv, **kw) == (B.PS_OK, "")
+    torch.cuda.synchronize()
+    assert not pool.any()
+
+
 def test_rope_slots_outside_the_pool_are_reported_and_skipped():
     T, hkv, D = 4, 2, 64
     q, k, v = rope_inputs(T, 2, hkv, D, torch.bfloat16, 3)
@@ -624,6 +634,32 @@ def test_a_captured_decode_step_replayed_with_other_lengths():
         torch.cuda.synchronize()
         engines[0].check(new_a, qkv_a)
         engines[1].check(new_b, qkv_b)
+
+
+def test_a_captured_step_with_room_for_prompts():
+    """Lengths, stack and tables updated in place by the whole chip, and attended right behind it, over many replays."""
+    rng = np.random.default_rng(25)
+    e = Engine(rng, 40, 4, 2, 64, 16, 2400, 60, 5000, torch.bfloat16)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        e.enqueue()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        e.enqueue()
+    for step in range(12):
+        new = rng.integers(0, 120, e.rows) if step % 3 == 0 else np.ones(e.rows, int)
+        new[rng.random(e.rows) < 0.1] = -1
+        new[[c + max(n, 0) > e.stride * e.S for c, n in zip(e.m_ctx, new)]] = -1
+        qkv = torch.randn(tuple(e.qkv.shape), device="cuda").to(e.qkv.dtype)
+        e.new.copy_(dev(new.tolist()))
+        e.qkv.copy_(qkv)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            g.replay()
+        torch.cuda.synchronize()
+        e.check(new.tolist(), qkv)
 
 
 def test_calls_on_several_streams_at_once():
