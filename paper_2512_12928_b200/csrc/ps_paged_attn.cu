@@ -27,8 +27,8 @@
 // For the product with V a weight is split into two numbers of the inputs' type: one alone makes the result's error
 // 1.4 times what its own rounding costs, and the second product costs less than 1 % of the time.
 //
-// Work: the rows' tiles form one sequence that is cut into equal shares, one per CTA, from the lengths each CTA
-// reads itself: no plan is made on the host or by another kernel.  A row cut by a share's end leaves partial
+// Work: the rows' tiles form one sequence (with two places more for each row's start and end, which cost about two tiles'
+// time) that is cut into equal shares, one per CTA, from the lengths each CTA reads itself: no plan is made on the host or by another kernel.  A row cut by a share's end leaves partial
 // results (m, sum, accumulators) in the workspace, which a second kernel (paged_join_kernel) combines in order.
 // The join is a second launch rather than a last-arrival counter in the first: the workspace then needs no
 // initial state, and neither a replayed graph nor a call that shares it in turn can find a stale counter.
@@ -77,6 +77,7 @@ struct AttnParams {
     int32_t units, chunks, subs;     // units per CTA, CTAs' worth of units per row, token slices
     int32_t ctas;                    // of the main kernel
     int32_t step_log2;               // tokens of a tile of all slices
+    int32_t segment;                 // places that a segment's start and end take in the sequence that is shared out
     float scale_log2e;
 };
 
@@ -174,22 +175,27 @@ __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* k
     *n = min(p.rows, p.group - s * p.rows);
 }
 
-// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`.
+// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`, at `place` of
+// the sequence that is cut into shares: a segment (row and chunk) takes p.segment places for its start and end, then one
+// for each tile.
 struct Cursor {
-    int32_t b, chunk, i, tiles, first, end;
+    int32_t b, chunk, i, tiles, first, end, place;
     int32_t next_len;                        // of row b + 1, asked for while row b is worked on
     __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
         row_span(p, len, &first, &end);
         tiles = row_tiles(p, len);
         if (end != len && p.status) *(volatile int32_t*)p.status = kStatusLength;
     }
-    __device__ __forceinline__ void next(const AttnParams& p, bool more) {
+    __device__ __forceinline__ bool ends_segment() const { return i + 1 == tiles; }
+    __device__ __forceinline__ int32_t next_place(const AttnParams& p) const { return place + 1 + (ends_segment() ? p.segment : 0); }
+    __device__ __forceinline__ void next(const AttnParams& p, int32_t share_end) {
+        place = next_place(p);
         if (++i < tiles) return;
         i = 0;
         if (++chunk < p.chunks) return;
         chunk = 0;
         ++b;
-        if (more) row(p, next_len);
+        if (place < share_end) row(p, next_len);
         look_ahead(p);
     }
     __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? p.ctx[b + 1] : 0; }
@@ -456,6 +462,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     __shared__ float2 sh_ml[kMaxWarps][8 * NT];
     __shared__ int sh_sum[kMaxWarps];
     __shared__ int4 sh_begin;          // where the share begins: row, chunk, tile; the row's length
+    __shared__ int sh_place;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nwarps = blockDim.x >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -469,7 +476,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 4
     for (int b = b_lo; b < b_hi; ++b) {
         len = p.ctx[b];
-        mine += row_tiles(p, len) * p.chunks;
+        mine += (row_tiles(p, len) + p.segment) * p.chunks;
     }
     Cursor cur;
     int before = mine;
@@ -498,7 +505,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 1
             for (;; ++cur.b) {
                 len = p.ctx[cur.b];
-                const int n = row_tiles(p, len) * p.chunks;
+                const int n = (row_tiles(p, len) + p.segment) * p.chunks;
                 if (begin < a + n) break;
                 a += n;
             }
@@ -506,10 +513,12 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         cur.chunk = 0;
         cur.i = begin - a;
         if (p.chunks > 1) {
-            cur.chunk = cur.i / cur.tiles;
-            cur.i -= cur.chunk * cur.tiles;
+            cur.chunk = cur.i / (cur.tiles + p.segment);
+            cur.i -= cur.chunk * (cur.tiles + p.segment);
         }
+        cur.i = max(cur.i - p.segment, 0);        // a share that begins in a segment's first places has its first tile
         sh_begin = make_int4(cur.b, cur.chunk, cur.i, len);
+        sh_place = a + cur.chunk * (cur.tiles + p.segment) + p.segment + cur.i;
         // the first block ids, into L1 while the CTA meets
         const int32_t t = cur.first + (cur.i << p.step_log2);
         if (t < cur.end) {
@@ -519,15 +528,15 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     }
     __syncthreads();
     int4 cut = make_int4(0, 0, 0, 0);
-    if (begin < end) {
+    if (begin < end && sh_place < end) {         // else there is no tile in it
         const int4 start = sh_begin;
         cur.b = start.x;
         cur.chunk = start.y;
         cur.i = start.z;
+        cur.place = sh_place;
         cur.look_ahead(p);
         cur.row(p, start.w);
         Cursor ahead = cur;                      // the tile that is requested next
-        int asked = begin;
         int slot = 0;                            // stage that is filled next
         wk.enter(ahead);
         wk.load_ids(ahead);
@@ -536,7 +545,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         int32_t lo = 0;
         bool fresh = true;
 #pragma unroll 1
-        for (int at = begin - (R::kStages - 1); at < end; ++at) {   // the first rounds only fill the ring
+        for (int fill = R::kStages - 1; cur.place < end;) {
             copies_wait<R::kStages - 2>();
             __syncwarp();                        // the other lanes' copies too, and they have left the stage before
             const int filled = slot;             // the stage that the tile before left
@@ -545,16 +554,19 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
             wk.mask = wk.next_mask;
             uint4 k[Worker<T, D, NT>::kSub][D / 16];
             wk.read_keys(slot, k);               // in the first rounds what it reads is not used
-            if (asked < end) {
+            if (ahead.place < end) {
                 wk.next_mask = wk.copy_tile(filled);
-                if (++asked < end) {
-                    ahead.next(p, true);
+                ahead.next(p, end);
+                if (ahead.place < end) {
                     if (ahead.i == 0) wk.enter(ahead);
                     wk.load_ids(ahead);
                 }
             }
             copies_commit();
-            if (at < begin) continue;
+            if (fill > 0) {                      // the first rounds only fill the ring
+                --fill;
+                continue;
+            }
             const int unit = cur.chunk * p.units + wk.unit_in_cta;
             if (fresh) {
                 state_reset(st);
@@ -565,8 +577,8 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 fresh = false;
             }
             wk.attend(slot, k, on, st);
-            const bool seg_end = cur.i + 1 == cur.tiles;
-            if (seg_end || at + 1 == end) {
+            const bool seg_end = cur.ends_segment();
+            if (seg_end || cur.next_place(p) >= end) {
                 const bool whole = lo == 0 && seg_end;
                 // The states of the slices go through the stage that has just been read, heads as rows, and come
                 // back as rows of four dims a lane.  (The places' exclusive or keeps the writes free of conflicts.)
@@ -649,12 +661,12 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 }
                 if (p.subs > 1) __syncthreads(); else __syncwarp();      // the stage is free again
                 if (!seg_end) {
-                    const int from = (at - cur.i) / share;
-                    cut = make_int4(cur.b, cur.chunk, (at + cur.tiles - cur.i - 1) / share - from + 1, from);
+                    const int from = (cur.place - cur.i) / share;      // the CTAs of the segment's first and last tile
+                    cut = make_int4(cur.b, cur.chunk, (cur.place + cur.tiles - cur.i - 1) / share - from + 1, from);
                 }
                 fresh = true;
             }
-            cur.next(p, at + 1 < end);
+            cur.next(p, end);
         }
     }
     if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
@@ -977,7 +989,11 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     p.splits = y.splits, p.rows = y.rows, p.units = y.units, p.chunks = y.chunks, p.subs = y.subs, p.ctas = y.ctas;
     for (p.step_log2 = a.head_dim == 128 ? 4 : 5; (1 << p.step_log2) < 2048 / a.head_dim * y.subs; ++p.step_log2) {}   // Ring::kTokens
     p.scale_log2e = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * kLog2e;
-    if ((p.room >> p.step_log2) + 2 > (1 << 30) / ((int64_t)a.batch * y.chunks))
+    // A segment's start and end take about the time of two tiles.  Not counted (1 in brackets), 200 rows of 10 to 100 tokens
+    // take 20.2 instead of 17.2 us (17.9), 33 ragged rows with a window 19.6 instead of 18.1 (18.8), 64 rows of 1024 to
+    // 4096 102.4 either way.  With few segments a CTA has one whatever it costs.
+    p.segment = (int64_t)a.batch * y.chunks >= y.ctas / 8 ? 2 : 0;
+    if ((p.room >> p.step_log2) + 4 > (1 << 30) / ((int64_t)a.batch * y.chunks))
         return bad("ps_paged_attn: the tables of the batch have room for more than 2^30 tiles of tokens");
     // rows that cannot be longer than one tile are never cut
     const int64_t longest = a.window > 0 && a.window < p.room ? a.window : p.room;
