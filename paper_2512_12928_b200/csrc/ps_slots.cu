@@ -10,13 +10,13 @@
 // The work is a few words per row and token; what bounds it is latency: the chain "load lengths, scan, load a free
 // id, store".  Two ways, chosen by the room for tokens:
 //   - slots_one_cta_kernel: one CTA scans, pushes, pops and maps; barriers order its steps and one launch does all.
-//     Up to 2048 tokens, or 4096 in place (64 rows of a token each: 3.1 us; 200 rows: 5.4 us for 2000 tokens, 7.0 for
-//     4000, 14.4 for 16000).
+//     For room for up to 512 tokens (2048 with over 512 rows, 4096 in place): 64 rows of a token each 3.1 us; 200 rows
+//     4.6 us for 1000 tokens, 5.4 for 2000, 7.0 for 4000, 14.4 for 16000.
 //   - slots_wide_kernel: every CTA scans all rows for itself (cheaper than another launch) and takes its part of
 //     pushes, pops and tokens.  A popped id is found without waiting for the pushes: an index above the old top
 //     belongs to the table of a row that ended, which a search in the scanned counts names.  Where lengths or count are
 //     updated in place, a second kernel of one CTA does that when nobody reads them any more, which takes 2.5 us more.
-//     (200 rows: 5.8 us for 2000 to 16000 tokens.)
+//     (200 rows: 4.1 us for 1000 to 16000 tokens; 1024 rows of a token each 6.5 us and 5.8 in one CTA.)
 // Work on blocks and tokens is dealt to threads by the scanned counts (binary search in shared memory), so one long
 // prompt costs the same as many short ones.
 #include <algorithm>
@@ -32,9 +32,7 @@ constexpr int kStatusLength = 5;    // a length, a total or the free count is ou
 constexpr int kStatusBadId = 2;     // a block id outside the pool
 
 constexpr int kMaxThreads = 1024;
-constexpr int kWideThreads = 1024;
-constexpr int32_t kOneCtaTokens = 2048;  // room for at most so many tokens: one CTA; in place twice as many
-constexpr int kWideCtas = 148;          // one per SM: each scans all rows
+constexpr int kWideAtOnce = 148 * 1024;  // threads: each CTA scans all rows
 constexpr int32_t kWideRows = 4096;      // the scanned counts of so many rows fit into shared memory
 
 struct Row {
@@ -241,7 +239,7 @@ __device__ __forceinline__ void update_count(const ps_slots_args& a, int code, i
 
 // Every CTA knows all rows; the CTAs share pushes, pops and tokens.  Reads what it does not write: table entries of
 // blocks that rows have, and the stack below its top.  apart: lengths and count have places of their own to go to.
-__global__ void __launch_bounds__(kWideThreads)
+__global__ void __launch_bounds__(kMaxThreads)
 slots_wide_kernel(const ps_slots_args a, bool apart) {
     extern __shared__ int32_t rows_smem[];     // [batch] each: tokens, needs, returns before the row; its length
     int32_t *tok = rows_smem, *need = tok + a.batch, *back = need + a.batch, *ctx = back + a.batch;
@@ -251,7 +249,7 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int32_t count = pool ? *a.free_count : 0;
-    const int per = (a.batch + kWideThreads - 1) / kWideThreads;
+    const int per = (a.batch + (int)blockDim.x - 1) / (int)blockDim.x;
     const int b_lo = min(a.batch, tid * per), b_hi = min(a.batch, b_lo + per);
     bool bad = false;
     Row r{0, 0, 0, 0, 0};
@@ -266,7 +264,7 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
     const int code = refusal(a, __syncthreads_or(bad), all.v[0], all.v[1], all.v[2], count);
     const bool failed = code != 0;
     if (apart && blockIdx.x == 0) {
-        for (int b = tid; b < a.batch; b += kWideThreads) update_row(a, b, code);
+        for (int b = tid; b < a.batch; b += blockDim.x) update_row(a, b, code);
         if (tid == 0) update_count(a, code, count, all);
     }
     const int32_t total = failed ? 0 : (int32_t)all.v[0];
@@ -285,7 +283,7 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
         }
         __syncthreads();
     }
-    const int64_t me = (int64_t)blockIdx.x * kWideThreads + tid, everyone = (int64_t)gridDim.x * kWideThreads;
+    const int64_t me = (int64_t)blockIdx.x * blockDim.x + tid, everyone = (int64_t)gridDim.x * blockDim.x;
     for (int64_t b = me; b <= a.batch; b += everyone) a.token_start[b] = failed ? 0 : b < a.batch ? tok[b] : total;
     auto returned = [&](int e) {                // the e-th id that goes back
         const int k = row_of(back, a.batch, e);
@@ -296,7 +294,8 @@ slots_wide_kernel(const ps_slots_args a, bool apart) {
         return at < count ? a.free_ids[at] : returned(at - count);
     };
     if (!failed && pool) {
-        for (int64_t e = me; e < all.v[2]; e += everyone) a.free_ids[count + e] = returned((int)e);
+        // by the last CTAs first: the first ones take the blocks
+        for (int64_t e = everyone - 1 - me; e < all.v[2]; e += everyone) a.free_ids[count + e] = returned((int)e);
         for (int64_t e = me; e < all.v[1]; e += everyone) {
             const int k = row_of(need, a.batch, (int)e);
             a.block_tables[(int64_t)k * a.table_stride + blocks_of(a, ctx[k]) + ((int)e - need[k])] = popped((int)e);
@@ -358,17 +357,19 @@ extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char*
     cudaStream_t s = (cudaStream_t)stream;
     const bool apart = a.ctx_lens_out != a.ctx_lens && (!a.free_ids || a.free_count_out != a.free_count);
     cudaError_t e;
-    if (a.max_tokens <= (apart ? 1 : 2) * kOneCtaTokens || a.batch > kWideRows) {
+    const int32_t one_cta = !apart ? 4096 : a.batch <= 512 ? 512 : 2048;    // room for so many tokens
+    if (a.max_tokens <= one_cta || a.batch > kWideRows) {
         // few rows and tokens: fewer warps make the barriers of the scan cheaper
         const int threads = a.batch <= 256 && a.max_tokens <= 1024 ? 256 : kMaxThreads;
         e = ps::launch_dependent(slots_one_cta_kernel, dim3(1), dim3(threads), 0, s, a);
     } else {
-        // a token a thread, at most a CTA per SM
-        const int ctas = (int)std::min<int64_t>(((int64_t)a.max_tokens + kWideThreads - 1) / kWideThreads, kWideCtas);
+        // a row a thread in the scan, and a token a thread
+        const int threads = a.batch <= 256 ? 256 : a.batch <= 512 ? 512 : kMaxThreads;
+        const int ctas = (int)std::min<int64_t>(((int64_t)a.max_tokens + threads - 1) / threads, kWideAtOnce / threads);
         const size_t smem = (size_t)a.batch * 4 * sizeof(int32_t);
         e = smem > 48 << 10 ? cudaFuncSetAttribute(slots_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kWideRows * 4 * sizeof(int32_t)))
                             : cudaSuccess;
-        if (e == cudaSuccess) e = ps::launch_dependent(slots_wide_kernel, dim3(ctas), dim3(kWideThreads), smem, s, a, apart);
+        if (e == cudaSuccess) e = ps::launch_dependent(slots_wide_kernel, dim3(ctas), dim3(threads), smem, s, a, apart);
         if (e == cudaSuccess && !apart) e = ps::launch_dependent(slots_update_kernel, dim3(1), dim3(kMaxThreads), 0, s, a);
     }
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_build_slots", e);
