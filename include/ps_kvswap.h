@@ -446,7 +446,8 @@ typedef struct ps_rope_args {
  * two tokens of a call may have the same slot: which of them the pool then holds is not defined.  In training the gradient of
  * q and k is the same call on the outputs' gradients with PS_ROPE_INVERSE added.
  * head_dim up to 512, rot_dim even, up to 8 axes.  Rows on 16-byte boundaries with rot_dim a multiple of 16 (8 with
- * PS_ROPE_NEIGHBOURS) and head_dim of 8 are read 16 bytes at a time, everything else element by element.
+ * PS_ROPE_NEIGHBOURS) and head_dim of 8 are read 16 bytes at a time; 8 or 4 bytes where halves of these numbers fit,
+ * else element by element.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* err_buf, int32_t err_cap);
 

@@ -57,19 +57,26 @@ template <typename T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f(float x) { return __float2half_rn(x); }
 
-template <typename T>
-struct alignas(16) Vec8 {
-    T e[8];
+// W elements that are loaded and stored at once: 16, 8 or 4 bytes.
+template <typename T, int W>
+struct alignas(2 * W) Vec {
+    T e[W];
 };
-template <typename T>
-__device__ __forceinline__ Vec8<T> ld8(const T* p) {
-    Vec8<T> r;
-    *reinterpret_cast<uint4*>(&r) = *reinterpret_cast<const uint4*>(p);
+template <int W> struct Bits;
+template <> struct Bits<8> { using type = uint4; };
+template <> struct Bits<4> { using type = uint2; };
+template <> struct Bits<2> { using type = uint32_t; };
+template <int W, typename T>
+__device__ __forceinline__ Vec<T, W> ld(const T* p) {
+    using B = typename Bits<W>::type;
+    Vec<T, W> r;
+    *reinterpret_cast<B*>(&r) = *reinterpret_cast<const B*>(p);
     return r;
 }
-template <typename T>
-__device__ __forceinline__ void st8(T* p, const Vec8<T>& v) {
-    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&v);
+template <int W, typename T>
+__device__ __forceinline__ void st(T* p, const Vec<T, W>& v) {
+    using B = typename Bits<W>::type;
+    *reinterpret_cast<B*>(p) = *reinterpret_cast<const B*>(&v);
 }
 
 // Places and sines of the CTA's tokens.
@@ -138,18 +145,21 @@ __device__ __forceinline__ void head_target(const RopeParams& p, int64_t t, int 
     }
 }
 
-// 16 bytes per access: every address and row is 16-byte aligned, and a pair's partners lie in whole vectors.
+// W elements per access: every address and row is aligned to as many, and a pair's partners lie in whole vectors.  W is
+// 8 for most heads; a part of a head whose half is no multiple of 8 (24 of 96 dims, 40 of 80) has 4 or 2 (4096 tokens of
+// 48 heads, bf16: 40 of 80 dims 16.3 us, 24 of 96 20.8, 20 of 80 28.5; element by element 91, 104 and 98).
 //
-// A CTA's threads are dealt evenly to its tokens.  A head has `units`: vectors of pairs (two vectors each where the
-// partners lie half a rotation apart) and vectors that pass; a thread has one unit of every `slots`-th head of its
-// token, so its sines stay in registers.  kAtOnce heads are loaded at a time, and the first of them before the sines
-// are made, whose latency hides behind the loads'.
-template <typename T, bool kNeighbours>
+// A CTA's threads are dealt evenly to its tokens.  A head has `units`: vectors of neighbouring pairs and single ones
+// that pass, or two vectors each: those of partners half a rotation apart, and two of those that pass (32 of 128 dims,
+// 4096 tokens of 48 heads: 18.9 us, one that passes a unit 27.0).  A thread has one unit of every `slots`-th head of its
+// token, so its sines stay in registers.  kAtOnce heads are loaded at a time, and the first of them before the sines are
+// made, whose latency hides behind the loads'.
+template <typename T, bool kNeighbours, int W>
 __global__ void __launch_bounds__(kThreads, 4)
 rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads, int32_t units, int32_t slots) {
     extern __shared__ float2 cs[];
     __shared__ TokenPlace place[kTokensPerCta];
-    constexpr int kPairs = kNeighbours ? 4 : 8, kAtOnce = kNeighbours ? 3 : 2;
+    constexpr int kPairs = kNeighbours ? W / 2 : W, kAtOnce = (kNeighbours ? 3 : 2) * (W == 8 ? 1 : 2);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     const int n = min(p.tok_per_cta, p.tokens - t0);
@@ -157,13 +167,14 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
     const int k = threadIdx.x / threads, me = threadIdx.x - k * threads;
     const int slot = me / units, lane = me - slot * units;
     const int64_t t = t0 + k;
-    const int half = p.rot >> 1, turned = kNeighbours ? p.rot >> 3 : half >> 3;
+    const int half = p.rot >> 1, turned = kNeighbours ? p.rot / W : half / W;
     // this thread's vectors of a query or key head, and of a value head; -1: none
     const bool pairs = lane < turned;
-    const int first = pairs || kNeighbours ? 8 * lane : 8 * (turned + lane);      // what passes lies behind both halves
-    const int second = pairs && !kNeighbours ? half + 8 * lane : -1;
-    const int v_first = 8 * lane, v_second = units + lane < (p.dim >> 3) ? 8 * (units + lane) : -1;
-    Vec8<T> a[kAtOnce], b[kAtOnce];
+    const int passing = (p.dim - p.rot) / W, pass = lane - turned, pass_units = units - turned;
+    const int first = pairs || kNeighbours ? W * lane : p.rot + W * pass;
+    const int second = kNeighbours ? -1 : pairs ? half + W * lane : pass + pass_units < passing ? first + W * pass_units : -1;
+    const int v_first = W * lane, v_second = units + lane < p.dim / W ? W * (units + lane) : -1;
+    Vec<T, W> a[kAtOnce], b[kAtOnce];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     auto load = [&](int h0) {
 #pragma unroll
@@ -174,9 +185,9 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
             const T* src = h < p.hq ? (const T*)p.q + t * p.q_stride + (int64_t)h * p.dim
                            : !value ? (const T*)p.k + t * p.k_stride + (int64_t)(h - p.hq) * p.dim
                                     : (const T*)p.v + t * p.v_stride + (int64_t)(h - p.hq - p.hkv) * p.dim;
-            a[i] = ld8(src + (value ? v_first : first));
+            a[i] = ld<W>(src + (value ? v_first : first));
             const int s = value ? v_second : second;
-            if (s >= 0) b[i] = ld8(src + s);
+            if (s >= 0) b[i] = ld<W>(src + s);
         }
     };
     const bool busy = k < n && slot < slots;
@@ -199,8 +210,8 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
             if (pairs && !value)
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j) {
-                    T& e1 = kNeighbours ? a[i].e[(2 * j) & 7] : a[i].e[j];
-                    T& e2 = kNeighbours ? a[i].e[(2 * j + 1) & 7] : b[i].e[j];
+                    T& e1 = kNeighbours ? a[i].e[(2 * j) % W] : a[i].e[j];
+                    T& e2 = kNeighbours ? a[i].e[(2 * j + 1) % W] : b[i].e[j];
                     const float x1 = to_f(e1), x2 = to_f(e2);
                     e1 = from_f<T>(fmaf(x1, w[j].x, -x2 * w[j].y));
                     e2 = from_f<T>(fmaf(x2, w[j].x, x1 * w[j].y));
@@ -216,12 +227,12 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
                 dst = (T*)p.vpool + pl.v_off + (int64_t)(h - p.hq - p.hkv) * p.dim;
             }
             if (dst) {
-                st8(dst + f, a[i]);
-                if (s >= 0) st8(dst + s, b[i]);
+                st<W>(dst + f, a[i]);
+                if (s >= 0) st<W>(dst + s, b[i]);
             }
             if (dst2) {
-                st8(dst2 + f, a[i]);
-                if (s >= 0) st8(dst2 + s, b[i]);
+                st<W>(dst2 + f, a[i]);
+                if (s >= 0) st<W>(dst2 + s, b[i]);
             }
         }
         h0 += kAtOnce * slots;
@@ -229,7 +240,7 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
     }
 }
 
-// Element by element, for rows or pairs that are not on 16-byte boundaries.
+// Element by element, for rows that are not even on 4-byte boundaries and halves of an odd number of pairs.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads,
@@ -271,11 +282,12 @@ rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_c
     }
 }
 
-bool on16(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
+// Whether rows that begin there are aligned to w elements.
+bool aligned(const void* p, int64_t stride, int w) { return (reinterpret_cast<uintptr_t>(p) % (2 * w)) == 0 && stride % w == 0; }
 
-template <typename T>
-cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool neighbours, bool vec, cudaStream_t s) {
-    const int units = neighbours ? p.dim / 8 : p.rot / 16 + (p.dim - p.rot) / 8;
+template <typename T, bool kNeighbours, int W>
+cudaError_t launch_vectors(RopeParams p, const FreqAxes& axes, int32_t heads, cudaStream_t s) {
+    const int units = kNeighbours ? p.dim / W : p.rot / 2 / W + ((p.dim - p.rot) / W + 1) / 2;
     // Few tokens: one per CTA, so that they spread over the chip.  Many: a round of four CTAs per SM costs about 2 us
     // that its sines take, so as many as make a sine per thread and leave the chip filled, but not a little more than
     // a round, whose rest then runs alone (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.8 / 7.6 / 8.3 us, 2048
@@ -287,11 +299,22 @@ cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool 
         if (ctas >= kFilled && (ctas <= kRound || ctas > kRound * 3 / 2)) p.tok_per_cta = n;
     }
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
-    const size_t smem = (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2);
-    if (!vec) return ps::launch_dependent(rope_append_elements_kernel<T>, grid, dim3(kThreads), smem, s, p, axes, heads, neighbours);
-    const int slots = kThreads / p.tok_per_cta / units;
-    return neighbours ? ps::launch_dependent(rope_append_kernel<T, true>, grid, dim3(kThreads), smem, s, p, axes, heads, units, slots)
-                      : ps::launch_dependent(rope_append_kernel<T, false>, grid, dim3(kThreads), smem, s, p, axes, heads, units, slots);
+    return ps::launch_dependent(rope_append_kernel<T, kNeighbours, W>, grid, dim3(kThreads),
+                                (size_t)p.tok_per_cta * (p.rot / 2) * sizeof(float2), s, p, axes, heads, units,
+                                kThreads / p.tok_per_cta / units);
+}
+
+// width: elements per access, 1 = element by element.
+template <typename T>
+cudaError_t launch_rope(RopeParams p, const FreqAxes& axes, int32_t heads, bool neighbours, int width, cudaStream_t s) {
+    switch (width) {
+        case 8: return neighbours ? launch_vectors<T, true, 8>(p, axes, heads, s) : launch_vectors<T, false, 8>(p, axes, heads, s);
+        case 4: return neighbours ? launch_vectors<T, true, 4>(p, axes, heads, s) : launch_vectors<T, false, 4>(p, axes, heads, s);
+        case 2: return neighbours ? launch_vectors<T, true, 2>(p, axes, heads, s) : launch_vectors<T, false, 2>(p, axes, heads, s);
+    }
+    p.tok_per_cta = 1;
+    return ps::launch_dependent(rope_append_elements_kernel<T>, dim3((unsigned)p.tokens), dim3(kThreads), (size_t)(p.rot / 2) * sizeof(float2), s,
+                                p, axes, heads, neighbours);
 }
 
 }  // namespace
@@ -343,12 +366,18 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
     p.sign = a.flags & PS_ROPE_INVERSE ? -1.f : 1.f;
     const int32_t heads = p.hq + p.hkv + (append ? p.hkv : 0);
     const bool neighbours = a.flags & PS_ROPE_NEIGHBOURS;
-    bool vec = a.head_dim % 8 == 0 && a.rot_dim % (neighbours ? 8 : 16) == 0;
-    if (do_q) vec = vec && on16(a.q, a.q_stride) && on16(a.q_out, a.q_out_stride);
-    if (do_k) vec = vec && on16(a.k, a.k_stride) && on16(a.k_out, a.k_out ? a.k_out_stride : 0);
-    if (append) vec = vec && on16(a.v, a.v_stride) && on16(a.kpool, a.k_block_stride) && on16(a.vpool, a.v_block_stride);
-    cudaError_t e = a.dtype == PS_DTYPE_BF16 ? launch_rope<__nv_bfloat16>(p, axes, heads, neighbours, vec, (cudaStream_t)stream)
-                                             : launch_rope<__half>(p, axes, heads, neighbours, vec, (cudaStream_t)stream);
+    // the widest access that rows, heads and the parts of a head allow
+    int width = 8;
+    auto fits = [&](int w) {
+        bool ok = a.head_dim % w == 0 && a.rot_dim % (neighbours ? w : 2 * w) == 0;
+        if (do_q) ok = ok && aligned(a.q, a.q_stride, w) && aligned(a.q_out, a.q_out_stride, w);
+        if (do_k) ok = ok && aligned(a.k, a.k_stride, w) && aligned(a.k_out, a.k_out ? a.k_out_stride : 0, w);
+        if (append) ok = ok && aligned(a.v, a.v_stride, w) && aligned(a.kpool, a.k_block_stride, w) && aligned(a.vpool, a.v_block_stride, w);
+        return ok;
+    };
+    while (width > 1 && !fits(width)) width /= 2;
+    cudaError_t e = a.dtype == PS_DTYPE_BF16 ? launch_rope<__nv_bfloat16>(p, axes, heads, neighbours, width, (cudaStream_t)stream)
+                                             : launch_rope<__half>(p, axes, heads, neighbours, width, (cudaStream_t)stream);
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_rope_append", e);
     return PS_OK;
 }

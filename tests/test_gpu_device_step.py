@@ -227,6 +227,43 @@ def test_rope_and_append(dtype, T, hq, hkv, D, rot, axes, neighbours, S):
             assert torch.equal(now.view(-1, hkv, D)[rest], was.view(-1, hkv, D)[rest])
 
 
+@pytest.mark.parametrize("D,rot,neighbours", [
+    (512, 4, True), (512, 2, True), (512, 4, False), (512, 504, False), (510, 510, True), (80, 40, False), (80, 20, False), (96, 24, False),
+    (64, 64, True), (64, 64, False), (12, 12, True), (20, 8, False), (34, 18, False), (7, 4, True)])
+@pytest.mark.parametrize("T", [6, 2600])
+def test_rope_rows_of_every_alignment(T, D, rot, neighbours):
+    """How wide the accesses are follows from addresses, strides and sizes; what comes out does not."""
+    hq, hkv, S = 3, 2, 4
+    nb = T // S + 3
+    q, k, v = rope_inputs(T, hq, hkv, D, torch.bfloat16, D + T, fused=False)
+    pos = torch.arange(T, device="cuda", dtype=torch.int32) * 7
+    inv = torch.rand(rot // 2, device="cuda")
+    axis = [0] * (rot // 2)
+    slots = torch.randperm(nb * S, device="cuda")[:T]
+    (wq, tq), (wk, tk) = rope_want(q, pos[None], inv, axis, neighbours, False), rope_want(k, pos[None], inv, axis, neighbours, False)
+    n = hq + 2 * hkv
+    first = None
+    for shift, gap in ((0, 0), (1, 0), (2, 0), (4, 8), (0, 1), (0, 2), (8, 4)):
+        x = torch.full((T * (n * D + gap) + shift,), 5.0, device="cuda", dtype=torch.bfloat16)
+        rows = x[shift:].view(T, n * D + gap)
+        parts = [rows[:, a * D: b * D].view(T, b - a, D) for a, b in ((0, hq), (hq, hq + hkv), (hq + hkv, n))]
+        for dst, src in zip(parts, (q, k, v)):
+            dst.copy_(src)
+        kp, vp = (torch.zeros(nb * S * hkv * D + shift, device="cuda", dtype=torch.bfloat16)[shift:].view(nb, S, hkv, D) for _ in range(2))
+        rc, text = B.ps_rope_append(parts[0], parts[1], parts[0], None, pos, inv, v=parts[2], kpool=kp, vpool=vp, slots=slots,
+                                    neighbours=neighbours)
+        assert rc == B.PS_OK, text
+        got = parts[0].clone(), kp.clone(), vp.clone()
+        assert torch.equal(parts[1], k) and torch.equal(parts[2], v)
+        assert (rows[:, n * D:] == 5.0).all() and (x[:shift] == 5.0).all()
+        if first is None:
+            first = got
+            check_within(got[0], wq, tq)
+            check_within(kp.view(-1, hkv, D)[slots], wk, tk)
+            assert torch.equal(vp.view(-1, hkv, D)[slots], v)
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
 def test_rope_in_place_alone_and_of_keys_alone():
     T, hq, hkv, D = 19, 6, 2, 128
     q, k, _ = rope_inputs(T, hq, hkv, D, torch.bfloat16, 1)
