@@ -149,17 +149,18 @@ __device__ __forceinline__ void head_target(const RopeParams& p, int64_t t, int 
 // 8 for most heads; a part of a head whose half is no multiple of 8 (24 of 96 dims, 40 of 80) has 4 or 2 (4096 tokens of
 // 48 heads, bf16: 40 of 80 dims 16.3 us, 24 of 96 20.8, 20 of 80 28.5; element by element 91, 104 and 98).
 //
-// A CTA's threads are dealt evenly to its tokens.  A head has `units`: vectors of neighbouring pairs and single ones
-// that pass, or two vectors each: those of partners half a rotation apart, and two of those that pass (32 of 128 dims,
-// 4096 tokens of 48 heads: 18.9 us, one that passes a unit 27.0).  A thread has one unit of every `slots`-th head of its
-// token, so its sines stay in registers.  kAtOnce heads are loaded at a time, and the first of them before the sines are
-// made, whose latency hides behind the loads'.
+// A CTA's threads are dealt evenly to its tokens.  A head has `units` of two vectors: of partners half a rotation apart
+// and of what passes, or, with neighbouring pairs, of dims half a head apart (one vector a unit: 4096 tokens of 48 heads
+// of 128, 32 dims rotated, 27.0 instead of 18.9 us, 128 as neighbours 22.7 instead of 19.7).  A thread has one unit of
+// every `slots`-th head of its token, so its sines stay in registers.  kAtOnce heads are loaded at a time, and the first
+// of them before the sines are made, whose latency hides behind the loads' (three at a time spill: 21.6 instead of
+// 20.2 us for 48 heads of 128).
 template <typename T, bool kNeighbours, int W>
 __global__ void __launch_bounds__(kThreads, 4)
 rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ FreqAxes axes, int32_t heads, int32_t units, int32_t slots) {
     extern __shared__ float2 cs[];
     __shared__ TokenPlace place[kTokensPerCta];
-    constexpr int kPairs = kNeighbours ? W / 2 : W, kAtOnce = (kNeighbours ? 3 : 2) * (W == 8 ? 1 : 2);
+    constexpr int kAtOnce = W == 8 ? 2 : 4;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     const int n = min(p.tok_per_cta, p.tokens - t0);
@@ -169,11 +170,11 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
     const int64_t t = t0 + k;
     const int half = p.rot >> 1, turned = kNeighbours ? p.rot / W : half / W;
     // this thread's vectors of a query or key head, and of a value head; -1: none
-    const bool pairs = lane < turned;
+    const bool pairs = lane < turned, pairs2 = kNeighbours && units + lane < turned;
     const int passing = (p.dim - p.rot) / W, pass = lane - turned, pass_units = units - turned;
-    const int first = pairs || kNeighbours ? W * lane : p.rot + W * pass;
-    const int second = kNeighbours ? -1 : pairs ? half + W * lane : pass + pass_units < passing ? first + W * pass_units : -1;
     const int v_first = W * lane, v_second = units + lane < p.dim / W ? W * (units + lane) : -1;
+    const int first = pairs || kNeighbours ? v_first : p.rot + W * pass;
+    const int second = kNeighbours ? v_second : pairs ? half + W * lane : pass + pass_units < passing ? first + W * pass_units : -1;
     Vec<T, W> a[kAtOnce], b[kAtOnce];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     auto load = [&](int h0) {
@@ -197,10 +198,12 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
     if (!busy) return;
     const TokenPlace pl = place[k];
     if (!pl.live) return;
-    float2 w[kPairs];
-    if (pairs)
+    float2 w[W];
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) w[j] = cs[k * half + kPairs * lane + j];
+    for (int j = 0; j < W; ++j) {
+        if (!kNeighbours && pairs) w[j] = cs[k * half + W * lane + j];
+        if (kNeighbours && (j < W / 2 ? pairs : pairs2)) w[j] = cs[k * half + W / 2 * (j < W / 2 ? lane : units + lane - 1) + j];
+    }
     for (int h0 = slot; h0 < heads;) {
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
@@ -209,9 +212,11 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
             const bool value = h >= p.hq + p.hkv;
             if (pairs && !value)
 #pragma unroll
-                for (int j = 0; j < kPairs; ++j) {
-                    T& e1 = kNeighbours ? a[i].e[(2 * j) % W] : a[i].e[j];
-                    T& e2 = kNeighbours ? a[i].e[(2 * j + 1) % W] : b[i].e[j];
+                for (int j = 0; j < W; ++j) {
+                    if (kNeighbours && j == W / 2 && !pairs2) break;
+                    Vec<T, W>& at = kNeighbours && j >= W / 2 ? b[i] : a[i];
+                    T& e1 = kNeighbours ? at.e[(2 * j) % W] : a[i].e[j];
+                    T& e2 = kNeighbours ? at.e[(2 * j + 1) % W] : b[i].e[j];
                     const float x1 = to_f(e1), x2 = to_f(e2);
                     e1 = from_f<T>(fmaf(x1, w[j].x, -x2 * w[j].y));
                     e2 = from_f<T>(fmaf(x2, w[j].x, x1 * w[j].y));
@@ -287,11 +292,12 @@ bool aligned(const void* p, int64_t stride, int w) { return (reinterpret_cast<ui
 
 template <typename T, bool kNeighbours, int W>
 cudaError_t launch_vectors(RopeParams p, const FreqAxes& axes, int32_t heads, cudaStream_t s) {
-    const int units = kNeighbours ? p.dim / W : p.rot / 2 / W + ((p.dim - p.rot) / W + 1) / 2;
+    const int units = kNeighbours ? (p.dim / W + 1) / 2 : p.rot / 2 / W + ((p.dim - p.rot) / W + 1) / 2;
     // Few tokens: one per CTA, so that they spread over the chip.  Many: a round of four CTAs per SM costs about 2 us
     // that its sines take, so as many as make a sine per thread and leave the chip filled, but not a little more than
-    // a round, whose rest then runs alone (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.8 / 7.6 / 8.3 us, 2048
-    // 22.7 / 18.5 / 16.9, 8192 75.9 / 61.0 / 57.9; 32 heads of 80, 1 / 2 / 4 / 8: 5003 tokens 25.2 / 18.2 / 15.8 / 17.3).
+    // a round, whose rest then runs alone (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.6 / 7.0 / 7.8 us, 2048
+    // 22.4 / 18.2 / 16.7, 8192 74.7 / 60.1 / 57.6; 32 heads of 80, 1 / 2 / 4 / 8: 2500 tokens 11.3 / 8.5 / 8.0 / 9.0, 5003
+    // 22.8 / 16.5 / 14.7 / 14.8, 9000 39.2 / 26.9 / 22.6 / 19.6).
     constexpr int kRound = 4 * 148, kFilled = 350;
     p.tok_per_cta = 1;
     for (int n = 2; n <= kTokensPerCta && n * p.rot <= 2 * kThreads && n * units <= kThreads; n *= 2) {
