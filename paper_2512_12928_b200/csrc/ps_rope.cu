@@ -171,10 +171,13 @@ rope_append_kernel(const __grid_constant__ RopeParams p, const __grid_constant__
     const int half = p.rot >> 1, turned = kNeighbours ? p.rot / W : half / W;
     // this thread's vectors of a query or key head, and of a value head; -1: none
     const bool pairs = lane < turned, pairs2 = kNeighbours && units + lane < turned;
+    // (spelled out twice: shared between the two, they cost small calls 0.2 us)
     const int passing = (p.dim - p.rot) / W, pass = lane - turned, pass_units = units - turned;
+    const int first = pairs || kNeighbours ? W * lane : p.rot + W * pass;
+    const int second = kNeighbours ? (units + lane < p.dim / W ? W * (units + lane) : -1)
+                       : pairs     ? half + W * lane
+                                   : pass + pass_units < passing ? first + W * pass_units : -1;
     const int v_first = W * lane, v_second = units + lane < p.dim / W ? W * (units + lane) : -1;
-    const int first = pairs || kNeighbours ? v_first : p.rot + W * pass;
-    const int second = kNeighbours ? v_second : pairs ? half + W * lane : pass + pass_units < passing ? first + W * pass_units : -1;
     Vec<T, W> a[kAtOnce], b[kAtOnce];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     auto load = [&](int h0) {
