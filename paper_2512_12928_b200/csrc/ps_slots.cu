@@ -20,6 +20,7 @@
 // Work on blocks and tokens is dealt to threads by the scanned counts (binary search in shared memory), so one long
 // prompt costs the same as many short ones.
 #include <algorithm>
+#include <atomic>
 #include <cstdio>
 
 #include "ps_internal.h"
@@ -340,6 +341,21 @@ slots_update_kernel(const ps_slots_args a) {
     if (tid == 0) update_count(a, code, count, all);
 }
 
+// Lets slots_wide_kernel have the shared memory of kWideRows rows on the current device: asked for once per device, and
+// not by the size of a call, whose limit would then depend on the calls before it.
+constexpr int kMaxDevices = 64;
+cudaError_t allow_wide_rows() {
+    static std::atomic<bool> allowed[kMaxDevices];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (allowed[dev].load(std::memory_order_acquire)) return cudaSuccess;
+    e = cudaFuncSetAttribute(slots_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kWideRows * 4 * sizeof(int32_t)));
+    if (e == cudaSuccess) allowed[dev].store(true, std::memory_order_release);
+    return e;
+}
+
 }  // namespace
 
 extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char* err_buf, int32_t err_cap) {
@@ -367,8 +383,7 @@ extern "C" int32_t ps_build_slots(const ps_slots_args* args, void* stream, char*
         const int threads = a.batch <= 256 ? 256 : a.batch <= 512 ? 512 : kMaxThreads;
         const int ctas = (int)std::min<int64_t>(((int64_t)a.max_tokens + threads - 1) / threads, kWideAtOnce / threads);
         const size_t smem = (size_t)a.batch * 4 * sizeof(int32_t);
-        e = smem > 48 << 10 ? cudaFuncSetAttribute(slots_wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kWideRows * 4 * sizeof(int32_t)))
-                            : cudaSuccess;
+        e = allow_wide_rows();
         if (e == cudaSuccess) e = ps::launch_dependent(slots_wide_kernel, dim3(ctas), dim3(threads), smem, s, a, apart);
         if (e == cudaSuccess && !apart) e = ps::launch_dependent(slots_update_kernel, dim3(1), dim3(kMaxThreads), 0, s, a);
     }
