@@ -1,14 +1,18 @@
-"""Calls of the device-side step that its other tests do not make: row counts around the kernels' limits."""
+"""Calls of the device-side step that its other tests do not make: row counts around the kernels' limits, README's loop."""
 import os
+import re
 import subprocess
 import sys
 
 import numpy as np
 import pytest
+import torch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 sys.path.insert(0, ROOT)                                            # as a script too
-from test_gpu_device_step import slot_case
+from device_step_util import attn_want, check_within, rope_want
+from paper_2512_12928_b200 import binding as B
+from test_gpu_device_step import Engine, dev, slot_case
 
 pytestmark = pytest.mark.gpu
 
@@ -29,6 +33,37 @@ def test_slots_as_a_process_first_call(rows, in_place):
     call may not depend on what an earlier call of the process has asked for."""
     p = subprocess.run([sys.executable, os.path.abspath(__file__), str(rows), str(int(in_place))], capture_output=True, text=True, timeout=300)
     assert p.returncode == 0, p.stdout[-2000:] + p.stderr[-2000:]
+
+
+def test_readmes_loop_with_requests_that_end_and_pause():
+    """README's step as it stands there, in a batch where tokens and rows are not numbered alike: a row that ended and one
+    without a new token have no query among the tokens."""
+    text = open(os.path.join(ROOT, "README.md")).read()
+    code, = [c for c in re.findall(r"```python\n(.*?)```", text, re.S) if "ps_build_slots" in c]
+    rng = np.random.default_rng(30)
+    rows, L, hq, hkv, D, S, M = 6, 2, 8, 2, 64, 16, 60
+    e = Engine(rng, rows, hq, hkv, D, S, M, 12, rows, torch.bfloat16)       # the room of a captured decode step
+    K, V = (torch.zeros((L, M, S, hkv, D), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    q, k, v = e.parts()
+    ns = dict(torch=torch, B=B, L=L, M=M, K=K, V=V, q=q, k=k, v=v, q_rot=e.q_rot, out=e.out, inv_freq=e.inv, ctx_lens=e.ctx, new_lens=e.new,
+              tables=e.tables, slots=e.slots, positions=e.pos, token_start=e.start, stack=e.ids, top=e.count)
+    for new in ([1] * 6, [1, 1, 0, 1, 1, 1], [1, -1, 1, 0, 1, 1], [1, 1, -1, -1, 0, 1], [0, 1, 1, 0, -1, 1]):
+        e.new.copy_(dev(new))
+        e.qkv.copy_(torch.randn(tuple(e.qkv.shape), device="cuda"))
+        e.q_rot.fill_(7.0)
+        exec(code, ns)
+        assert ns["rc"] == B.PS_OK, ns["err"]
+        torch.cuda.synchronize()
+        st, e.m_tables, slots, pos, start, e.m_ctx = e.model.step(e.m_ctx, new, e.m_tables, 12, rows)
+        assert st == 0 and e.slots.tolist() == slots and e.start.tolist() == start and e.ctx.tolist() == e.m_ctx
+        wq, tq = rope_want(q, e.pos, e.inv, [0] * (D // 2), False, False)
+        check_within(e.q_rot[: start[-1]], wq[: start[-1]], tq[: start[-1]])
+        live = [b for b in range(rows) if new[b] > 0]
+        own = e.q_rot[dev([start[b] for b in live], torch.int64)]           # a row's token is its query
+        tables = [e.m_tables[b][: -(-e.m_ctx[b] // S)] for b in live]
+        o, _, tol, _ = attn_want(K[L - 1], V[L - 1], own, tables, [e.m_ctx[b] for b in live])
+        check_within(e.out[dev(live, torch.int64)], o, tol)
+        assert not e.out[dev([b for b in range(rows) if new[b] < 0], torch.int64)].any()
 
 
 if __name__ == "__main__":
