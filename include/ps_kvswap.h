@@ -421,8 +421,8 @@ typedef struct ps_rope_args {
     const void* q;            /* device [tokens][num_q_heads][head_dim], rows q_stride apart, or NULL */
     const void* k;            /* device [tokens][num_kv_heads][head_dim], or NULL */
     const void* v;            /* device, as k; needed with pools */
-    void* q_out;              /* as q; may be q itself (same stride) */
-    void* k_out;              /* as k, or NULL; may be k itself */
+    void* q_out;              /* as q; may be q itself (same stride); otherwise no element may be one of q, k, v or k_out */
+    void* k_out;              /* as k, or NULL; may be k itself; otherwise as q_out */
     void* kpool;              /* pools the keys and values are appended to, or both NULL */
     void* vpool;
     const int64_t* slots;     /* device [tokens]: row of the pools, block * block_size + place; negative = padding */

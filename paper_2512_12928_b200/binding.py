@@ -297,7 +297,7 @@ def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=Non
     """Rotary positions on q and k and the append of k and v to the paged pools: (status, error text).
 
     q, q_out [tokens][q heads][dim], k, v, k_out [tokens][kv heads][dim] (any of q, k, k_out may be None; q_out may be
-    q, k_out may be k; rows may be strided); positions int32 [tokens] or [axes][tokens] (an axis stride of 0 is fine);
+    q, k_out may be k, and share no element with another of them otherwise; rows may be strided); positions int32 [tokens] or [axes][tokens] (an axis stride of 0 is fine);
     inv_freq float32 [rot_dim / 2], or None for no rotation; freq_axis: a list with the axis of every frequency, or None
     for axis 0; kpool, vpool [blocks][block_size][kv heads][dim] with slots int64 [tokens].  See ps_rope_append in the header."""
     return (_tensor_args or _load_tensor_args()).rope_append(

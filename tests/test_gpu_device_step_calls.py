@@ -66,5 +66,28 @@ def test_readmes_loop_with_requests_that_end_and_pause():
         assert not e.out[dev([b for b in range(rows) if new[b] < 0], torch.int64)].any()
 
 
+def test_rope_outputs_between_the_inputs_rows():
+    """Outputs in the gaps of the inputs' buffer: one stride for all, and keys whose rows lie twice as far apart."""
+    T, hq, hkv, D = 9, 3, 2, 64
+    buf = torch.randn((2 * T, 12 * D), device="cuda").bfloat16()
+    part = lambda rows, at, heads: rows[:, at * D: (at + heads) * D].view(T, heads, D)
+    q, q_out, k = part(buf[:T], 0, hq), part(buf[:T], 3, hq), part(buf[:T], 6, hkv)
+    far = part(buf[::2], 8, hkv)
+    pos, inv = dev(list(range(T))), torch.rand(D // 2, device="cuda")
+    (wq, tq), (wk, tk) = rope_want(q, pos, inv, [0] * 32, False, False), rope_want(k, pos, inv, [0] * 32, False, False)
+    was = buf.clone()
+    assert B.ps_rope_append(q, k, q_out, far, pos, inv) == (B.PS_OK, "")
+    check_within(q_out, wq, tq)
+    check_within(far, wk, tk)
+    q_out.copy_(part(was[:T], 3, hq))
+    far.copy_(part(was[::2], 8, hkv))
+    assert torch.equal(buf, was)
+    rc, text = B.ps_rope_append(q, k, part(buf[:T], 1, hq), None, pos, inv, v=k, kpool=buf[:4].view(-1)[: 4 * hkv * D].view(1, 4, hkv, D),
+                                vpool=buf[4:8].view(-1)[: 4 * hkv * D].view(1, 4, hkv, D), slots=dev([-1] * T, torch.int64))
+    assert rc == B.PS_ERR_INVALID and "overlap" in text
+    torch.cuda.synchronize()
+    assert torch.equal(buf, was)
+
+
 if __name__ == "__main__":
     slots_steps(int(sys.argv[1]), bool(int(sys.argv[2])))
