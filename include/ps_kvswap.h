@@ -476,8 +476,9 @@ typedef struct ps_paged_attn_args {
  * no score above -inf, gives zeros (lse = -inf).  A length that is
  * negative counts as 0, one beyond table_stride * block_size as that many (status 5).  Blocks may be shared by rows,
  * and nothing outside the attended tokens is read into a result, whatever the pools hold there.
- * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, any batch whose tables have room for
- * fewer than about 2^37 tokens times KV heads.  out must not overlap the inputs.  The same inputs give the same bits.
+ * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, and any batch whose tables,
+ * counting 1024 tokens more for every row, have room for up to 2^34 tokens times KV heads (of most heads 2^35 to 2^38; the
+ * call is refused where they do not fit).  out must not overlap the inputs.  The same inputs give the same bits.
  * One workspace serves calls in order; calls that may overlap on the device need one each.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_buf, int32_t err_cap);

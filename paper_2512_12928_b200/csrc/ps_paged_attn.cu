@@ -841,7 +841,7 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 
 // How the heads are dealt to warps.
 struct Layout {
-    int32_t splits, rows, units, chunks, subs, ctas;
+    int32_t splits, rows, units, chunks, subs, ctas, step_log2;
     int nt;                                // column tiles of 8 heads of a unit
     size_t part_o, part_ml, cuts, bytes;   // offsets and size of the workspace
 };
@@ -861,6 +861,7 @@ Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, int sms) {
     y.chunks = (all + most - 1) / most;
     y.units = (all + y.chunks - 1) / y.chunks;
     for (y.subs = 1; 2 * y.subs * y.units <= kMaxWarps; y.subs *= 2) {}
+    for (y.step_log2 = dim == 128 ? 4 : 5; (1 << y.step_log2) < 2048 / dim * y.subs; ++y.step_log2) {}   // Ring::kTokens
     y.ctas = sms;                          // the rings take an SM's shared memory
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
@@ -967,6 +968,13 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     if (!on(a.kpool, a.k_block_stride, 16) || !on(a.vpool, a.v_block_stride, 16) || !on(a.q, a.q_stride, 16) || !on(a.out, a.out_stride, 16))
         return bad("ps_paged_attn: pools, q, out and their strides must be multiples of 16 bytes");
     if (a.batch > 1 && a.out_stride < (int64_t)a.num_q_heads * a.head_dim) return bad("ps_paged_attn: rows of out overlap");
+    // The places of all segments are counted in 32 bits.  A segment has a place for every tile that its table row has room
+    // for and at most 4 more, and a tile's tokens times the KV heads are 24 (3 KV heads of 33 query heads each) times a
+    // row's segments or more: with 1024 more tokens a row, 2^34 tokens times KV heads always fit.
+    const int64_t room = std::min<int64_t>((int64_t)a.table_stride * a.block_size, kMaxTokens);
+    const Layout places = layout_of(a.batch, a.num_kv_heads, a.num_q_heads, a.head_dim, 1);
+    if ((room >> places.step_log2) + 4 > (1 << 30) / ((int64_t)a.batch * places.chunks))
+        return bad("ps_paged_attn: the tables of the batch have room for more than 2^30 tiles of tokens");
     int sms = 0;
     cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_paged_attn: device", e);
@@ -981,20 +989,17 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
     p.part_ml = (float2*)(ws + y.part_ml);
     p.cuts = (int4*)(ws + y.cuts);
     p.k_block_stride = a.k_block_stride, p.v_block_stride = a.v_block_stride, p.q_stride = a.q_stride, p.out_stride = a.out_stride;
-    p.room = (int64_t)a.table_stride * a.block_size;
-    if (p.room > kMaxTokens) p.room = kMaxTokens;
+    p.room = room;
     p.block_magic = a.block_size > 1 ? ~0ull / (uint64_t)a.block_size + 1 : 0;
     p.batch = a.batch, p.table_stride = a.table_stride, p.num_blocks = a.num_gpu_blocks, p.block_size = a.block_size, p.window = a.window;
     p.hkv = a.num_kv_heads, p.hq = a.num_q_heads, p.group = a.num_q_heads / a.num_kv_heads;
     p.splits = y.splits, p.rows = y.rows, p.units = y.units, p.chunks = y.chunks, p.subs = y.subs, p.ctas = y.ctas;
-    for (p.step_log2 = a.head_dim == 128 ? 4 : 5; (1 << p.step_log2) < 2048 / a.head_dim * y.subs; ++p.step_log2) {}   // Ring::kTokens
+    p.step_log2 = y.step_log2;
     p.scale_log2e = (a.scale != 0.f ? a.scale : 1.f / sqrtf((float)a.head_dim)) * kLog2e;
     // A segment's start and end take about the time of two tiles.  Not counted (1 in brackets), 200 rows of 10 to 100 tokens
     // take 20.2 instead of 17.2 us (17.9), 33 ragged rows with a window 19.6 instead of 18.1 (18.8), 64 rows of 1024 to
     // 4096 102.4 either way.  With few segments a CTA has one whatever it costs.
     p.segment = (int64_t)a.batch * y.chunks >= y.ctas / 8 ? 2 : 0;
-    if ((p.room >> p.step_log2) + 4 > (1 << 30) / ((int64_t)a.batch * y.chunks))
-        return bad("ps_paged_attn: the tables of the batch have room for more than 2^30 tiles of tokens");
     // rows that cannot be longer than one tile are never cut
     const int64_t longest = a.window > 0 && a.window < p.room ? a.window : p.room;
     const bool may_cut = longest > (int64_t)1 << p.step_log2;
