@@ -10,9 +10,9 @@ import torch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 sys.path.insert(0, ROOT)                                            # as a script too
-from device_step_util import attn_want, check_within, rope_want
+from device_step_util import attn_want, check_attn, check_within, rope_want
 from paper_2512_12928_b200 import binding as B
-from test_gpu_device_step import Engine, dev, slot_case
+from test_gpu_device_step import Engine, attn_case, dev, run_attn, slot_case
 
 pytestmark = pytest.mark.gpu
 
@@ -87,6 +87,16 @@ def test_rope_outputs_between_the_inputs_rows():
     assert rc == B.PS_ERR_INVALID and "overlap" in text
     torch.cuda.synchronize()
     assert torch.equal(buf, was)
+
+
+@pytest.mark.parametrize("hq,hkv,D,ctx", [
+    (1024, 1024, 64, [0, 1, 40, 200]), (1040, 130, 128, [700, 3]), (65 * 33, 65, 64, [5, 300, 0]), (576, 9, 128, [33] * 40 + [900])])
+def test_attn_many_heads(hq, hkv, D, ctx):
+    """Rows whose heads are many CTAs' work, up to the 1024 KV heads that are accepted."""
+    rng = np.random.default_rng(hq)
+    kp, vp, q, tables = attn_case(rng, ctx, hq, hkv, D, 16, torch.bfloat16)
+    out, lse = run_attn(kp, vp, q, tables, ctx)
+    check_attn(out, lse, attn_want(kp, vp, q, tables, ctx))
 
 
 if __name__ == "__main__":
