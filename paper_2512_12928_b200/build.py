@@ -3,7 +3,7 @@
     python -m paper_2512_12928_b200.build [--force] [--verbose]
 
 Output: paper_2512_12928_b200/lib/libps_kvswap.so (C ABI declared in include/ps_kvswap.h) and
-paper_2512_12928_b200/lib/_ps_tensor_args.so (where torch is installed; the library does not need it).
+paper_2512_12928_b200/lib/_ps_tensor_args.so (where torch with CUDA is installed; the library does not need it).
 """
 from __future__ import annotations
 
@@ -34,9 +34,12 @@ TENSOR_ARGS_SOURCE = os.path.join(CSRC, "ps_tensor_args.cpp")
 
 
 def build_tensor_args(force: bool = False) -> str:
-    """The module that takes torch tensors apart; nothing to do where torch is not installed."""
+    """The module that takes torch tensors apart; nothing to do where torch is not installed or knows no CUDA."""
     import importlib.util
     if importlib.util.find_spec("torch") is None:
+        return ""
+    import torch
+    if torch.version.cuda is None:
         return ""
     deps = [TENSOR_ARGS_SOURCE, os.path.join(ROOT, "include", "ps_kvswap.h")]
     if not force and os.path.exists(TENSOR_ARGS_PATH) and all(
@@ -44,7 +47,6 @@ def build_tensor_args(force: bool = False) -> str:
         return TENSOR_ARGS_PATH
     import sysconfig
 
-    import torch
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
     os.makedirs(LIB_DIR, exist_ok=True)
@@ -67,8 +69,7 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    build_tensor_args(force)
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)
@@ -87,6 +88,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         sys.stderr.write(proc.stdout)
     if proc.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + proc.stdout[-4000:])
+    return LIB_PATH
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """The library first: it does not need the module."""
+    build_library(force, verbose)
+    build_tensor_args(force)
     return LIB_PATH
 
 
