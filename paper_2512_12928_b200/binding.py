@@ -255,7 +255,6 @@ def ps_decode_attn_static(kpool, vpool, q, out, block_tables, ctx_lens: Sequence
 # since the library sees addresses only; what does not fit comes back as (PS_ERR_INVALID, text), as from the library.
 # Work is enqueued on torch's current stream of the tensors' device.
 
-TENSOR_ARGS_PATH = os.path.join(_PKG, "lib", "_ps_tensor_args.so")
 _tensor_args = None
 
 
@@ -267,9 +266,11 @@ def _load_tensor_args():
         import importlib.util
 
         import torch  # noqa: F401  (its libraries are the module's)
-        if not os.path.exists(TENSOR_ARGS_PATH):
-            raise ImportError(f"{TENSOR_ARGS_PATH} is missing: build it with `python -m paper_2512_12928_b200.build`")
-        loader = importlib.machinery.ExtensionFileLoader("_ps_tensor_args", TENSOR_ARGS_PATH)
+        from .build import tensor_args_path
+        path = tensor_args_path()
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is missing: build it with `python -m paper_2512_12928_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_ps_tensor_args", path)
         m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_ps_tensor_args", loader))
         loader.exec_module(m)
         lib = load()

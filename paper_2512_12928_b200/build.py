@@ -2,8 +2,8 @@
 
     python -m paper_2512_12928_b200.build [--force] [--verbose]
 
-Output: paper_2512_12928_b200/lib/libps_kvswap.so (C ABI declared in include/ps_kvswap.h) and
-paper_2512_12928_b200/lib/_ps_tensor_args.so (where torch with CUDA is installed; the library does not need it).
+Output: paper_2512_12928_b200/lib/libps_kvswap.so (C ABI declared in include/ps_kvswap.h) and beside it
+_ps_tensor_args.<torch and Python>.so (where torch with CUDA is installed; the library does not need it).
 """
 from __future__ import annotations
 
@@ -29,8 +29,17 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found; set NVCC or put CUDA's bin directory on PATH")
 
 
-TENSOR_ARGS_PATH = os.path.join(LIB_DIR, "_ps_tensor_args.so")
 TENSOR_ARGS_SOURCE = os.path.join(CSRC, "ps_tensor_args.cpp")
+
+
+def tensor_args_path() -> str:
+    """Where the module for torch tensors lies.  It is compiled against the insides of one torch and one Python, so its name
+    has both: another torch finds no module rather than one that misreads its tensors."""
+    import sysconfig
+
+    import torch
+    return os.path.join(LIB_DIR, f"_ps_tensor_args.torch-{torch.__version__}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+                                 f"{sysconfig.get_config_var('EXT_SUFFIX')}")
 
 
 def build_tensor_args(force: bool = False) -> str:
@@ -38,27 +47,31 @@ def build_tensor_args(force: bool = False) -> str:
     import importlib.util
     if importlib.util.find_spec("torch") is None:
         return ""
+    import sysconfig
+
     import torch
     if torch.version.cuda is None:
         return ""
+    path = tensor_args_path()
     deps = [TENSOR_ARGS_SOURCE, os.path.join(ROOT, "include", "ps_kvswap.h")]
-    if not force and os.path.exists(TENSOR_ARGS_PATH) and all(
-            os.path.getmtime(d) <= os.path.getmtime(TENSOR_ARGS_PATH) for d in deps):
-        return TENSOR_ARGS_PATH
-    import sysconfig
-
+    if not force and os.path.exists(path) and all(os.path.getmtime(d) <= os.path.getmtime(path) for d in deps):
+        return path
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
     os.makedirs(LIB_DIR, exist_ok=True)
+    partial = f"{path}.{os.getpid()}.tmp"     # another process may be loading the module meanwhile
     cmd = [shutil.which("g++") or "g++", "-shared", "-std=c++17", "-O2", "-fPIC", "-fvisibility=hidden",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
            "-I", os.path.join(base, "include"), "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-o", TENSOR_ARGS_PATH,
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-o", partial,
            TENSOR_ARGS_SOURCE, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if proc.returncode != 0:
+        if os.path.exists(partial):
+            os.remove(partial)
         raise RuntimeError("g++ failed:\n" + proc.stdout[-4000:])
-    return TENSOR_ARGS_PATH
+    os.replace(partial, path)
+    return path
 
 
 def needs_build() -> bool:
