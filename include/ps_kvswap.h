@@ -455,7 +455,7 @@ typedef struct ps_paged_attn_args {
     const void* kpool;           /* device pools of one layer; like q and out on 16-byte boundaries */
     const void* vpool;
     const void* q;               /* device [batch][num_q_heads][head_dim], rows q_stride apart */
-    void* out;                   /* as q, rows out_stride apart */
+    void* out;                   /* as q, rows out_stride apart; may be q itself (same stride) */
     float* lse;                  /* device [batch][num_q_heads], natural log, or NULL */
     const int32_t* block_tables; /* device [batch][table_stride] */
     const int32_t* ctx_lens;     /* device [batch]: tokens of every row, the new one included */
@@ -478,7 +478,7 @@ typedef struct ps_paged_attn_args {
  * and nothing outside the attended tokens is read into a result, whatever the pools hold there.
  * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, and any batch whose tables,
  * counting 1024 tokens more for every row, have room for up to 2^34 tokens times KV heads (of most heads 2^35 to 2^38; the
- * call is refused where they do not fit).  out must not overlap the inputs.  The same inputs give the same bits.
+ * call is refused where they do not fit).  out must not overlap the inputs otherwise.  The same inputs give the same bits.
  * One workspace serves calls in order; calls that may overlap on the device need one each.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_buf, int32_t err_cap);

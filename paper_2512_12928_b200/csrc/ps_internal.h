@@ -38,6 +38,41 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// ---- whether outputs overlap inputs ---------------------------------------------------------------
+
+// Rows of so many elements of 2 bytes each, so far apart.
+struct RowSet {
+    const void* p;
+    int64_t stride, width;
+};
+// Whether two of n rows each share an element.  Sets with one stride (parts of a buffer) are told apart by a division; others
+// only if they lie interleaved, and then row by row.
+inline bool rows_meet(const RowSet& x, const RowSet& y, int64_t n) {
+    struct Span {
+        int64_t at, step, bytes;
+    };
+    auto span = [&](const RowSet& r) {       // by rising address
+        Span s{(int64_t)reinterpret_cast<uintptr_t>(r.p), n > 1 ? 2 * r.stride : 0, 2 * r.width};
+        if (s.step < 0) s.at += (n - 1) * s.step, s.step = -s.step;
+        return s;
+    };
+    const Span a = span(x), b = span(y);
+    if (a.at + (n - 1) * a.step + a.bytes <= b.at || b.at + (n - 1) * b.step + b.bytes <= a.at) return false;
+    if (a.step == b.step && a.step > 0) {    // row i of a and row j of b meet if d - a.bytes < (i - j) step < d + b.bytes
+        const int64_t d = b.at - a.at, low = d - a.bytes;
+        int64_t k = low / a.step - (low % a.step < 0) + 1;
+        if (k < 1 - n) k = 1 - n;
+        return k < n && k * a.step < d + b.bytes;
+    }
+    for (int64_t i = 0, j = 0; i < n && j < n;) {
+        const int64_t s = a.at + i * a.step, t = b.at + j * b.step;
+        if (s + a.bytes <= t) ++i;
+        else if (t + b.bytes <= s) ++j;
+        else return true;
+    }
+    return false;
+}
+
 // ---- block gather / scatter (swap-out and swap-in kernels) -----------------------------------
 
 // A "slab" is one block of one layer in one pool: slab_vec 16-byte vectors, contiguous.

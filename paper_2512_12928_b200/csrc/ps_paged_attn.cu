@@ -967,7 +967,13 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
         return bad("ps_paged_attn: a pool's block stride is smaller than a block");
     if (!on(a.kpool, a.k_block_stride, 16) || !on(a.vpool, a.v_block_stride, 16) || !on(a.q, a.q_stride, 16) || !on(a.out, a.out_stride, 16))
         return bad("ps_paged_attn: pools, q, out and their strides must be multiples of 16 bytes");
-    if (a.batch > 1 && a.out_stride < (int64_t)a.num_q_heads * a.head_dim) return bad("ps_paged_attn: rows of out overlap");
+    const int64_t width = (int64_t)a.num_q_heads * a.head_dim;
+    if (a.batch > 1 && a.out_stride < width) return bad("ps_paged_attn: rows of out overlap");
+    // In place a row's queries are loaded by the CTAs that attend it before its result is stored: by the CTA that has the
+    // whole row, or behind all of them by the join.
+    if (!(a.out == a.q && (a.out_stride == a.q_stride || a.batch == 1)) &&
+        ps::rows_meet({a.out, a.out_stride, width}, {a.q, a.q_stride, width}, a.batch))
+        return bad("ps_paged_attn: out overlaps q by another stride or in part");
     // The places of all segments are counted in 32 bits.  A segment has a place for every tile that its table row has room
     // for and at most 4 more, and a tile's tokens times the KV heads are 24 (3 KV heads of 33 query heads each) times a
     // row's segments or more: with 1024 more tokens a row, 2^34 tokens times KV heads always fit.

@@ -293,39 +293,6 @@ rope_append_elements_kernel(const __grid_constant__ RopeParams p, const __grid_c
 // Whether rows that begin there are aligned to w elements.
 bool aligned(const void* p, int64_t stride, int w) { return (reinterpret_cast<uintptr_t>(p) % (2 * w)) == 0 && stride % w == 0; }
 
-// n rows of so many elements each, so far apart.
-struct RowSet {
-    const void* p;
-    int64_t stride, width;
-};
-// Whether two of n rows each share an element.  Sets with one stride (parts of a buffer) are told apart by a division; others
-// only if they lie interleaved, and then row by row.
-bool rows_meet(const RowSet& x, const RowSet& y, int64_t n) {
-    struct Span {
-        int64_t at, step, bytes;
-    };
-    auto span = [&](const RowSet& r) {       // by rising address
-        Span s{(int64_t)reinterpret_cast<uintptr_t>(r.p), n > 1 ? 2 * r.stride : 0, 2 * r.width};
-        if (s.step < 0) s.at += (n - 1) * s.step, s.step = -s.step;
-        return s;
-    };
-    const Span a = span(x), b = span(y);
-    if (a.at + (n - 1) * a.step + a.bytes <= b.at || b.at + (n - 1) * b.step + b.bytes <= a.at) return false;
-    if (a.step == b.step && a.step > 0) {    // row i of a and row j of b meet if d - a.bytes < (i - j) step < d + b.bytes
-        const int64_t d = b.at - a.at, low = d - a.bytes;
-        int64_t k = low / a.step - (low % a.step < 0) + 1;
-        if (k < 1 - n) k = 1 - n;
-        return k < n && k * a.step < d + b.bytes;
-    }
-    for (int64_t i = 0, j = 0; i < n && j < n;) {
-        const int64_t s = a.at + i * a.step, t = b.at + j * b.step;
-        if (s + a.bytes <= t) ++i;
-        else if (t + b.bytes <= s) ++j;
-        else return true;
-    }
-    return false;
-}
-
 template <typename T, bool kNeighbours, int W>
 cudaError_t launch_vectors(RopeParams p, const FreqAxes& axes, int32_t heads, cudaStream_t s) {
     const int units = kNeighbours ? (p.dim / W + 1) / 2 : p.rot / 2 / W + ((p.dim - p.rot) / W + 1) / 2;
@@ -396,11 +363,12 @@ extern "C" int32_t ps_rope_append(const ps_rope_args* args, void* stream, char* 
     // An output may be its own input, whose elements a thread has loaded before it stores theirs; anything else that an
     // output shares with an input or with the other output would be stored by one thread while another reads or stores it.
     const int64_t q_width = (int64_t)a.num_q_heads * a.head_dim, kv_width = (int64_t)a.num_kv_heads * a.head_dim;
+    using ps::RowSet;
     const RowSet q{a.q, a.q_stride, q_width}, k{a.k, a.k_stride, kv_width}, v{a.v, a.v_stride, kv_width};
     const RowSet q_out{a.q_out, a.q_out_stride, q_width}, k_out{a.k_out, a.k_out_stride, kv_width};
     const bool to_k = do_k && a.k_out;
     auto apart = [&](const RowSet& out, const RowSet& in, bool may_be) {
-        return (may_be && out.p == in.p && (out.stride == in.stride || a.tokens == 1)) || !rows_meet(out, in, a.tokens);
+        return (may_be && out.p == in.p && (out.stride == in.stride || a.tokens == 1)) || !ps::rows_meet(out, in, a.tokens);
     };
     auto rows_apart = [&](const RowSet& out) { return a.tokens == 1 || out.stride >= out.width || -out.stride >= out.width; };
     if ((do_q && !rows_apart(q_out)) || (to_k && !rows_apart(k_out))) return bad("ps_rope_append: rows of q_out or k_out overlap");

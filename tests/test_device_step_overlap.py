@@ -1,6 +1,6 @@
-"""Outputs of ps_rope_append that share elements with what it reads or writes elsewhere are refused: no GPU.
+"""Outputs of ps_rope_append and ps_paged_attn that share elements with what they read or write elsewhere are refused: no GPU.
 
-Every call here is refused: those whose rows are apart lack positions, which is found out last."""
+Every call here is refused: those whose rows are apart lack positions, or a workspace, which is found out last."""
 import ctypes as C
 import random
 
@@ -98,3 +98,20 @@ def test_against_sets_of_elements():
         seen[want] += 1
         assert answer(rows, tokens) == want, rows
     assert min(seen.values()) > 500, seen
+
+
+@pytest.mark.parametrize("batch,q,out,want", [
+    (3, (0, 512), (1536, 512), False), (3, (0, 512), (1528, 512), True), (3, (0, 512), (0, 512), False), (3, (0, 512), (0, 520), True),
+    (3, (0, 512), (8, 512), True), (3, (0, 1024), (512, 1024), False), (3, (0, 1024), (504, 1024), True), (3, (0, 0), (512, 512), False),
+    (3, (0, 0), (0, 512), True), (1, (0, 8), (0, 16), False), (1, (0, 8), (504, 512), True), (40, (512, 2048), (0, 512), True),
+    (3, (512, 1536), (1024, 1536), False)])
+def test_attention_in_place_and_beside(batch, q, out, want):
+    a = B.PsPagedAttnArgs(kpool=A << 1, vpool=A << 2, q=A + 2 * q[0], out=A + 2 * out[0], q_stride=q[1], out_stride=out[1], block_tables=A, ctx_lens=A,
+                          workspace=A, workspace_bytes=0, k_block_stride=1 << 14, v_block_stride=1 << 14, batch=batch, table_stride=4,
+                          num_kv_heads=2, num_q_heads=4, head_dim=128, block_size=16, num_gpu_blocks=4)
+    err = C.create_string_buffer(256)
+    rc = B.load().ps_paged_attn(C.byref(a), None, err, 256)
+    text = err.value.decode()
+    assert (rc == B.PS_ERR_INVALID and "overlaps q" in text) == want
+    if not want:
+        assert rc == B.PS_ERR_CUDA or "workspace" in text, text          # no device, or one

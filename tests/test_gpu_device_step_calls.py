@@ -10,7 +10,7 @@ import torch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 sys.path.insert(0, ROOT)                                            # as a script too
-from device_step_util import attn_want, check_attn, check_within, rope_want
+from device_step_util import attn_want, check_attn, check_within, rope_want, tables_tensor
 from paper_2512_12928_b200 import binding as B
 from test_gpu_device_step import Engine, attn_case, dev, run_attn, slot_case
 
@@ -97,6 +97,23 @@ def test_attn_many_heads(hq, hkv, D, ctx):
     kp, vp, q, tables = attn_case(rng, ctx, hq, hkv, D, 16, torch.bfloat16)
     out, lse = run_attn(kp, vp, q, tables, ctx)
     check_attn(out, lse, attn_want(kp, vp, q, tables, ctx))
+
+
+@pytest.mark.parametrize("hq,hkv,D,ctx", [(32, 8, 128, [300]), (32, 8, 128, [0, 5000, 17, 900]), (16, 1, 64, [60000]), (64, 1, 128, [700] * 9),
+                                          (24, 24, 64, [1] * 30 + [4000] + [90] * 200)])
+def test_attn_in_place(hq, hkv, D, ctx):
+    """out may be q, whether a row is one CTA's or cut."""
+    rng = np.random.default_rng(hq + D)
+    kp, vp, q, tables = attn_case(rng, ctx, hq, hkv, D, 16, torch.bfloat16)
+    out, lse = run_attn(kp, vp, q, tables, ctx)
+    t = tables_tensor(tables, max(1, max(len(x) for x in tables)))
+    for _ in range(20):
+        rows = torch.full((len(ctx), hq + 2, D), 3.0, device="cuda", dtype=torch.bfloat16)
+        own, own_lse = rows[:, 1: 1 + hq], torch.empty_like(lse)
+        own.copy_(q)
+        assert B.ps_paged_attn(kp, vp, own, own, t, dev(ctx), lse=own_lse) == (B.PS_OK, "")
+        assert torch.equal(own, out) and torch.equal(own_lse, lse)
+        assert (rows[:, 0] == 3.0).all() and (rows[:, -1] == 3.0).all()
 
 
 if __name__ == "__main__":
