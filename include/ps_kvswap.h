@@ -475,7 +475,8 @@ typedef struct ps_paged_attn_args {
  * weight is the sum of two numbers of the inputs' type, and the result is rounded once.  A row with ctx_lens 0, or with
  * no score above -inf, gives zeros (lse = -inf).  A length that is
  * negative counts as 0, one beyond table_stride * block_size as that many (status 5).  Blocks may be shared by rows,
- * and nothing outside the attended tokens is read into a result, whatever the pools hold there.
+ * and nothing outside the attended tokens is read into a result, whatever the pools hold there.  An infinite value among
+ * the attended ones may make its dim of the row NaN instead of infinite (its weight's second number may be 0 or negative).
  * head_dim 64 or 128, num_q_heads / num_kv_heads from 1 to 64, any block size, and any batch whose tables,
  * counting 1024 tokens more for every row, have room for up to 2^34 tokens times KV heads (of most heads 2^35 to 2^38; the
  * call is refused where they do not fit).  out must not overlap the inputs otherwise.  The same inputs give the same bits.

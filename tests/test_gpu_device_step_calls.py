@@ -116,5 +116,22 @@ def test_attn_in_place(hq, hkv, D, ctx):
         assert (rows[:, 0] == 3.0).all() and (rows[:, -1] == 3.0).all()
 
 
+def test_attn_infinite_values():
+    """Of an infinite value among the attended ones its own dims are not finite and no others; scores of -inf have no weight."""
+    rng = np.random.default_rng(31)
+    ctx = [40, 700]
+    for dt in (torch.bfloat16, torch.float16):
+        kp, vp, q, tables = attn_case(rng, ctx, 8, 2, 64, 16, dt)
+        want = attn_want(kp, vp, q, tables, ctx)
+        vp[tables[1][3], 5, 1, 7] = float("inf")
+        out, lse = run_attn(kp, vp, q, tables, ctx)
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[1, 4:, 7] = True
+        assert not torch.isfinite(out[hit]).any()
+        o, l, tol, tol_lse = want
+        o[hit.cpu().numpy()], tol[hit.cpu().numpy()] = 0.0, 0.0
+        check_attn(torch.where(hit, 0.0, out), lse, (o, l, tol, tol_lse))
+
+
 if __name__ == "__main__":
     slots_steps(int(sys.argv[1]), bool(int(sys.argv[2])))
