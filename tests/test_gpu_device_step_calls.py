@@ -133,5 +133,59 @@ def test_attn_infinite_values():
         check_attn(torch.where(hit, 0.0, out), lse, (o, l, tol, tol_lse))
 
 
+def test_attn_very_many_rows():
+    """More rows than a CTA's threads read in a few rounds, some empty, in blocks that rows share."""
+    rows, S, hq, hkv, D, nb = 40001, 16, 4, 2, 64, 50
+    g = torch.Generator(device="cuda").manual_seed(33)
+    kp, vp = (torch.randn((nb, S, hkv, D), device="cuda", generator=g).bfloat16() for _ in range(2))
+    q = torch.randn((rows, hq, D), device="cuda", generator=g).bfloat16()
+    tables = torch.randint(0, nb, (rows, 3), device="cuda", generator=g, dtype=torch.int32)
+    ctx = torch.randint(0, 3 * S + 1, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    out, lse = run_attn(kp, vp, q, tables, ctx.tolist())
+    some = list(range(0, rows, 397)) + [rows - 1]
+    check_attn(out[some], lse[some], attn_want(kp, vp, q[some], tables[some].tolist(), ctx[some].tolist()))
+    t = torch.arange(3 * S, device="cuda")                              # all rows, loosely: a half step of the result and some room
+    at = tables.long()[:, t // S] * S + t % S
+    x = torch.einsum("bhgd,bthd->bhgt", q.view(rows, hkv, 2, D).float(), kp.view(-1, hkv, D)[at].float()) / 8
+    p = torch.softmax(x.masked_fill(t >= ctx[:, None, None, None], -1e30), -1) * (ctx > 0)[:, None, None, None]
+    want = torch.einsum("bhgt,bthd->bhgd", p, vp.view(-1, hkv, D)[at].float()).reshape(rows, hq, D)
+    assert ((out.float() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all()
+
+
+def first_calls_captured():
+    """A process's first calls, inside a capture that a side stream's kernels feed."""
+    rng = np.random.default_rng(34)
+    e = Engine(rng, 7, 8, 2, 64, 16, 200, 60, 5000, torch.bfloat16)          # 903 tokens in the longest row
+    base = torch.randn(tuple(e.qkv.shape), device="cuda").to(e.qkv.dtype)
+    new_in, factor = torch.zeros_like(e.new), torch.ones((), device="cuda", dtype=e.qkv.dtype)
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                torch.mul(base, factor, out=e.qkv)
+            e.new.copy_(new_in)
+        here.wait_stream(side)
+        e.enqueue()
+    for step in range(6):
+        new = [40, 1, 0, 300, 1, 1, 17] if step % 2 == 0 else [1, -1, 1, 1, 0, -1, 1]
+        new_in.copy_(dev(new))
+        factor.fill_(float(step + 1))
+        torch.cuda.synchronize()
+        g.replay()
+        e.check(new, None)
+        assert torch.equal(e.qkv, base * factor)
+
+
+def test_first_calls_of_a_process_captured_behind_another_stream():
+    p = subprocess.run([sys.executable, os.path.abspath(__file__), "captured"], capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0, p.stdout[-2000:] + p.stderr[-2000:]
+
+
 if __name__ == "__main__":
-    slots_steps(int(sys.argv[1]), bool(int(sys.argv[2])))
+    if sys.argv[1] == "captured":
+        first_calls_captured()
+    else:
+        slots_steps(int(sys.argv[1]), bool(int(sys.argv[2])))
