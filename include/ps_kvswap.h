@@ -401,11 +401,11 @@ typedef struct ps_slots_args {
  * With a free stack the blocks that a row is short of are taken from it: first every row with PS_SLOTS_END gives its
  * blocks back (rows in order, each table in order, every id on top of the stack) and has ctx_lens_out 0, then the
  * growing rows take one id at a time from the top, in order.  That is what ps_kv_free of the former and ps_kv_alloc
- * of the latter do on the host.  The stack is the caller's own: a context neither counts ids taken here as used nor knows
- * the rows' tables, so ps_kv_alloc would hand the same blocks out again and ps_swap_out would move the request without
- * them.  Blocks of a context's pools come from ps_kv_alloc, and the call has no stack.
- * Ids handed out stay in free_ids' entries above the new top.  A block that several
+ * of the latter do on the host.  Ids handed out stay in free_ids' entries above the new top.  A block that several
  * rows share must not be given back by more than one of them.
+ * The stack is the caller's own: a context neither counts ids taken here as used nor knows the rows' tables, so
+ * ps_kv_alloc would hand the same blocks out again and ps_swap_out would move a request without them.  Blocks of a
+ * context's pools come from ps_kv_alloc, and the call has no stack.
  * Without one (free_ids NULL) the tables hold the blocks already, e.g. from ps_kv_alloc; PS_SLOTS_END only sets
  * ctx_lens_out to 0.
  * All or nothing: if a length is negative or does not fit into table_stride blocks, the new tokens are more than

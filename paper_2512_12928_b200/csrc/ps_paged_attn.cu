@@ -4,10 +4,13 @@
 //   out[b][h] = sum_t p_t V[t][h / G] / sum_t p_t,   p_t = 2^(s_t - m),   s_t = log2(e) scale q[b][h] . K[t][h / G],
 //   max(0, ctx_b - window) <= t < ctx_b,   m = max_t s_t (running),   lse = ln 2 (m + log2 sum_t p_t)
 //
-// Bound: HBM.  A token and KV head cost 4 D bytes and 4 G D flops; up to G = 64 the card computes faster than it
-// loads.  So every warp streams its own tiles of 16 or 32 tokens (4 KiB of K and of V) through a ring of three in
-// shared memory (cp.async, 16 bytes a lane, whole 128-byte lines), across the ends of rows, and no barrier lies between
-// HBM and the tensor cores.  Tokens may lie anywhere; what is not attended is filled with zeros instead of being read.
+// Bound: HBM, for up to 16 query heads on a KV head.  A token and KV head cost 4 D bytes and 4 G D flops, and the card
+// would compute faster than it loads up to G = 64; but a unit (see Warps) has at most 16 query heads, and with more of them
+// every unit of a KV head copies the tiles for itself, 2 to 4 times the cache's bytes in all (the 672 MB case below with
+// 16 query heads on each of 8 KV heads 110.5 us, with 20 155, 32 167, 64 294).  Every warp streams its own tiles of 16 or
+// 32 tokens (4 KiB of K and of V) through a ring of three in shared memory (cp.async, 16 bytes a lane, whole 128-byte
+// lines), across the ends of rows, and no barrier lies between HBM and the tensor cores.  Tokens may lie anywhere; what is
+// not attended is filled with zeros instead of being read.
 // Measured: 672 MB of cache (64 rows of 1024 to 4096 tokens, 32 query heads on 8 KV heads of 128, bf16) 101.5 us, or
 // 6.6 TB/s, which is what a copy reaches; about 6 us of it pass before the first tile is there and in the join, and
 // bound small calls (one row of 300 tokens: 7.0 us).  Heads of 64 need as many instructions for half the bytes and
@@ -25,13 +28,17 @@
 // Softmax: the reference m of a head is raised only when a score exceeds it by more than kSlack, so that a tile needs
 // one vote instead of a maximum over the lanes; weights stay below 2^kSlack and sums in 32 bits lose nothing by it.
 // For the product with V a weight is split into two numbers of the inputs' type: one alone makes the result's error
-// 1.4 times what its own rounding costs, and the second product costs less than 1 % of the time.
+// 1.4 times what its own rounding costs, and the second product costs less than 1 % of the time.  A third number gains
+// nothing: of the 672 MB case's outputs in bf16 0.3 % are not the nearest to the exact value either way (0.08 % of a sum in
+// plain 32-bit arithmetic), which then is the tensor cores' order and rounding of sums.
 //
 // Work: the rows' tiles form one sequence (with two places more for each row's start and end, which cost about two tiles'
-// time) that is cut into equal shares, one per CTA, from the lengths each CTA reads itself: no plan is made on the host or by another kernel.  A row cut by a share's end leaves partial
-// results (m, sum, accumulators) in the workspace, which a second kernel (paged_join_kernel) combines in order.
-// The join is a second launch rather than a last-arrival counter in the first: the workspace then needs no
-// initial state, and neither a replayed graph nor a call that shares it in turn can find a stale counter.
+// time) that is cut into equal shares, one per CTA, from the lengths each CTA reads itself: no plan is made on the host or
+// by another kernel.  A row cut by a share's end leaves partial results (m, sum, accumulators) in the workspace, which a
+// second kernel (paged_join_kernel) combines in order.  The join is a second launch rather than a last-arrival counter in
+// the first: the workspace then needs no initial state, and neither a replayed graph nor a call that shares it in turn can
+// find a stale counter.  It is launched early, but its CTAs (80 registers a thread) do not fit beside one of 8
+// warps of the first kernel (207 to 249), so they start as those leave.
 //
 // Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of two);
 // the units of a token are neighbours in memory.  The slices' states are combined through shared memory at a segment's

@@ -298,7 +298,8 @@ cudaError_t launch_vectors(RopeParams p, const FreqAxes& axes, int32_t heads, cu
     const int units = kNeighbours ? (p.dim / W + 1) / 2 : p.rot / 2 / W + ((p.dim - p.rot) / W + 1) / 2;
     // Few tokens: one per CTA, so that they spread over the chip.  Many: a round of four CTAs per SM costs about 2 us
     // that its sines take, so as many as make a sine per thread and leave the chip filled, but not a little more than
-    // a round, whose rest then runs alone (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.6 / 7.0 / 7.8 us, 2048
+    // a round, whose rest then runs alone (only the first round's rest is avoided: 5003 tokens of 32 heads of 80 are two
+    // full rounds and a third of 67 CTAs).  Times (80 heads of 128, 1 / 2 / 4 tokens a CTA: 512 tokens 5.6 / 7.0 / 7.8 us, 2048
     // 22.4 / 18.2 / 16.7, 8192 74.7 / 60.1 / 57.6; 32 heads of 80, 1 / 2 / 4 / 8: 2500 tokens 11.3 / 8.5 / 8.0 / 9.0, 5003
     // 22.8 / 16.5 / 14.7 / 14.8, 9000 39.2 / 26.9 / 22.6 / 19.6).
     constexpr int kRound = 4 * 148, kFilled = 350;

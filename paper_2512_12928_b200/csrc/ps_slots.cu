@@ -8,14 +8,17 @@
 // a time in row order: the free stack and the tables come out as from ps_kv_free and ps_kv_alloc in those orders.
 //
 // The work is a few words per row and token; what bounds it is latency: the chain "load lengths, scan, load a free
-// id, store".  Two ways, chosen by the room for tokens:
+// id, store".  Two ways, chosen by the room for tokens and the number of rows:
 //   - slots_one_cta_kernel: one CTA scans, pushes, pops and maps; barriers order its steps and one launch does all.
 //     For room for up to 512 tokens (2048 with over 512 rows, 4096 in place): 64 rows of a token each 3.1 us; 200 rows
-//     4.6 us for 1000 tokens, 5.4 for 2000, 7.0 for 4000, 14.4 for 16000.
+//     4.6 us for 1000 tokens, 5.4 for 2000, 7.0 for 4000, 14.4 for 16000.  And for over 4096 rows, whose counts the other
+//     way does not hold in shared memory, whatever the room: 4097 rows of a token each 20.9 us, 24.7 with room for 16000
+//     more; 5000 rows 42 us with room for 100000 tokens and 89 with as many live ones (4096 rows the other way: 9.8).
 //   - slots_wide_kernel: every CTA scans all rows for itself (cheaper than another launch) and takes its part of
 //     pushes, pops and tokens.  A popped id is found without waiting for the pushes: an index above the old top
 //     belongs to the table of a row that ended, which a search in the scanned counts names.  Where lengths or count are
-//     updated in place, a second kernel of one CTA does that when nobody reads them any more, which takes 2.5 us more.
+//     updated in place, a second kernel of one CTA does that when nobody reads them any more, which takes 2.5 us more
+//     (256 rows with prompt chunks 7.1 instead of 4.5), 3 to 4 with 1000 rows and over.
 //     (200 rows: 4.1 us for 1000 to 16000 tokens; 1024 rows of a token each 6.5 us and 5.8 in one CTA.)
 // Work on blocks and tokens is dealt to threads by the scanned counts (binary search in shared memory), so one long
 // prompt costs the same as many short ones.
