@@ -490,6 +490,109 @@ int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_bu
 /* Bytes of workspace that ps_paged_attn needs on the current device for these heads, whatever the batch. */
 int32_t ps_paged_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes);
 
+/* ---- a cache of 8 bits ------------------------------------------------------------------------ */
+
+/* The paper has no counterpart.  Decode attention is bound by the cache's bytes and a reload by the host link, and a
+ * cache of 8 bits halves both.  Its blocks hold codes of 8 bits, and every block and KV head has one 32-bit scale for its
+ * keys and one for its values: a value is code * scale.  The calls belong to a step whose lengths stay on the device and
+ * share that section's manner (streams, errors, status words, capture, programmatic launches): ps_build_slots gives slots
+ * and tables, ps_rope_append without pools rotates, and then
+ *
+ *   ps_quant_append  quantises the new tokens' keys and values into their slots and keeps the blocks' scales
+ *   ps_quant_attn    attends them, as ps_paged_attn does those of a 16-bit cache
+ *   ps_quant_read    gives any tokens back in 16 bits, e.g. the context that a prompt's chunk attends
+ *
+ * Codes of a pool are [num_gpu_blocks][block_size][num_kv_heads][head_dim] bytes, scales [num_gpu_blocks][num_kv_heads]
+ * floats.  Blocks of either may lie any stride apart, so that a block's scales can stand behind its codes: then a block is
+ * one range of bytes, which a context offloads and reloads like any other pool's (its block_size, num_kv_heads and head_dim
+ * only have to give the same number of bytes).  Scales are finite numbers, 0 or more; a context's fresh blocks need none. */
+
+enum ps_code { PS_CODE_INT8 = 0, PS_CODE_E4M3 = 1 };
+
+/* Either side may be absent (its two pointers NULL) for ps_quant_append and ps_quant_read. */
+typedef struct ps_quant_cache {
+    void* kpool;                 /* device, codes */
+    void* vpool;
+    float* k_scale;              /* device, 4-byte boundaries */
+    float* v_scale;
+    int64_t k_block_stride, v_block_stride;   /* codes (bytes) from block to block, at least a block's */
+    int64_t k_scale_stride, v_scale_stride;   /* floats from block to block, at least num_kv_heads */
+    int32_t num_gpu_blocks, block_size, num_kv_heads, head_dim;
+    int32_t codes;               /* ps_code: whole numbers from -127 to 127, or 8-bit floats with 4 bits of exponent up to 448 */
+    int32_t reserved0;
+} ps_quant_cache;
+
+typedef struct ps_quant_append_args {
+    ps_quant_cache cache;
+    const void* k;               /* device [tokens][num_kv_heads][head_dim], rows k_stride apart; NULL if the cache has no keys */
+    const void* v;               /* as k */
+    const int64_t* slots;        /* device [tokens]: block * block_size + place; negative = padding */
+    int32_t* status_word;        /* 1 = a slot outside the pool (that token is not appended) */
+    int64_t k_stride, v_stride;
+    int32_t tokens, dtype;       /* ps_dtype of k and v */
+} ps_quant_append_args;
+
+/* Writes keys and values into their slots, quantised.  For every block and head that tokens of the call go to, with Q =
+ * 127 (PS_CODE_INT8) or 448 (PS_CODE_E4M3) and all arithmetic in 32 bits, rounding to nearest even:
+ *   need  = (1 / Q) * the largest magnitude among the call's tokens of the block and head
+ *   scale = max(old scale, need, 2^-100); a call that writes the block's place 0 begins the block, which has no old scale
+ *   code  = x * (1 / scale), rounded: the exact product to a whole number, the 32-bit product to an 8-bit float
+ * Where the scale of a block that is not begun rises, the codes at all its other places become code * (old scale * (1 /
+ * scale)), rounded likewise, so that they go on standing for nearly the same values: a value is off by half a code's step
+ * when it is written, and by up to half a step of the new scale whenever the scale rises later.  The other places of a
+ * block that is begun, and all other blocks, keep their bytes.  With an infinite or NaN input its block and head get a NaN
+ * scale: all its values then read as NaN until it is begun anew.
+ * Tokens that go to one block stand next to one another in the call, in any order, as ps_build_slots numbers them (the tokens
+ * of a row are neighbours); a block that the call comes back to after tokens of others, or after padding, and one that two
+ * tokens give the same slot, has undefined contents afterwards.  head_dim up to 512, up to 1024 KV heads.  Pools, scales and
+ * inputs must not overlap.  Rows of k and v on 16-byte boundaries with blocks on 8-byte boundaries and head_dim a multiple of
+ * 8 are read 16 bytes at a time, else element by element.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_quant_append(const ps_quant_append_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+typedef struct ps_quant_read_args {
+    ps_quant_cache cache;
+    void* k_out;                 /* device [tokens][num_kv_heads][head_dim], rows k_out_stride apart; NULL if no keys are read */
+    void* v_out;
+    const int64_t* slots;        /* device [tokens], as for ps_quant_append */
+    int32_t* status_word;
+    int64_t k_out_stride, v_out_stride;
+    int32_t tokens, dtype;       /* ps_dtype of k_out and v_out */
+} ps_quant_read_args;
+
+/* Reads tokens back: row t of k_out and v_out is code * scale of slots[t], the 32-bit product rounded once.  Rows of padding
+ * and of slots outside the pool are left as they are.  Slots may repeat and stand in any order (ps_build_slots from lengths
+ * of 0 gives those of whole contexts).  Limits and alignments as for ps_quant_append, with blocks on 16-byte boundaries and
+ * head_dim a multiple of 16 for the widest accesses.  The outputs must not overlap each other or the cache.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_quant_read(const ps_quant_read_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+typedef struct ps_quant_attn_args {
+    ps_quant_cache cache;        /* both sides; codes on 16-byte boundaries, as q and out */
+    const void* q;               /* from here on as in ps_paged_attn_args */
+    void* out;
+    float* lse;
+    const int32_t* block_tables;
+    const int32_t* ctx_lens;
+    int32_t* status_word;
+    void* workspace;
+    int64_t workspace_bytes;     /* at least what ps_quant_attn_workspace says */
+    int64_t q_stride, out_stride;
+    int32_t batch, table_stride, num_q_heads, window;
+    float scale;                 /* factor on q . k; 0 = 1 / sqrt(head_dim) */
+    int32_t dtype;               /* ps_dtype of q and out */
+} ps_quant_attn_args;
+
+/* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
+ * scale.  Codes are exact in the products; a query's values are to within 2^-38 of the largest of their head.  Scores,
+ * softmax and sums are in 32 bits; for the product with V a softmax weight times its token's value scale is the sum of two
+ * fp16 numbers next to the largest value scale that the row has met (a scale 2^-20 of that one still leaves 13 bits).
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
+
+/* Bytes of workspace that ps_quant_attn needs on the current device for these heads, whatever the batch. */
+int32_t ps_quant_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes);
+
 /* ---- one engine step under the copy budget (Section 4.3 "Put it Together"; Alg. 1) -------- */
 
 /* In order: reaps finished offloads; turns copy_budget_bytes into blocks (floor(bytes /

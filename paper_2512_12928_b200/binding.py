@@ -124,6 +124,26 @@ class PsPagedAttnArgs(C.Structure):
                 + [("scale", C.c_float), ("dtype", C.c_int32)])
 
 
+class PsQuantCache(C.Structure):
+    _fields_ = _fields("kpool vpool k_scale v_scale", "k_block_stride v_block_stride k_scale_stride v_scale_stride",
+                       "num_gpu_blocks block_size num_kv_heads head_dim codes reserved0")
+
+
+class PsQuantAppendArgs(C.Structure):
+    _fields_ = [("cache", PsQuantCache)] + _fields("k v slots status_word", "k_stride v_stride", "tokens dtype")
+
+
+class PsQuantReadArgs(C.Structure):
+    _fields_ = [("cache", PsQuantCache)] + _fields("k_out v_out slots status_word", "k_out_stride v_out_stride", "tokens dtype")
+
+
+class PsQuantAttnArgs(C.Structure):
+    _fields_ = ([("cache", PsQuantCache)]
+                + _fields("q out lse block_tables ctx_lens status_word workspace", "workspace_bytes q_stride out_stride",
+                          "batch table_stride num_q_heads window")
+                + [("scale", C.c_float), ("dtype", C.c_int32)])
+
+
 TRACE_KINDS = ["attn", "merge", "gather", "scatter", "d2h", "h2d"]
 
 
@@ -196,6 +216,10 @@ def load() -> C.CDLL:
         "ps_rope_append": (i32, [C.POINTER(PsRopeArgs), vp, C.c_char_p, i32]),
         "ps_paged_attn": (i32, [C.POINTER(PsPagedAttnArgs), vp, C.c_char_p, i32]),
         "ps_paged_attn_workspace": (i32, [i32, i32, i32, p64]),
+        "ps_quant_append": (i32, [C.POINTER(PsQuantAppendArgs), vp, C.c_char_p, i32]),
+        "ps_quant_read": (i32, [C.POINTER(PsQuantReadArgs), vp, C.c_char_p, i32]),
+        "ps_quant_attn": (i32, [C.POINTER(PsQuantAttnArgs), vp, C.c_char_p, i32]),
+        "ps_quant_attn_workspace": (i32, [i32, i32, i32, p64]),
     }
     for name, (res, args) in proto.items():
         fn = getattr(lib, name)
@@ -275,7 +299,8 @@ def _load_tensor_args():
         loader.exec_module(m)
         lib = load()
         m.bind(*[C.cast(getattr(lib, n), C.c_void_p).value
-                 for n in ("ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace")])
+                 for n in ("ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace", "ps_quant_append",
+                           "ps_quant_read", "ps_quant_attn", "ps_quant_attn_workspace")])
         _tensor_args = m
     return _tensor_args
 
@@ -307,12 +332,16 @@ def ps_rope_append(q, k, q_out, k_out, positions, inv_freq, *, v=None, kpool=Non
 
 def ps_paged_attn_workspace(num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int] = None) -> int:
     """Bytes of workspace that ps_paged_attn needs for these heads on a device (default: the current one)."""
+    return _workspace("ps_paged_attn_workspace", num_kv_heads, num_q_heads, head_dim, device)
+
+
+def _workspace(name: str, num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int]) -> int:
     import torch
     out = C.c_int64()
     with torch.cuda.device(torch.cuda.current_device() if device is None else device):
-        rc = load().ps_paged_attn_workspace(num_kv_heads, num_q_heads, head_dim, C.byref(out))
+        rc = getattr(load(), name)(num_kv_heads, num_q_heads, head_dim, C.byref(out))
     if rc != PS_OK:
-        raise PsError(rc, "ps_paged_attn_workspace", "unsupported heads, or no device")
+        raise PsError(rc, name, "unsupported heads, or no device")
     return out.value
 
 
@@ -326,6 +355,40 @@ def ps_paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, *, lse=None, win
     taken from torch's allocator on the current stream for the duration of the call.  See ps_paged_attn in the header."""
     return (_tensor_args or _load_tensor_args()).paged_attn(kpool, vpool, q, out, block_tables, ctx_lens, lse, window, scale,
                                                             status_word, workspace)
+
+
+# ---- a cache of 8 bits: codes int8 or float8_e4m3fn [blocks][block_size][kv heads][dim], scales float32 [blocks][kv heads];
+# blocks of any of the four may be strided
+
+def ps_quant_append(k, v, kpool, vpool, k_scale, v_scale, slots, *, status_word=None):
+    """Quantises the new tokens' keys and values into their slots and keeps the blocks' scales: (status, error text).
+
+    k, v bfloat16 or float16 [tokens][kv heads][dim], rows may be strided; slots int64 [tokens], negative = padding, the
+    tokens of a block next to one another.  k or v may be None with its pool and scales.  See ps_quant_append in the header."""
+    return (_tensor_args or _load_tensor_args()).quant_append(k, v, kpool, vpool, k_scale, v_scale, slots, status_word)
+
+
+def ps_quant_read(kpool, vpool, k_scale, v_scale, slots, k_out, v_out, *, status_word=None):
+    """Reads the tokens of slots back into 16 bits: (status, error text).
+
+    k_out, v_out bfloat16 or float16 [tokens][kv heads][dim], rows may be strided; either may be None, and its pool and scales
+    with it.  Rows of padding are left as they are.  See ps_quant_read in the header."""
+    return (_tensor_args or _load_tensor_args()).quant_read(kpool, vpool, k_scale, v_scale, slots, k_out, v_out, status_word)
+
+
+def ps_quant_attn_workspace(num_kv_heads: int, num_q_heads: int, head_dim: int, device: Optional[int] = None) -> int:
+    """Bytes of workspace that ps_quant_attn needs for these heads on a device (default: the current one)."""
+    return _workspace("ps_quant_attn_workspace", num_kv_heads, num_q_heads, head_dim, device)
+
+
+def ps_quant_attn(kpool, vpool, k_scale, v_scale, q, out, block_tables, ctx_lens, *, lse=None, window: int = 0,
+                  scale: Optional[float] = None, status_word=None, workspace=None):
+    """Decode attention over a cache of 8 bits, from lengths and block tables on the device: (status, error text).
+
+    The other arguments are those of ps_paged_attn; workspace: of ps_quant_attn_workspace bytes.  See ps_quant_attn in the
+    header."""
+    return (_tensor_args or _load_tensor_args()).quant_attn(kpool, vpool, k_scale, v_scale, q, out, block_tables, ctx_lens, lse,
+                                                            window, scale, status_word, workspace)
 
 
 def ps_order_queue(exec_us, remain_us, weight, *, eta: float, gamma: float, t_c: float, waited_us=None, tau: float = 0.0):

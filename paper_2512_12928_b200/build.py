@@ -18,8 +18,10 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libps_kvswap.so")
 SOURCES = ["ps_runtime.cu", "ps_swap.cu", "ps_step.cu", "ps_policy.cu", "ps_measure.cu", "ps_copy_kernels.cu",
-           "ps_attn_kernels.cu", "ps_static_scratch.cu", "ps_slots.cu", "ps_rope.cu", "ps_paged_attn.cu"]
-HEADERS = [os.path.join(CSRC, "ps_internal.h"), os.path.join(CSRC, "ps_ctx.h"), os.path.join(ROOT, "include", "ps_kvswap.h")]
+           "ps_attn_kernels.cu", "ps_static_scratch.cu", "ps_slots.cu", "ps_rope.cu", "ps_paged_attn.cu",
+           "ps_quant.cu", "ps_quant_attn.cu"]
+HEADERS = [os.path.join(CSRC, "ps_internal.h"), os.path.join(CSRC, "ps_ctx.h"), os.path.join(CSRC, "ps_paged_attn.cuh"),
+           os.path.join(ROOT, "include", "ps_kvswap.h")]
 
 
 def _nvcc() -> str:
@@ -87,7 +89,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)
     cmd = [
-        _nvcc(), "-shared", "-std=c++17", "-O3", "-lineinfo",
+        _nvcc(), "-shared", "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
         "-gencode", "arch=compute_100a,code=sm_100a",
         "-Xcompiler", "-fPIC,-Wall,-Wno-unused-function",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,

@@ -1,0 +1,407 @@
+// ps_quant_append and ps_quant_read: a paged cache of 8-bit codes with one scale for each block and KV head, written from
+// 16-bit keys and values and read back into 16 bits.
+//
+//   need = max |x| / Q over the call's tokens of a block and head,   scale' = max(scale, need, 2^-100),
+//   code = round(x / scale'),   and codes that are there: round(code scale / scale') where scale' > scale
+//
+// Bound: memory; a value written is 2 bytes read and 1 written, a value read back 1 and 2.  A scale needs all of its
+// block's new values before the first code can be rounded, so a warp takes one block's tokens of one head ("unit") and holds
+// them in registers between the two: 16 tokens of 128 dims are 8 vectors of 16 bytes a lane.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math_constants.h>
+
+#include <algorithm>
+
+#include "ps_internal.h"
+#include "ps_kvswap.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxDim = 512, kMaxHeads = 1024;
+constexpr int kStatusBadSlot = 1;
+constexpr float kLeastScale = 7.888609052210118e-31f;   // 2^-100: its reciprocal is finite
+
+template <typename T> struct Num;
+template <> struct Num<__nv_bfloat16> {
+    static constexpr uint32_t kInf = 0x7f80;
+    static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+};
+template <> struct Num<__half> {
+    static constexpr uint32_t kInf = 0x7c00;
+    static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+};
+
+struct Int8 {
+    static constexpr float kTop = 127.f;
+    // Two codes of x times r.  The exact product is rounded to a whole number by the addition: 1.5 2^23 + n has n as its low
+    // bits.
+    static __device__ __forceinline__ uint32_t pair(float a, float b, float r) {
+        return __byte_perm(__float_as_uint(fmaf(a, r, 12582912.f)), __float_as_uint(fmaf(b, r, 12582912.f)), 0x0040) & 0xffff;
+    }
+    static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2((float)(int8_t)v, (float)(int8_t)(v >> 8)); }
+};
+struct E4m3 {
+    static constexpr float kTop = 448.f;
+    static __device__ __forceinline__ uint32_t pair(float a, float b, float r) {
+        return __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(a, r), __fmul_rn(b, r)), __NV_SATFINITE, __NV_E4M3);
+    }
+    static __device__ __forceinline__ float2 unpack(uint32_t v) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3);
+        return __half22float2(__half2(h));
+    }
+};
+
+// W values that are loaded and stored at once.
+template <int Bytes> struct Bits;
+template <> struct Bits<1> { using type = uint8_t; };
+template <> struct Bits<2> { using type = uint16_t; };
+template <> struct Bits<4> { using type = uint32_t; };
+template <> struct Bits<8> { using type = uint2; };
+template <> struct Bits<16> { using type = uint4; };
+template <int Bytes>
+struct alignas(Bytes < 4 ? 4 : Bytes) Vec {
+    uint32_t w[(Bytes + 3) / 4];             // a value of one or two bytes is the low ones of a word
+    __device__ __forceinline__ void load(const void* p) {
+        using B = typename Bits<Bytes>::type;
+        if constexpr (Bytes < 4) w[0] = *static_cast<const B*>(p);
+        else *reinterpret_cast<B*>(w) = *static_cast<const B*>(p);
+    }
+    __device__ __forceinline__ void store(void* p) const {
+        using B = typename Bits<Bytes>::type;
+        if constexpr (Bytes < 4) *static_cast<B*>(p) = (B)w[0];
+        else *static_cast<B*>(p) = *reinterpret_cast<const B*>(w);
+    }
+};
+
+// t / size for 0 <= t < 2^32 is umulhi of magic = 2^64 / size rounded up; slots may be longer
+__device__ __forceinline__ int64_t block_of(int64_t slot, int32_t size, uint64_t magic) {
+    if (size == 1) return slot;
+    return slot >> 32 ? slot / size : (int64_t)__umul64hi((uint64_t)slot, magic);
+}
+
+struct Side {                     // keys or values
+    const void* rows;             // 16-bit rows: read by the append, written by the read-back
+    unsigned char* pool;
+    float* scale;
+    int64_t row_stride, block_stride, scale_stride;
+};
+struct QuantParams {
+    Side side[2];
+    const int64_t* slots;
+    int32_t* status;
+    int64_t num_slots;
+    uint64_t block_magic;
+    int32_t tokens, hkv, dim, block_size, sides, tok_per_cta;
+};
+
+// ------------------------------------------------------------------------------------------------ append
+
+// Tokens [t0, t0 + n) of a CTA, one a lane.  A segment is a run of tokens that go to one block; the CTA in whose range it
+// begins has the whole of it.  Every warp finds the segments for itself: no barrier, and nothing in shared memory.
+template <typename T, typename C, int W>
+__global__ void __launch_bounds__(kThreads)
+quant_append_kernel(const __grid_constant__ QuantParams p) {
+    constexpr int kHold = 8;                 // vectors of a lane that stay in registers between maximum and rounding
+    const int lane = threadIdx.x & 31;
+    const int nwarps = (kThreads / 32) * gridDim.y, me = (kThreads / 32) * blockIdx.y + (threadIdx.x >> 5);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t t0 = blockIdx.x * p.tok_per_cta;
+    const int n = min(p.tok_per_cta, p.tokens - t0);
+    auto look_up = [&](int32_t t, bool report) -> int64_t {      // the token's slot, or -1
+        if (t < 0 || t >= p.tokens) return -1;
+        const int64_t s = p.slots[t];
+        if (s < p.num_slots) return s < 0 ? -1 : s;
+        if (report && p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+        return -1;
+    };
+    const int64_t slot = look_up(lane < n ? t0 + lane : -1, true);
+    const int64_t block = slot < 0 ? -1 : block_of(slot, p.block_size, p.block_magic);
+    int64_t before = __shfl_up_sync(0xffffffffu, block, 1);
+    if (lane == 0) {
+        const int64_t s = look_up(t0 - 1, false);
+        before = s < 0 ? -1 : block_of(s, p.block_size, p.block_magic);
+    }
+    uint32_t starts = __ballot_sync(0xffffffffu, block >= 0 && block != before);
+    const int units = p.sides * p.hkv;       // of a segment
+    const int row_vecs = p.dim / W;
+    for (int u = me, skip = 0; starts; u += nwarps) {
+        while (starts && u - skip >= units) {
+            starts &= starts - 1;
+            skip += units;
+        }
+        if (!starts) break;
+        const int first = __ffs(starts) - 1;
+        const int head = (u - skip) % p.hkv;
+        const Side& side = p.side[(u - skip) / p.hkv];
+        const int64_t blk = __shfl_sync(0xffffffffu, block, first);
+        const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
+        int len = (other ? __ffs(other) - 1 : 32) - first;
+        const int64_t block_begin = blk * p.block_size;
+        bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && slot == block_begin);
+        if (first + len >= n) {              // it may go on behind the CTA's tokens
+            len = n - first;
+            for (;;) {
+                const int64_t s = look_up(t0 + first + len + lane, false);
+                const bool in = s >= block_begin && s - block_begin < p.block_size;
+                const uint32_t out = __ballot_sync(0xffffffffu, !in);
+                const int more = out ? __ffs(out) - 1 : 32;
+                begun |= __any_sync(0xffffffffu, lane < more && s == block_begin);
+                len += more;
+                if (more < 32) break;
+            }
+        }
+        const T* src = (const T*)side.rows + (t0 + first) * side.row_stride + (int64_t)head * p.dim;
+        unsigned char* pool = side.pool + blk * side.block_stride + (int64_t)head * p.dim;
+        const int64_t place_bytes = (int64_t)p.hkv * p.dim;
+        float* scale_at = side.scale + blk * side.scale_stride + head;
+        const float old = begun ? 0.f : *scale_at;
+        // The unit's vectors, rows first: this lane has every 32nd.
+        const int row_step = 32 / row_vecs, piece_step = 32 % row_vecs;
+        const int row0 = lane / row_vecs, piece0 = lane - row0 * row_vecs;
+        auto next = [&](int& row, int& piece) {
+            row += row_step;
+            piece += piece_step;
+            if (piece >= row_vecs) {
+                piece -= row_vecs;
+                ++row;
+            }
+        };
+        Vec<2 * W> held[kHold];
+        uint32_t most = 0;                   // of both halves of a word
+        auto meet = [&](const Vec<2 * W>& x) {
+#pragma unroll
+            for (int i = 0; i < (W + 1) / 2; ++i) most = __vmaxu2(most, x.w[i] & 0x7fff7fffu);
+        };
+        int row = row0, piece = piece0;
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) {
+            if (row < len) held[i].load(src + row * side.row_stride + piece * W);
+            next(row, piece);
+        }
+        row = row0, piece = piece0;
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) {
+            if (row < len) meet(held[i]);
+            next(row, piece);
+        }
+        while (row < len) {
+            Vec<2 * W> x;
+            x.load(src + row * side.row_stride + piece * W);
+            meet(x);
+            next(row, piece);
+        }
+        most = __reduce_max_sync(0xffffffffu, max(most & 0xffff, most >> 16));
+        const float need = Num<T>::unpack(most).x * (1.f / C::kTop);
+        const float now = most >= Num<T>::kInf || old != old ? CUDART_NAN_F : fmaxf(fmaxf(old, need), kLeastScale);
+        const float r = 1.f / now;
+        if (!begun && now > old) {           // the codes that are there, all places of the block
+            const float f = __fmul_rn(old, r);
+            int q = row0, c = piece0;
+            while (q < p.block_size) {
+                Vec<W> x;
+                unsigned char* at = pool + q * place_bytes + c * W;
+                x.load(at);
+#pragma unroll
+                for (int i = 0; i < (W + 3) / 4; ++i) {
+                    const float2 lo = C::unpack(x.w[i]), hi = C::unpack(x.w[i] >> 16);
+                    x.w[i] = C::pair(lo.x, lo.y, f) | C::pair(hi.x, hi.y, f) << 16;
+                }
+                x.store(at);
+                next(q, c);
+            }
+            __syncwarp();                    // the new tokens' codes come on top
+        }
+        auto put = [&](const Vec<2 * W>& x, int row, int piece) {
+            Vec<W> y;
+#pragma unroll
+            for (int i = 0; i < (W + 1) / 2; ++i) {
+                const float2 v = Num<T>::unpack(x.w[i]);
+                const uint32_t two = C::pair(v.x, v.y, r);
+                if (i & 1) y.w[i / 2] |= two << 16;
+                else y.w[i / 2] = two;
+            }
+            y.store(pool + (p.slots[t0 + first + row] - block_begin) * place_bytes + piece * W);
+        };
+        row = row0, piece = piece0;
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) {
+            if (row < len) put(held[i], row, piece);
+            next(row, piece);
+        }
+        while (row < len) {
+            Vec<2 * W> x;
+            x.load(src + row * side.row_stride + piece * W);
+            put(x, row, piece);
+            next(row, piece);
+        }
+        if (lane == 0) *scale_at = now;
+    }
+}
+
+// -------------------------------------------------------------------------------------------------- read
+
+template <typename T, typename C, int W>
+__global__ void __launch_bounds__(kThreads)
+quant_read_kernel(const __grid_constant__ QuantParams p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t t0 = blockIdx.x * p.tok_per_cta;
+    const int n = min(p.tok_per_cta, p.tokens - t0);
+    const int side_vecs = p.hkv * p.dim / W, per = p.sides * side_vecs;     // vectors of a token
+    for (int i = threadIdx.x; i < n * per; i += kThreads) {
+        const int k = i / per, j = i - k * per, which = j / side_vecs, vec = j - which * side_vecs;
+        const Side& side = p.side[which];
+        const int64_t slot = p.slots[t0 + k];
+        if (slot < 0) continue;
+        if (slot >= p.num_slots) {
+            if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+            continue;
+        }
+        const int64_t blk = block_of(slot, p.block_size, p.block_magic);
+        Vec<W> x;
+        x.load(side.pool + blk * side.block_stride + (slot - blk * p.block_size) * ((int64_t)p.hkv * p.dim) + vec * W);
+        const float scale = side.scale[blk * side.scale_stride + vec * W / p.dim];
+        Vec<2 * W> y;
+#pragma unroll
+        for (int h = 0; h < (W + 1) / 2; ++h) {
+            const float2 v = C::unpack(x.w[h / 2] >> (16 * (h & 1)));
+            y.w[h] = Num<T>::pack(v.x * scale, v.y * scale);
+        }
+        y.store((T*)side.rows + (t0 + k) * side.row_stride + vec * W);
+    }
+}
+
+// -------------------------------------------------------------------------------------------------- host
+
+struct Given {                    // one side as the caller gave it
+    const void* rows;
+    void* pool;
+    float* scale;
+    int64_t row_stride, block_stride, scale_stride;
+};
+
+// Fills in p; *p.sides is 0 where there is nothing to do.  Returns the text of what is wrong, or null.
+const char* plan(const ps_quant_cache& c, const Given (&given)[2], const int64_t* slots, int32_t* status, int32_t tokens, int32_t dtype,
+                 bool rows_written, QuantParams* params) {
+    if (tokens < 0 || c.block_size <= 0 || c.num_gpu_blocks <= 0) return "negative count or non-positive size";
+    if (c.num_kv_heads <= 0 || c.num_kv_heads > kMaxHeads || c.head_dim <= 0 || c.head_dim > kMaxDim)
+        return "num_kv_heads must be from 1 to 1024, head_dim from 1 to 512";
+    if (dtype != PS_DTYPE_BF16 && dtype != PS_DTYPE_FP16) return "dtype must be PS_DTYPE_BF16 or PS_DTYPE_FP16";
+    if (c.codes != PS_CODE_INT8 && c.codes != PS_CODE_E4M3) return "codes must be PS_CODE_INT8 or PS_CODE_E4M3";
+    if (tokens == 0) return nullptr;         // tensors without elements have no address
+    const int64_t width = (int64_t)c.num_kv_heads * c.head_dim, block = width * c.block_size;
+    QuantParams& p = *params;
+    ps::RowSet sets[2][3];
+    for (const Given& g : given) {
+        if (!g.rows && !g.pool && !g.scale) continue;
+        if (!g.rows || !g.pool || !g.scale) return "keys and values need rows, codes and scales, or none of them";
+        if (c.num_gpu_blocks > 1 && (g.block_stride < block || g.scale_stride < c.num_kv_heads))
+            return "a pool's block stride is smaller than a block, or its scales' than a block's";
+        if (reinterpret_cast<uintptr_t>(g.scale) % 4 || reinterpret_cast<uintptr_t>(g.rows) % 2) return "scales or rows are not aligned to their elements";
+        if (rows_written && tokens > 1 && g.row_stride < width && -g.row_stride < width) return "rows of k_out or v_out overlap";
+        sets[p.sides][0] = {g.rows, g.row_stride, width, 2};
+        sets[p.sides][1] = {g.pool, g.block_stride, block, 1};
+        sets[p.sides][2] = {g.scale, g.scale_stride, c.num_kv_heads, 4};
+        p.side[p.sides++] = {g.rows, (unsigned char*)g.pool, g.scale, g.row_stride, g.block_stride, g.scale_stride};
+    }
+    if (p.sides == 0) return "neither keys nor values are given";
+    if (!slots) return "null pointer";
+    // whatever is written is apart from everything else
+    auto count = [&](int kind) -> int64_t { return kind == 0 ? tokens : c.num_gpu_blocks; };
+    for (int i = 0; i < 3 * p.sides; ++i)
+        for (int j = 0; j < i; ++j) {
+            const bool written = rows_written ? i % 3 == 0 || j % 3 == 0 : i % 3 != 0 || j % 3 != 0;
+            if (written && ps::rows_meet(sets[i / 3][i % 3], count(i % 3), sets[j / 3][j % 3], count(j % 3)))
+                return "what is written overlaps another argument";
+        }
+    p.slots = slots, p.status = status;
+    p.num_slots = (int64_t)c.num_gpu_blocks * c.block_size;
+    p.block_magic = c.block_size > 1 ? ~0ull / (uint64_t)c.block_size + 1 : 0;
+    p.tokens = tokens, p.hkv = c.num_kv_heads, p.dim = c.head_dim, p.block_size = c.block_size;
+    return nullptr;
+}
+
+// Whether w values can be moved at once everywhere.
+bool fits(const QuantParams& p, int w) {
+    bool ok = p.dim % w == 0;
+    for (int i = 0; i < p.sides; ++i) {
+        const Side& s = p.side[i];
+        const int rows = std::min(2 * w, 16);
+        ok = ok && reinterpret_cast<uintptr_t>(s.rows) % rows == 0 && 2 * s.row_stride % rows == 0 &&
+             reinterpret_cast<uintptr_t>(s.pool) % w == 0 && s.block_stride % w == 0;
+    }
+    return ok;
+}
+
+template <typename T, typename C>
+cudaError_t launch_append(QuantParams p, cudaStream_t s) {
+    p.tok_per_cta = 1;
+    const int warps = kThreads / 32;
+    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((p.sides * p.hkv + warps - 1) / warps));
+    return fits(p, 8) ? ps::launch_dependent(quant_append_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
+                      : ps::launch_dependent(quant_append_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
+}
+template <typename T, typename C>
+cudaError_t launch_read(QuantParams p, cudaStream_t s) {
+    p.tok_per_cta = 1;
+    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
+    return fits(p, 8) ? ps::launch_dependent(quant_read_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
+                      : ps::launch_dependent(quant_read_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
+}
+
+int32_t refuse(const char* name, const char* text, char* buf, int32_t cap) {
+    if (buf && cap > 0) snprintf(buf, (size_t)cap, "%s: %s", name, text);
+    return PS_ERR_INVALID;
+}
+
+}  // namespace
+
+extern "C" int32_t ps_quant_append(const ps_quant_append_args* args, void* stream, char* err_buf, int32_t err_cap) {
+    if (err_buf && err_cap > 0) err_buf[0] = 0;
+    if (!args) return refuse("ps_quant_append", "null arguments", err_buf, err_cap);
+    const ps_quant_append_args a = *args;
+    const ps_quant_cache& c = a.cache;
+    const Given given[2] = {{a.k, c.kpool, c.k_scale, a.k_stride, c.k_block_stride, c.k_scale_stride},
+                            {a.v, c.vpool, c.v_scale, a.v_stride, c.v_block_stride, c.v_scale_stride}};
+    QuantParams p{};
+    if (const char* m = plan(c, given, a.slots, a.status_word, a.tokens, a.dtype, false, &p)) return refuse("ps_quant_append", m, err_buf, err_cap);
+    if (a.tokens == 0) return PS_OK;
+    cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e;
+    if (a.dtype == PS_DTYPE_BF16) e = c.codes == PS_CODE_INT8 ? launch_append<__nv_bfloat16, Int8>(p, s) : launch_append<__nv_bfloat16, E4m3>(p, s);
+    else e = c.codes == PS_CODE_INT8 ? launch_append<__half, Int8>(p, s) : launch_append<__half, E4m3>(p, s);
+    if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_quant_append", e);
+    return PS_OK;
+}
+
+extern "C" int32_t ps_quant_read(const ps_quant_read_args* args, void* stream, char* err_buf, int32_t err_cap) {
+    if (err_buf && err_cap > 0) err_buf[0] = 0;
+    if (!args) return refuse("ps_quant_read", "null arguments", err_buf, err_cap);
+    const ps_quant_read_args a = *args;
+    ps_quant_cache c = a.cache;
+    if (!a.k_out) c.kpool = nullptr, c.k_scale = nullptr;
+    if (!a.v_out) c.vpool = nullptr, c.v_scale = nullptr;
+    const Given given[2] = {{a.k_out, c.kpool, c.k_scale, a.k_out_stride, c.k_block_stride, c.k_scale_stride},
+                            {a.v_out, c.vpool, c.v_scale, a.v_out_stride, c.v_block_stride, c.v_scale_stride}};
+    QuantParams p{};
+    if (const char* m = plan(c, given, a.slots, a.status_word, a.tokens, a.dtype, true, &p)) return refuse("ps_quant_read", m, err_buf, err_cap);
+    if (a.tokens == 0) return PS_OK;
+    cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e;
+    if (a.dtype == PS_DTYPE_BF16) e = c.codes == PS_CODE_INT8 ? launch_read<__nv_bfloat16, Int8>(p, s) : launch_read<__nv_bfloat16, E4m3>(p, s);
+    else e = c.codes == PS_CODE_INT8 ? launch_read<__half, Int8>(p, s) : launch_read<__half, E4m3>(p, s);
+    if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_quant_read", e);
+    return PS_OK;
+}

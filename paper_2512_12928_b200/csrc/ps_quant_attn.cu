@@ -1,0 +1,416 @@
+// ps_quant_attn: attention of one new token per row over a paged cache of 8-bit codes with a scale for each block and KV
+// head, K[t] = a_t k_t and V[t] = b_t v_t with whole numbers or 8-bit floats k_t, v_t.
+//
+//   out[b][h] = sum_t p_t b_t v_t / sum_t p_t,   p_t = 2^(s_t - m),   s_t = log2(e) scale a_t (q[b][h] . k_t)
+//
+// with the frame of ps_paged_attn.cuh: the sequence's cut, the walk, segment ends and the join are ps_paged_attn's.
+//
+// Bound: HBM, and next to it the instructions that widen the codes: a token and KV head are half the bytes of a 16-bit
+// cache's and as many products.
+//
+// Products: S^T = K Q^T and O^T = V^T P^T as mma.m16n8k16 in fp16, into which every code goes exactly.  A tile of 32 tokens
+// comes to shared memory as it lies in the pool (cp.async) and is widened between ldmatrix and the product, four codes of a
+// register to two registers.  ldmatrix sees pairs of codes as its elements: a lane gets four neighbouring dims of a token's key, and
+// through the transposing form two neighbouring dims of two tokens' values.  Which dims and tokens a product's rows and
+// columns stand for is free, so what comes together stays together: of keys the four dims are the k places 2c, 2c + 1,
+// 2c + 8, 2c + 9 and the queries are laid out alike; of values row g is dim 2g and row g + 8 dim 2g + 1.
+//
+// Scales: a_t multiplies a score in 32 bits.  b_t goes into the weight, p_t (b_t / r) with r a power of two next to the
+// largest b that the warp has met, so that weights stay within fp16; sums are multiplied by r where a segment ends.  A weight
+// is the sum of two fp16 numbers.  Queries in bf16 are multiplied by a power of two that puts their head's largest
+// magnitude next to 2^13, and the scores by its inverse.
+#include <cuda_fp8.h>
+
+#include "ps_paged_attn.cuh"
+
+namespace {
+
+// Four codes of a register as two pairs of fp16 numbers.
+struct Int8 {
+    static constexpr bool kNeighbours = false;           // keys: pairs are codes 0 and 2, 1 and 3
+    // a byte b with its top bit turned is k + 128; as the low bits of 0x6400 = 1024 that is 1152 + k, exactly
+    static __device__ __forceinline__ uint32_t widen(uint32_t x) {
+        const uint32_t v = (x & 0x00ff00ffu) ^ 0x64806480u, off = 0x64806480u;
+        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&off));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) { values(x, lo, hi); }
+    static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) {
+        lo = widen(x);
+        hi = widen(x >> 8);
+    }
+};
+struct E4m3 {
+    static constexpr bool kNeighbours = true;
+    static __device__ __forceinline__ uint32_t widen(uint32_t x) {      // of the low two codes
+        uint32_t r;
+        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(x));
+        return r;
+    }
+    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) {
+        lo = widen(x);
+        hi = widen(x >> 16);
+    }
+    static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) { keys(__byte_perm(x, 0, 0x3120), lo, hi); }
+};
+
+template <int D>
+struct Ring {
+    static constexpr int kTokens = 32;                       // of a tile
+    static constexpr int kRowBytes = D;
+    static constexpr int kSideBytes = kTokens * kRowBytes;   // keys, then values, then their scales
+    static constexpr int kStageBytes = 2 * kSideBytes + 2 * kTokens * (int)sizeof(float);
+    static constexpr int kStages = D == 128 ? 3 : 6;         // as many bytes on their way
+    static constexpr int kWarpBytes = kStages * kStageBytes;
+};
+
+template <int D, int NT>
+struct QuantState : State<D, NT> {
+    float inv_ref;                             // 1 / r
+};
+
+template <typename T, typename C, int D, int NT>
+struct Worker {
+    using Stages = Ring<D>;
+    using R = Stages;
+    using Type = T;
+    using Softmax = QuantState<D, NT>;
+    using Keys = uint4[2][D / 32];
+    using N = Num<__half>;
+    static constexpr int kDim = D, kColumns = NT;
+    static constexpr int kPieces = D / 16;     // of a token's row, 16 bytes each
+    static constexpr int kRows = 32 / kPieces; // of a warp's copy
+    const AttnParams& p;
+    const int lane, g, c, unit_in_cta, sub;
+    const uint32_t ring;                       // the warp's first stage
+    const uint64_t policy;
+    uint32_t put;                              // this lane's place in a stage: row lane / kPieces and, in place, piece lane % kPieces
+    uint32_t at_piece[kPieces / 2];            // what this lane reads of a stage's half: pieces 2 j + .. of its row
+    uint32_t q[NT][D / 16][2];                 // query head 8 t + g, dims 16 j + 4 c + .. of four
+    float factor[NT][2];                       // of the scores of heads 8 t + 2 c and 8 t + 2 c + 1, with log2(e) scale in it
+    const unsigned char *k_src, *v_src;        // pools at this lane's head and piece
+    const float *k_scale, *v_scale;            // scales of the head
+    const int32_t* table;
+    int32_t id, at;                            // block and place of token `lane`; at = -1: no token
+    bool idle;                                 // the unit does not exist
+    uint32_t masks[R::kStages - 1];            // which tokens of the tiles in the ring are attended, the oldest first
+
+    __device__ __forceinline__ Worker(const AttnParams& pp, uint32_t smem)
+        : p(pp), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), c(threadIdx.x & 3), unit_in_cta((threadIdx.x >> 5) % pp.units),
+          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), masks{} {
+        const int x = lane & 7, up = lane >> 4, mid = lane >> 3 & 1, row = lane / kPieces;
+        put = row * D + (((lane % kPieces) ^ swap(row)) << 4);
+#pragma unroll
+        for (int j = 0; j < kPieces / 2; ++j) at_piece[j] = (x + 8 * mid) * D + (((2 * j + up) ^ swap(x)) << 4);
+    }
+
+    // A token's pieces are exclusive-ored with this, so that eight tokens' same piece lie in different banks.
+    static __device__ __forceinline__ int swap(int token) { return D == 128 ? token & 7 : token >> 1 & 3; }
+
+    __device__ __forceinline__ void load_query(int b, int h0, int n) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const T* src = (const T*)p.q + b * p.q_stride + (int64_t)(h0 + 8 * t + g) * D + 4 * c;
+            uint2 v[D / 16];
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) v[j] = 8 * t + g < n ? *reinterpret_cast<const uint2*>(src + 16 * j) : make_uint2(0u, 0u);
+            float up = 1.f, down = 1.f;
+            if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+                uint32_t most = 0;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) most = __vmaxu2(most, __vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu));
+                most = max(most & 0xffffu, most >> 16);
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                // 2^(13 - e) for a magnitude of 2^e, and its inverse: both are normal numbers
+                const int e = min(max((int)(most >> 7), 14), 253);
+                up = __uint_as_float((uint32_t)(267 - e) << 23);
+                down = __uint_as_float((uint32_t)(e - 13) << 23);
+            }
+            factor[t][0] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c);
+            factor[t][1] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c + 4);
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
+                if (!C::kNeighbours) {
+                    const float x = a.y;
+                    a.y = e.x;
+                    e.x = x;
+                }
+                q[t][j][0] = N::pack(a.x * up, a.y * up);
+                q[t][j][1] = N::pack(e.x * up, e.y * up);
+            }
+        }
+    }
+
+    // The row and chunk of the tiles to come.
+    __device__ __forceinline__ void enter(const Cursor& cur) {
+        int kv, h0, n;
+        unit_heads(p, cur.chunk * p.units + unit_in_cta, &kv, &h0, &n);
+        idle = kv >= p.hkv;
+        if (idle) kv = 0;
+        const int64_t o = (int64_t)kv * D + 16 * (lane % kPieces);
+        k_src = (const unsigned char*)p.kpool + o;
+        v_src = (const unsigned char*)p.vpool + o;
+        k_scale = p.k_scale + kv;
+        v_scale = p.v_scale + kv;
+        table = p.tables + (int64_t)cur.b * p.table_stride;
+        // the unit's queries, into L1: they are loaded when its tiles have come, and then nothing hides their latency
+        if (!idle && lane < n * D / 64) {
+            uint32_t unused;
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + cur.b * p.q_stride + (int64_t)h0 * D + lane * 64));
+        }
+    }
+
+    // Looks the tile's tokens up.
+    __device__ __forceinline__ void load_ids(const Cursor& cur) {
+        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - 5)) + sub) + lane;
+        id = 0;
+        at = -1;
+        if (t < cur.end) {
+            const int32_t blk = block_of(t, p);
+            at = t - blk * p.block_size;
+            id = table[blk];
+        }
+    }
+
+    // Requests the tile that load_ids looked up, into a stage; returns which of its tokens are attended.
+    __device__ __forceinline__ uint32_t copy_tile(int stage) {
+        const bool known = (unsigned)id < (unsigned)p.num_blocks;
+        if (at >= 0 && !known && p.status) *(volatile int32_t*)p.status = kStatusBadId;
+        const bool read = at >= 0 && known && !idle;
+        const uint32_t on = __ballot_sync(0xffffffffu, read);
+        // where the lane's token lies in the pools; what is not read has the address of the first block's first token
+        const int64_t in_block = (int64_t)at * p.hkv * D;
+        const int64_t k_off = read ? id * p.k_block_stride + in_block : 0, v_off = read ? id * p.v_block_stride + in_block : 0;
+        const uint32_t base = ring + stage * R::kStageBytes, dst = base + put;
+#pragma unroll
+        for (int i = 0; i < R::kTokens / kRows; ++i) {
+            const int row = kRows * i + lane / kPieces;
+            const uint32_t bytes = (on >> row & 1) << 4;
+            const int64_t ko = __shfl_sync(0xffffffffu, k_off, row);
+            const int64_t vo = p.k_block_stride == p.v_block_stride ? ko : __shfl_sync(0xffffffffu, v_off, row);
+            const uint32_t to = (D == 128 ? dst ^ (64 * (i & 1)) : dst) + kRows * i * D;     // rows 4 to 7 of 8: piece ^ 4
+            copy16(to, k_src + ko, bytes, policy);
+            copy16(to + R::kSideBytes, v_src + vo, bytes, policy);
+        }
+        // scales, tokens g, 8 + g, 16 + g, 24 + g next to one another
+        const uint32_t scales = base + 2 * R::kSideBytes + 4 * (4 * (lane & 7) + (lane >> 3));
+        copy4(scales, k_scale + (read ? id * p.k_scale_stride : 0), read ? 4 : 0);
+        copy4(scales + 4 * R::kTokens, v_scale + (read ? id * p.v_scale_stride : 0), read ? 4 : 0);
+        return on;
+    }
+    static __device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    }
+    static __device__ __forceinline__ void four(uint32_t src, float (&v)[4]) {
+        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(src) : "memory");
+    }
+
+    // The keys of the tile in a stage: k[u][j] has 32 dims of 16 tokens.
+    __device__ __forceinline__ void read_keys(int stage, Keys& k) const {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) k[u][j] = ldsm(ring + stage * R::kStageBytes + 16 * u * D + at_piece[j]);
+    }
+
+    __device__ __forceinline__ void reset(Softmax& st) const {
+        state_reset(static_cast<State<D, NT>&>(st));
+        st.inv_ref = 1.7014118e38f;            // 2^127: any scale raises the reference, and 0 times it is 0
+    }
+    __device__ __forceinline__ void put_sums(float* row, const Softmax& st, int t, int h) const {
+        const float ref = 1.f / st.inv_ref;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+            *reinterpret_cast<float2*>(row + ((16 * j + 2 * g) ^ (8 * c))) = make_float2(st.acc[t][j][h] * ref, st.acc[t][j][2 + h] * ref);
+    }
+    // Weights are 2^N::kLift times larger; the frame knows of as much as T's products have.
+    __device__ __forceinline__ float reference(const Softmax& st, int t, int h) const { return st.m[t][h] - (N::kLift - Num<T>::kLift); }
+
+    // Attends the tile in a stage; `on`: its tokens that count.
+    __device__ __forceinline__ void attend(int stage, const Keys& k, uint32_t on, Softmax& st) {
+        const uint32_t src = ring + stage * R::kStageBytes;
+        float s[2][NT][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[u][t][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint4 x = k[u][j];       // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
+                uint4 a, b;
+                C::keys(x.x, a.x, a.z);
+                C::keys(x.y, a.y, a.w);
+                C::keys(x.z, b.x, b.z);
+                C::keys(x.w, b.y, b.w);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) N::mma(s[u][t], a, q[t][2 * j][0], q[t][2 * j][1]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][2 * j + 1][0], q[t][2 * j + 1][1]);
+            }
+        uint4 v[2][D / 32];                    // asked for before the softmax
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) v[u][j] = ldsm_t(src + R::kSideBytes + 16 * u * D + at_piece[j]);
+        float ks[4], vs[4];                    // of tokens g, 8 + g, 16 + g, 24 + g
+        four(src + 2 * R::kSideBytes + 16 * g, ks);
+        four(src + 2 * R::kSideBytes + 4 * R::kTokens + 16 * g, vs);
+        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g.  The weights' exponents:
+        float e[2][NT][4], w[4];
+        bool over = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = vs[i] * st.inv_ref;
+            over |= fabsf(w[i]) > 2.f;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float x = s[u][t][i] * (ks[2 * u + (i >> 1)] * factor[t][i & 1]);
+                    x = on >> (16 * u + g + 4 * (i & 2)) & 1 ? x : -CUDART_INF_F;
+                    s[u][t][i] = x;
+                    e[u][t][i] = x - st.m[t][i & 1];
+                    over |= e[u][t][i] > N::kSlack;
+                }
+        if (__any_sync(0xffffffffu, over)) {
+            // the reference of the values' scales: the power of two below the largest, or the present one
+            float top = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vs[2]), fabsf(vs[3])));
+            const uint32_t ex = min(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 252u);
+            const float inv = fminf(st.inv_ref, __uint_as_float((254u - ex) << 23));
+            const float sink = inv / st.inv_ref;
+            st.inv_ref = inv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = vs[i] * inv;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float mx = fmaxf(fmaxf(s[0][t][h], s[0][t][2 + h]), fmaxf(s[1][t][h], s[1][t][2 + h]));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    mx = fmaxf(mx, st.m[t][h]);
+                    const float alpha = ex2(st.m[t][h] - mx);
+                    st.m[t][h] = mx;
+                    st.l[t][h] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        st.acc[t][j][h] *= alpha * sink;
+                        st.acc[t][j][2 + h] *= alpha * sink;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        e[u][t][h] = s[u][t][h] - mx;
+                        e[u][t][2 + h] = s[u][t][2 + h] - mx;
+                    }
+                }
+        }
+        // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 (of 16) of head 8t + g, as the sum of two fp16 numbers
+        uint32_t pt[2][NT][2], rest[2][NT][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[u][t][i] = ex2(e[u][t][i] + N::kLift);
+                st.l[t][0] += e[u][t][0] + e[u][t][2];
+                st.l[t][1] += e[u][t][1] + e[u][t][3];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float x = e[u][t][2 * i] * w[2 * u + i], y = e[u][t][2 * i + 1] * w[2 * u + i];
+                    const uint32_t pair = N::pack(x, y);
+                    const float2 f = N::unpack(pair);
+                    pt[u][t][i] = transpose8(pair);
+                    rest[u][t][i] = transpose8(N::pack(x - f.x, y - f.y));
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const uint4 x = v[u][j];       // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
+                uint4 a, b;
+                C::values(x.x, a.x, a.y);
+                C::values(x.y, a.z, a.w);
+                C::values(x.z, b.x, b.y);
+                C::values(x.w, b.z, b.w);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    N::mma(st.acc[t][2 * j], a, pt[u][t][0], pt[u][t][1]);
+                    N::mma(st.acc[t][2 * j], a, rest[u][t][0], rest[u][t][1]);
+                    N::mma(st.acc[t][2 * j + 1], b, pt[u][t][0], pt[u][t][1]);
+                    N::mma(st.acc[t][2 * j + 1], b, rest[u][t][0], rest[u][t][1]);
+                }
+            }
+    }
+};
+
+// ---------------------------------------------------------------------------------------------------- host
+
+int32_t tile_of(int32_t) { return Ring<128>::kTokens; }
+
+template <typename T, typename C, int D>
+cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
+    return launch_attn<Worker<T, C, D, 1>, Worker<T, C, D, 2>>(p, y, may_cut, s);
+}
+template <typename T, typename C>
+cudaError_t launch(const AttnParams& p, int32_t dim, const Layout& y, bool may_cut, cudaStream_t s) {
+    return dim == 128 ? launch<T, C, 128>(p, y, may_cut, s) : launch<T, C, 64>(p, y, may_cut, s);
+}
+cudaError_t sms_here(int* sms) {
+    using B = __nv_bfloat16;
+    using H = __half;
+    return device_sms<Worker<B, Int8, 64, 1>, Worker<B, Int8, 64, 2>, Worker<B, Int8, 128, 1>, Worker<B, Int8, 128, 2>,
+                      Worker<B, E4m3, 64, 1>, Worker<B, E4m3, 64, 2>, Worker<B, E4m3, 128, 1>, Worker<B, E4m3, 128, 2>,
+                      Worker<H, Int8, 64, 1>, Worker<H, Int8, 64, 2>, Worker<H, Int8, 128, 1>, Worker<H, Int8, 128, 2>,
+                      Worker<H, E4m3, 64, 1>, Worker<H, E4m3, 64, 2>, Worker<H, E4m3, 128, 1>, Worker<H, E4m3, 128, 2>>(sms);
+}
+
+}  // namespace
+
+extern "C" int32_t ps_quant_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes) {
+    return workspace_of(num_kv_heads, num_q_heads, head_dim, tile_of(head_dim), sms_here, bytes);
+}
+
+extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap) {
+    const Refusal refuse{"ps_quant_attn", err_buf, err_cap};
+    if (!args) return refuse("null arguments");
+    const ps_quant_attn_args a = *args;
+    const ps_quant_cache& c = a.cache;
+    if (c.codes != PS_CODE_INT8 && c.codes != PS_CODE_E4M3) return refuse("codes must be PS_CODE_INT8 or PS_CODE_E4M3");
+    AttnParams p{};
+    Layout y{};
+    bool may_cut = false;
+    auto pools = [&]() -> const char* {
+        if (!c.kpool || !c.vpool || !c.k_scale || !c.v_scale) return "null pointer";
+        const int64_t block = (int64_t)c.block_size * c.num_kv_heads * c.head_dim;
+        if (c.num_gpu_blocks > 1 && (c.k_block_stride < block || c.v_block_stride < block || c.k_scale_stride < c.num_kv_heads ||
+                                     c.v_scale_stride < c.num_kv_heads))
+            return "a pool's block stride is smaller than a block, or its scales' than a block's";
+        if (!on_bytes(c.k_scale, 0, 4) || !on_bytes(c.v_scale, 0, 4)) return "scales must be on 4-byte boundaries";
+        if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
+        return nullptr;
+    };
+    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tile_of, sms_here, pools, refuse, &p, &y, &may_cut);
+    if (rc != PS_OK || a.batch == 0) return rc;
+    p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
+    p.k_block_stride = c.k_block_stride, p.v_block_stride = c.v_block_stride;
+    p.k_scale_stride = c.k_scale_stride, p.v_scale_stride = c.v_scale_stride;
+    cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e;
+    if (a.dtype == PS_DTYPE_BF16)
+        e = c.codes == PS_CODE_INT8 ? launch<__nv_bfloat16, Int8>(p, c.head_dim, y, may_cut, s) : launch<__nv_bfloat16, E4m3>(p, c.head_dim, y, may_cut, s);
+    else
+        e = c.codes == PS_CODE_INT8 ? launch<__half, Int8>(p, c.head_dim, y, may_cut, s) : launch<__half, E4m3>(p, c.head_dim, y, may_cut, s);
+    if (e != cudaSuccess) return ps::launch_fail(err_buf, err_cap, "ps_quant_attn", e);
+    return PS_OK;
+}

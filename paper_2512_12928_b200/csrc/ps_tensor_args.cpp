@@ -1,5 +1,5 @@
-// Python module _ps_tensor_args: takes the torch tensors of ps_build_slots, ps_rope_append and ps_paged_attn apart,
-// checks them and calls the library.
+// Python module _ps_tensor_args: takes the torch tensors of ps_build_slots, ps_rope_append, ps_paged_attn and of the
+// ps_quant_ calls apart, checks them and calls the library.
 //
 // The calls are made for every layer of every step and a small one takes 3 us on the device.  Asking 8 to 12 tensors
 // for type, device, shape, strides and address took 5 to 8 us in Python; here it takes less than the launch.
@@ -29,6 +29,10 @@ decltype(&ps_build_slots) g_build_slots = nullptr;
 decltype(&ps_rope_append) g_rope_append = nullptr;
 decltype(&ps_paged_attn) g_paged_attn = nullptr;
 decltype(&ps_paged_attn_workspace) g_workspace = nullptr;
+decltype(&ps_quant_append) g_quant_append = nullptr;
+decltype(&ps_quant_read) g_quant_read = nullptr;
+decltype(&ps_quant_attn) g_quant_attn = nullptr;
+decltype(&ps_quant_attn_workspace) g_quant_workspace = nullptr;
 
 PyObject* answer(int32_t rc, const std::string& text) { return Py_BuildValue("(is)", (int)rc, text.c_str()); }
 
@@ -263,6 +267,49 @@ PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// What ps_paged_attn and ps_quant_attn take alike: q, out, block_tables, ctx_lens, lse, window, scale, status_word, workspace.
+template <typename Args, typename Fn, typename Workspace>
+PyObject* attend(Args& p, PyObject* const* a, const at::Tensor& q, const at::Tensor& out, const at::Tensor& tables, const at::Device& dev, Fn fn,
+                 Workspace workspace_of, int32_t hkv, int32_t dim, const char* name) {
+    const ScalarType dt = q.scalar_type();
+    p.q_stride = outer_stride("q", q, q.sizes(), dt, dev);
+    p.out_stride = outer_stride("out", out, q.sizes(), dt, dev);
+    p.q = q.const_data_ptr();
+    p.out = out.mutable_data_ptr();
+    p.lse = vec<float>("lse", a[4], ScalarType::Float, (int64_t)p.batch * p.num_q_heads, dev);
+    p.block_tables = vec<const int32_t>("block_tables", a[2], ScalarType::Int, (int64_t)p.batch * p.table_stride, dev);
+    p.ctx_lens = vec<const int32_t>("ctx_lens", a[3], ScalarType::Int, p.batch, dev);
+    p.window = int_arg("window", a[5]);
+    if (a[6] != Py_None) {
+        const double s = PyFloat_AsDouble(a[6]);
+        if (PyErr_Occurred() || (float)s == 0.f) {
+            PyErr_Clear();
+            throw BadArg{"scale: need a factor that is not 0"};
+        }
+        p.scale = (float)s;
+    }
+    p.status_word = vec<int32_t>("status_word", a[7], ScalarType::Int, 1, dev);
+    at::Tensor scratch;   // kept until the launches are enqueued; then the allocator's order on the stream protects it
+    if (a[8] == Py_None) {
+        int64_t need = 0;
+        {
+            std::optional<c10::cuda::CUDAGuard> guard;
+            if (c10::cuda::current_device() != dev.index()) guard.emplace(dev);
+            const int32_t rc = workspace_of(hkv, p.num_q_heads, dim, &need);
+            if (rc == PS_ERR_CUDA) return answer(rc, std::string(name) + ": device");
+        }
+        if (need > 0) {   // else the shape is refused below
+            scratch = at::empty({need}, at::TensorOptions().dtype(at::kByte).device(dev));
+            p.workspace = scratch.mutable_data_ptr();
+            p.workspace_bytes = need;
+        }
+    } else {
+        p.workspace = vec<void>("workspace", a[8], ScalarType::Byte, 0, dev);
+        p.workspace_bytes = THPVariable_Unpack(a[8]).numel();
+    }
+    return enqueue(fn, p, dev);
+}
+
 // kpool, vpool, q, out, block_tables, ctx_lens, lse, window, scale, status_word, workspace
 PyObject* py_paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call("ps_paged_attn", n, 11, [&]() {
@@ -286,53 +333,118 @@ PyObject* py_paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t shape[4] = {kpool.size(0), kpool.size(1), kpool.size(2), q.size(2)};
         p.k_block_stride = outer_stride("kpool", kpool, shape, dt, dev);
         p.v_block_stride = outer_stride("vpool", vpool, shape, dt, dev);
-        p.q_stride = outer_stride("q", q, q.sizes(), dt, dev);
-        p.out_stride = outer_stride("out", out, q.sizes(), dt, dev);
         p.kpool = kpool.const_data_ptr();
         p.vpool = vpool.const_data_ptr();
-        p.q = q.const_data_ptr();
-        p.out = out.mutable_data_ptr();
-        p.lse = vec<float>("lse", a[6], ScalarType::Float, (int64_t)p.batch * p.num_q_heads, dev);
-        p.block_tables = vec<const int32_t>("block_tables", a[4], ScalarType::Int, (int64_t)p.batch * p.table_stride, dev);
-        p.ctx_lens = vec<const int32_t>("ctx_lens", a[5], ScalarType::Int, p.batch, dev);
-        p.window = int_arg("window", a[7]);
-        if (a[8] != Py_None) {
-            const double s = PyFloat_AsDouble(a[8]);
-            if (PyErr_Occurred() || (float)s == 0.f) {
-                PyErr_Clear();
-                throw BadArg{"scale: need a factor that is not 0"};
-            }
-            p.scale = (float)s;
-        }
-        p.status_word = vec<int32_t>("status_word", a[9], ScalarType::Int, 1, dev);
-        at::Tensor scratch;   // kept until the launches are enqueued; then the allocator's order on the stream protects it
-        if (a[10] == Py_None) {
-            int64_t need = 0;
-            {
-                std::optional<c10::cuda::CUDAGuard> guard;
-                if (c10::cuda::current_device() != dev.index()) guard.emplace(dev);
-                const int32_t rc = g_workspace(p.num_kv_heads, p.num_q_heads, p.head_dim, &need);
-                if (rc == PS_ERR_CUDA) return answer(rc, "ps_paged_attn: device");
-            }
-            if (need > 0) {   // else the shape is refused below
-                scratch = at::empty({need}, at::TensorOptions().dtype(at::kByte).device(dev));
-                p.workspace = scratch.mutable_data_ptr();
-                p.workspace_bytes = need;
-            }
-        } else {
-            p.workspace = vec<void>("workspace", a[10], ScalarType::Byte, 0, dev);
-            p.workspace_bytes = THPVariable_Unpack(a[10]).numel();
-        }
-        return enqueue(g_paged_attn, p, dev);
+        return attend(p, a + 2, q, out, tables, dev, g_paged_attn, g_workspace, p.num_kv_heads, p.head_dim, "ps_paged_attn");
+    });
+}
+
+// The 8-bit cache of kpool, vpool, k_scale, v_scale; heads and dim come from the first pool.
+ps_quant_cache quant_cache(PyObject* const* a, bool k, bool v, const at::Device& dev) {
+    ps_quant_cache c{};
+    const at::Tensor* pools[2] = {k ? &must("kpool", a[0]) : nullptr, v ? &must("vpool", a[1]) : nullptr};
+    if (!k && !v) throw BadArg{"need keys or values"};
+    const at::Tensor& first = on_device("pools: need [blocks][block_size][heads][dim]", k ? *pools[0] : *pools[1], 4);
+    if (first.scalar_type() == ScalarType::Char) c.codes = PS_CODE_INT8;
+    else if (first.scalar_type() == ScalarType::Float8_e4m3fn) c.codes = PS_CODE_E4M3;
+    else throw BadArg{"pools: need int8 or float8_e4m3fn, " + describe(first)};
+    const int64_t shape[4] = {first.size(0), first.size(1), first.size(2), first.size(3)}, scales[2] = {shape[0], shape[2]};
+    c.num_gpu_blocks = int_size("blocks", shape[0]);
+    c.block_size = int_size("block_size", shape[1]);
+    c.num_kv_heads = int_size("heads", shape[2]);
+    c.head_dim = int_size("dim", shape[3]);
+    if (k) {
+        const at::Tensor& s = must("k_scale", a[2]);
+        c.k_block_stride = outer_stride("kpool", *pools[0], shape, first.scalar_type(), dev);
+        c.k_scale_stride = outer_stride("k_scale", s, scales, ScalarType::Float, dev);
+        c.kpool = pools[0]->mutable_data_ptr();
+        c.k_scale = (float*)s.mutable_data_ptr();
+    }
+    if (v) {
+        const at::Tensor& s = must("v_scale", a[3]);
+        c.v_block_stride = outer_stride("vpool", *pools[1], shape, first.scalar_type(), dev);
+        c.v_scale_stride = outer_stride("v_scale", s, scales, ScalarType::Float, dev);
+        c.vpool = pools[1]->mutable_data_ptr();
+        c.v_scale = (float*)s.mutable_data_ptr();
+    }
+    return c;
+}
+
+// Rows [tokens][heads][dim] of keys or values: their address; null for None.
+const at::Tensor* quant_rows(const char* name, PyObject* o, const ps_quant_cache& c, ScalarType dt, int64_t tokens, const at::Device& dev,
+                             int64_t* stride) {
+    const at::Tensor* t = tensor(name, o);
+    if (t) *stride = outer_stride(name, *t, {tokens, c.num_kv_heads, c.head_dim}, dt, dev);
+    return t;
+}
+
+// k, v, kpool, vpool, k_scale, v_scale, slots, status_word
+PyObject* py_quant_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call("ps_quant_append", n, 8, [&]() {
+        const at::Tensor *k = tensor("k", a[0]), *v = tensor("v", a[1]);
+        if ((!k && (a[2] != Py_None || a[4] != Py_None)) || (!v && (a[3] != Py_None || a[5] != Py_None)))
+            throw BadArg{"keys and values need rows, codes and scales, or none of them"};
+        if (!k && !v) throw BadArg{"need k or v"};
+        const at::Tensor& ref = on_device("k and v: need [tokens][heads][dim]", k ? *k : *v, 3);
+        const at::Device dev = ref.device();
+        ps_quant_append_args p{};
+        p.dtype = dtype_code(ref);
+        p.tokens = int_size("tokens", ref.size(0));
+        p.cache = quant_cache(a + 2, k != nullptr, v != nullptr, dev);
+        if (quant_rows("k", a[0], p.cache, ref.scalar_type(), ref.size(0), dev, &p.k_stride)) p.k = k->const_data_ptr();
+        if (quant_rows("v", a[1], p.cache, ref.scalar_type(), ref.size(0), dev, &p.v_stride)) p.v = v->const_data_ptr();
+        must("slots", a[6]);
+        p.slots = vec<const int64_t>("slots", a[6], ScalarType::Long, p.tokens, dev);
+        p.status_word = vec<int32_t>("status_word", a[7], ScalarType::Int, 1, dev);
+        return enqueue(g_quant_append, p, dev);
+    });
+}
+
+// kpool, vpool, k_scale, v_scale, slots, k_out, v_out, status_word
+PyObject* py_quant_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call("ps_quant_read", n, 8, [&]() {
+        const at::Tensor *k = tensor("k_out", a[5]), *v = tensor("v_out", a[6]);
+        if (!k && !v) throw BadArg{"need k_out or v_out"};
+        const at::Tensor& ref = on_device("k_out and v_out: need [tokens][heads][dim]", k ? *k : *v, 3);
+        const at::Device dev = ref.device();
+        ps_quant_read_args p{};
+        p.dtype = dtype_code(ref);
+        p.tokens = int_size("tokens", ref.size(0));
+        p.cache = quant_cache(a, k != nullptr, v != nullptr, dev);
+        if (quant_rows("k_out", a[5], p.cache, ref.scalar_type(), ref.size(0), dev, &p.k_out_stride)) p.k_out = k->mutable_data_ptr();
+        if (quant_rows("v_out", a[6], p.cache, ref.scalar_type(), ref.size(0), dev, &p.v_out_stride)) p.v_out = v->mutable_data_ptr();
+        must("slots", a[4]);
+        p.slots = vec<const int64_t>("slots", a[4], ScalarType::Long, p.tokens, dev);
+        p.status_word = vec<int32_t>("status_word", a[7], ScalarType::Int, 1, dev);
+        return enqueue(g_quant_read, p, dev);
+    });
+}
+
+// kpool, vpool, k_scale, v_scale, q, out, block_tables, ctx_lens, lse, window, scale, status_word, workspace
+PyObject* py_quant_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call("ps_quant_attn", n, 13, [&]() {
+        const at::Tensor& q = on_device("q: need [batch][heads][dim]", must("q", a[4]), 3);
+        const at::Tensor& out = must("out", a[5]);
+        const at::Tensor& tables = on_device("block_tables: need [batch][stride]", must("block_tables", a[6]), 2);
+        must("ctx_lens", a[7]);
+        const at::Device dev = q.device();
+        ps_quant_attn_args p{};
+        p.dtype = dtype_code(q);
+        p.batch = int_size("batch", q.size(0));
+        p.num_q_heads = int_size("heads", q.size(1));
+        p.cache = quant_cache(a, true, true, dev);
+        if (q.size(2) != p.cache.head_dim) throw BadArg{"q: need the pools' dim, " + describe(q)};
+        p.table_stride = int_size("block_tables", tables.size(1));
+        return attend(p, a + 4, q, out, tables, dev, g_quant_attn, g_quant_workspace, p.cache.num_kv_heads, p.cache.head_dim, "ps_quant_attn");
     });
 }
 
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* p[4];
-    for (int i = 0; i < 4; ++i) {
-        p[i] = n == 4 ? PyLong_AsVoidPtr(a[i]) : nullptr;
+    void* p[8];
+    for (int i = 0; i < 8; ++i) {
+        p[i] = n == 8 ? PyLong_AsVoidPtr(a[i]) : nullptr;
         if (!p[i]) {
-            if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind: need four addresses");
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind: need eight addresses");
             return nullptr;
         }
     }
@@ -340,6 +452,10 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_rope_append = (decltype(g_rope_append))p[1];
     g_paged_attn = (decltype(g_paged_attn))p[2];
     g_workspace = (decltype(g_workspace))p[3];
+    g_quant_append = (decltype(g_quant_append))p[4];
+    g_quant_read = (decltype(g_quant_read))p[5];
+    g_quant_attn = (decltype(g_quant_attn))p[6];
+    g_quant_workspace = (decltype(g_quant_workspace))p[7];
     Py_RETURN_NONE;
 }
 
@@ -348,6 +464,9 @@ PyMethodDef methods[] = {{"bind", PS_FAST(py_bind), nullptr},
                          {"build_slots", PS_FAST(py_build_slots), nullptr},
                          {"rope_append", PS_FAST(py_rope_append), nullptr},
                          {"paged_attn", PS_FAST(py_paged_attn), nullptr},
+                         {"quant_append", PS_FAST(py_quant_append), nullptr},
+                         {"quant_read", PS_FAST(py_quant_read), nullptr},
+                         {"quant_attn", PS_FAST(py_quant_attn), nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ps_tensor_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
