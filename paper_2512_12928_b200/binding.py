@@ -36,7 +36,8 @@ EXPORTS = [
     "ps_decode_attn_static", "ps_copy_budget", "ps_offload_progress", "ps_host_blocks", "ps_host_segment",
     "ps_select_victims", "ps_copy_condition", "ps_order_queue", "ps_estimate_batch", "ps_resume_cost",
     "ps_reload_fence", "ps_offload_sweep", "ps_step_ruled", "ps_step_host", "ps_inject_status", "ps_hbm_probe", "ps_reload_backlog",
-    "ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace",
+    "ps_build_slots", "ps_rope_append", "ps_paged_attn", "ps_paged_attn_workspace", "ps_quant_append", "ps_quant_read",
+    "ps_quant_attn", "ps_quant_attn_workspace",
 ]
 
 
