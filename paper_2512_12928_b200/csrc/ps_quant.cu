@@ -69,17 +69,24 @@ template <> struct Bits<2> { using type = uint16_t; };
 template <> struct Bits<4> { using type = uint32_t; };
 template <> struct Bits<8> { using type = uint2; };
 template <> struct Bits<16> { using type = uint4; };
+template <> struct Bits<32> { using type = uint4; };     // in two halves, or by one access of 32 bytes
 template <int Bytes>
-struct alignas(Bytes < 4 ? 4 : Bytes) Vec {
+struct alignas(Bytes < 4 ? 4 : Bytes > 16 ? 16 : Bytes) Vec {
     uint32_t w[(Bytes + 3) / 4];             // a value of one or two bytes is the low ones of a word
     __device__ __forceinline__ void load(const void* p) {
         using B = typename Bits<Bytes>::type;
-        if constexpr (Bytes < 4) w[0] = *static_cast<const B*>(p);
+        if constexpr (Bytes == 32)
+            asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+        else if constexpr (Bytes < 4) w[0] = *static_cast<const B*>(p);
         else *reinterpret_cast<B*>(w) = *static_cast<const B*>(p);
     }
     __device__ __forceinline__ void store(void* p) const {
         using B = typename Bits<Bytes>::type;
-        if constexpr (Bytes < 4) *static_cast<B*>(p) = (B)w[0];
+        if constexpr (Bytes == 32)
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                         "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        else if constexpr (Bytes < 4) *static_cast<B*>(p) = (B)w[0];
         else *static_cast<B*>(p) = *reinterpret_cast<const B*>(w);
     }
 };
@@ -107,18 +114,33 @@ struct QuantParams {
 
 // ------------------------------------------------------------------------------------------------ append
 
-// Tokens [t0, t0 + n) of a CTA, one a lane.  A segment is a run of tokens that go to one block; the CTA in whose range it
-// begins has the whole of it.  Every warp finds the segments for itself: no barrier, and nothing in shared memory.
+// A segment is a run of tokens that go to one block.  A warp has one head of keys or values, and the segments that begin
+// among the CTA's n tokens, which it finds for itself: no barrier, and nothing in shared memory.
 template <typename T, typename C, int W>
 __global__ void __launch_bounds__(kThreads)
 quant_append_kernel(const __grid_constant__ QuantParams p) {
-    constexpr int kHold = 8;                 // vectors of a lane that stay in registers between maximum and rounding
+    constexpr int kHold = W == 16 ? 4 : 8;   // vectors of a lane that stay in registers between maximum and rounding
     const int lane = threadIdx.x & 31;
-    const int nwarps = (kThreads / 32) * gridDim.y, me = (kThreads / 32) * blockIdx.y + (threadIdx.x >> 5);
+    const int unit = (kThreads / 32) * blockIdx.y + (threadIdx.x >> 5);
+    if (unit >= p.sides * p.hkv) return;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int head = unit < p.hkv ? unit : unit - p.hkv;
+    const Side& side = p.side[unit < p.hkv ? 0 : 1];
+    // The vectors of a segment, rows first: this lane has every 32nd.
+    const int row_vecs = p.dim / W;
+    const int row_step = 32 / row_vecs, piece_step = 32 - row_step * row_vecs;
+    const int row0 = lane / row_vecs, piece0 = lane - row0 * row_vecs;
+    auto next = [&](int& row, int& piece) {
+        row += row_step;
+        piece += piece_step;
+        if (piece >= row_vecs) {
+            piece -= row_vecs;
+            ++row;
+        }
+    };
+    const int64_t place_bytes = (int64_t)p.hkv * p.dim;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
-    const int n = min(p.tok_per_cta, p.tokens - t0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     auto look_up = [&](int32_t t, bool report) -> int64_t {      // the token's slot, or -1
         if (t < 0 || t >= p.tokens) return -1;
         const int64_t s = p.slots[t];
@@ -126,58 +148,35 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         if (report && p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
         return -1;
     };
-    const int64_t slot = look_up(lane < n ? t0 + lane : -1, true);
+    // 32 tokens from t0 on, one a lane: what begins among the first n mostly ends there too
+    const int64_t slot = look_up(t0 + lane, lane < p.tok_per_cta);
     const int64_t block = slot < 0 ? -1 : block_of(slot, p.block_size, p.block_magic);
+    const int32_t my_place = (int32_t)(slot - block * p.block_size);
     int64_t before = __shfl_up_sync(0xffffffffu, block, 1);
     if (lane == 0) {
         const int64_t s = look_up(t0 - 1, false);
         before = s < 0 ? -1 : block_of(s, p.block_size, p.block_magic);
     }
-    uint32_t starts = __ballot_sync(0xffffffffu, block >= 0 && block != before);
-    const int units = p.sides * p.hkv;       // of a segment
-    const int row_vecs = p.dim / W;
-    for (int u = me, skip = 0; starts; u += nwarps) {
-        while (starts && u - skip >= units) {
-            starts &= starts - 1;
-            skip += units;
-        }
-        if (!starts) break;
+    uint32_t starts = __ballot_sync(0xffffffffu, lane < p.tok_per_cta && block >= 0 && block != before);
+    for (; starts; starts &= starts - 1) {
         const int first = __ffs(starts) - 1;
-        const int head = (u - skip) % p.hkv;
-        const Side& side = p.side[(u - skip) / p.hkv];
         const int64_t blk = __shfl_sync(0xffffffffu, block, first);
         const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
         int len = (other ? __ffs(other) - 1 : 32) - first;
         const int64_t block_begin = blk * p.block_size;
-        bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && slot == block_begin);
-        if (first + len >= n) {              // it may go on behind the CTA's tokens
-            len = n - first;
-            for (;;) {
-                const int64_t s = look_up(t0 + first + len + lane, false);
-                const bool in = s >= block_begin && s - block_begin < p.block_size;
-                const uint32_t out = __ballot_sync(0xffffffffu, !in);
-                const int more = out ? __ffs(out) - 1 : 32;
-                begun |= __any_sync(0xffffffffu, lane < more && s == block_begin);
-                len += more;
-                if (more < 32) break;
-            }
+        bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && my_place == 0);
+        while (first + len >= 32) {          // it goes on
+            const int64_t s = look_up(t0 + first + len + lane, false);
+            const uint32_t out = __ballot_sync(0xffffffffu, s < block_begin || s - block_begin >= p.block_size);
+            const int more = out ? __ffs(out) - 1 : 32;
+            begun |= __any_sync(0xffffffffu, lane < more && s == block_begin);
+            len += more;
+            if (more < 32) break;
         }
         const T* src = (const T*)side.rows + (t0 + first) * side.row_stride + (int64_t)head * p.dim;
         unsigned char* pool = side.pool + blk * side.block_stride + (int64_t)head * p.dim;
-        const int64_t place_bytes = (int64_t)p.hkv * p.dim;
         float* scale_at = side.scale + blk * side.scale_stride + head;
         const float old = begun ? 0.f : *scale_at;
-        // The unit's vectors, rows first: this lane has every 32nd.
-        const int row_step = 32 / row_vecs, piece_step = 32 % row_vecs;
-        const int row0 = lane / row_vecs, piece0 = lane - row0 * row_vecs;
-        auto next = [&](int& row, int& piece) {
-            row += row_step;
-            piece += piece_step;
-            if (piece >= row_vecs) {
-                piece -= row_vecs;
-                ++row;
-            }
-        };
         Vec<2 * W> held[kHold];
         uint32_t most = 0;                   // of both halves of a word
         auto meet = [&](const Vec<2 * W>& x) {
@@ -190,11 +189,11 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             if (row < len) held[i].load(src + row * side.row_stride + piece * W);
             next(row, piece);
         }
-        row = row0, piece = piece0;
+        int row2 = row0, piece2 = piece0;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) {
-            if (row < len) meet(held[i]);
-            next(row, piece);
+            if (row2 < len) meet(held[i]);
+            next(row2, piece2);
         }
         while (row < len) {
             Vec<2 * W> x;
@@ -223,7 +222,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             }
             __syncwarp();                    // the new tokens' codes come on top
         }
-        auto put = [&](const Vec<2 * W>& x, int row, int piece) {
+        auto put = [&](const Vec<2 * W>& x, int32_t place, int piece) {
             Vec<W> y;
 #pragma unroll
             for (int i = 0; i < (W + 1) / 2; ++i) {
@@ -232,18 +231,25 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
                 if (i & 1) y.w[i / 2] |= two << 16;
                 else y.w[i / 2] = two;
             }
-            y.store(pool + (p.slots[t0 + first + row] - block_begin) * place_bytes + piece * W);
+            y.store(pool + place * place_bytes + piece * W);
+        };
+        auto place_of = [&](int row) {       // of a row that is not among the lanes' tokens
+            return (int32_t)(p.slots[t0 + first + row] - block_begin);
         };
         row = row0, piece = piece0;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) {
-            if (row < len) put(held[i], row, piece);
+            int32_t place = __shfl_sync(0xffffffffu, my_place, first + row);
+            if (row < len) {
+                if (first + row >= 32) place = place_of(row);
+                put(held[i], place, piece);
+            }
             next(row, piece);
         }
         while (row < len) {
             Vec<2 * W> x;
             x.load(src + row * side.row_stride + piece * W);
-            put(x, row, piece);
+            put(x, place_of(row), piece);
             next(row, piece);
         }
         if (lane == 0) *scale_at = now;
@@ -252,34 +258,54 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
 
 // -------------------------------------------------------------------------------------------------- read
 
+// A thread has one vector of a token, the same of every `at_once`-th token, and kAhead tokens on their way.
+constexpr int kAhead = 4;
 template <typename T, typename C, int W>
 __global__ void __launch_bounds__(kThreads)
 quant_read_kernel(const __grid_constant__ QuantParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int side_vecs = p.hkv * p.dim / W, per = p.sides * side_vecs;     // vectors of a token
+    const int lanes = min(per, kThreads), at_once = kThreads / lanes;
+    const int k0 = threadIdx.x / lanes, row_vecs = p.dim / W;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     const int n = min(p.tok_per_cta, p.tokens - t0);
-    const int side_vecs = p.hkv * p.dim / W, per = p.sides * side_vecs;     // vectors of a token
-    for (int i = threadIdx.x; i < n * per; i += kThreads) {
-        const int k = i / per, j = i - k * per, which = j / side_vecs, vec = j - which * side_vecs;
-        const Side& side = p.side[which];
-        const int64_t slot = p.slots[t0 + k];
-        if (slot < 0) continue;
-        if (slot >= p.num_slots) {
-            if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
-            continue;
-        }
-        const int64_t blk = block_of(slot, p.block_size, p.block_magic);
-        Vec<W> x;
-        x.load(side.pool + blk * side.block_stride + (slot - blk * p.block_size) * ((int64_t)p.hkv * p.dim) + vec * W);
-        const float scale = side.scale[blk * side.scale_stride + vec * W / p.dim];
-        Vec<2 * W> y;
+    if (k0 >= at_once) return;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int j = threadIdx.x - k0 * lanes; j < per; j += lanes) {
+        const int vec = j < side_vecs ? j : j - side_vecs;
+        const Side& side = p.side[j < side_vecs ? 0 : 1];
+        const unsigned char* pool = side.pool + vec * W;
+        const float* scales = side.scale + vec / row_vecs;
+        T* rows = (T*)side.rows + t0 * side.row_stride + vec * W;
+        for (int k = k0; k < n; k += kAhead * at_once) {
+            int64_t slot[kAhead];
+            Vec<W> x[kAhead];
+            float scale[kAhead];
 #pragma unroll
-        for (int h = 0; h < (W + 1) / 2; ++h) {
-            const float2 v = C::unpack(x.w[h / 2] >> (16 * (h & 1)));
-            y.w[h] = Num<T>::pack(v.x * scale, v.y * scale);
+            for (int i = 0; i < kAhead; ++i) slot[i] = k + i * at_once < n ? p.slots[t0 + k + i * at_once] : -1;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (slot[i] >= p.num_slots) {
+                    if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+                    slot[i] = -1;
+                }
+                if (slot[i] < 0) continue;
+                const int64_t blk = block_of(slot[i], p.block_size, p.block_magic);
+                x[i].load(pool + blk * side.block_stride + (slot[i] - blk * p.block_size) * ((int64_t)p.hkv * p.dim));
+                scale[i] = scales[blk * side.scale_stride];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (slot[i] < 0) continue;
+                Vec<2 * W> y;
+#pragma unroll
+                for (int h = 0; h < (W + 1) / 2; ++h) {
+                    const float2 v = C::unpack(x[i].w[h / 2] >> (16 * (h & 1)));
+                    y.w[h] = Num<T>::pack(v.x * scale[i], v.y * scale[i]);
+                }
+                y.store(rows + (k + i * at_once) * side.row_stride);
+            }
         }
-        y.store((T*)side.rows + (t0 + k) * side.row_stride + vec * W);
     }
 }
 
@@ -338,8 +364,7 @@ bool fits(const QuantParams& p, int w) {
     bool ok = p.dim % w == 0;
     for (int i = 0; i < p.sides; ++i) {
         const Side& s = p.side[i];
-        const int rows = std::min(2 * w, 16);
-        ok = ok && reinterpret_cast<uintptr_t>(s.rows) % rows == 0 && 2 * s.row_stride % rows == 0 &&
+        ok = ok && reinterpret_cast<uintptr_t>(s.rows) % (2 * w) == 0 && s.row_stride % w == 0 &&
              reinterpret_cast<uintptr_t>(s.pool) % w == 0 && s.block_stride % w == 0;
     }
     return ok;
@@ -347,18 +372,24 @@ bool fits(const QuantParams& p, int w) {
 
 template <typename T, typename C>
 cudaError_t launch_append(QuantParams p, cudaStream_t s) {
+    const int warps = kThreads / 32, units = p.sides * p.hkv;
     p.tok_per_cta = 1;
-    const int warps = kThreads / 32;
-    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((p.sides * p.hkv + warps - 1) / warps));
-    return fits(p, 8) ? ps::launch_dependent(quant_append_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
-                      : ps::launch_dependent(quant_append_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
+    while (2 * p.tok_per_cta <= std::min(p.block_size, 16) && (int64_t)p.tokens / (2 * p.tok_per_cta) * units >= 148 * 16) p.tok_per_cta *= 2;
+    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((units + warps - 1) / warps));
+    return fits(p, 16)  ? ps::launch_dependent(quant_append_kernel<T, C, 16>, grid, dim3(kThreads), 0, s, p)
+           : fits(p, 8) ? ps::launch_dependent(quant_append_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
+                        : ps::launch_dependent(quant_append_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
 }
 template <typename T, typename C>
 cudaError_t launch_read(QuantParams p, cudaStream_t s) {
-    p.tok_per_cta = 1;
+    const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1;
+    const int at_once = std::max(1, kThreads / std::min(kThreads, p.sides * p.hkv * p.dim / w));
+    p.tok_per_cta = at_once;
+    while (p.tok_per_cta < kAhead * at_once && p.tokens / (2 * p.tok_per_cta) >= 148 * 4) p.tok_per_cta *= 2;
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
-    return fits(p, 8) ? ps::launch_dependent(quant_read_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
-                      : ps::launch_dependent(quant_read_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
+    return w == 16  ? ps::launch_dependent(quant_read_kernel<T, C, 16>, grid, dim3(kThreads), 0, s, p)
+           : w == 8 ? ps::launch_dependent(quant_read_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
+                    : ps::launch_dependent(quant_read_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
 }
 
 int32_t refuse(const char* name, const char* text, char* buf, int32_t cap) {
