@@ -44,21 +44,30 @@ template <> struct Num<__half> {
 
 struct Int8 {
     static constexpr float kTop = 127.f;
-    // Two codes of x times r.  The exact product is rounded to a whole number by the addition: 1.5 2^23 + n has n as its low
-    // bits.
-    static __device__ __forceinline__ uint32_t pair(float a, float b, float r) {
-        return __byte_perm(__float_as_uint(fmaf(a, r, 12582912.f)), __float_as_uint(fmaf(b, r, 12582912.f)), 0x0040) & 0xffff;
+    // Codes of four values times r.  The exact product is rounded to a whole number by the addition: 1.5 2^23 + n has n as its
+    // low bits.
+    static __device__ __forceinline__ uint32_t pack(const float4& v, float r) {
+        auto one = [&](float x) { return __float_as_uint(fmaf(x, r, 12582912.f)); };
+        return __byte_perm(__byte_perm(one(v.x), one(v.y), 0x0040), __byte_perm(one(v.z), one(v.w), 0x0040), 0x5410);
     }
-    static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2((float)(int8_t)v, (float)(int8_t)(v >> 8)); }
+    // Four codes.  A byte with its top bit turned is n + 128; as the low bits of 2^23 that is 2^23 + 128 + n, exactly.
+    static __device__ __forceinline__ float4 unpack(uint32_t v) {
+        const uint32_t x = v ^ 0x80808080u;
+        auto one = [&](uint32_t select) { return __uint_as_float(__byte_perm(x, 0x4b000000u, select)) - 8388736.f; };
+        return make_float4(one(0x7540), one(0x7541), one(0x7542), one(0x7543));
+    }
 };
 struct E4m3 {
     static constexpr float kTop = 448.f;
-    static __device__ __forceinline__ uint32_t pair(float a, float b, float r) {
-        return __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(a, r), __fmul_rn(b, r)), __NV_SATFINITE, __NV_E4M3);
+    static __device__ __forceinline__ uint32_t pack(const float4& v, float r) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(v.x, r), __fmul_rn(v.y, r)), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(v.z, r), __fmul_rn(v.w, r)), __NV_SATFINITE, __NV_E4M3);
+        return __byte_perm(lo, hi, 0x5410);
     }
-    static __device__ __forceinline__ float2 unpack(uint32_t v) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3);
-        return __half22float2(__half2(h));
+    static __device__ __forceinline__ float4 unpack(uint32_t v) {
+        const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3)));
+        const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v >> 16), __NV_E4M3)));
+        return make_float4(a.x, a.y, b.x, b.y);
     }
 };
 
@@ -91,10 +100,9 @@ struct alignas(Bytes < 4 ? 4 : Bytes > 16 ? 16 : Bytes) Vec {
     }
 };
 
-// t / size for 0 <= t < 2^32 is umulhi of magic = 2^64 / size rounded up; slots may be longer
-__device__ __forceinline__ int64_t block_of(int64_t slot, int32_t size, uint64_t magic) {
-    if (size == 1) return slot;
-    return slot >> 32 ? slot / size : (int64_t)__umul64hi((uint64_t)slot, magic);
+// slot / size: magic is 2^64 / size rounded up, which is exact where slot * size < 2^64
+__device__ __forceinline__ int64_t block_of(int64_t slot, uint64_t magic) {
+    return magic == 0 ? slot : (int64_t)__umul64hi((uint64_t)slot, magic);     // 0: blocks of one token
 }
 
 struct Side {                     // keys or values
@@ -116,8 +124,8 @@ struct QuantParams {
 
 // A segment is a run of tokens that go to one block.  A warp has one head of keys or values, and the segments that begin
 // among the CTA's n tokens, which it finds for itself: no barrier, and nothing in shared memory.
-template <typename T, typename C, int W>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, typename C, int W, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas)
 quant_append_kernel(const __grid_constant__ QuantParams p) {
     constexpr int kHold = W == 16 ? 4 : 8;   // vectors of a lane that stay in registers between maximum and rounding
     const int lane = threadIdx.x & 31;
@@ -141,39 +149,34 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
     const int64_t place_bytes = (int64_t)p.hkv * p.dim;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    auto look_up = [&](int32_t t, bool report) -> int64_t {      // the token's slot, or -1
-        if (t < 0 || t >= p.tokens) return -1;
-        const int64_t s = p.slots[t];
-        if (s < p.num_slots) return s < 0 ? -1 : s;
-        if (report && p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
-        return -1;
-    };
-    // 32 tokens from t0 on, one a lane: what begins among the first n mostly ends there too
-    const int64_t slot = look_up(t0 + lane, lane < p.tok_per_cta);
-    const int64_t block = slot < 0 ? -1 : block_of(slot, p.block_size, p.block_magic);
-    const int32_t my_place = (int32_t)(slot - block * p.block_size);
-    int64_t before = __shfl_up_sync(0xffffffffu, block, 1);
-    if (lane == 0) {
-        const int64_t s = look_up(t0 - 1, false);
-        before = s < 0 ? -1 : block_of(s, p.block_size, p.block_magic);
+    // 32 tokens from the one before on, one a lane: what begins among the CTA's mostly ends there too
+    const int32_t t = t0 - 1 + lane;
+    int64_t slot = t >= 0 && t < p.tokens ? p.slots[t] : -1;
+    if (slot >= p.num_slots) {
+        if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+        slot = -1;
     }
-    uint32_t starts = __ballot_sync(0xffffffffu, lane < p.tok_per_cta && block >= 0 && block != before);
+    const int32_t block = slot < 0 ? -1 : (int32_t)block_of(slot, p.block_magic);
+    const int32_t my_place = (int32_t)(slot - (int64_t)block * p.block_size);
+    const int32_t before = __shfl_up_sync(0xffffffffu, block, 1);
+    uint32_t starts = __ballot_sync(0xffffffffu, lane > 0 && lane <= p.tok_per_cta && block >= 0 && block != before);
     for (; starts; starts &= starts - 1) {
         const int first = __ffs(starts) - 1;
-        const int64_t blk = __shfl_sync(0xffffffffu, block, first);
+        const int32_t blk = __shfl_sync(0xffffffffu, block, first);
         const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
         int len = (other ? __ffs(other) - 1 : 32) - first;
-        const int64_t block_begin = blk * p.block_size;
+        const int64_t block_begin = (int64_t)blk * p.block_size;
         bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && my_place == 0);
         while (first + len >= 32) {          // it goes on
-            const int64_t s = look_up(t0 + first + len + lane, false);
+            const int32_t u = t0 - 1 + first + len + lane;
+            const int64_t s = u < p.tokens ? p.slots[u] : -1;
             const uint32_t out = __ballot_sync(0xffffffffu, s < block_begin || s - block_begin >= p.block_size);
             const int more = out ? __ffs(out) - 1 : 32;
             begun |= __any_sync(0xffffffffu, lane < more && s == block_begin);
             len += more;
             if (more < 32) break;
         }
-        const T* src = (const T*)side.rows + (t0 + first) * side.row_stride + (int64_t)head * p.dim;
+        const T* src = (const T*)side.rows + (t0 - 1 + first) * side.row_stride + (int64_t)head * p.dim;
         unsigned char* pool = side.pool + blk * side.block_stride + (int64_t)head * p.dim;
         float* scale_at = side.scale + blk * side.scale_stride + head;
         const float old = begun ? 0.f : *scale_at;
@@ -181,7 +184,8 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         uint32_t most = 0;                   // of both halves of a word
         auto meet = [&](const Vec<2 * W>& x) {
 #pragma unroll
-            for (int i = 0; i < (W + 1) / 2; ++i) most = __vmaxu2(most, x.w[i] & 0x7fff7fffu);
+            for (int i = 0; i < W / 2; i += 2) most = __vimax3_u16x2(most, x.w[i] & 0x7fff7fffu, x.w[i + 1] & 0x7fff7fffu);
+            if (W == 1) most = max(most, x.w[0] & 0x7fffu);
         };
         int row = row0, piece = piece0;
 #pragma unroll
@@ -213,10 +217,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
                 unsigned char* at = pool + q * place_bytes + c * W;
                 x.load(at);
 #pragma unroll
-                for (int i = 0; i < (W + 3) / 4; ++i) {
-                    const float2 lo = C::unpack(x.w[i]), hi = C::unpack(x.w[i] >> 16);
-                    x.w[i] = C::pair(lo.x, lo.y, f) | C::pair(hi.x, hi.y, f) << 16;
-                }
+                for (int i = 0; i < (W + 3) / 4; ++i) x.w[i] = C::pack(C::unpack(x.w[i]), f);
                 x.store(at);
                 next(q, c);
             }
@@ -225,16 +226,14 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         auto put = [&](const Vec<2 * W>& x, int32_t place, int piece) {
             Vec<W> y;
 #pragma unroll
-            for (int i = 0; i < (W + 1) / 2; ++i) {
-                const float2 v = Num<T>::unpack(x.w[i]);
-                const uint32_t two = C::pair(v.x, v.y, r);
-                if (i & 1) y.w[i / 2] |= two << 16;
-                else y.w[i / 2] = two;
+            for (int i = 0; i < (W + 3) / 4; ++i) {
+                const float2 lo = Num<T>::unpack(x.w[2 * i]), hi = W > 1 ? Num<T>::unpack(x.w[2 * i + (W > 1)]) : lo;
+                y.w[i] = C::pack(make_float4(lo.x, lo.y, hi.x, hi.y), r);
             }
             y.store(pool + place * place_bytes + piece * W);
         };
         auto place_of = [&](int row) {       // of a row that is not among the lanes' tokens
-            return (int32_t)(p.slots[t0 + first + row] - block_begin);
+            return (int32_t)(p.slots[t0 - 1 + first + row] - block_begin);
         };
         row = row0, piece = piece0;
 #pragma unroll
@@ -258,50 +257,65 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
 
 // -------------------------------------------------------------------------------------------------- read
 
-// A thread has one vector of a token, the same of every `at_once`-th token, and kAhead tokens on their way.
-constexpr int kAhead = 4;
+// Where a token lies: found once for a CTA's tokens and kept in shared memory.
+struct Place {
+    int64_t codes, scales;        // offsets in the pool and its scales; codes < 0: nothing of it is written
+};
+
+// A thread has one vector of a token, the same of every `at_once`-th token.
+constexpr int kAhead = 4;        // tokens that it has on their way at once
+constexpr int kMaxTokens = 256;   // of a CTA
 template <typename T, typename C, int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 quant_read_kernel(const __grid_constant__ QuantParams p) {
+    __shared__ Place place[2][kMaxTokens];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int side_vecs = p.hkv * p.dim / W, per = p.sides * side_vecs;     // vectors of a token
     const int lanes = min(per, kThreads), at_once = kThreads / lanes;
     const int k0 = threadIdx.x / lanes, row_vecs = p.dim / W;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     const int n = min(p.tok_per_cta, p.tokens - t0);
-    if (k0 >= at_once) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (threadIdx.x < n) {
+        const int64_t slot = p.slots[t0 + threadIdx.x];
+        const bool live = slot >= 0 && slot < p.num_slots;
+        if (slot >= p.num_slots && p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
+        const int64_t blk = block_of(live ? slot : 0, p.block_magic), in_block = (slot - blk * p.block_size) * ((int64_t)p.hkv * p.dim);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const Side& s = p.side[i < p.sides ? i : 0];
+            place[i][threadIdx.x] = {live ? blk * s.block_stride + in_block : -1, blk * s.scale_stride};
+        }
+    }
+    __syncthreads();
+    if (k0 >= at_once) return;
     for (int j = threadIdx.x - k0 * lanes; j < per; j += lanes) {
-        const int vec = j < side_vecs ? j : j - side_vecs;
-        const Side& side = p.side[j < side_vecs ? 0 : 1];
+        const int which = j < side_vecs ? 0 : 1, vec = j - which * side_vecs;
+        const Side& side = p.side[which];
         const unsigned char* pool = side.pool + vec * W;
         const float* scales = side.scale + vec / row_vecs;
         T* rows = (T*)side.rows + t0 * side.row_stride + vec * W;
         for (int k = k0; k < n; k += kAhead * at_once) {
-            int64_t slot[kAhead];
+            bool live[kAhead];
             Vec<W> x[kAhead];
             float scale[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) slot[i] = k + i * at_once < n ? p.slots[t0 + k + i * at_once] : -1;
-#pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (slot[i] >= p.num_slots) {
-                    if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
-                    slot[i] = -1;
-                }
-                if (slot[i] < 0) continue;
-                const int64_t blk = block_of(slot[i], p.block_size, p.block_magic);
-                x[i].load(pool + blk * side.block_stride + (slot[i] - blk * p.block_size) * ((int64_t)p.hkv * p.dim));
-                scale[i] = scales[blk * side.scale_stride];
+                const Place at = place[which][min(k + i * at_once, n - 1)];
+                live[i] = k + i * at_once < n && at.codes >= 0;
+                if (!live[i]) continue;
+                x[i].load(pool + at.codes);
+                scale[i] = scales[at.scales];
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (slot[i] < 0) continue;
+                if (!live[i]) continue;
                 Vec<2 * W> y;
 #pragma unroll
-                for (int h = 0; h < (W + 1) / 2; ++h) {
-                    const float2 v = C::unpack(x[i].w[h / 2] >> (16 * (h & 1)));
-                    y.w[h] = Num<T>::pack(v.x * scale[i], v.y * scale[i]);
+                for (int h = 0; h < (W + 3) / 4; ++h) {
+                    const float4 v = C::unpack(x[i].w[h]);
+                    y.w[2 * h] = Num<T>::pack(v.x * scale[i], v.y * scale[i]);
+                    if (W > 2) y.w[2 * h + (W > 2)] = Num<T>::pack(v.z * scale[i], v.w * scale[i]);
                 }
                 y.store(rows + (k + i * at_once) * side.row_stride);
             }
@@ -344,6 +358,8 @@ const char* plan(const ps_quant_cache& c, const Given (&given)[2], const int64_t
     }
     if (p.sides == 0) return "neither keys nor values are given";
     if (!slots) return "null pointer";
+    // slots are divided by block_size as block_of says
+    if ((double)c.num_gpu_blocks * c.block_size * c.block_size >= 18e18) return "num_gpu_blocks * block_size^2 must be below 1.8e19";
     // whatever is written is apart from everything else
     auto count = [&](int kind) -> int64_t { return kind == 0 ? tokens : c.num_gpu_blocks; };
     for (int i = 0; i < 3 * p.sides; ++i)
@@ -372,20 +388,25 @@ bool fits(const QuantParams& p, int w) {
 
 template <typename T, typename C>
 cudaError_t launch_append(QuantParams p, cudaStream_t s) {
+    // Few tokens: one a CTA, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins one, while that
+    // leaves every SM 16 warps.  A CTA then has 80 registers a thread, and three fit an SM, instead of two of up to 127 (9700
+    // tokens of 8 heads of 128 in bf16 14.6 instead of 15.5 us); what spills for it costs a few tokens 0.1 to 0.3 us.
     const int warps = kThreads / 32, units = p.sides * p.hkv;
     p.tok_per_cta = 1;
     while (2 * p.tok_per_cta <= std::min(p.block_size, 16) && (int64_t)p.tokens / (2 * p.tok_per_cta) * units >= 148 * 16) p.tok_per_cta *= 2;
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((units + warps - 1) / warps));
-    return fits(p, 16)  ? ps::launch_dependent(quant_append_kernel<T, C, 16>, grid, dim3(kThreads), 0, s, p)
-           : fits(p, 8) ? ps::launch_dependent(quant_append_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
-                        : ps::launch_dependent(quant_append_kernel<T, C, 1>, grid, dim3(kThreads), 0, s, p);
+    auto launch = [&](auto kernel) { return ps::launch_dependent(kernel, grid, dim3(kThreads), 0, s, p); };
+    const bool few = p.tok_per_cta == 1;
+    if (fits(p, 16)) return few ? launch(quant_append_kernel<T, C, 16, 2>) : launch(quant_append_kernel<T, C, 16, 3>);
+    if (fits(p, 8)) return few ? launch(quant_append_kernel<T, C, 8, 2>) : launch(quant_append_kernel<T, C, 8, 3>);
+    return launch(quant_append_kernel<T, C, 1, 2>);
 }
 template <typename T, typename C>
 cudaError_t launch_read(QuantParams p, cudaStream_t s) {
     const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1;
-    const int at_once = std::max(1, kThreads / std::min(kThreads, p.sides * p.hkv * p.dim / w));
-    p.tok_per_cta = at_once;
-    while (p.tok_per_cta < kAhead * at_once && p.tokens / (2 * p.tok_per_cta) >= 148 * 4) p.tok_per_cta *= 2;
+    const int at_once = kThreads / std::min(kThreads, p.sides * p.hkv * p.dim / w);
+    p.tok_per_cta = std::min(at_once, kMaxTokens);
+    while (2 * p.tok_per_cta <= 8 && p.tokens / (2 * p.tok_per_cta) >= 148 * 2) p.tok_per_cta *= 2;
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta));
     return w == 16  ? ps::launch_dependent(quant_read_kernel<T, C, 16>, grid, dim3(kThreads), 0, s, p)
            : w == 8 ? ps::launch_dependent(quant_read_kernel<T, C, 8>, grid, dim3(kThreads), 0, s, p)
