@@ -585,8 +585,9 @@ typedef struct ps_quant_attn_args {
 
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
  * scale.  Codes are exact in the products; a query's values are to within 2^-38 of the largest of their head.  Scores,
- * softmax and sums are in 32 bits; for the product with V a softmax weight times its token's value scale is the sum of two
- * fp16 numbers next to the largest value scale that the row has met (a scale 2^-20 of that one still leaves 13 bits).
+ * softmax and sums are in 32 bits; for the product with V a softmax weight times its token's value scale is an fp16
+ * number next to the largest value scale that the row has met (of a scale 2^-20 of that one weights still have 2 bits), and for
+ * results in fp16 the sum of two.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
 

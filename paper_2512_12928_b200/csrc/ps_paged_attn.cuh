@@ -54,6 +54,7 @@ struct AttnParams {
     int64_t k_block_stride, v_block_stride, q_stride, out_stride;
     const float *k_scale, *v_scale;  // of an 8-bit cache: [block][KV head]
     int64_t k_scale_stride, v_scale_stride;
+    bool far;                        // a pool's blocks lie more than 2^36 bytes apart
     int64_t room;        // tokens a table row has room for
     uint64_t block_magic;
     int32_t batch, table_stride, num_blocks, block_size, window;

@@ -78,6 +78,7 @@ struct Worker {
     using Keys = uint4[2][D / 32];
     using N = Num<__half>;
     static constexpr int kDim = D, kColumns = NT;
+    static constexpr bool kRest = std::is_same_v<T, __half>;
     static constexpr int kPieces = D / 16;     // of a token's row, 16 bytes each
     static constexpr int kRows = 32 / kPieces; // of a warp's copy
     const AttnParams& p;
@@ -180,25 +181,37 @@ struct Worker {
         if (at >= 0 && !known && p.status) *(volatile int32_t*)p.status = kStatusBadId;
         const bool read = at >= 0 && known && !idle;
         const uint32_t on = __ballot_sync(0xffffffffu, read);
-        // where the lane's token lies in the pools; what is not read has the address of the first block's first token
-        const int64_t in_block = (int64_t)at * p.hkv * D;
-        const int64_t k_off = read ? id * p.k_block_stride + in_block : 0, v_off = read ? id * p.v_block_stride + in_block : 0;
+        // where the lane's token lies in the pools, in steps of 16 bytes; what is not read has the address of the first
+        // block's first token
+        const uint64_t in_block = (uint64_t)((uint32_t)at * (uint64_t)(uint32_t)(p.hkv * (D / 16)));
+        const uint64_t k_off = read ? (uint32_t)id * (uint64_t)(p.k_block_stride >> 4) + in_block : 0;
+        const uint64_t v_off = read ? (uint32_t)id * (uint64_t)(p.v_block_stride >> 4) + in_block : 0;
         const uint32_t base = ring + stage * R::kStageBytes, dst = base + put;
-#pragma unroll
-        for (int i = 0; i < R::kTokens / kRows; ++i) {
-            const int row = kRows * i + lane / kPieces;
-            const uint32_t bytes = (on >> row & 1) << 4;
-            const int64_t ko = __shfl_sync(0xffffffffu, k_off, row);
-            const int64_t vo = p.k_block_stride == p.v_block_stride ? ko : __shfl_sync(0xffffffffu, v_off, row);
-            const uint32_t to = (D == 128 ? dst ^ (64 * (i & 1)) : dst) + kRows * i * D;     // rows 4 to 7 of 8: piece ^ 4
-            copy16(to, k_src + ko, bytes, policy);
-            copy16(to + R::kSideBytes, v_src + vo, bytes, policy);
-        }
+        if (on == 0xffffffffu) copy_rows<true>(k_off, v_off, on, dst);       // as nearly always
+        else copy_rows<false>(k_off, v_off, on, dst);
         // scales, tokens g, 8 + g, 16 + g, 24 + g next to one another
         const uint32_t scales = base + 2 * R::kSideBytes + 4 * (4 * (lane & 7) + (lane >> 3));
         copy4(scales, k_scale + (read ? id * p.k_scale_stride : 0), read ? 4 : 0);
         copy4(scales + 4 * R::kTokens, v_scale + (read ? id * p.v_scale_stride : 0), read ? 4 : 0);
         return on;
+    }
+    template <bool kAll>
+    __device__ __forceinline__ void copy_rows(uint64_t k_off, uint64_t v_off, uint32_t on, uint32_t dst) {
+        const bool one_stride = p.k_block_stride == p.v_block_stride;
+#pragma unroll
+        for (int i = 0; i < R::kTokens / kRows; ++i) {
+            const int row = kRows * i + lane / kPieces;
+            const uint32_t bytes = kAll ? 16u : (on >> row & 1) << 4;
+            const uint32_t to = (D == 128 ? dst ^ (64 * (i & 1)) : dst) + kRows * i * D;     // rows 4 to 7 of 8: piece ^ 4
+            auto from = [&](const unsigned char* src, uint64_t off) {
+                const unsigned char* a = src + 16 * (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)off, row);
+                if (p.far) a += (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)(off >> 32), row) << 36;
+                return a;
+            };
+            const unsigned char* k = from(k_src, k_off);
+            copy16(to, k, bytes, policy);
+            copy16(to + R::kSideBytes, one_stride ? v_src + (k - k_src) : from(v_src, v_off), bytes, policy);
+        }
     }
     static __device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -225,8 +238,8 @@ struct Worker {
         for (int j = 0; j < D / 16; ++j)
             *reinterpret_cast<float2*>(row + ((16 * j + 2 * g) ^ (8 * c))) = make_float2(st.acc[t][j][h] * ref, st.acc[t][j][2 + h] * ref);
     }
-    // Weights are 2^N::kLift times larger; the frame knows of as much as T's products have.
-    __device__ __forceinline__ float reference(const Softmax& st, int t, int h) const { return st.m[t][h] - (N::kLift - Num<T>::kLift); }
+    // st.m is the reference less N::kLift, so that weights are 2^N::kLift times larger; the frame knows of 2^Num<T>::kLift.
+    __device__ __forceinline__ float reference(const Softmax& st, int t, int h) const { return st.m[t][h] + Num<T>::kLift; }
 
     // Attends the tile in a stage; `on`: its tokens that count.
     __device__ __forceinline__ void attend(int stage, const Keys& k, uint32_t on, Softmax& st) {
@@ -261,13 +274,27 @@ struct Worker {
         float ks[4], vs[4];                    // of tokens g, 8 + g, 16 + g, 24 + g
         four(src + 2 * R::kSideBytes + 16 * g, ks);
         four(src + 2 * R::kSideBytes + 4 * R::kTokens + 16 * g, vs);
-        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g.  The weights' exponents:
-        float e[2][NT][4], w[4];
-        bool over = false;
+        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u][t][i] *= ks[2 * u + (i >> 1)] * factor[t][i & 1];
+        if (on != 0xffffffffu)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        if (!(on >> (16 * u + g + 4 * (i & 2)) & 1)) s[u][t][i] = -CUDART_INF_F;
+        // The weights' exponents, and the largest of them: max does not see a NaN, which then gives a NaN weight
+        float e[2][NT][4], w[4], top = 0.f, most = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = vs[i] * st.inv_ref;
-            over |= fabsf(w[i]) > 2.f;
+            most = fmaxf(most, fabsf(w[i]));
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -275,16 +302,14 @@ struct Worker {
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    float x = s[u][t][i] * (ks[2 * u + (i >> 1)] * factor[t][i & 1]);
-                    x = on >> (16 * u + g + 4 * (i & 2)) & 1 ? x : -CUDART_INF_F;
-                    s[u][t][i] = x;
-                    e[u][t][i] = x - st.m[t][i & 1];
-                    over |= e[u][t][i] > N::kSlack;
+                    e[u][t][i] = s[u][t][i] - st.m[t][i & 1];
+                    top = fmaxf(top, e[u][t][i]);
                 }
+        const bool over = top > N::kSlack + N::kLift || most > 2.f;
         if (__any_sync(0xffffffffu, over)) {
             // the reference of the values' scales: the power of two below the largest, or the present one
-            float top = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vs[2]), fabsf(vs[3])));
-            const uint32_t ex = min(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 252u);
+            const float largest = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vs[2]), fabsf(vs[3])));
+            const uint32_t ex = min(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)) >> 23, 252u);
             const float inv = fminf(st.inv_ref, __uint_as_float((254u - ex) << 23));
             const float sink = inv / st.inv_ref;
             st.inv_ref = inv;
@@ -298,7 +323,7 @@ struct Worker {
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    mx = fmaxf(mx, st.m[t][h]);
+                    mx = fmaxf(mx - N::kLift, st.m[t][h]);
                     const float alpha = ex2(st.m[t][h] - mx);
                     st.m[t][h] = mx;
                     st.l[t][h] *= alpha;
@@ -321,16 +346,18 @@ struct Worker {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[u][t][i] = ex2(e[u][t][i] + N::kLift);
+                for (int i = 0; i < 4; ++i) e[u][t][i] = ex2(e[u][t][i]);
                 st.l[t][0] += e[u][t][0] + e[u][t][2];
                 st.l[t][1] += e[u][t][1] + e[u][t][3];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const float x = e[u][t][2 * i] * w[2 * u + i], y = e[u][t][2 * i + 1] * w[2 * u + i];
                     const uint32_t pair = N::pack(x, y);
-                    const float2 f = N::unpack(pair);
                     pt[u][t][i] = transpose8(pair);
-                    rest[u][t][i] = transpose8(N::pack(x - f.x, y - f.y));
+                    if (kRest) {
+                        const float2 f = N::unpack(pair);
+                        rest[u][t][i] = transpose8(N::pack(x - f.x, y - f.y));
+                    }
                 }
             }
 #pragma unroll
@@ -346,9 +373,11 @@ struct Worker {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     N::mma(st.acc[t][2 * j], a, pt[u][t][0], pt[u][t][1]);
-                    N::mma(st.acc[t][2 * j], a, rest[u][t][0], rest[u][t][1]);
                     N::mma(st.acc[t][2 * j + 1], b, pt[u][t][0], pt[u][t][1]);
-                    N::mma(st.acc[t][2 * j + 1], b, rest[u][t][0], rest[u][t][1]);
+                    if (kRest) {
+                        N::mma(st.acc[t][2 * j], a, rest[u][t][0], rest[u][t][1]);
+                        N::mma(st.acc[t][2 * j + 1], b, rest[u][t][0], rest[u][t][1]);
+                    }
                 }
             }
     }
@@ -405,6 +434,7 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
     p.k_block_stride = c.k_block_stride, p.v_block_stride = c.v_block_stride;
     p.k_scale_stride = c.k_scale_stride, p.v_scale_stride = c.v_scale_stride;
+    p.far = (double)c.num_gpu_blocks * (double)std::max(c.k_block_stride, c.v_block_stride) >= 68719476736.0;   // 2^36
     cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e;
     if (a.dtype == PS_DTYPE_BF16)

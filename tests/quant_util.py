@@ -89,13 +89,13 @@ def make_cache(shape, dt, g, spread=0.5):
 def quant_attn_want(kpool, vpool, ks, vs, q, tables, ctx, window=0, scale=None):
     """attn_want over the values that the cache stands for.
 
-    Over that, a weight times its value scale is a product in 32 bits (2^-24) and the sum of two fp16 numbers, off by 2^-22 of
-    itself, or by 2^-25 where fp16 has no smaller steps; largest weights are 2^8 or more and refer to the power of two below
+    Over that, a weight times its value scale is a product in 32 bits (2^-24), held as one fp16 number for results in bf16 (off by
+    2^-11 of itself) and as the sum of two for results in fp16 (2^-22), or by 2^-25 where fp16 has no smaller steps; largest weights are 2^8 or more and refer to the power of two below
     the row's largest value scale, so that the latter is 2^-33 of a token's largest possible value, times the tokens.  A score
     is multiplied by two factors (2^-23, within what attn_want gives it)."""
     K = kpool.double() * ks.double()[:, None, :, None]
     V = vpool.double() * vs.double()[:, None, :, None]
-    out, lse, tol, tol_lse = attn_want(K, V, q, tables, ctx, window, scale, weight_error=2.0 ** -21)
+    out, lse, tol, tol_lse = attn_want(K, V, q, tables, ctx, window, scale, weight_error=2.0 ** -21 + (2.0 ** -11 if q.dtype == torch.bfloat16 else 0.0))
     nb, S = kpool.shape[:2]
     G = q.shape[1] // kpool.shape[2]
     for b, n in enumerate(ctx):
