@@ -27,32 +27,37 @@ namespace {
 
 // Four codes of a register as two pairs of fp16 numbers.
 struct Int8 {
-    static constexpr bool kNeighbours = false;           // keys: pairs are codes 0 and 2, 1 and 3
+    static constexpr bool kDigits = true;                // keys are multiplied as they are
     // a byte b with its top bit turned is k + 128; as the low bits of 0x6400 = 1024 that is 1152 + k, exactly
     static __device__ __forceinline__ uint32_t widen(uint32_t x) {
         const uint32_t v = (x & 0x00ff00ffu) ^ 0x64806480u, off = 0x64806480u;
         const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&off));
         return *reinterpret_cast<const uint32_t*>(&r);
     }
-    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) { values(x, lo, hi); }
-    static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) {
+    static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) {      // codes 0 and 2, 1 and 3
         lo = widen(x);
         hi = widen(x >> 8);
     }
 };
 struct E4m3 {
-    static constexpr bool kNeighbours = true;
+    static constexpr bool kDigits = false;
     static __device__ __forceinline__ uint32_t widen(uint32_t x) {      // of the low two codes
         uint32_t r;
         asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(x));
         return r;
     }
-    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) {
+    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) {        // codes 0 and 1, 2 and 3
         lo = widen(x);
         hi = widen(x >> 16);
     }
     static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) { keys(__byte_perm(x, 0, 0x3120), lo, hi); }
 };
+
+__device__ __forceinline__ void mma_s8(int32_t (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
 
 template <int D>
 struct Ring {
@@ -87,7 +92,9 @@ struct Worker {
     const uint64_t policy;
     uint32_t put;                              // this lane's place in a stage: row lane / kPieces and, in place, piece lane % kPieces
     uint32_t at_piece[kPieces / 2];            // what this lane reads of a stage's half: pieces 2 j + .. of its row
-    uint32_t q[NT][D / 16][2];                 // query head 8 t + g, dims 16 j + 4 c + .. of four
+    // query head 8 t + g, dims 32 j + 4 c + .. of four and dims 32 j + 16 + 4 c + .. of four: two fp16 numbers a register, or
+    // a digit of all four, digit by digit
+    uint32_t q[NT][D / 32][C::kDigits ? 6 : 4];
     float factor[NT][2];                       // of the scores of heads 8 t + 2 c and 8 t + 2 c + 1, with log2(e) scale in it
     const unsigned char *k_src, *v_src;        // pools at this lane's head and piece
     const float *k_scale, *v_scale;            // scales of the head
@@ -109,6 +116,7 @@ struct Worker {
     static __device__ __forceinline__ int swap(int token) { return D == 128 ? token & 7 : token >> 1 & 3; }
 
     __device__ __forceinline__ void load_query(int b, int h0, int n) {
+        constexpr bool kScaled = C::kDigits || std::is_same_v<T, __nv_bfloat16>;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const T* src = (const T*)p.q + b * p.q_stride + (int64_t)(h0 + 8 * t + g) * D + 4 * c;
@@ -116,30 +124,42 @@ struct Worker {
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) v[j] = 8 * t + g < n ? *reinterpret_cast<const uint2*>(src + 16 * j) : make_uint2(0u, 0u);
             float up = 1.f, down = 1.f;
-            if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            if constexpr (kScaled) {
                 uint32_t most = 0;
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) most = __vmaxu2(most, __vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu));
+                for (int j = 0; j < D / 16; ++j) most = __vimax3_u16x2(most, v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu);
                 most = max(most & 0xffffu, most >> 16);
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                // 2^(13 - e) for a magnitude of 2^e, and its inverse: both are normal numbers
-                const int e = min(max((int)(most >> 7), 14), 253);
-                up = __uint_as_float((uint32_t)(267 - e) << 23);
-                down = __uint_as_float((uint32_t)(e - 13) << 23);
+                // 2^(top - e) for a magnitude of 2^e, and its inverse: both are normal numbers
+                constexpr int kTop = C::kDigits ? 21 : 13;
+                const uint32_t bits = __float_as_uint(Num<T>::unpack(most).x);
+                const int e = min(max((int)(bits >> 23), kTop + 1), 254);
+                up = __uint_as_float((uint32_t)(254 + kTop - e) << 23);
+                down = __uint_as_float((uint32_t)(e - kTop) << 23);
+                if (C::kDigits && bits >= 0x7f800000u) down = CUDART_NAN_F;      // whole numbers know neither infinity nor NaN
             }
             factor[t][0] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c);
             factor[t][1] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c + 4);
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
-                float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
-                if (!C::kNeighbours) {
-                    const float x = a.y;
-                    a.y = e.x;
-                    e.x = x;
+                const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
+                uint32_t* to = q[t][j / 2];
+                if constexpr (C::kDigits) {
+                    // x up as a whole number n, |n| <= 2^22: its digits d, n = d0 + 2^8 d1 + 2^16 d2, from -128 to 127, are the bytes
+                    // of n + 0x808080 with their top bits turned
+                    auto digits = [&](float x) {
+                        return (__float_as_uint(fmaf(x, up, 12582912.f)) - 0x4b400000u + 0x00808080u) ^ 0x00808080u;
+                    };
+                    const uint32_t n0 = digits(a.x), n1 = digits(a.y), n2 = digits(e.x), n3 = digits(e.y);
+                    const uint32_t lo = __byte_perm(n0, n1, 0x5140), lo2 = __byte_perm(n2, n3, 0x5140);      // bytes 0 and 1 of two
+                    to[j % 2] = __byte_perm(lo, lo2, 0x5410);
+                    to[2 + j % 2] = __byte_perm(lo, lo2, 0x7632);
+                    to[4 + j % 2] = __byte_perm(__byte_perm(n0, n1, 0x0062), __byte_perm(n2, n3, 0x0062), 0x5410);
+                } else {
+                    to[2 * (j % 2)] = N::pack(a.x * up, a.y * up);
+                    to[2 * (j % 2) + 1] = N::pack(e.x * up, e.y * up);
                 }
-                q[t][j][0] = N::pack(a.x * up, a.y * up);
-                q[t][j][1] = N::pack(e.x * up, e.y * up);
             }
         }
     }
@@ -245,27 +265,57 @@ struct Worker {
     __device__ __forceinline__ void attend(int stage, const Keys& k, uint32_t on, Softmax& st) {
         const uint32_t src = ring + stage * R::kStageBytes;
         float s[2][NT][4];
+        if constexpr (C::kDigits) {
+            // Products of each digit, in whole numbers below 2^21: from 1.5 2^23's bits on, so that they are floats
+            int32_t n[3][2][NT][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int d = 0; d < 3; ++d)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[u][t][i] = 0.f;
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j)
+                        for (int i = 0; i < 4; ++i) n[d][u][t][i] = 0x4b400000;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint4 x = k[u][j];       // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
-                uint4 a, b;
-                C::keys(x.x, a.x, a.z);
-                C::keys(x.y, a.y, a.w);
-                C::keys(x.z, b.x, b.z);
-                C::keys(x.w, b.y, b.w);
+            for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) N::mma(s[u][t], a, q[t][2 * j][0], q[t][2 * j][1]);
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][2 * j + 1][0], q[t][2 * j + 1][1]);
-            }
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int d = 0; d < 3; ++d) mma_s8(n[d][u][t], k[u][j], q[t][j][2 * d], q[t][j][2 * d + 1]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        auto digit = [&](int d) { return __int_as_float(n[d][u][t][i]) - 12582912.f; };
+                        s[u][t][i] = fmaf(digit(2), 65536.f, fmaf(digit(1), 256.f, digit(0)));
+                    }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[u][t][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint4 x = k[u][j];   // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
+                    uint4 a, b;
+                    C::keys(x.x, a.x, a.z);
+                    C::keys(x.y, a.y, a.w);
+                    C::keys(x.z, b.x, b.z);
+                    C::keys(x.w, b.y, b.w);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) N::mma(s[u][t], a, q[t][j][0], q[t][j][1]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][j][2], q[t][j][3]);
+                }
+        }
         uint4 v[2][D / 32];                    // asked for before the softmax
 #pragma unroll
         for (int u = 0; u < 2; ++u)
