@@ -53,7 +53,7 @@ struct Worker {
     using Stages = R;
     using Type = T;
     using Softmax = State<D, NT>;
-    static constexpr int kDim = D, kColumns = NT;
+    static constexpr int kDim = D, kColumns = NT, kWarps = 8;
     static constexpr int kSub = R::kTokens / 16;             // groups of 16 tokens in a tile
     const AttnParams& p;
     const int lane, g, c, unit_in_cta, sub;
@@ -262,7 +262,7 @@ struct Worker {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-int32_t tile_of(int32_t dim) { return dim == 128 ? Ring<128>::kTokens : Ring<64>::kTokens; }
+Tiling tiling_of(int32_t dim, int32_t) { return {dim == 128 ? Ring<128>::kTokens : Ring<64>::kTokens, 8}; }
 
 template <typename T, int D>
 cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
@@ -278,7 +278,7 @@ cudaError_t sms_here(int* sms) {
 }  // namespace
 
 extern "C" int32_t ps_paged_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes) {
-    return workspace_of(num_kv_heads, num_q_heads, head_dim, tile_of(head_dim), sms_here, bytes);
+    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of, sms_here, bytes);
 }
 
 extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, char* err_buf, int32_t err_cap) {
@@ -296,7 +296,7 @@ extern "C" int32_t ps_paged_attn(const ps_paged_attn_args* args, void* stream, c
         if (!on_bytes(a.kpool, 2 * a.k_block_stride, 16) || !on_bytes(a.vpool, 2 * a.v_block_stride, 16)) return kUneven;
         return nullptr;
     };
-    const int32_t rc = plan_call(a, {a.num_kv_heads, a.head_dim, a.block_size, a.num_gpu_blocks}, tile_of, sms_here, pools, refuse, &p, &y, &may_cut);
+    const int32_t rc = plan_call(a, {a.num_kv_heads, a.head_dim, a.block_size, a.num_gpu_blocks}, tiling_of, sms_here, pools, refuse, &p, &y, &may_cut);
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = a.kpool, p.vpool = a.vpool;
     p.k_block_stride = a.k_block_stride, p.v_block_stride = a.v_block_stride;

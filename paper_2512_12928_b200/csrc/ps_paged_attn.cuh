@@ -33,7 +33,7 @@
 
 namespace {
 
-constexpr int kMaxWarps = 8;
+constexpr int kMaxUnits = 8;          // of a CTA
 constexpr int kMaxGroup = 16;         // query heads of a unit
 constexpr int kJoinThreads = 256;
 constexpr int32_t kMaxTokens = INT32_MAX - 1024;   // of a row, so that a tile's end cannot wrap
@@ -230,9 +230,16 @@ __device__ __forceinline__ void store4(T* dst, const float4& o, float f) {
 
 // -------------------------------------------------------------------------------------------- main kernel
 
+// A barrier of a unit's warps; other units go their own way.
+__device__ __forceinline__ void slices_meet(const AttnParams& p, int unit_in_cta) {
+    if (p.subs > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + unit_in_cta), "r"(32 * p.subs) : "memory");
+    else __syncwarp();
+}
+
 template <typename W>
-__global__ void __launch_bounds__(kMaxWarps * 32, 1)
+__global__ void __launch_bounds__(W::kWarps * 32, 1)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
+    constexpr int kMaxWarps = W::kWarps;
     using R = typename W::Stages;
     using T = typename W::Type;
     constexpr int D = W::kDim, NT = W::kColumns;
@@ -376,7 +383,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                         l += __shfl_xor_sync(0xffffffffu, l, 16);
                         if (wk.g == 0) sh_ml[warp][r] = make_float2(wk.reference(st, t, h), l);
                     }
-                if (p.subs > 1) __syncthreads(); else __syncwarp();
+                slices_meet(p, wk.unit_in_cta);
                 constexpr int kLanes = D / 4, kHeads = 32 / kLanes;      // heads that a warp works on at a time
                 const int dim = 4 * (lane % kLanes);
                 auto put = [&](int r, const float4& o, float m, float l) {
@@ -399,7 +406,7 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 } else {
                     // eight parts are loaded at a time: of all slices of one, two or four heads
                     auto combine = [&](auto slices) {
-                        constexpr int kSlices = decltype(slices)::value, kAtOnce = kMaxWarps / kSlices;
+                        constexpr int kSlices = decltype(slices)::value, kAtOnce = kSlices < 8 ? 8 / kSlices : 1;
                         constexpr int kStep = kSlices * kHeads;
 #pragma unroll 1
                         for (int r0 = wk.sub * kHeads + lane / kLanes; r0 < n; r0 += kAtOnce * kStep) {
@@ -435,9 +442,10 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                     };
                     if (p.subs == 2) combine(std::integral_constant<int, 2>());
                     else if (p.subs == 4) combine(std::integral_constant<int, 4>());
-                    else combine(std::integral_constant<int, 8>());
+                    else if (kMaxWarps == 8 || p.subs == 8) combine(std::integral_constant<int, 8>());
+                    else combine(std::integral_constant<int, kMaxWarps>());
                 }
-                if (p.subs > 1) __syncthreads(); else __syncwarp();      // the stage is free again
+                slices_meet(p, wk.unit_in_cta);      // the stage is free again
                 if (!seg_end) {
                     const int from = (cur.place - cur.i) / share;      // the CTAs of the segment's first and last tile
                     cut = make_int4(cur.b, cur.chunk, (cur.place + cur.tiles - cur.i - 1) / share - from + 1, from);
@@ -617,6 +625,13 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 
 // ---------------------------------------------------------------------------------------------------- host
 
+// Of a kernel: tokens that a warp takes at a time, and most warps of a CTA.
+#ifndef FEWW
+#define FEWW 8
+#endif
+struct Tiling {
+    int32_t tile, warps;
+};
 // How the heads are dealt to warps.
 struct Layout {
     int32_t splits, rows, units, chunks, subs, ctas, step_log2;
@@ -627,19 +642,20 @@ struct Layout {
 // a segment's end.  For one or two rows fewer, whose warps share the tokens: a long row is then cut into a quarter as
 // many parts, and a short one may not be cut at all (one row of 8 KV heads of 128: 300 tokens 7.5 instead of 7.7 us,
 // 4096 9.7 instead of 10.8, 32768 29.1 instead of 30.3; but 4 rows of 30000 80.4 instead of 78.6 us).
-// tile: tokens that a warp takes at a time.
-Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, int32_t tile, int sms) {
+template <typename TilingOf>
+Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, TilingOf tiling_of, int sms) {
     Layout y{};
     const int32_t group = hq / hkv;
     y.splits = (group + kMaxGroup - 1) / kMaxGroup;
     y.rows = (group + y.splits - 1) / y.splits;
     y.nt = (y.rows + 7) / 8;
     const int32_t all = hkv * y.splits;
-    const int32_t most = (int64_t)batch * all <= 2 * kMaxWarps ? 2 : kMaxWarps;
+    const Tiling tiling = tiling_of(dim, y.nt);
+    const int32_t most = (int64_t)batch * all <= 2 * kMaxUnits ? 2 : kMaxUnits;
     y.chunks = (all + most - 1) / most;
     y.units = (all + y.chunks - 1) / y.chunks;
-    for (y.subs = 1; 2 * y.subs * y.units <= kMaxWarps; y.subs *= 2) {}
-    for (y.step_log2 = 0; (1 << y.step_log2) < tile * y.subs; ++y.step_log2) {}
+    for (y.subs = 1; 2 * y.subs * y.units <= (most == 2 ? std::min(tiling.warps, FEWW) : tiling.warps); y.subs *= 2) {}
+    for (y.step_log2 = 0; (1 << y.step_log2) < tiling.tile * y.subs; ++y.step_log2) {}
     y.ctas = sms;                          // the rings take an SM's shared memory
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
@@ -659,7 +675,7 @@ constexpr int attn_smem(int warps) { return 128 + warps * W::Stages::kWarpBytes;
 template <typename... W>
 cudaError_t allow_smem() {
     cudaError_t e = cudaSuccess;
-    ((e = e != cudaSuccess ? e : cudaFuncSetAttribute(paged_attn_kernel<W>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem<W>(kMaxWarps))), ...);
+    ((e = e != cudaSuccess ? e : cudaFuncSetAttribute(paged_attn_kernel<W>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem<W>(W::kWarps))), ...);
     return e;
 }
 
@@ -703,15 +719,15 @@ const char* shape_error(int32_t hkv, int32_t hq, int32_t dim) {
     return nullptr;
 }
 
-template <typename Sms>
-int32_t workspace_of(int32_t hkv, int32_t hq, int32_t dim, int32_t tile, Sms sms_here, int64_t* bytes) {
+template <typename TilingOf, typename Sms>
+int32_t workspace_of(int32_t hkv, int32_t hq, int32_t dim, TilingOf tiling_of, Sms sms_here, int64_t* bytes) {
     if (!bytes || shape_error(hkv, hq, dim)) return PS_ERR_INVALID;
     int sms = 0;
     if (sms_here(&sms) != cudaSuccess) {
         cudaGetLastError();
         return PS_ERR_CUDA;
     }
-    *bytes = (int64_t)std::max(layout_of(1, hkv, hq, dim, tile, sms).bytes, layout_of(1 << 30, hkv, hq, dim, tile, sms).bytes);
+    *bytes = (int64_t)std::max(layout_of(1, hkv, hq, dim, tiling_of, sms).bytes, layout_of(1 << 30, hkv, hq, dim, tiling_of, sms).bytes);
     return PS_OK;
 }
 
@@ -735,8 +751,8 @@ struct CacheShape {
 
 // Checks a call's arguments (Args: ps_paged_attn_args or ps_quant_attn_args; `pools` checks the cache's own) and fills in
 // all parameters but the cache's.  Nothing to do for a batch of 0.
-template <typename Args, typename Tile, typename Sms, typename Pools>
-int32_t plan_call(const Args& a, const CacheShape& c, Tile tile_of, Sms sms_here, Pools pools, const Refusal& refuse, AttnParams* params,
+template <typename Args, typename TilingOf, typename Sms, typename Pools>
+int32_t plan_call(const Args& a, const CacheShape& c, TilingOf tiling_of, Sms sms_here, Pools pools, const Refusal& refuse, AttnParams* params,
                   Layout* layout, bool* may_cut) {
     if (refuse.buf && refuse.cap > 0) refuse.buf[0] = 0;
     if (const char* m = shape_error(c.hkv, a.num_q_heads, c.dim)) return refuse(m);
@@ -759,8 +775,7 @@ int32_t plan_call(const Args& a, const CacheShape& c, Tile tile_of, Sms sms_here
     // for and at most 4 more, and a tile's tokens times the KV heads are 24 (3 KV heads of 33 query heads each) times a
     // row's segments or more: with 1024 more tokens a row, 2^34 tokens times KV heads always fit.
     const int64_t room = std::min<int64_t>((int64_t)a.table_stride * c.block_size, kMaxTokens);
-    const int32_t tile = tile_of(c.dim);
-    const Layout places = layout_of(a.batch, c.hkv, a.num_q_heads, c.dim, tile, 1);
+    const Layout places = layout_of(a.batch, c.hkv, a.num_q_heads, c.dim, tiling_of, 1);
     if ((room >> places.step_log2) + 4 > (1 << 30) / ((int64_t)a.batch * places.chunks))
         return refuse("the tables of the batch have room for more than 2^30 tiles of tokens");
     int sms = 0;
@@ -769,7 +784,7 @@ int32_t plan_call(const Args& a, const CacheShape& c, Tile tile_of, Sms sms_here
         snprintf(where, sizeof where, "%s: device", refuse.name);
         return ps::launch_fail(refuse.buf, refuse.cap, where, e);
     }
-    const Layout y = layout_of(a.batch, c.hkv, a.num_q_heads, c.dim, tile, sms);
+    const Layout y = layout_of(a.batch, c.hkv, a.num_q_heads, c.dim, tiling_of, sms);
     if (a.workspace_bytes < (int64_t)y.bytes || (reinterpret_cast<uintptr_t>(a.workspace) & 255)) {
         char text[128];
         snprintf(text, sizeof text, "the workspace is smaller than %s_workspace says, or not on a 256-byte boundary", refuse.name);

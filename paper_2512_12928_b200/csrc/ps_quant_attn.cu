@@ -59,13 +59,14 @@ __device__ __forceinline__ void mma_s8(int32_t (&d)[4], const uint4& a, uint32_t
                  : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
-template <int D>
+// Tiles of 16 U tokens, and as many bytes on their way for either head size.
+template <int D, int U, int Warps>
 struct Ring {
-    static constexpr int kTokens = 32;                       // of a tile
+    static constexpr int kTokens = 16 * U;                   // of a tile
     static constexpr int kRowBytes = D;
     static constexpr int kSideBytes = kTokens * kRowBytes;   // keys, then values, then their scales
     static constexpr int kStageBytes = 2 * kSideBytes + 2 * kTokens * (int)sizeof(float);
-    static constexpr int kStages = D == 128 ? 3 : 6;         // as many bytes on their way
+    static constexpr int kStages = (D == 128 ? 6 : 12) * 8 / (Warps * U);
     static constexpr int kWarpBytes = kStages * kStageBytes;
 };
 
@@ -74,13 +75,18 @@ struct QuantState : State<D, NT> {
     float inv_ref;                             // 1 / r
 };
 
+// Units of up to 8 query heads: 16 warps; of up to 16, whose registers do not allow as many: 8.
+constexpr int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+constexpr int groups_of(int dim, int nt) { return nt == 1 && dim == 128 ? 1 : 2; }     // of 16 tokens, in a tile
+
 template <typename T, typename C, int D, int NT>
 struct Worker {
-    using Stages = Ring<D>;
+    static constexpr int U = groups_of(D, NT), kWarps = warps_of(NT);
+    using Stages = Ring<D, U, kWarps>;
     using R = Stages;
     using Type = T;
     using Softmax = QuantState<D, NT>;
-    using Keys = uint4[2][D / 32];
+    using Keys = uint4[U][D / 32];
     using N = Num<__half>;
     static constexpr int kDim = D, kColumns = NT;
     static constexpr bool kRest = std::is_same_v<T, __half>;
@@ -99,7 +105,7 @@ struct Worker {
     const unsigned char *k_src, *v_src;        // pools at this lane's head and piece
     const float *k_scale, *v_scale;            // scales of the head
     const int32_t* table;
-    int32_t id, at;                            // block and place of token `lane`; at = -1: no token
+    int32_t id, at;                            // block and place of token lane % kTokens; at = -1: no token
     bool idle;                                 // the unit does not exist
     uint32_t masks[R::kStages - 1];            // which tokens of the tiles in the ring are attended, the oldest first
 
@@ -185,7 +191,7 @@ struct Worker {
 
     // Looks the tile's tokens up.
     __device__ __forceinline__ void load_ids(const Cursor& cur) {
-        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - 5)) + sub) + lane;
+        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - (U == 2 ? 5 : 4))) + sub) + lane % R::kTokens;
         id = 0;
         at = -1;
         if (t < cur.end) {
@@ -209,10 +215,10 @@ struct Worker {
         const uint32_t base = ring + stage * R::kStageBytes, dst = base + put;
         if (on == 0xffffffffu) copy_rows<true>(k_off, v_off, on, dst);       // as nearly always
         else copy_rows<false>(k_off, v_off, on, dst);
-        // scales, tokens g, 8 + g, 16 + g, 24 + g next to one another
-        const uint32_t scales = base + 2 * R::kSideBytes + 4 * (4 * (lane & 7) + (lane >> 3));
-        copy4(scales, k_scale + (read ? id * p.k_scale_stride : 0), read ? 4 : 0);
-        copy4(scales + 4 * R::kTokens, v_scale + (read ? id * p.v_scale_stride : 0), read ? 4 : 0);
+        // scales, tokens g, 8 + g, .. next to one another
+        const uint32_t scales = base + 2 * R::kSideBytes + 4 * (2 * U * (lane & 7) + (lane % R::kTokens >> 3));
+        if (U == 2 || lane < 16) copy4(scales, k_scale + (read ? id * p.k_scale_stride : 0), read ? 4 : 0);
+        if (U == 2 || lane >= 16) copy4(scales + 4 * R::kTokens, v_scale + (read ? id * p.v_scale_stride : 0), read ? 4 : 0);
         return on;
     }
     template <bool kAll>
@@ -236,14 +242,17 @@ struct Worker {
     static __device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
     }
-    static __device__ __forceinline__ void four(uint32_t src, float (&v)[4]) {
+    static __device__ __forceinline__ void floats(uint32_t src, float (&v)[2]) {
+        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(src) : "memory");
+    }
+    static __device__ __forceinline__ void floats(uint32_t src, float (&v)[4]) {
         asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(src) : "memory");
     }
 
     // The keys of the tile in a stage: k[u][j] has 32 dims of 16 tokens.
     __device__ __forceinline__ void read_keys(int stage, Keys& k) const {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) k[u][j] = ldsm(ring + stage * R::kStageBytes + 16 * u * D + at_piece[j]);
     }
@@ -264,14 +273,14 @@ struct Worker {
     // Attends the tile in a stage; `on`: its tokens that count.
     __device__ __forceinline__ void attend(int stage, const Keys& k, uint32_t on, Softmax& st) {
         const uint32_t src = ring + stage * R::kStageBytes;
-        float s[2][NT][4];
+        float s[U][NT][4];
         if constexpr (C::kDigits) {
             // Products of each digit, in whole numbers below 2^21: from 1.5 2^23's bits on, so that they are floats
-            int32_t n[3][2][NT][4];
+            int32_t n[3][U][NT][4];
 #pragma unroll
             for (int d = 0; d < 3; ++d)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -279,13 +288,13 @@ struct Worker {
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int d = 0; d < 3; ++d) mma_s8(n[d][u][t], k[u][j], q[t][j][2 * d], q[t][j][2 * d + 1]);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -295,7 +304,7 @@ struct Worker {
                     }
         } else {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -303,7 +312,7 @@ struct Worker {
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < U; ++u) {
                     const uint4 x = k[u][j];   // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
                     uint4 a, b;
                     C::keys(x.x, a.x, a.z);
@@ -316,33 +325,33 @@ struct Worker {
                     for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][j][2], q[t][j][3]);
                 }
         }
-        uint4 v[2][D / 32];                    // asked for before the softmax
+        uint4 v[U][D / 32];                    // asked for before the softmax
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) v[u][j] = ldsm_t(src + R::kSideBytes + 16 * u * D + at_piece[j]);
-        float ks[4], vs[4];                    // of tokens g, 8 + g, 16 + g, 24 + g
-        four(src + 2 * R::kSideBytes + 16 * g, ks);
-        four(src + 2 * R::kSideBytes + 4 * R::kTokens + 16 * g, vs);
+        float ks[2 * U], vs[2 * U];            // of tokens g, 8 + g, ..
+        floats(src + 2 * R::kSideBytes + 8 * U * g, ks);
+        floats(src + 2 * R::kSideBytes + 4 * R::kTokens + 8 * U * g, vs);
         // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) s[u][t][i] *= ks[2 * u + (i >> 1)] * factor[t][i & 1];
+                for (int u = 0; u < U; ++u) s[u][t][i] *= ks[2 * u + (i >> 1)] * factor[t][i & 1];
         if (on != 0xffffffffu)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < U; ++u)
                         if (!(on >> (16 * u + g + 4 * (i & 2)) & 1)) s[u][t][i] = -CUDART_INF_F;
         // The weights' exponents, and the largest of them: max does not see a NaN, which then gives a NaN weight
-        float e[2][NT][4], w[4], top = 0.f, most = 0.f;
+        float e[U][NT][4], w[2 * U], top = 0.f, most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * U; ++i) {
             w[i] = vs[i] * st.inv_ref;
             most = fmaxf(most, fabsf(w[i]));
         }
@@ -351,25 +360,28 @@ struct Worker {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < U; ++u) {
                     e[u][t][i] = s[u][t][i] - st.m[t][i & 1];
                     top = fmaxf(top, e[u][t][i]);
                 }
         const bool over = top > N::kSlack + N::kLift || most > 2.f;
         if (__any_sync(0xffffffffu, over)) {
             // the reference of the values' scales: the power of two below the largest, or the present one
-            const float largest = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vs[2]), fabsf(vs[3])));
+            float largest = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * U; ++i) largest = fmaxf(largest, fabsf(vs[i]));
             const uint32_t ex = min(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)) >> 23, 252u);
             const float inv = fminf(st.inv_ref, __uint_as_float((254u - ex) << 23));
             const float sink = inv / st.inv_ref;
             st.inv_ref = inv;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = vs[i] * inv;
+            for (int i = 0; i < 2 * U; ++i) w[i] = vs[i] * inv;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float mx = fmaxf(fmaxf(s[0][t][h], s[0][t][2 + h]), fmaxf(s[1][t][h], s[1][t][2 + h]));
+                    float mx = fmaxf(s[0][t][h], s[0][t][2 + h]);
+                    if (U == 2) mx = fmaxf(mx, fmaxf(s[U - 1][t][h], s[U - 1][t][2 + h]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -383,16 +395,16 @@ struct Worker {
                         st.acc[t][j][2 + h] *= alpha * sink;
                     }
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
+                    for (int u = 0; u < U; ++u) {
                         e[u][t][h] = s[u][t][h] - mx;
                         e[u][t][2 + h] = s[u][t][2 + h] - mx;
                     }
                 }
         }
         // P^T: tokens 2c, 2c + 1 and 2c + 8, 2c + 9 (of 16) of head 8t + g, as the sum of two fp16 numbers
-        uint32_t pt[2][NT][2], rest[2][NT][2];
+        uint32_t pt[U][NT][2], rest[U][NT][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -411,7 +423,7 @@ struct Worker {
                 }
             }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 const uint4 x = v[u][j];       // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
@@ -435,7 +447,7 @@ struct Worker {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-int32_t tile_of(int32_t) { return Ring<128>::kTokens; }
+Tiling tiling_of(int32_t dim, int32_t nt) { return {16 * groups_of(dim, nt), warps_of(nt)}; }
 
 template <typename T, typename C, int D>
 cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
@@ -457,7 +469,7 @@ cudaError_t sms_here(int* sms) {
 }  // namespace
 
 extern "C" int32_t ps_quant_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes) {
-    return workspace_of(num_kv_heads, num_q_heads, head_dim, tile_of(head_dim), sms_here, bytes);
+    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of, sms_here, bytes);
 }
 
 extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap) {
@@ -479,7 +491,7 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
         if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
         return nullptr;
     };
-    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tile_of, sms_here, pools, refuse, &p, &y, &may_cut);
+    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tiling_of, sms_here, pools, refuse, &p, &y, &may_cut);
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
     p.k_block_stride = c.k_block_stride, p.v_block_stride = c.v_block_stride;
