@@ -94,28 +94,26 @@ struct Worker {
         }
     }
 
-    // The row and chunk of the tiles to come.
-    __device__ __forceinline__ void enter(const Cursor& cur) {
-        int kv, h0, n;
-        unit_heads(p, cur.chunk * p.units + unit_in_cta, &kv, &h0, &n);
-        idle = kv >= p.hkv;
-        const int64_t o = idle ? 0 : (int64_t)kv * D + 8 * (lane & 7);
+    // The part whose tiles come next.
+    __device__ __forceinline__ void enter(const Part& s, int kv) {
+        idle = s.n == 0;
+        const int64_t o = (int64_t)kv * D + 8 * (lane & 7);
         k_src = (const T*)p.kpool + o;
         v_src = (const T*)p.vpool + o;
-        table = p.tables + (int64_t)cur.b * p.table_stride;
+        table = p.tables + (int64_t)s.b * p.table_stride;
         // the unit's queries, into L1: they are loaded when its tiles have come, and then nothing hides their latency
-        if (!idle && lane < n * D / 64) {
+        if (lane < s.n * D / 64) {
             uint32_t unused;
-            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + cur.b * p.q_stride + (int64_t)h0 * D + lane * 64));
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + s.b * p.q_stride + (int64_t)s.h0 * D + lane * 64));
         }
     }
 
-    // Looks the tile's tokens up.
-    __device__ __forceinline__ void load_ids(const Cursor& cur) {
-        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - (D == 128 ? 4 : 5))) + sub) + lane % R::kTokens;
+    // Looks up the tokens of the tile that the slices' from token t0 on are, in a row that ends at `end`.
+    __device__ __forceinline__ void load_ids(int32_t t0, int32_t end) {
+        const int32_t t = t0 + R::kTokens * sub + lane % R::kTokens;
         id = 0;
         at = -1;
-        if (t < cur.end) {
+        if (t < end) {
             const int32_t blk = block_of(t, p);
             at = t - blk * p.block_size;
             id = table[blk];

@@ -53,8 +53,8 @@ struct AttnParams {
     int4* cuts;          // [cta]: the segment that this CTA did not finish: {row, chunk, parts, first CTA}; parts 0: none
     int64_t k_block_stride, v_block_stride, q_stride, out_stride;
     const float *k_scale, *v_scale;  // of an 8-bit cache: [block][KV head]
-    int64_t k_scale_stride, v_scale_stride;
-    bool far;                        // a pool's blocks lie more than 2^36 bytes apart
+    uint32_t k_step, v_step, k_scale_step, v_scale_step;      // its blocks, in steps of 16 bytes, and their scales' in floats
+    bool far;                        // a pool's last block begins 2^36 bytes or more behind its first
     int64_t room;        // tokens a table row has room for
     uint64_t block_magic;
     int32_t batch, table_stride, num_blocks, block_size, window;
@@ -155,36 +155,49 @@ __device__ __forceinline__ int32_t row_tiles(const AttnParams& p, int32_t n) {
 
 // Where a unit's queries are: heads [h0, h0 + n).
 __device__ __forceinline__ void unit_heads(const AttnParams& p, int unit, int* kv, int* h0, int* n) {
-    *kv = unit / p.splits;
+    *kv = p.splits == 1 ? unit : unit / p.splits;
     const int s = unit - *kv * p.splits;
     *h0 = *kv * p.group + s * p.rows;
     *n = min(p.rows, p.group - s * p.rows);
 }
 
-// The tiles of a CTA's share, one after the other: row b, chunk of its units, tile i of the row's `tiles`, at `place` of
-// the sequence that is cut into shares: a segment (row and chunk) takes p.segment places for its start and end, then one
-// for each tile.
-struct Cursor {
-    int32_t b, chunk, i, tiles, first, end, place;
+// A segment is a row and a chunk of units.  It takes p.segment places of the sequence that is cut into shares for its start
+// and end, then one for each of its tiles.  What a share has of one:
+struct Part {
+    int32_t b, chunk;
+    int32_t h0, n;                           // the warp's unit: query heads [h0, h0 + n)
+    int32_t lo, count, tiles;                // tiles [lo, lo + count) of the segment's
+    int32_t base;                            // place of the segment's first tile
+};
+constexpr int kParts = 8;                    // of a warp between the request of a tile and the end of its attention
+
+// The tiles of a CTA's share, one after the other, as they are requested.
+struct Walk {
+    int32_t b, chunk, len;                   // row b of len tokens
     int32_t next_len;                        // of row b + 1, asked for while row b is worked on
-    __device__ __forceinline__ void row(const AttnParams& p, int32_t len) {
+    int32_t t, end;                          // the next tile's first token, and where the row's end
+    int32_t left;                            // tiles of the segment still to be requested; 0: of the share
+    int32_t place;                           // where the next segment's first tile is
+    __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? p.ctx[b + 1] : 0; }
+    // Begins with tile i of the segment, at a place before share_end.
+    __device__ __forceinline__ Part enter(const AttnParams& p, int32_t i, int32_t at, int32_t share_end) {
+        int32_t first;
         row_span(p, len, &first, &end);
-        tiles = row_tiles(p, len);
         if (end != len && p.status) *(volatile int32_t*)p.status = kStatusLength;
+        const int32_t tiles = row_tiles(p, len);
+        t = first + (i << p.step_log2);
+        left = min(tiles - i, share_end - at);
+        place = at - i + tiles + p.segment;
+        return {b, chunk, 0, 0, i, left, tiles, at - i};
     }
-    __device__ __forceinline__ bool ends_segment() const { return i + 1 == tiles; }
-    __device__ __forceinline__ int32_t next_place(const AttnParams& p) const { return place + 1 + (ends_segment() ? p.segment : 0); }
-    __device__ __forceinline__ void next(const AttnParams& p, int32_t share_end) {
-        place = next_place(p);
-        if (++i < tiles) return;
-        i = 0;
+    // To the next segment, whose first tile is before the share's end.
+    __device__ __forceinline__ void step(const AttnParams& p) {
         if (++chunk < p.chunks) return;
         chunk = 0;
         ++b;
-        if (place < share_end) row(p, next_len);
+        len = next_len;
         look_ahead(p);
     }
-    __device__ __forceinline__ void look_ahead(const AttnParams& p) { next_len = b + 1 < p.batch ? p.ctx[b + 1] : 0; }
 };
 
 // The softmax state of a warp.  Lane (g = lane / 4, c = lane % 4) holds heads 8 t + 2 c and 8 t + 2 c + 1 of column tile t:
@@ -250,6 +263,8 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     __shared__ int sh_sum[kMaxWarps];
     __shared__ int4 sh_begin;          // where the share begins: row, chunk, tile; the row's length
     __shared__ int sh_place;
+    __shared__ Part sh_parts[kMaxWarps][kParts];
+    static_assert(R::kStages + 1 <= kParts, "parts in the ring, one being attended and one entered");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nwarps = blockDim.x >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -265,7 +280,6 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
         len = p.ctx[b];
         mine += (row_tiles(p, len) + p.segment) * p.chunks;
     }
-    Cursor cur;
     int before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -286,53 +300,59 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     const int share = (total + gridDim.x - 1) / gridDim.x;
     const int begin = share * blockIdx.x, end = min(total, begin + share);
     if (begin >= before && begin < before + mine) {
-        int a = before;
-        cur.b = b_lo;                            // and of a single row the length is still there
+        int a = before, b = b_lo;                // and of a single row the length is still there
         if (per > 1)
 #pragma unroll 1
-            for (;; ++cur.b) {
-                len = p.ctx[cur.b];
+            for (;; ++b) {
+                len = p.ctx[b];
                 const int n = (row_tiles(p, len) + p.segment) * p.chunks;
                 if (begin < a + n) break;
                 a += n;
             }
-        cur.row(p, len);
-        cur.chunk = 0;
-        cur.i = begin - a;
+        const int tiles = row_tiles(p, len);
+        int chunk = 0, i = begin - a;
         if (p.chunks > 1) {
-            cur.chunk = cur.i / (cur.tiles + p.segment);
-            cur.i -= cur.chunk * (cur.tiles + p.segment);
+            chunk = i / (tiles + p.segment);
+            i -= chunk * (tiles + p.segment);
         }
-        cur.i = max(cur.i - p.segment, 0);        // a share that begins in a segment's first places has its first tile
-        sh_begin = make_int4(cur.b, cur.chunk, cur.i, len);
-        sh_place = a + cur.chunk * (cur.tiles + p.segment) + p.segment + cur.i;
+        i = max(i - p.segment, 0);                // a share that begins in a segment's first places has its first tile
+        sh_begin = make_int4(b, chunk, i, len);
+        sh_place = a + chunk * (tiles + p.segment) + p.segment + i;
         // the first block ids, into L1 while the CTA meets
-        const int32_t t = cur.first + (cur.i << p.step_log2);
-        if (t < cur.end) {
+        int32_t first, last;
+        row_span(p, len, &first, &last);
+        const int32_t t = first + (i << p.step_log2);
+        if (t < last) {
             uint32_t unused;
-            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"(p.tables + (int64_t)cur.b * p.table_stride + block_of(t, p)));
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"(p.tables + (int64_t)b * p.table_stride + block_of(t, p)));
         }
     }
     __syncthreads();
     int4 cut = make_int4(0, 0, 0, 0);
     if (begin < end && sh_place < end) {         // else there is no tile in it
+        Walk walk;                               // to the tile that is requested next
+        int32_t parts = 0, part = 0;             // entered, and attended: parts part to parts - 1 wait in sh_parts
+        auto enter = [&](int32_t i, int32_t at) {
+            Part s = walk.enter(p, i, at, end);
+            const int unit = s.chunk * p.units + wk.unit_in_cta;
+            int kv = 0;
+            if (unit < p.hkv * p.splits) unit_heads(p, unit, &kv, &s.h0, &s.n);      // else the unit does not exist: no heads
+            wk.enter(s, kv);
+            if (lane == 0) sh_parts[warp][parts % kParts] = s;
+            ++parts;
+        };
         const int4 start = sh_begin;
-        cur.b = start.x;
-        cur.chunk = start.y;
-        cur.i = start.z;
-        cur.place = sh_place;
-        cur.look_ahead(p);
-        cur.row(p, start.w);
-        Cursor ahead = cur;                      // the tile that is requested next
+        walk.b = start.x;
+        walk.chunk = start.y;
+        walk.len = start.w;
+        walk.look_ahead(p);
+        enter(start.z, sh_place);
+        wk.load_ids(walk.t, walk.end);
         int slot = 0;                            // stage that is filled next
-        wk.enter(ahead);
-        wk.load_ids(ahead);
         typename W::Softmax st;
-        int kv = 0, h0 = 0, n = 0;
-        int32_t lo = 0;
-        bool fresh = true;
+        int32_t left = 0, due = 0;               // tiles of the part to be attended, and of those requested
 #pragma unroll 1
-        for (int fill = R::kStages - 1; cur.place < end;) {
+        for (int fill = R::kStages - 1; walk.left > 0 || due > 0;) {
             copies_wait<R::kStages - 2>();
             __syncwarp();                        // the other lanes' copies too, and they have left the stage before
             const int filled = slot;             // the stage that the tile before left
@@ -342,31 +362,34 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
             for (int i = 0; i + 1 < R::kStages - 1; ++i) wk.masks[i] = wk.masks[i + 1];
             typename W::Keys k;
             wk.read_keys(slot, k);               // in the first rounds what it reads is not used
-            if (ahead.place < end) {
+            if (walk.left > 0) {
                 wk.masks[R::kStages - 2] = wk.copy_tile(filled);
-                ahead.next(p, end);
-                if (ahead.place < end) {
-                    if (ahead.i == 0) wk.enter(ahead);
-                    wk.load_ids(ahead);
+                ++due;
+                walk.t += 1 << p.step_log2;
+                if (--walk.left == 0 && walk.place < end) {
+                    walk.step(p);
+                    enter(0, walk.place);
                 }
+                if (walk.left > 0) wk.load_ids(walk.t, walk.end);
             }
             copies_commit();
             if (fill > 0) {                      // the first rounds only fill the ring
                 --fill;
                 continue;
             }
-            const int unit = cur.chunk * p.units + wk.unit_in_cta;
-            if (fresh) {
+            if (left == 0) {
+                const Part& s = sh_parts[warp][part % kParts];
+                left = s.count;
                 wk.reset(st);
-                n = 0;
-                if (unit < p.hkv * p.splits) unit_heads(p, unit, &kv, &h0, &n);
-                wk.load_query(cur.b, h0, n);
-                lo = cur.i;
-                fresh = false;
+                wk.load_query(s.b, s.h0, s.n);
             }
             wk.attend(slot, k, on, st);
-            const bool seg_end = cur.ends_segment();
-            if (seg_end || cur.next_place(p) >= end) {
+            --due;
+            if (--left == 0) {
+                const Part s = sh_parts[warp][part % kParts];
+                ++part;
+                const bool seg_end = s.lo + s.count == s.tiles;
+                const int32_t h0 = s.h0, n = s.n, lo = s.lo;
                 const bool whole = lo == 0 && seg_end;
                 // The states of the slices go through the stage that has just been read, heads as rows, and come
                 // back as rows of four dims a lane.  (The places' exclusive or keeps the writes free of conflicts.)
@@ -388,8 +411,8 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 const int dim = 4 * (lane % kLanes);
                 auto put = [&](int r, const float4& o, float m, float l) {
                     if (whole) {
-                        store4((T*)p.out + cur.b * p.out_stride + (int64_t)(h0 + r) * D + dim, o, inverse_sum(l));
-                        if (p.lse && dim == 0) p.lse[(int64_t)cur.b * p.hq + h0 + r] = natural_log_sum<T>(m, l);
+                        store4((T*)p.out + s.b * p.out_stride + (int64_t)(h0 + r) * D + dim, o, inverse_sum(l));
+                        if (p.lse && dim == 0) p.lse[(int64_t)s.b * p.hq + h0 + r] = natural_log_sum<T>(m, l);
                     } else {
                         const int64_t part = (((int64_t)blockIdx.x * 2 + (lo == 0)) * p.units + wk.unit_in_cta) * p.rows + r;
                         *reinterpret_cast<float4*>(p.part_o + part * D + dim) = o;
@@ -447,12 +470,10 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
                 }
                 slices_meet(p, wk.unit_in_cta);      // the stage is free again
                 if (!seg_end) {
-                    const int from = (cur.place - cur.i) / share;      // the CTAs of the segment's first and last tile
-                    cut = make_int4(cur.b, cur.chunk, (cur.place + cur.tiles - cur.i - 1) / share - from + 1, from);
+                    const int from = s.base / share;      // the CTAs of the segment's first and last tile
+                    cut = make_int4(s.b, s.chunk, (s.base + s.tiles - 1) / share - from + 1, from);
                 }
-                fresh = true;
             }
-            cur.next(p, end);
         }
     }
     if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
@@ -626,9 +647,6 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 // ---------------------------------------------------------------------------------------------------- host
 
 // Of a kernel: tokens that a warp takes at a time, and most warps of a CTA.
-#ifndef FEWW
-#define FEWW 8
-#endif
 struct Tiling {
     int32_t tile, warps;
 };
@@ -654,7 +672,7 @@ Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, TilingOf t
     const int32_t most = (int64_t)batch * all <= 2 * kMaxUnits ? 2 : kMaxUnits;
     y.chunks = (all + most - 1) / most;
     y.units = (all + y.chunks - 1) / y.chunks;
-    for (y.subs = 1; 2 * y.subs * y.units <= (most == 2 ? std::min(tiling.warps, FEWW) : tiling.warps); y.subs *= 2) {}
+    for (y.subs = 1; 2 * y.subs * y.units <= tiling.warps; y.subs *= 2) {}
     for (y.step_log2 = 0; (1 << y.step_log2) < tiling.tile * y.subs; ++y.step_log2) {}
     y.ctas = sms;                          // the rings take an SM's shared memory
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };

@@ -97,13 +97,13 @@ struct Worker {
     const uint32_t ring;                       // the warp's first stage
     const uint64_t policy;
     uint32_t put;                              // this lane's place in a stage: row lane / kPieces and, in place, piece lane % kPieces
-    uint32_t at_piece[kPieces / 2];            // what this lane reads of a stage's half: pieces 2 j + .. of its row
+    uint32_t get;                              // what this lane reads of a stage's half: piece 0 or 1 of its row; piece 2 j + .. is at get ^ 32 j
     // query head 8 t + g, dims 32 j + 4 c + .. of four and dims 32 j + 16 + 4 c + .. of four: two fp16 numbers a register, or
     // a digit of all four, digit by digit
     uint32_t q[NT][D / 32][C::kDigits ? 6 : 4];
     float factor[NT][2];                       // of the scores of heads 8 t + 2 c and 8 t + 2 c + 1, with log2(e) scale in it
     const unsigned char *k_src, *v_src;        // pools at this lane's head and piece
-    const float *k_scale, *v_scale;            // scales of the head
+    const float* scale_src;                    // scales of the head: keys', and with one group of tokens the upper lanes' values'
     const int32_t* table;
     int32_t id, at;                            // block and place of token lane % kTokens; at = -1: no token
     bool idle;                                 // the unit does not exist
@@ -114,8 +114,7 @@ struct Worker {
           sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), masks{} {
         const int x = lane & 7, up = lane >> 4, mid = lane >> 3 & 1, row = lane / kPieces;
         put = row * D + (((lane % kPieces) ^ swap(row)) << 4);
-#pragma unroll
-        for (int j = 0; j < kPieces / 2; ++j) at_piece[j] = (x + 8 * mid) * D + (((2 * j + up) ^ swap(x)) << 4);
+        get = (x + 8 * mid) * D + ((up ^ swap(x)) << 4);
     }
 
     // A token's pieces are exclusive-ored with this, so that eight tokens' same piece lie in different banks.
@@ -170,31 +169,27 @@ struct Worker {
         }
     }
 
-    // The row and chunk of the tiles to come.
-    __device__ __forceinline__ void enter(const Cursor& cur) {
-        int kv, h0, n;
-        unit_heads(p, cur.chunk * p.units + unit_in_cta, &kv, &h0, &n);
-        idle = kv >= p.hkv;
-        if (idle) kv = 0;
+    // The part whose tiles come next.
+    __device__ __forceinline__ void enter(const Part& s, int kv) {
+        idle = s.n == 0;
         const int64_t o = (int64_t)kv * D + 16 * (lane % kPieces);
         k_src = (const unsigned char*)p.kpool + o;
         v_src = (const unsigned char*)p.vpool + o;
-        k_scale = p.k_scale + kv;
-        v_scale = p.v_scale + kv;
-        table = p.tables + (int64_t)cur.b * p.table_stride;
+        scale_src = (U == 2 || lane < 16 ? p.k_scale : p.v_scale) + kv;
+        table = p.tables + (int64_t)s.b * p.table_stride;
         // the unit's queries, into L1: they are loaded when its tiles have come, and then nothing hides their latency
-        if (!idle && lane < n * D / 64) {
+        if (lane < s.n * D / 64) {
             uint32_t unused;
-            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + cur.b * p.q_stride + (int64_t)h0 * D + lane * 64));
+            asm volatile("ld.global.ca.b32 %0, [%1];" : "=r"(unused) : "l"((const T*)p.q + s.b * p.q_stride + (int64_t)s.h0 * D + lane * 64));
         }
     }
 
-    // Looks the tile's tokens up.
-    __device__ __forceinline__ void load_ids(const Cursor& cur) {
-        const int32_t t = cur.first + R::kTokens * ((cur.i << (p.step_log2 - (U == 2 ? 5 : 4))) + sub) + lane % R::kTokens;
+    // Looks up the tokens of the tile that the slices' from token t0 on are, in a row that ends at `end`.
+    __device__ __forceinline__ void load_ids(int32_t t0, int32_t end) {
+        const int32_t t = t0 + R::kTokens * sub + lane % R::kTokens;
         id = 0;
         at = -1;
-        if (t < cur.end) {
+        if (t < end) {
             const int32_t blk = block_of(t, p);
             at = t - blk * p.block_size;
             id = table[blk];
@@ -207,36 +202,45 @@ struct Worker {
         if (at >= 0 && !known && p.status) *(volatile int32_t*)p.status = kStatusBadId;
         const bool read = at >= 0 && known && !idle;
         const uint32_t on = __ballot_sync(0xffffffffu, read);
-        // where the lane's token lies in the pools, in steps of 16 bytes; what is not read has the address of the first
-        // block's first token
-        const uint64_t in_block = (uint64_t)((uint32_t)at * (uint64_t)(uint32_t)(p.hkv * (D / 16)));
-        const uint64_t k_off = read ? (uint32_t)id * (uint64_t)(p.k_block_stride >> 4) + in_block : 0;
-        const uint64_t v_off = read ? (uint32_t)id * (uint64_t)(p.v_block_stride >> 4) + in_block : 0;
         const uint32_t base = ring + stage * R::kStageBytes, dst = base + put;
-        if (on == 0xffffffffu) copy_rows<true>(k_off, v_off, on, dst);       // as nearly always
-        else copy_rows<false>(k_off, v_off, on, dst);
+        // what is not read has the address of the first block's first token
+        const uint32_t blk = read ? id : 0, place = read ? at : 0;
+        if (on == 0xffffffffu && !p.far) copy_rows<true>(blk, place, on, dst);       // as nearly always
+        else copy_rows<false>(blk, place, on, dst);
         // scales, tokens g, 8 + g, .. next to one another
         const uint32_t scales = base + 2 * R::kSideBytes + 4 * (2 * U * (lane & 7) + (lane % R::kTokens >> 3));
-        if (U == 2 || lane < 16) copy4(scales, k_scale + (read ? id * p.k_scale_stride : 0), read ? 4 : 0);
-        if (U == 2 || lane >= 16) copy4(scales + 4 * R::kTokens, v_scale + (read ? id * p.v_scale_stride : 0), read ? 4 : 0);
+        if (U == 1) {
+            copy4(scales + (lane & 16) * 4, scale_src + blk * (uint64_t)(lane < 16 ? p.k_scale_step : p.v_scale_step), read ? 4 : 0);
+        } else {
+            copy4(scales, scale_src + blk * (uint64_t)p.k_scale_step, read ? 4 : 0);
+            copy4(scales + 4 * R::kTokens, scale_src + (p.v_scale - p.k_scale) + blk * (uint64_t)p.v_scale_step, read ? 4 : 0);
+        }
         return on;
     }
+    // The rows of a tile: a lane's token lies in block blk at `place`.  kAll: all are read, and 32 bits count a pool's 16-byte
+    // steps.
     template <bool kAll>
-    __device__ __forceinline__ void copy_rows(uint64_t k_off, uint64_t v_off, uint32_t on, uint32_t dst) {
-        const bool one_stride = p.k_block_stride == p.v_block_stride;
+    __device__ __forceinline__ void copy_rows(uint32_t blk, uint32_t place, uint32_t on, uint32_t dst) {
+        const uint32_t row16 = p.hkv * (D / 16);
+        const bool one_step = p.k_step == p.v_step;
+        const uint32_t k_off = blk * p.k_step + place * row16, v_off = blk * p.v_step + place * row16;
 #pragma unroll
         for (int i = 0; i < R::kTokens / kRows; ++i) {
             const int row = kRows * i + lane / kPieces;
             const uint32_t bytes = kAll ? 16u : (on >> row & 1) << 4;
             const uint32_t to = (D == 128 ? dst ^ (64 * (i & 1)) : dst) + kRows * i * D;     // rows 4 to 7 of 8: piece ^ 4
-            auto from = [&](const unsigned char* src, uint64_t off) {
-                const unsigned char* a = src + 16 * (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)off, row);
-                if (p.far) a += (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)(off >> 32), row) << 36;
-                return a;
-            };
-            const unsigned char* k = from(k_src, k_off);
+            const unsigned char *k, *v;
+            if (kAll) {
+                const uint32_t o = __shfl_sync(0xffffffffu, k_off, row);
+                k = k_src + 16 * (uint64_t)o;
+                v = v_src + 16 * (uint64_t)(one_step ? o : __shfl_sync(0xffffffffu, v_off, row));
+            } else {
+                const uint64_t b = __shfl_sync(0xffffffffu, blk, row), in_block = __shfl_sync(0xffffffffu, place, row) * (uint64_t)row16;
+                k = k_src + 16 * (b * p.k_step + in_block);
+                v = v_src + 16 * (b * p.v_step + in_block);
+            }
             copy16(to, k, bytes, policy);
-            copy16(to + R::kSideBytes, one_stride ? v_src + (k - k_src) : from(v_src, v_off), bytes, policy);
+            copy16(to + R::kSideBytes, v, bytes, policy);
         }
     }
     static __device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {
@@ -254,7 +258,7 @@ struct Worker {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) k[u][j] = ldsm(ring + stage * R::kStageBytes + 16 * u * D + at_piece[j]);
+            for (int j = 0; j < D / 32; ++j) k[u][j] = ldsm(((ring + stage * R::kStageBytes + get) ^ 32 * j) + 16 * u * D);
     }
 
     __device__ __forceinline__ void reset(Softmax& st) const {
@@ -329,7 +333,7 @@ struct Worker {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) v[u][j] = ldsm_t(src + R::kSideBytes + 16 * u * D + at_piece[j]);
+            for (int j = 0; j < D / 32; ++j) v[u][j] = ldsm_t(((src + get) ^ 32 * j) + R::kSideBytes + 16 * u * D);
         float ks[2 * U], vs[2 * U];            // of tokens g, 8 + g, ..
         floats(src + 2 * R::kSideBytes + 8 * U * g, ks);
         floats(src + 2 * R::kSideBytes + 4 * R::kTokens + 8 * U * g, vs);
@@ -487,6 +491,8 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
         if (c.num_gpu_blocks > 1 && (c.k_block_stride < block || c.v_block_stride < block || c.k_scale_stride < c.num_kv_heads ||
                                      c.v_scale_stride < c.num_kv_heads))
             return "a pool's block stride is smaller than a block, or its scales' than a block's";
+        if (std::max(c.k_block_stride, c.v_block_stride) >> 36 || std::max(c.k_scale_stride, c.v_scale_stride) >> 32)
+            return "blocks lie 2^36 bytes apart or more, or scales 2^32 floats";
         if (!on_bytes(c.k_scale, 0, 4) || !on_bytes(c.v_scale, 0, 4)) return "scales must be on 4-byte boundaries";
         if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
         return nullptr;
@@ -494,8 +500,8 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
     const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tiling_of, sms_here, pools, refuse, &p, &y, &may_cut);
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
-    p.k_block_stride = c.k_block_stride, p.v_block_stride = c.v_block_stride;
-    p.k_scale_stride = c.k_scale_stride, p.v_scale_stride = c.v_scale_stride;
+    p.k_step = (uint32_t)(c.k_block_stride >> 4), p.v_step = (uint32_t)(c.v_block_stride >> 4);
+    p.k_scale_step = (uint32_t)c.k_scale_stride, p.v_scale_step = (uint32_t)c.v_scale_stride;
     p.far = (double)c.num_gpu_blocks * (double)std::max(c.k_block_stride, c.v_block_stride) >= 68719476736.0;   // 2^36
     cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e;
