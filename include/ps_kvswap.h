@@ -584,7 +584,7 @@ typedef struct ps_quant_attn_args {
 } ps_quant_attn_args;
 
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
- * scale.  Codes are exact in the products; a query's values are to within 2^-22 of the largest of their head.  Scores,
+ * scale.  Codes are exact in the products; a query's values are to within 2^-21 of the largest of their head.  Scores,
  * softmax and sums are in 32 bits; for the product with V a softmax weight times its token's value scale is an fp16
  * number next to the largest value scale that the row has met (of a scale 2^-20 of that one weights still have 2 bits), and for
  * results in fp16 the sum of two.

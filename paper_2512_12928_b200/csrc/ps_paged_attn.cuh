@@ -169,7 +169,6 @@ struct Part {
     int32_t lo, count, tiles;                // tiles [lo, lo + count) of the segment's
     int32_t base;                            // place of the segment's first tile
 };
-constexpr int kParts = 8;                    // of a warp between the request of a tile and the end of its attention
 
 // The tiles of a CTA's share, one after the other, as they are requested.
 struct Walk {
@@ -263,8 +262,8 @@ paged_attn_kernel(const __grid_constant__ AttnParams p) {
     __shared__ int sh_sum[kMaxWarps];
     __shared__ int4 sh_begin;          // where the share begins: row, chunk, tile; the row's length
     __shared__ int sh_place;
+    constexpr int kParts = R::kStages + 1;   // those whose tiles are in the ring, or being attended, and one entered
     __shared__ Part sh_parts[kMaxWarps][kParts];
-    static_assert(R::kStages + 1 <= kParts, "parts in the ring, one being attended and one entered");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nwarps = blockDim.x >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -555,7 +554,7 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads, 3)
+__global__ void __launch_bounds__(kJoinThreads, 4)
 paged_join_kernel(const __grid_constant__ AttnParams p) {
     using J = Joiner<T, D>;
     constexpr int kLanes = J::kLanes, kWarps = kJoinThreads / 32;
@@ -575,7 +574,7 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 1
     for (int item = first; wide && item < j.per; item += sharers) {
         if (!j.set(cut, item)) continue;
-        constexpr int kSlices = kJoinThreads / kLanes, kAhead = 6;
+        constexpr int kSlices = kJoinThreads / kLanes, kAhead = 4;
         const int lane = tid % kLanes, slice = tid / kLanes, parts = j.cut.z;
         float4 x[kAhead];
         j.request(x, slice, kSlices, lane);
@@ -623,7 +622,7 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll 1
     for (int item = first * kWarps + warp; !wide && item < j.per; item += sharers * kWarps) {
         if (!j.set(cut, item)) continue;
-        constexpr int kSlices = 32 / kLanes, kAhead = 8 / kSlices;
+        constexpr int kSlices = 32 / kLanes, kAhead = 4 / kSlices;
         const int lane = (tid & 31) % kLanes, slice = (tid & 31) / kLanes, parts = j.cut.z;
         float4 x[kAhead];
         j.request(x, slice, kSlices, lane);
@@ -723,7 +722,8 @@ template <typename W1, typename W2>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
     cudaError_t e = y.nt == 1 ? launch_main<W1>(p, y, s) : launch_main<W2>(p, y, s);
     if (e == cudaSuccess && may_cut) {
-        const dim3 grid((unsigned)((y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
+        // at most as many CTAs as four an SM: a second round would begin only when the first has waited for the main kernel
+        const dim3 grid((unsigned)std::min(4, (y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
         e = ps::launch_dependent(paged_join_kernel<typename W1::Type, W1::kDim>, grid, dim3(kJoinThreads), (size_t)y.ctas * 2 * sizeof(float), s, p);
     }
     return e;

@@ -60,13 +60,15 @@ __device__ __forceinline__ void mma_s8(int32_t (&d)[4], const uint4& a, uint32_t
 }
 
 // Tiles of 16 U tokens, and as many bytes on their way for either head size.
-template <int D, int U, int Warps>
+template <int D, int NT, int U, int Warps>
 struct Ring {
     static constexpr int kTokens = 16 * U;                   // of a tile
     static constexpr int kRowBytes = D;
     static constexpr int kSideBytes = kTokens * kRowBytes;   // keys, then values, then their scales
-    static constexpr int kStageBytes = 2 * kSideBytes + 2 * kTokens * (int)sizeof(float);
-    static constexpr int kStages = (D == 128 ? 6 : 12) * 8 / (Warps * U);
+    static constexpr int kTileBytes = 2 * kSideBytes + 2 * kTokens * (int)sizeof(float);
+    static constexpr int kStateBytes = 8 * NT * D * (int)sizeof(float);      // a stage takes a unit's sums where a segment ends
+    static constexpr int kStageBytes = kTileBytes > kStateBytes ? kTileBytes : kStateBytes;
+    static constexpr int kStages = (Warps == 16 ? 13056 : 26112) / kStageBytes;
     static constexpr int kWarpBytes = kStages * kStageBytes;
 };
 
@@ -82,7 +84,7 @@ constexpr int groups_of(int dim, int nt) { return nt == 1 && dim == 128 ? 1 : 2;
 template <typename T, typename C, int D, int NT>
 struct Worker {
     static constexpr int U = groups_of(D, NT), kWarps = warps_of(NT);
-    using Stages = Ring<D, U, kWarps>;
+    using Stages = Ring<D, NT, U, kWarps>;
     using R = Stages;
     using Type = T;
     using Softmax = QuantState<D, NT>;
@@ -137,7 +139,7 @@ struct Worker {
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 // 2^(top - e) for a magnitude of 2^e, and its inverse: both are normal numbers
-                constexpr int kTop = C::kDigits ? 21 : 13;
+                constexpr int kTop = C::kDigits ? 20 : 13;
                 const uint32_t bits = __float_as_uint(Num<T>::unpack(most).x);
                 const int e = min(max((int)(bits >> 23), kTop + 1), 254);
                 up = __uint_as_float((uint32_t)(254 + kTop - e) << 23);
@@ -146,24 +148,27 @@ struct Worker {
             }
             factor[t][0] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c);
             factor[t][1] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c + 4);
+            if constexpr (C::kDigits) {
+                // x up as a whole number n, |n| <= 2^21: its digits d, n = d0 + 2^8 d1 + 2^16 d2, d0 and d1 from -128 to 127, are the
+                // bytes of n + 0x208080 less 128, 128 and 32
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-                const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
-                uint32_t* to = q[t][j / 2];
-                if constexpr (C::kDigits) {
-                    // x up as a whole number n, |n| <= 2^22: its digits d, n = d0 + 2^8 d1 + 2^16 d2, from -128 to 127, are the bytes
-                    // of n + 0x808080 with their top bits turned
-                    auto digits = [&](float x) {
-                        return (__float_as_uint(fmaf(x, up, 12582912.f)) - 0x4b400000u + 0x00808080u) ^ 0x00808080u;
-                    };
-                    const uint32_t n0 = digits(a.x), n1 = digits(a.y), n2 = digits(e.x), n3 = digits(e.y);
+                for (int j = 0; j < D / 16; ++j) {
+                    const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
+                    auto whole = [&](float x) { return __float_as_uint(fmaf(x, up, 8388608.f + 0x208080)); };
+                    const uint32_t n0 = whole(a.x), n1 = whole(a.y), n2 = whole(e.x), n3 = whole(e.y);
                     const uint32_t lo = __byte_perm(n0, n1, 0x5140), lo2 = __byte_perm(n2, n3, 0x5140);      // bytes 0 and 1 of two
-                    to[j % 2] = __byte_perm(lo, lo2, 0x5410);
-                    to[2 + j % 2] = __byte_perm(lo, lo2, 0x7632);
-                    to[4 + j % 2] = __byte_perm(__byte_perm(n0, n1, 0x0062), __byte_perm(n2, n3, 0x0062), 0x5410);
-                } else {
-                    to[2 * (j % 2)] = N::pack(a.x * up, a.y * up);
-                    to[2 * (j % 2) + 1] = N::pack(e.x * up, e.y * up);
+                    uint32_t* to = q[t][j / 2] + j % 2;
+                    to[0] = __byte_perm(lo, lo2, 0x5410) ^ 0x80808080u;
+                    to[2] = __byte_perm(lo, lo2, 0x7632) ^ 0x80808080u;
+                    // a byte of at most 0x41: + 0x60, and the top bit turned is - 0x80
+                    to[4] = (__byte_perm(__byte_perm(n0, n1, 0x0062), __byte_perm(n2, n3, 0x0062), 0x5410) + 0x60606060u) ^ 0x80808080u;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
+                    q[t][j / 2][2 * (j % 2)] = N::pack(a.x * up, a.y * up);
+                    q[t][j / 2][2 * (j % 2) + 1] = N::pack(e.x * up, e.y * up);
                 }
             }
         }

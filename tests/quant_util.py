@@ -92,7 +92,7 @@ def quant_attn_want(kpool, vpool, ks, vs, q, tables, ctx, window=0, scale=None):
     Over that, a weight times its value scale is a product in 32 bits (2^-24), held as one fp16 number for results in bf16 (off by
     2^-11 of itself) and as the sum of two for results in fp16 (2^-22), or by 2^-25 where fp16 has no smaller steps; largest weights are 2^8 or more and refer to the power of two below
     the row's largest value scale, so that the latter is 2^-33 of a token's largest possible value, times the tokens.  A score
-    is multiplied by two factors (2^-23, within what attn_want gives it).  A query's values are held to 2^-22 of their head's
+    is multiplied by two factors (2^-23, within what attn_want gives it).  A query's values are held to 2^-21 of their head's
     largest: a score is off by that times the key's magnitudes, and a result by twice as much of its largest value."""
     K = kpool.double() * ks.double()[:, None, :, None]
     V = vpool.double() * vs.double()[:, None, :, None]
@@ -105,7 +105,7 @@ def quant_attn_want(kpool, vpool, ks, vs, q, tables, ctx, window=0, scale=None):
             at = torch.tensor(ids, device="cuda")
             top = vs[at].abs().amax(0).double().cpu().numpy() * TOP[vpool.dtype]
             tol[b] += np.repeat(top, G)[:, None] * (n * 2.0 ** -33)
-            ds = np.abs(f64(q[b])).max(-1) * np.repeat(K[at].abs().sum(-1).amax((0, 1)).cpu().numpy(), G) * 2.0 ** -22
+            ds = np.abs(f64(q[b])).max(-1) * np.repeat(K[at].abs().sum(-1).amax((0, 1)).cpu().numpy(), G) * 2.0 ** -21
             ds *= q.shape[2] ** -0.5 if scale is None else abs(scale)
             tol[b] += (2 * ds * np.repeat(V[at].abs().amax((0, 1, 3)).cpu().numpy(), G))[:, None]
             tol_lse[b] += ds
