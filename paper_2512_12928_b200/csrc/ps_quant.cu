@@ -118,13 +118,15 @@ struct QuantParams {
     int64_t num_slots;
     uint64_t block_magic;
     int32_t tokens, hkv, dim, block_size, sides, tok_per_cta;
+    int32_t row_vecs, row_magic, row_step, piece_step;      // vectors of a head's row; 2^16 / row_vecs rounded up; 32 vectors on
 };
 
 // ------------------------------------------------------------------------------------------------ append
 
 // A segment is a run of tokens that go to one block.  A warp has one head of keys or values, and the segments that begin
-// among the CTA's n tokens, which it finds for itself: no barrier, and nothing in shared memory.
-template <typename T, typename C, int W, int kCtas>
+// among the CTA's n tokens, which it finds for itself: no barrier, and nothing in shared memory.  kEven: a row's vectors
+// divide a warp's lanes, so that a lane has the same piece of every row it has.
+template <typename T, typename C, int W, bool kEven, int kCtas>
 __global__ void __launch_bounds__(kThreads, kCtas)
 quant_append_kernel(const __grid_constant__ QuantParams p) {
     constexpr int kHold = W == 16 ? 4 : 8;   // vectors of a lane that stay in registers between maximum and rounding
@@ -135,18 +137,17 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
     const int head = unit < p.hkv ? unit : unit - p.hkv;
     const Side& side = p.side[unit < p.hkv ? 0 : 1];
     // The vectors of a segment, rows first: this lane has every 32nd.
-    const int row_vecs = p.dim / W;
-    const int row_step = 32 / row_vecs, piece_step = 32 - row_step * row_vecs;
-    const int row0 = lane / row_vecs, piece0 = lane - row0 * row_vecs;
+    const int row0 = lane * p.row_magic >> 16, piece0 = lane - row0 * p.row_vecs;
     auto next = [&](int& row, int& piece) {
-        row += row_step;
-        piece += piece_step;
-        if (piece >= row_vecs) {
-            piece -= row_vecs;
+        row += p.row_step;
+        if (kEven) return;
+        piece += p.piece_step;
+        if (piece >= p.row_vecs) {
+            piece -= p.row_vecs;
             ++row;
         }
     };
-    const int64_t place_bytes = (int64_t)p.hkv * p.dim;
+    const uint32_t place_bytes = p.hkv * p.dim;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // 32 tokens from the one before on, one a lane: what begins among the CTA's mostly ends there too
@@ -157,7 +158,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         slot = -1;
     }
     const int32_t block = slot < 0 ? -1 : (int32_t)block_of(slot, p.block_magic);
-    const int32_t my_place = (int32_t)(slot - (int64_t)block * p.block_size);
+    const int32_t my_place = (int32_t)slot - block * p.block_size;          // modulo 2^32: a place is less
     const int32_t before = __shfl_up_sync(0xffffffffu, block, 1);
     uint32_t starts = __ballot_sync(0xffffffffu, lane > 0 && lane <= p.tok_per_cta && block >= 0 && block != before);
     for (; starts; starts &= starts - 1) {
@@ -165,9 +166,10 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         const int32_t blk = __shfl_sync(0xffffffffu, block, first);
         const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
         int len = (other ? __ffs(other) - 1 : 32) - first;
-        const int64_t block_begin = (int64_t)blk * p.block_size;
         bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && my_place == 0);
-        while (first + len >= 32) {          // it goes on
+        const bool ends = first + len < 32;  // among the lanes' tokens
+        const int64_t block_begin = (int64_t)blk * p.block_size;
+        while (!ends) {                      // it may go on
             const int32_t u = t0 - 1 + first + len + lane;
             const int64_t s = u < p.tokens ? p.slots[u] : -1;
             const uint32_t out = __ballot_sync(0xffffffffu, s < block_begin || s - block_begin >= p.block_size);
@@ -176,9 +178,11 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             len += more;
             if (more < 32) break;
         }
-        const T* src = (const T*)side.rows + (t0 - 1 + first) * side.row_stride + (int64_t)head * p.dim;
+        const int32_t token0 = t0 - 1 + first;
+        const T* src = (const T*)side.rows + token0 * side.row_stride + (int64_t)head * p.dim;
         unsigned char* pool = side.pool + blk * side.block_stride + (int64_t)head * p.dim;
         float* scale_at = side.scale + blk * side.scale_stride + head;
+        auto from = [&](int row, int piece) { return src + (int64_t)row * (int32_t)side.row_stride + piece * W; };
         const float old = begun ? 0.f : *scale_at;
         Vec<2 * W> held[kHold];
         uint32_t most = 0;                   // of both halves of a word
@@ -190,7 +194,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         int row = row0, piece = piece0;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) {
-            if (row < len) held[i].load(src + row * side.row_stride + piece * W);
+            if (row < len) held[i].load(from(row, piece));
             next(row, piece);
         }
         int row2 = row0, piece2 = piece0;
@@ -201,7 +205,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         }
         while (row < len) {
             Vec<2 * W> x;
-            x.load(src + row * side.row_stride + piece * W);
+            x.load(from(row, piece));
             meet(x);
             next(row, piece);
         }
@@ -214,7 +218,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             int q = row0, c = piece0;
             while (q < p.block_size) {
                 Vec<W> x;
-                unsigned char* at = pool + q * place_bytes + c * W;
+                unsigned char* at = pool + (uint32_t)q * (uint64_t)place_bytes + c * W;
                 x.load(at);
 #pragma unroll
                 for (int i = 0; i < (W + 3) / 4; ++i) x.w[i] = C::pack(C::unpack(x.w[i]), f);
@@ -223,31 +227,29 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             }
             __syncwarp();                    // the new tokens' codes come on top
         }
-        auto put = [&](const Vec<2 * W>& x, int32_t place, int piece) {
+        auto put = [&](const Vec<2 * W>& x, uint32_t place, int piece) {
             Vec<W> y;
 #pragma unroll
             for (int i = 0; i < (W + 3) / 4; ++i) {
                 const float2 lo = Num<T>::unpack(x.w[2 * i]), hi = W > 1 ? Num<T>::unpack(x.w[2 * i + (W > 1)]) : lo;
                 y.w[i] = C::pack(make_float4(lo.x, lo.y, hi.x, hi.y), r);
             }
-            y.store(pool + place * place_bytes + piece * W);
+            y.store(pool + place * (uint64_t)place_bytes + piece * W);
         };
-        auto place_of = [&](int row) {       // of a row that is not among the lanes' tokens
-            return (int32_t)(p.slots[t0 - 1 + first + row] - block_begin);
-        };
+        auto place_of = [&](int row) { return (uint32_t)(p.slots[token0 + row] - block_begin); };
         row = row0, piece = piece0;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) {
-            int32_t place = __shfl_sync(0xffffffffu, my_place, first + row);
+            uint32_t place = __shfl_sync(0xffffffffu, my_place, first + row);
             if (row < len) {
-                if (first + row >= 32) place = place_of(row);
+                if (!ends && first + row >= 32) place = place_of(row);
                 put(held[i], place, piece);
             }
             next(row, piece);
         }
         while (row < len) {
             Vec<2 * W> x;
-            x.load(src + row * side.row_stride + piece * W);
+            x.load(from(row, piece));
             put(x, place_of(row), piece);
             next(row, piece);
         }
@@ -336,6 +338,7 @@ struct Given {                    // one side as the caller gave it
 const char* plan(const ps_quant_cache& c, const Given (&given)[2], const int64_t* slots, int32_t* status, int32_t tokens, int32_t dtype,
                  bool rows_written, QuantParams* params) {
     if (tokens < 0 || c.block_size <= 0 || c.num_gpu_blocks <= 0) return "negative count or non-positive size";
+    if (tokens > INT32_MAX - 1024) return "too many tokens";   // so that what a warp looks ahead cannot wrap
     if (c.num_kv_heads <= 0 || c.num_kv_heads > kMaxHeads || c.head_dim <= 0 || c.head_dim > kMaxDim)
         return "num_kv_heads must be from 1 to 1024, head_dim from 1 to 512";
     if (dtype != PS_DTYPE_BF16 && dtype != PS_DTYPE_FP16) return "dtype must be PS_DTYPE_BF16 or PS_DTYPE_FP16";
@@ -350,6 +353,7 @@ const char* plan(const ps_quant_cache& c, const Given (&given)[2], const int64_t
         if (c.num_gpu_blocks > 1 && (g.block_stride < block || g.scale_stride < c.num_kv_heads))
             return "a pool's block stride is smaller than a block, or its scales' than a block's";
         if (reinterpret_cast<uintptr_t>(g.scale) % 4 || reinterpret_cast<uintptr_t>(g.rows) % 2) return "scales or rows are not aligned to their elements";
+        if (tokens > 1 && (g.row_stride > INT32_MAX || g.row_stride < INT32_MIN)) return "rows lie 2^31 elements apart or more";
         if (rows_written && tokens > 1 && g.row_stride < width && -g.row_stride < width) return "rows of k_out or v_out overlap";
         sets[p.sides][0] = {g.rows, g.row_stride, width, 2};
         sets[p.sides][1] = {g.pool, g.block_stride, block, 1};
@@ -395,11 +399,17 @@ cudaError_t launch_append(QuantParams p, cudaStream_t s) {
     p.tok_per_cta = 1;
     while (2 * p.tok_per_cta <= std::min(p.block_size, 16) && (int64_t)p.tokens / (2 * p.tok_per_cta) * units >= 148 * 16) p.tok_per_cta *= 2;
     const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((units + warps - 1) / warps));
+    const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1;
+    p.row_vecs = p.dim / w;
+    p.row_magic = (65536 + p.row_vecs - 1) / p.row_vecs;     // exact for the 32 lanes and up to 512 vectors
+    p.row_step = 32 / p.row_vecs;
+    p.piece_step = 32 % p.row_vecs;
+    const bool even = p.piece_step == 0, few = p.tok_per_cta == 1;
     auto launch = [&](auto kernel) { return ps::launch_dependent(kernel, grid, dim3(kThreads), 0, s, p); };
-    const bool few = p.tok_per_cta == 1;
-    if (fits(p, 16)) return few ? launch(quant_append_kernel<T, C, 16, 2>) : launch(quant_append_kernel<T, C, 16, 3>);
-    if (fits(p, 8)) return few ? launch(quant_append_kernel<T, C, 8, 2>) : launch(quant_append_kernel<T, C, 8, 3>);
-    return launch(quant_append_kernel<T, C, 1, 2>);
+    if (w == 16 && even) return few ? launch(quant_append_kernel<T, C, 16, true, 2>) : launch(quant_append_kernel<T, C, 16, true, 3>);
+    if (w == 16) return few ? launch(quant_append_kernel<T, C, 16, false, 2>) : launch(quant_append_kernel<T, C, 16, false, 3>);
+    if (w == 8) return launch(quant_append_kernel<T, C, 8, false, 2>);
+    return launch(quant_append_kernel<T, C, 1, false, 2>);
 }
 template <typename T, typename C>
 cudaError_t launch_read(QuantParams p, cudaStream_t s) {
