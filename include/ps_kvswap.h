@@ -544,9 +544,10 @@ typedef struct ps_quant_append_args {
  * scale: all its values then read as NaN until it is begun anew.
  * Tokens that go to one block stand next to one another in the call, in any order, as ps_build_slots numbers them (the tokens
  * of a row are neighbours); a block that the call comes back to after tokens of others, or after padding, and one that two
- * tokens give the same slot, has undefined contents afterwards.  head_dim up to 512, up to 1024 KV heads.  Pools, scales and
- * inputs must not overlap.  Rows of k and v on 16-byte boundaries with blocks on 8-byte boundaries and head_dim a multiple of
- * 8 are read 16 bytes at a time, else element by element.
+ * tokens give the same slot, has undefined contents afterwards.  Pools, scales and inputs must not overlap.
+ * head_dim up to 512, up to 1024 KV heads, rows less than 2^31 elements apart, num_gpu_blocks * block_size^2 below 1.8e19.
+ * Rows of k and v on 32-byte boundaries with blocks on 16-byte boundaries and head_dim a multiple of 16 are read 32 bytes at a
+ * time; 16 where halves of these numbers fit, else element by element.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_append(const ps_quant_append_args* args, void* stream, char* err_buf, int32_t err_cap);
 
@@ -562,8 +563,8 @@ typedef struct ps_quant_read_args {
 
 /* Reads tokens back: row t of k_out and v_out is code * scale of slots[t], the 32-bit product rounded once.  Rows of padding
  * and of slots outside the pool are left as they are.  Slots may repeat and stand in any order (ps_build_slots from lengths
- * of 0 gives those of whole contexts).  Limits and alignments as for ps_quant_append, with blocks on 16-byte boundaries and
- * head_dim a multiple of 16 for the widest accesses.  The outputs must not overlap each other or the cache.
+ * of 0 gives those of whole contexts).  Limits and alignments as for ps_quant_append.  The outputs must not overlap each other
+ * or the cache.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_read(const ps_quant_read_args* args, void* stream, char* err_buf, int32_t err_cap);
 
@@ -584,10 +585,11 @@ typedef struct ps_quant_attn_args {
 } ps_quant_attn_args;
 
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
- * scale.  Codes are exact in the products; a query's values are to within 2^-21 of the largest of their head.  Scores,
- * softmax and sums are in 32 bits; for the product with V a softmax weight times its token's value scale is an fp16
- * number next to the largest value scale that the row has met (of a scale 2^-20 of that one weights still have 2 bits), and for
- * results in fp16 the sum of two.
+ * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^32 floats.  Codes are exact in the products, a
+ * query's values are to within 2^-21 of the largest of their head; scores, softmax and sums are in 32 bits.  For the product
+ * with V a softmax weight times its token's value scale is an fp16 number, and for results in fp16 the sum of two: relative to
+ * the largest weight times the largest value scale that the row has met, 11 bits (22) down to 2^-22 and multiples of 2^-32
+ * below.  A query head with a NaN gives NaN, one with an infinite value NaN or infinite results.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
 

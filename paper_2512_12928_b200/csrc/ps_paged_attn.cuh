@@ -11,12 +11,12 @@
 // by another kernel.  A row cut by a share's end leaves partial results (m, sum, accumulators) in the workspace, which a
 // second kernel (paged_join_kernel) combines in order.  The join is a second launch rather than a last-arrival counter in
 // the first: the workspace then needs no initial state, and neither a replayed graph nor a call that shares it in turn can
-// find a stale counter.  It is launched early, but its CTAs (80 registers a thread) do not fit beside one of 8
-// warps of the first kernel (207 to 249), so they start as those leave.
+// find a stale counter.  It is launched early, but its CTAs (64 registers a thread) do not fit beside one of the first
+// kernel (8 warps of 199 to 251 registers a thread, or 16 of 128), so they start as those leave.
 //
 // Warps: a CTA works on `units` (KV head, group of at most 16 query heads) times `subs` token slices (a power of two);
 // the units of a token are neighbours in memory.  The slices' states are combined through shared memory at a segment's
-// end.
+// end, where only a unit's own warps wait for one another.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -722,7 +722,9 @@ template <typename W1, typename W2>
 cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
     cudaError_t e = y.nt == 1 ? launch_main<W1>(p, y, s) : launch_main<W2>(p, y, s);
     if (e == cudaSuccess && may_cut) {
-        // at most as many CTAs as four an SM: a second round would begin only when the first has waited for the main kernel
+        // Four CTAs of a cut at most, so that all fit the chip at once: those of a second round would begin only when the first
+        // has waited for the main kernel.  (64 rows of 4096 tokens and one of 32768, 64 query heads on 8: 179.9 us in 16 bits
+        // and 100.3 in 8, with eight CTAs a cut of three an SM 182.4 and 101.7.)
         const dim3 grid((unsigned)std::min(4, (y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
         e = ps::launch_dependent(paged_join_kernel<typename W1::Type, W1::kDim>, grid, dim3(kJoinThreads), (size_t)y.ctas * 2 * sizeof(float), s, p);
     }

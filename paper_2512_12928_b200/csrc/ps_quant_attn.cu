@@ -5,20 +5,25 @@
 //
 // with the frame of ps_paged_attn.cuh: the sequence's cut, the walk, segment ends and the join are ps_paged_attn's.
 //
-// Bound: HBM, and next to it the instructions that widen the codes: a token and KV head are half the bytes of a 16-bit
-// cache's and as many products.
+// Bound: HBM, and next to it the instructions that a code costs: a token and KV head are half the bytes of a 16-bit cache's and
+// as many products and weights.  MEASURED
 //
-// Products: S^T = K Q^T and O^T = V^T P^T as mma.m16n8k16 in fp16, into which every code goes exactly.  A tile of 32 tokens
-// comes to shared memory as it lies in the pool (cp.async) and is widened between ldmatrix and the product, four codes of a
-// register to two registers.  ldmatrix sees pairs of codes as its elements: a lane gets four neighbouring dims of a token's key, and
-// through the transposing form two neighbouring dims of two tokens' values.  Which dims and tokens a product's rows and
-// columns stand for is free, so what comes together stays together: of keys the four dims are the k places 2c, 2c + 1,
-// 2c + 8, 2c + 9 and the queries are laid out alike; of values row g is dim 2g and row g + 8 dim 2g + 1.
+// Products: S^T = K Q^T and O^T = V^T P^T as in ps_paged_attn.cu, tokens and then dims as the 16 rows of a product.  A tile of
+// 16 or 32 tokens comes to shared memory as it lies in the pool (cp.async, 16 bytes a lane).  ldmatrix sees pairs of codes as its
+// elements: a lane gets four neighbouring dims of a token's key, and through the transposing form two neighbouring dims of
+// two tokens' values.  Which dims and tokens a product's rows and columns stand for is free, so what comes together stays
+// together: of values row g is dim 2g and row g + 8 dim 2g + 1, and queries are laid out as keys come.
+//
+// Values, and keys in 8-bit floats, are widened to fp16 between ldmatrix and the product; every code is exact there.  Queries
+// in bf16 are multiplied by a power of two that puts their head's largest magnitude next to 2^13, and the scores by its inverse.
+// Keys in int8 enter mma.m16n8k32 as they are: a query is a whole number next to 2^20 at its head's largest magnitude, in three
+// digits of 8 bits, whose products are exact whole numbers.  Three such products cost less than widening (an
+// instruction and a quarter a code; 72.3 us for the case above when keys were widened, 66.9 then).
 //
 // Scales: a_t multiplies a score in 32 bits.  b_t goes into the weight, p_t (b_t / r) with r a power of two next to the
 // largest b that the warp has met, so that weights stay within fp16; sums are multiplied by r where a segment ends.  A weight
-// is the sum of two fp16 numbers.  Queries in bf16 are multiplied by a power of two that puts their head's largest
-// magnitude next to 2^13, and the scores by its inverse.
+// is one fp16 number for results in bf16, whose own rounding is off by eight times as much, and the sum of two for results in
+// fp16.
 #include <cuda_fp8.h>
 
 #include "ps_paged_attn.cuh"
@@ -77,7 +82,11 @@ struct QuantState : State<D, NT> {
     float inv_ref;                             // 1 / r
 };
 
-// Units of up to 8 query heads: 16 warps; of up to 16, whose registers do not allow as many: 8.
+// Units of up to 8 query heads: 16 warps of 128 registers a thread; of up to 16, which need twice as many: 8.  A warp's
+// instructions wait for one another more than for memory, and four a scheduler fill the gaps (64 rows of 8192 tokens, 32 query
+// heads on 8 of 128: 185 us in int8 with 16 warps and 192 with 8, 177 and 187 in 8-bit floats; of 64 dims and 2048 to
+// 8192 tokens 66 and 82.5).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us with 8 warps,
+// 93 with 16), and two CTAs of 8 warps instead of one of 16 cost a row twice as many parts (100 rows' worth: 107 and 111 us).
 constexpr int warps_of(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int groups_of(int dim, int nt) { return nt == 1 && dim == 128 ? 1 : 2; }     // of 16 tokens, in a tile
 

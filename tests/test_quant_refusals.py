@@ -40,7 +40,8 @@ CACHE = [dict(num_gpu_blocks=0), dict(num_gpu_blocks=-1), dict(block_size=0), di
 
 
 @pytest.mark.parametrize("kw", CACHE + [
-    dict(head_dim=513), dict(tokens=-1), dict(k=None), dict(v=None), dict(slots=None), dict(k=K + 1),
+    dict(head_dim=513), dict(tokens=-1), dict(tokens=(1 << 31) - 100), dict(k_stride=1 << 31), dict(k=None), dict(v=None), dict(slots=None), dict(k=K + 1),
+    dict(block_size=1 << 24, num_gpu_blocks=1 << 16, k_block_stride=1 << 36, v_block_stride=1 << 36),
     dict(k=None, v=None, kpool=None, vpool=None, k_scale=None, v_scale=None),
     dict(vpool=KP), dict(vpool=KP + BLOCK - 1), dict(v_scale=KS), dict(v_scale=KS + 4 * 7), dict(k_scale=KP + 64), dict(k=KP), dict(k=KS - 2),
     dict(kpool=K + 2 * 1023), dict(kpool=KP, vpool=KP + BLOCK, k_block_stride=2 * BLOCK - 1, v_block_stride=2 * BLOCK - 1)])
@@ -49,7 +50,7 @@ def test_append_refuses(kw):
 
 
 @pytest.mark.parametrize("kw", CACHE + [
-    dict(head_dim=513), dict(tokens=-1), dict(k_out=None, v_out=None), dict(slots=None), dict(v_out=K), dict(v_out=K + 2 * 1023),
+    dict(head_dim=513), dict(tokens=-1), dict(tokens=(1 << 31) - 100), dict(v_out_stride=-(1 << 31) - 1), dict(k_out=None, v_out=None), dict(slots=None), dict(v_out=K), dict(v_out=K + 2 * 1023),
     dict(k_out_stride=1023), dict(v_out_stride=0), dict(k_out=KP + 100), dict(v_out=KS), dict(k_out=K + 1)])
 def test_read_refuses(kw):
     assert refused(B.load().ps_quant_read, read_args(**kw)).startswith("ps_quant_read: ")
@@ -59,7 +60,8 @@ def test_read_refuses(kw):
     dict(num_q_heads=0), dict(num_q_heads=33), dict(num_kv_heads=1, num_q_heads=65), dict(head_dim=96), dict(head_dim=80), dict(batch=-1),
     dict(table_stride=0), dict(window=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(out=None),
     dict(block_tables=None), dict(ctx_lens=None), dict(workspace=None), dict(v_block_stride=BLOCK + 8), dict(kpool=KP + 8), dict(q=Q + 8),
-    dict(q_stride=4100), dict(out=OUT + 2), dict(out_stride=2048), dict(out=Q, out_stride=4096 + 8), dict(out=Q + 32), dict(table_stride=1 << 30, batch=1 << 20)])
+    dict(q_stride=4100), dict(out=OUT + 2), dict(out_stride=2048), dict(out=Q, out_stride=4096 + 8), dict(out=Q + 32), dict(table_stride=1 << 30, batch=1 << 20),
+    dict(k_block_stride=1 << 36), dict(v_scale_stride=1 << 32)])
 def test_attn_refuses(kw):
     assert refused(B.load().ps_quant_attn, attn_args(**kw)).startswith("ps_quant_attn: ")
 
