@@ -7,7 +7,7 @@
 // one vote instead of a maximum over the lanes; weights stay below 2^kSlack and sums in 32 bits lose nothing by it.
 //
 // Work: the rows' tiles form one sequence (with two places more for each row's start and end, which cost about two tiles'
-// time) that is cut into equal shares, one per CTA, from the lengths each CTA reads itself: no plan is made on the host or
+// time) that is cut into equal shares, one per CTA (one or two an SM), from the lengths each CTA reads itself: no plan is made on the host or
 // by another kernel.  A row cut by a share's end leaves partial results (m, sum, accumulators) in the workspace, which a
 // second kernel (paged_join_kernel) combines in order.  The join is a second launch rather than a last-arrival counter in
 // the first: the workspace then needs no initial state, and neither a replayed graph nor a call that shares it in turn can
@@ -249,7 +249,7 @@ __device__ __forceinline__ void slices_meet(const AttnParams& p, int unit_in_cta
 }
 
 template <typename W>
-__global__ void __launch_bounds__(W::kWarps * 32, 1)
+__global__ void __launch_bounds__(W::kWarps * 32, W::kCtas)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
     constexpr int kMaxWarps = W::kWarps;
     using R = typename W::Stages;
@@ -645,9 +645,9 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-// Of a kernel: tokens that a warp takes at a time, and most warps of a CTA.
+// Of a kernel: tokens that a warp takes at a time, most warps of a CTA, and CTAs of an SM.
 struct Tiling {
-    int32_t tile, warps;
+    int32_t tile, warps, ctas;
 };
 // How the heads are dealt to warps.
 struct Layout {
@@ -673,7 +673,7 @@ Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, TilingOf t
     y.units = (all + y.chunks - 1) / y.chunks;
     for (y.subs = 1; 2 * y.subs * y.units <= tiling.warps; y.subs *= 2) {}
     for (y.step_log2 = 0; (1 << y.step_log2) < tiling.tile * y.subs; ++y.step_log2) {}
-    y.ctas = sms;                          // the rings take an SM's shared memory
+    y.ctas = tiling.ctas * sms;            // as many as the rings leave shared memory for
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
     y.part_o = 0;

@@ -65,6 +65,7 @@ __device__ __forceinline__ void mma_s8(int32_t (&d)[4], const uint4& a, uint32_t
 }
 
 // Tiles of 16 U tokens, and as many bytes on their way for either head size.
+// Warps: of an SM.
 template <int D, int NT, int U, int Warps>
 struct Ring {
     static constexpr int kTokens = 16 * U;                   // of a tile
@@ -82,18 +83,25 @@ struct QuantState : State<D, NT> {
     float inv_ref;                             // 1 / r
 };
 
-// Units of up to 8 query heads: 16 warps of 128 registers a thread; of up to 16, which need twice as many: 8.  A warp's
+// Warps of an SM: 16 of 128 registers a thread for units of up to 8 query heads, 8 for up to 16, which need twice as many.  A warp's
 // instructions wait for one another more than for memory, and four a scheduler fill the gaps (64 rows of 8192 tokens, 32 query
-// heads on 8 of 128: 185 us in int8 with 16 warps and 192 with 8, 177 and 187 in 8-bit floats; of 64 dims and 2048 to
-// 8192 tokens 66 and 82.5).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us with 8 warps,
-// 93 with 16), and two CTAs of 8 warps instead of one of 16 cost a row twice as many parts (100 rows' worth: 107 and 111 us).
-constexpr int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+// heads on 8 of 128: 185 us in int8 with 16 warps and 192 with 8, 177 and 187 in 8-bit floats; of 64 dims and 2048 to 8192
+// tokens 66 and 82.5).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us with 8 warps, 93
+// with 16).
+// As two CTAs of 8 warps they do not wait for one another where a row ends, but a row has twice as many parts and what lies
+// next to one another is not read at the same time.  Int8 of 128, which is bound by its instructions, gains (1024 to 4096
+// tokens: 63.0 instead of 64.8 us, 200 rows of 10 to 100: 17.7 instead of 19.5); 8-bit floats lose (59.1 and 65), heads of 64 too
+// (62.7 and 65).
+template <typename C>
+constexpr int ctas_of(int dim, int nt) { return C::kDigits && nt == 1 && dim == 128 ? 2 : 1; }
+template <typename C>
+constexpr int warps_of(int dim, int nt) { return nt == 1 ? 16 / ctas_of<C>(dim, nt) : 8; }
 constexpr int groups_of(int dim, int nt) { return nt == 1 && dim == 128 ? 1 : 2; }     // of 16 tokens, in a tile
 
 template <typename T, typename C, int D, int NT>
 struct Worker {
-    static constexpr int U = groups_of(D, NT), kWarps = warps_of(NT);
-    using Stages = Ring<D, NT, U, kWarps>;
+    static constexpr int U = groups_of(D, NT), kWarps = warps_of<C>(D, NT), kCtas = ctas_of<C>(D, NT);
+    using Stages = Ring<D, NT, U, kWarps * kCtas>;
     using R = Stages;
     using Type = T;
     using Softmax = QuantState<D, NT>;
@@ -465,7 +473,8 @@ struct Worker {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-Tiling tiling_of(int32_t dim, int32_t nt) { return {16 * groups_of(dim, nt), warps_of(nt)}; }
+template <typename C>
+Tiling tiling_of(int32_t dim, int32_t nt) { return {16 * groups_of(dim, nt), warps_of<C>(dim, nt), ctas_of<C>(dim, nt)}; }
 
 template <typename T, typename C, int D>
 cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
@@ -487,7 +496,7 @@ cudaError_t sms_here(int* sms) {
 }  // namespace
 
 extern "C" int32_t ps_quant_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes) {
-    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of, sms_here, bytes);
+    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of<Int8>, sms_here, bytes);     // 8-bit floats never have more CTAs
 }
 
 extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap) {
@@ -511,7 +520,8 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
         if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
         return nullptr;
     };
-    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tiling_of, sms_here, pools, refuse, &p, &y, &may_cut);
+    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks},
+                                 c.codes == PS_CODE_INT8 ? tiling_of<Int8> : tiling_of<E4m3>, sms_here, pools, refuse, &p, &y, &may_cut);
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
     p.k_step = (uint32_t)(c.k_block_stride >> 4), p.v_step = (uint32_t)(c.v_block_stride >> 4);
