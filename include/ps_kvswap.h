@@ -585,7 +585,7 @@ typedef struct ps_quant_attn_args {
 } ps_quant_attn_args;
 
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
- * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^32 floats.  Codes are exact in the products, a
+ * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^30 floats.  Codes are exact in the products, a
  * query's values are to within 2^-21 of the largest of their head; scores, softmax and sums are in 32 bits.  For the product
  * with V a softmax weight times its token's value scale is an fp16 number, and for results in fp16 the sum of two: relative to
  * the largest weight times the largest value scale that the row has met, 11 bits (22) down to 2^-22 and multiples of 2^-32

@@ -53,8 +53,9 @@ struct AttnParams {
     int4* cuts;          // [cta]: the segment that this CTA did not finish: {row, chunk, parts, first CTA}; parts 0: none
     int64_t k_block_stride, v_block_stride, q_stride, out_stride;
     const float *k_scale, *v_scale;  // of an 8-bit cache: [block][KV head]
-    uint32_t k_step, v_step, k_scale_step, v_scale_step;      // its blocks, in steps of 16 bytes, and their scales' in floats
-    bool far;                        // a pool's last block begins 2^36 bytes or more behind its first
+    uint32_t k_step, v_step, row_step;         // from block to block and token to token, in steps of 16 bytes
+    uint32_t k_scale_step, v_scale_step;       // from block to block, in bytes
+    bool near;                       // both pools have one step, and 32 bits count a pool's steps
     int64_t room;        // tokens a table row has room for
     uint64_t block_magic;
     int32_t batch, table_stride, num_blocks, block_size, window;
@@ -137,7 +138,8 @@ __device__ __forceinline__ float ex2(float x) {
 
 // t / block_size for 0 <= t < 2^31: magic is 2^64 / block_size rounded up (block_size > 1)
 __device__ __forceinline__ int32_t block_of(int32_t t, const AttnParams& p) {
-    return p.block_size == 1 ? t : (int32_t)__umul64hi((uint64_t)(uint32_t)t, p.block_magic);
+    const uint32_t low = __umulhi((uint32_t)t, (uint32_t)p.block_magic);
+    return p.block_size == 1 ? t : (int32_t)((t * (uint64_t)(uint32_t)(p.block_magic >> 32) + low) >> 32);
 }
 
 // Tokens that are attended of a row of n: [first, end).
@@ -724,7 +726,8 @@ cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cuda
     if (e == cudaSuccess && may_cut) {
         // Four CTAs of a cut at most, so that all fit the chip at once: those of a second round would begin only when the first
         // has waited for the main kernel.  (64 rows of 4096 tokens and one of 32768, 64 query heads on 8: 179.9 us in 16 bits
-        // and 100.3 in 8, with eight CTAs a cut of three an SM 182.4 and 101.7.)
+        // and 100.3 in 8, with eight CTAs a cut of three an SM 182.4 and 101.7.  Where the main kernel has two CTAs an SM, two of
+        // a cut instead of four are no better: 62.8 and 63.0 us for 64 rows of 1024 to 4096, but 18.4 and 17.6 for 200 short ones.)
         const dim3 grid((unsigned)std::min(4, (y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
         e = ps::launch_dependent(paged_join_kernel<typename W1::Type, W1::kDim>, grid, dim3(kJoinThreads), (size_t)y.ctas * 2 * sizeof(float), s, p);
     }

@@ -35,9 +35,9 @@ struct Int8 {
     static constexpr bool kDigits = true;                // keys are multiplied as they are
     // a byte b with its top bit turned is k + 128; as the low bits of 0x6400 = 1024 that is 1152 + k, exactly
     static __device__ __forceinline__ uint32_t widen(uint32_t x) {
-        const uint32_t v = (x & 0x00ff00ffu) ^ 0x64806480u, off = 0x64806480u;
-        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&off));
-        return *reinterpret_cast<const uint32_t*>(&r);
+        uint32_t r;
+        asm("{\n.reg .b32 v;\nlop3.b32 v, %1, 0x00ff00ff, 0x64806480, 0x6a;\nsub.f16x2 %0, v, %2;\n}" : "=r"(r) : "r"(x), "r"(0x64806480u));
+        return r;
     }
     static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) {      // codes 0 and 2, 1 and 3
         lo = widen(x);
@@ -46,22 +46,30 @@ struct Int8 {
 };
 struct E4m3 {
     static constexpr bool kDigits = false;
-    static __device__ __forceinline__ uint32_t widen(uint32_t x) {      // of the low two codes
-        uint32_t r;
-        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(x));
-        return r;
-    }
     static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) {        // codes 0 and 1, 2 and 3
-        lo = widen(x);
-        hi = widen(x >> 16);
+        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(lo), "=r"(hi) : "r"(x));
     }
     static __device__ __forceinline__ void values(uint32_t x, uint32_t& lo, uint32_t& hi) { keys(__byte_perm(x, 0, 0x3120), lo, hi); }
 };
 
-__device__ __forceinline__ void mma_s8(int32_t (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+// d = a b (first), or d + a b
+__device__ __forceinline__ void mma_s8(bool first, int32_t (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+    if (first)
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "r"(0));
+    else
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(bool first, float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+    if (first)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        Num<__half>::mma(d, a, b0, b1);
 }
 
 // Tiles of 16 U tokens, and as many bytes on their way for either head size.
@@ -115,6 +123,8 @@ struct Worker {
     const int lane, g, c, unit_in_cta, sub;
     const uint32_t ring;                       // the warp's first stage
     const uint64_t policy;
+    const int32_t my_token;                    // of a tile of all slices: the one that this lane looks up
+    const uint32_t scale_put;                  // the place of its scale in a stage
     uint32_t put;                              // this lane's place in a stage: row lane / kPieces and, in place, piece lane % kPieces
     uint32_t get;                              // what this lane reads of a stage's half: piece 0 or 1 of its row; piece 2 j + .. is at get ^ 32 j
     // query head 8 t + g, dims 32 j + 4 c + .. of four and dims 32 j + 16 + 4 c + .. of four: two fp16 numbers a register, or
@@ -130,7 +140,10 @@ struct Worker {
 
     __device__ __forceinline__ Worker(const AttnParams& pp, uint32_t smem)
         : p(pp), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), c(threadIdx.x & 3), unit_in_cta((threadIdx.x >> 5) % pp.units),
-          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()), masks{} {
+          sub((threadIdx.x >> 5) / pp.units), ring(smem + (threadIdx.x >> 5) * R::kWarpBytes), policy(read_once_policy()),
+          my_token(R::kTokens * sub + lane % R::kTokens),
+          // tokens g, 8 + g, .. next to one another; with one group of tokens the upper lanes have the values' scales
+          scale_put(2 * R::kSideBytes + 4 * (2 * U * (lane & 7) + (lane % R::kTokens >> 3)) + (U == 1 ? 4 * (lane & 16) : 0)), masks{} {
         const int x = lane & 7, up = lane >> 4, mid = lane >> 3 & 1, row = lane / kPieces;
         put = row * D + (((lane % kPieces) ^ swap(row)) << 4);
         get = (x + 8 * mid) * D + ((up ^ swap(x)) << 4);
@@ -208,7 +221,7 @@ struct Worker {
 
     // Looks up the tokens of the tile that the slices' from token t0 on are, in a row that ends at `end`.
     __device__ __forceinline__ void load_ids(int32_t t0, int32_t end) {
-        const int32_t t = t0 + R::kTokens * sub + lane % R::kTokens;
+        const int32_t t = t0 + my_token;
         id = 0;
         at = -1;
         if (t < end) {
@@ -227,43 +240,44 @@ struct Worker {
         const uint32_t base = ring + stage * R::kStageBytes, dst = base + put;
         // what is not read has the address of the first block's first token
         const uint32_t blk = read ? id : 0, place = read ? at : 0;
-        if (on == 0xffffffffu && !p.far) copy_rows<true>(blk, place, on, dst);       // as nearly always
+        if (on == 0xffffffffu && p.near) copy_rows<true>(blk, place, on, dst);       // as nearly always
         else copy_rows<false>(blk, place, on, dst);
-        // scales, tokens g, 8 + g, .. next to one another
-        const uint32_t scales = base + 2 * R::kSideBytes + 4 * (2 * U * (lane & 7) + (lane % R::kTokens >> 3));
+        const uint32_t four = read ? 4 : 0;
         if (U == 1) {
-            copy4(scales + (lane & 16) * 4, scale_src + blk * (uint64_t)(lane < 16 ? p.k_scale_step : p.v_scale_step), read ? 4 : 0);
+            copy4(base + scale_put, bytes_on(scale_src, blk, lane < 16 ? p.k_scale_step : p.v_scale_step), four);
         } else {
-            copy4(scales, scale_src + blk * (uint64_t)p.k_scale_step, read ? 4 : 0);
-            copy4(scales + 4 * R::kTokens, scale_src + (p.v_scale - p.k_scale) + blk * (uint64_t)p.v_scale_step, read ? 4 : 0);
+            copy4(base + scale_put, bytes_on(scale_src, blk, p.k_scale_step), four);
+            copy4(base + scale_put + 4 * R::kTokens, bytes_on(scale_src + (p.v_scale - p.k_scale), blk, p.v_scale_step), four);
         }
         return on;
     }
-    // The rows of a tile: a lane's token lies in block blk at `place`.  kAll: all are read, and 32 bits count a pool's 16-byte
-    // steps.
+    // The rows of a tile: a lane's token lies in block blk at `place`.  kAll: all are read, and p.near holds.
     template <bool kAll>
     __device__ __forceinline__ void copy_rows(uint32_t blk, uint32_t place, uint32_t on, uint32_t dst) {
-        const uint32_t row16 = p.hkv * (D / 16);
-        const bool one_step = p.k_step == p.v_step;
-        const uint32_t k_off = blk * p.k_step + place * row16, v_off = blk * p.v_step + place * row16;
+        const uint32_t off = blk * p.k_step + place * p.row_step;
 #pragma unroll
         for (int i = 0; i < R::kTokens / kRows; ++i) {
             const int row = kRows * i + lane / kPieces;
-            const uint32_t bytes = kAll ? 16u : (on >> row & 1) << 4;
             const uint32_t to = (D == 128 ? dst ^ (64 * (i & 1)) : dst) + kRows * i * D;     // rows 4 to 7 of 8: piece ^ 4
-            const unsigned char *k, *v;
             if (kAll) {
-                const uint32_t o = __shfl_sync(0xffffffffu, k_off, row);
-                k = k_src + 16 * (uint64_t)o;
-                v = v_src + 16 * (uint64_t)(one_step ? o : __shfl_sync(0xffffffffu, v_off, row));
+                const uint32_t o = __shfl_sync(0xffffffffu, off, row);
+                copy_whole(to, bytes_on(k_src, o, 16), policy);
+                copy_whole(to + R::kSideBytes, bytes_on(v_src, o, 16), policy);
             } else {
-                const uint64_t b = __shfl_sync(0xffffffffu, blk, row), in_block = __shfl_sync(0xffffffffu, place, row) * (uint64_t)row16;
-                k = k_src + 16 * (b * p.k_step + in_block);
-                v = v_src + 16 * (b * p.v_step + in_block);
+                const uint32_t bytes = (on >> row & 1) << 4;
+                const uint64_t b = __shfl_sync(0xffffffffu, blk, row), in_block = __shfl_sync(0xffffffffu, place, row) * (uint64_t)p.row_step;
+                copy16(to, k_src + 16 * (b * p.k_step + in_block), bytes, policy);
+                copy16(to + R::kSideBytes, v_src + 16 * (b * p.v_step + in_block), bytes, policy);
             }
-            copy16(to, k, bytes, policy);
-            copy16(to + R::kSideBytes, v, bytes, policy);
         }
+    }
+    static __device__ __forceinline__ void copy_whole(uint32_t dst, const void* src, uint64_t policy) {
+        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+    }
+    static __device__ __forceinline__ const void* bytes_on(const void* src, uint32_t n, uint32_t step) {      // n steps on
+        uint64_t a;
+        asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(a) : "r"(n), "r"(step), "l"(src));
+        return reinterpret_cast<const void*>(a);
     }
     static __device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -301,16 +315,8 @@ struct Worker {
         const uint32_t src = ring + stage * R::kStageBytes;
         float s[U][NT][4];
         if constexpr (C::kDigits) {
-            // Products of each digit, in whole numbers below 2^21: from 1.5 2^23's bits on, so that they are floats
+            // Products of each digit, in whole numbers of at most 2^21
             int32_t n[3][U][NT][4];
-#pragma unroll
-            for (int d = 0; d < 3; ++d)
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) n[d][u][t][i] = 0x4b400000;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
@@ -318,23 +324,15 @@ struct Worker {
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int d = 0; d < 3; ++d) mma_s8(n[d][u][t], k[u][j], q[t][j][2 * d], q[t][j][2 * d + 1]);
+                        for (int d = 0; d < 3; ++d) mma_s8(j == 0, n[d][u][t], k[u][j], q[t][j][2 * d], q[t][j][2 * d + 1]);
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        auto digit = [&](int d) { return __int_as_float(n[d][u][t][i]) - 12582912.f; };
-                        s[u][t][i] = fmaf(digit(2), 65536.f, fmaf(digit(1), 256.f, digit(0)));
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        s[u][t][i] = fmaf((float)n[2][u][t][i], 65536.f, (float)(n[1][u][t][i] * 256 + n[0][u][t][i]));
         } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[u][t][i] = 0.f;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
@@ -346,7 +344,7 @@ struct Worker {
                     C::keys(x.z, b.x, b.z);
                     C::keys(x.w, b.y, b.w);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) N::mma(s[u][t], a, q[t][j][0], q[t][j][1]);
+                    for (int t = 0; t < NT; ++t) mma_f16(j == 0, s[u][t], a, q[t][j][0], q[t][j][1]);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][j][2], q[t][j][3]);
                 }
@@ -359,23 +357,12 @@ struct Worker {
         float ks[2 * U], vs[2 * U];            // of tokens g, 8 + g, ..
         floats(src + 2 * R::kSideBytes + 8 * U * g, ks);
         floats(src + 2 * R::kSideBytes + 4 * R::kTokens + 8 * U * g, vs);
-        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int u = 0; u < U; ++u) s[u][t][i] *= ks[2 * u + (i >> 1)] * factor[t][i & 1];
-        if (on != 0xffffffffu)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (!(on >> (16 * u + g + 4 * (i & 2)) & 1)) s[u][t][i] = -CUDART_INF_F;
-        // The weights' exponents, and the largest of them: max does not see a NaN, which then gives a NaN weight
+        // s[u][t][0], [1]: token 16 u + g, heads 8t + 2c, + 1; [2], [3]: token 16 u + 8 + g; each to be multiplied by the token's
+        // scale and the head's factor.  The weights' exponents, and the largest of them: max does not see a NaN, which then gives a
+        // NaN weight
         float e[U][NT][4], w[2 * U], top = 0.f, most = 0.f;
+        auto by = [&](int u, int t, int i) { return ks[2 * u + (i >> 1)] * factor[t][i & 1]; };
+        auto attended = [&](int u, int i) { return on >> (16 * u + g + 4 * (i & 2)) & 1; };
 #pragma unroll
         for (int i = 0; i < 2 * U; ++i) {
             w[i] = vs[i] * st.inv_ref;
@@ -386,10 +373,21 @@ struct Worker {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    e[u][t][i] = s[u][t][i] - st.m[t][i & 1];
-                    top = fmaxf(top, e[u][t][i]);
-                }
+                for (int u = 0; u < U; ++u) e[u][t][i] = fmaf(s[u][t][i], by(u, t, i), -st.m[t][i & 1]);
+        if (on != 0xffffffffu)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (!attended(u, i)) e[u][t][i] = -CUDART_INF_F;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int u = 0; u < U; ++u) top = fmaxf(top, e[u][t][i]);
         const bool over = top > N::kSlack + N::kLift || most > 2.f;
         if (__any_sync(0xffffffffu, over)) {
             // the reference of the values' scales: the power of two below the largest, or the present one
@@ -406,8 +404,14 @@ struct Worker {
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float mx = fmaxf(s[0][t][h], s[0][t][2 + h]);
-                    if (U == 2) mx = fmaxf(mx, fmaxf(s[U - 1][t][h], s[U - 1][t][2 + h]));
+                    float x[U][2], mx = -CUDART_INF_F;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            x[u][i] = attended(u, 2 * i) ? s[u][t][2 * i + h] * by(u, t, 2 * i + h) : -CUDART_INF_F;
+                            mx = fmaxf(mx, x[u][i]);
+                        }
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -422,8 +426,8 @@ struct Worker {
                     }
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        e[u][t][h] = s[u][t][h] - mx;
-                        e[u][t][2 + h] = s[u][t][2 + h] - mx;
+                        e[u][t][h] = x[u][0] - mx;
+                        e[u][t][2 + h] = x[u][1] - mx;
                     }
                 }
         }
@@ -514,8 +518,8 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
         if (c.num_gpu_blocks > 1 && (c.k_block_stride < block || c.v_block_stride < block || c.k_scale_stride < c.num_kv_heads ||
                                      c.v_scale_stride < c.num_kv_heads))
             return "a pool's block stride is smaller than a block, or its scales' than a block's";
-        if (std::max(c.k_block_stride, c.v_block_stride) >> 36 || std::max(c.k_scale_stride, c.v_scale_stride) >> 32)
-            return "blocks lie 2^36 bytes apart or more, or scales 2^32 floats";
+        if (std::max(c.k_block_stride, c.v_block_stride) >> 36 || std::max(c.k_scale_stride, c.v_scale_stride) >> 30)
+            return "blocks lie 2^36 bytes apart or more, or scales 2^30 floats";
         if (!on_bytes(c.k_scale, 0, 4) || !on_bytes(c.v_scale, 0, 4)) return "scales must be on 4-byte boundaries";
         if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
         return nullptr;
@@ -525,8 +529,9 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
     p.k_step = (uint32_t)(c.k_block_stride >> 4), p.v_step = (uint32_t)(c.v_block_stride >> 4);
-    p.k_scale_step = (uint32_t)c.k_scale_stride, p.v_scale_step = (uint32_t)c.v_scale_stride;
-    p.far = (double)c.num_gpu_blocks * (double)std::max(c.k_block_stride, c.v_block_stride) >= 68719476736.0;   // 2^36
+    p.k_scale_step = (uint32_t)(4 * c.k_scale_stride), p.v_scale_step = (uint32_t)(4 * c.v_scale_stride);
+    p.row_step = (uint32_t)(c.num_kv_heads * (c.head_dim / 16));
+    p.near = p.k_step == p.v_step && (double)c.num_gpu_blocks * (double)c.k_block_stride < 68719476736.0;      // 2^36
     cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e;
     if (a.dtype == PS_DTYPE_BF16)

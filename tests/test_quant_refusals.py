@@ -61,7 +61,7 @@ def test_read_refuses(kw):
     dict(table_stride=0), dict(window=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(out=None),
     dict(block_tables=None), dict(ctx_lens=None), dict(workspace=None), dict(v_block_stride=BLOCK + 8), dict(kpool=KP + 8), dict(q=Q + 8),
     dict(q_stride=4100), dict(out=OUT + 2), dict(out_stride=2048), dict(out=Q, out_stride=4096 + 8), dict(out=Q + 32), dict(table_stride=1 << 30, batch=1 << 20),
-    dict(k_block_stride=1 << 36), dict(v_scale_stride=1 << 32)])
+    dict(k_block_stride=1 << 36), dict(v_scale_stride=1 << 30)])
 def test_attn_refuses(kw):
     assert refused(B.load().ps_quant_attn, attn_args(**kw)).startswith("ps_quant_attn: ")
 
