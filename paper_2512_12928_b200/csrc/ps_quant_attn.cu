@@ -6,7 +6,12 @@
 // with the frame of ps_paged_attn.cuh: the sequence's cut, the walk, segment ends and the join are ps_paged_attn's.
 //
 // Bound: HBM, and next to it the instructions that a code costs: a token and KV head are half the bytes of a 16-bit cache's and
-// as many products and weights.  MEASURED
+// as many products and weights.  Measured: 337 MB of cache (64 rows of 1024 to 4096 tokens, 32 query heads on 8 KV heads of 128)
+// 60.5 us in int8 and 58.7 in 8-bit floats (16 bits: 101), about 7 us of which pass before the first tile is there, where rows
+// end and in the join; 1.07 GB (rows of 8192) 168 and 167 us, or 6.4 TB/s, which is what a copy reaches; one row of 500
+// tokens 8.9.  At the board's power limit, after some tenths of a second, the SMs run at 1.5 to 1.7 GHz and the batch takes 67
+// us.  Heads of 64 take 60.5 us for as many bytes; 16 query heads on a KV head of 128 78 and 69 us, of 64 94 and 80.  More
+// than 16 copy the tiles once for every 16, as in 16 bits.
 //
 // Products: S^T = K Q^T and O^T = V^T P^T as in ps_paged_attn.cu, tokens and then dims as the 16 rows of a product.  A tile of
 // 16 or 32 tokens comes to shared memory as it lies in the pool (cp.async, 16 bytes a lane).  ldmatrix sees pairs of codes as its
@@ -17,13 +22,13 @@
 // Values, and keys in 8-bit floats, are widened to fp16 between ldmatrix and the product; every code is exact there.  Queries
 // in bf16 are multiplied by a power of two that puts their head's largest magnitude next to 2^13, and the scores by its inverse.
 // Keys in int8 enter mma.m16n8k32 as they are: a query is a whole number next to 2^20 at its head's largest magnitude, in three
-// digits of 8 bits, whose products are exact whole numbers.  Three such products cost less than widening (an
-// instruction and a quarter a code; 72.3 us for the case above when keys were widened, 66.9 then).
+// digits of 8 bits, whose products are exact whole numbers.  Three such products cost less than widening, an instruction and a
+// quarter a code (the case above 72.3 us with widened keys when it took 66.9 with digits).
 //
 // Scales: a_t multiplies a score in 32 bits.  b_t goes into the weight, p_t (b_t / r) with r a power of two next to the
 // largest b that the warp has met, so that weights stay within fp16; sums are multiplied by r where a segment ends.  A weight
 // is one fp16 number for results in bf16, whose own rounding is off by eight times as much, and the sum of two for results in
-// fp16.
+// fp16, which cost it 1 to 2 % (the case above 61.8 us).
 #include <cuda_fp8.h>
 
 #include "ps_paged_attn.cuh"
@@ -97,9 +102,9 @@ struct QuantState : State<D, NT> {
 // tokens 66 and 82.5).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us with 8 warps, 93
 // with 16).
 // As two CTAs of 8 warps they do not wait for one another where a row ends, but a row has twice as many parts and what lies
-// next to one another is not read at the same time.  Int8 of 128, which is bound by its instructions, gains (1024 to 4096
-// tokens: 63.0 instead of 64.8 us, 200 rows of 10 to 100: 17.7 instead of 19.5); 8-bit floats lose (59.1 and 65), heads of 64 too
-// (62.7 and 65).
+// next to one another is not read at the same time.  Int8 of 128, whose instructions weigh most, gains (1024 to 4096
+// tokens: 63.0 instead of 64.8 us, 200 rows of 10 to 100: 17.7 instead of 19.5); 8-bit floats lose (65 instead of 59.1), heads of
+// 64 too (65 instead of 62.7).
 template <typename C>
 constexpr int ctas_of(int dim, int nt) { return C::kDigits && nt == 1 && dim == 128 ? 2 : 1; }
 template <typename C>
