@@ -6,7 +6,7 @@
 //
 // Bound: memory; a value written is 2 bytes read and 1 written, a value read back 1 and 2.  A scale needs all of its
 // block's new values before the first code can be rounded, so a warp takes one block's tokens of one head ("unit") and holds
-// them in registers between the two: 16 tokens of 128 dims are 4 vectors of 32 bytes a lane.
+// them in registers between the two: 16 tokens of 128 dims are 4 vectors of 32 bytes a lane.  Larger blocks have several warps.
 // Measured (8 KV heads of 128, bf16): 9350 tokens of prompt chunks appended in 13.6 us, whose bytes would take 8.9; a decode
 // batch's 200 of 4 heads 2.4, one 2.0.  71000 tokens read back in 68.3 us, or 6.4 TB/s, which is what a copy reaches; 300 in 2.3.
 // What the append spends above its bytes are two rounds and a half of CTAs, in each of which slots, then rows, then the maximum
@@ -123,40 +123,59 @@ struct QuantParams {
     int64_t num_slots;
     uint64_t block_magic;
     int32_t tokens, hkv, dim, block_size, sides, tok_per_cta;
-    int32_t row_vecs, row_magic, row_step, piece_step;      // vectors of a head's row; 2^16 / row_vecs rounded up; 32 vectors on
+    int32_t team;                 // warps of a unit
+    int32_t row_vecs, row_magic;  // vectors of a head's row; 2^16 / row_vecs rounded up
+    int32_t row_step, piece_step, team_row_step, team_piece_step;      // 32 vectors on, and 32 team
 };
 
 // ------------------------------------------------------------------------------------------------ append
 
+// Vectors of w values of a lane that stay in registers between maximum and rounding.
+constexpr __host__ __device__ int held_of(int w) { return w == 16 ? 4 : 8; }
+
 // A segment is a run of tokens that go to one block.  A warp has one head of keys or values, and the segments that begin
-// among the CTA's n tokens, which it finds for itself: no barrier, and nothing in shared memory.  kEven: a row's vectors
-// divide a warp's lanes, so that a lane has the same piece of every row it has.
-template <typename T, typename C, int W, bool kEven, int kCtas>
+// among the CTA's tokens; it finds them for itself, without barriers.  kTeam: blocks are larger than what a warp holds, and
+// several warps have a head together; the CTA looks up 256 tokens at once, so that few CTAs find nothing.  kEven: a row's
+// vectors divide a team's lanes, so that a lane has the same piece of every row it has.
+template <typename T, typename C, int W, bool kEven, bool kTeam, int kCtas>
 __global__ void __launch_bounds__(kThreads, kCtas)
 quant_append_kernel(const __grid_constant__ QuantParams p) {
-    constexpr int kHold = W == 16 ? 4 : 8;   // vectors of a lane that stay in registers between maximum and rounding
-    const int lane = threadIdx.x & 31;
-    const int unit = (kThreads / 32) * blockIdx.y + (threadIdx.x >> 5);
-    if (unit >= p.sides * p.hkv) return;
+    constexpr int kHold = held_of(W);
+    constexpr int kWindow = kTeam ? kThreads : 32;           // tokens that are looked up at once, from the one before on
+    __shared__ int32_t blocks[kWindow], places[kWindow];     // these only with teams
+    __shared__ uint32_t changes[kThreads / 32], zeros[kThreads / 32], tops[2][kThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = kTeam ? p.team : 1;
+    const int team_in_cta = warp / team, lane_in_team = threadIdx.x - 32 * team * team_in_cta;
+    const int unit = (kThreads / 32) / team * blockIdx.y + team_in_cta;
+    if (!kTeam && unit >= p.sides * p.hkv) return;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int head = unit < p.hkv ? unit : unit - p.hkv;
     const Side& side = p.side[unit < p.hkv ? 0 : 1];
-    // The vectors of a segment, rows first: this lane has every 32nd.
-    const int row0 = lane * p.row_magic >> 16, piece0 = lane - row0 * p.row_vecs;
+    // The vectors of a segment, rows first: this lane has every 32nd, or with the team `together` every one that is 32 team on.
+    bool together = false;
+    int row0, piece0, row_step, piece_step;
+    auto deal = [&] {
+        const int me = kTeam && together ? lane_in_team : lane;
+        row0 = me * p.row_magic >> 16, piece0 = me - row0 * p.row_vecs;
+        row_step = kTeam && together ? p.team_row_step : p.row_step, piece_step = kTeam && together ? p.team_piece_step : p.piece_step;
+    };
+    deal();
     auto next = [&](int& row, int& piece) {
-        row += p.row_step;
+        row += row_step;
         if (kEven) return;
-        piece += p.piece_step;
+        piece += piece_step;
         if (piece >= p.row_vecs) {
             piece -= p.row_vecs;
             ++row;
         }
     };
+    auto meet_team = [&] { asm volatile("bar.sync %0, %1;" ::"r"(1 + team_in_cta), "r"(32 * team) : "memory"); };
+    int turn = 0;
     const uint32_t place_bytes = p.hkv * p.dim;
     const int32_t t0 = blockIdx.x * p.tok_per_cta;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    // 32 tokens from the one before on, one a lane: what begins among the CTA's mostly ends there too
-    const int32_t t = t0 - 1 + lane;
+    // What begins among the CTA's tokens mostly ends within the window, too
+    const int32_t t = t0 - 1 + (kTeam ? threadIdx.x : lane);
     int64_t slot = t >= 0 && t < p.tokens ? p.slots[t] : -1;
     if (slot >= p.num_slots) {
         if (p.status) *(volatile int32_t*)p.status = kStatusBadSlot;
@@ -164,17 +183,12 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
     }
     const int32_t block = slot < 0 ? -1 : (int32_t)block_of(slot, p.block_magic);
     const int32_t my_place = (int32_t)slot - block * p.block_size;          // modulo 2^32: a place is less
-    const int32_t before = __shfl_up_sync(0xffffffffu, block, 1);
-    uint32_t starts = __ballot_sync(0xffffffffu, lane > 0 && lane <= p.tok_per_cta && block >= 0 && block != before);
-    for (; starts; starts &= starts - 1) {
-        const int first = __ffs(starts) - 1;
-        const int32_t blk = __shfl_sync(0xffffffffu, block, first);
-        const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
-        int len = (other ? __ffs(other) - 1 : 32) - first;
-        bool begun = __any_sync(0xffffffffu, lane >= first && lane < first + len && my_place == 0);
-        const bool ends = first + len < 32;  // among the lanes' tokens
+
+    // Tokens [first, first + len) of the window, or more where the segment goes on behind it.
+    auto segment = [&](int first, int len, int32_t blk, bool begun) {
+        const bool ends = first + len < kWindow;
         const int64_t block_begin = (int64_t)blk * p.block_size;
-        while (!ends) {                      // it may go on
+        while (!ends) {
             const int32_t u = t0 - 1 + first + len + lane;
             const int64_t s = u < p.tokens ? p.slots[u] : -1;
             const uint32_t out = __ballot_sync(0xffffffffu, s < block_begin || s - block_begin >= p.block_size);
@@ -215,6 +229,12 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             next(row, piece);
         }
         most = __reduce_max_sync(0xffffffffu, max(most & 0xffff, most >> 16));
+        if (kTeam && together) {             // all warps have the old scale by then, too
+            if (lane == 0) tops[turn][warp] = most;
+            meet_team();
+            most = __reduce_max_sync(0xffffffffu, tops[turn][team_in_cta * team + lane % team]);
+            turn ^= 1;
+        }
         const float need = Num<T>::unpack(most).x * (1.f / C::kTop);
         const float now = most >= Num<T>::kInf || old != old ? CUDART_NAN_F : fmaxf(fmaxf(old, need), kLeastScale);
         const float r = 1.f / now;
@@ -232,6 +252,7 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             }
             __syncwarp();                    // the new tokens' codes come on top
         }
+        if (kTeam && together && !begun) meet_team();
         auto put = [&](const Vec<2 * W>& x, uint32_t place, int piece) {
             Vec<W> y;
 #pragma unroll
@@ -245,9 +266,10 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
         row = row0, piece = piece0;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) {
-            uint32_t place = __shfl_sync(0xffffffffu, my_place, first + row);
+            uint32_t place = kTeam ? 0 : __shfl_sync(0xffffffffu, my_place, first + row);
             if (row < len) {
-                if (!ends && first + row >= 32) place = place_of(row);
+                if (kTeam && first + row < kWindow) place = places[first + row];
+                else if (!ends && first + row >= kWindow) place = place_of(row);
                 put(held[i], place, piece);
             }
             next(row, piece);
@@ -258,7 +280,50 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             put(x, place_of(row), piece);
             next(row, piece);
         }
-        if (lane == 0) *scale_at = now;
+        if (kTeam && together ? lane_in_team == 0 : lane == 0) *scale_at = now;
+    };
+
+    if constexpr (kTeam) {
+        blocks[threadIdx.x] = block;
+        places[threadIdx.x] = my_place;
+        __syncthreads();
+        const uint32_t change = __ballot_sync(0xffffffffu, threadIdx.x > 0 && block != blocks[max((int)threadIdx.x - 1, 0)]);
+        const uint32_t zero = __ballot_sync(0xffffffffu, slot >= 0 && my_place == 0);
+        if (lane == 0) changes[warp] = change, zeros[warp] = zero;
+        __syncthreads();
+        if (unit >= p.sides * p.hkv) return;
+        // the words of a mask from bit `from` on, one a lane
+        auto word_from = [&](const uint32_t* mask, int from) {
+            const int n = from - 32 * lane;
+            return lane >= kThreads / 32 || n >= 32 ? 0u : n <= 0 ? mask[lane] : mask[lane] & (0xffffffffu << n);
+        };
+        auto first_from = [&](const uint32_t* mask, int from) {
+            const uint32_t w = word_from(mask, from), any = __ballot_sync(0xffffffffu, w != 0);
+            const int at = any ? __ffs(any) - 1 : 0, in_word = __ffs(__shfl_sync(0xffffffffu, w, at)) - 1;
+            return any ? 32 * at + in_word : kWindow;
+        };
+        // What a warp holds goes to one after the other of the team's warps, what is longer to all of them together.
+        int whose = 0;
+        for (int first = first_from(changes, 1); first <= p.tok_per_cta;) {
+            const int end = first_from(changes, first + 1);
+            if (blocks[first] >= 0) {
+                together = end == kWindow || (end - first) * p.row_vecs > 32 * kHold;
+                deal();
+                if (together || whose++ % team == warp % team)
+                    segment(first, end - first, blocks[first], first_from(zeros, first) < end);
+            }
+            first = end;
+        }
+    } else {
+        const int32_t before = __shfl_up_sync(0xffffffffu, block, 1);
+        uint32_t starts = __ballot_sync(0xffffffffu, lane > 0 && lane <= p.tok_per_cta && block >= 0 && block != before);
+        for (; starts; starts &= starts - 1) {
+            const int first = __ffs(starts) - 1;
+            const int32_t blk = __shfl_sync(0xffffffffu, block, first);
+            const uint32_t other = __ballot_sync(0xffffffffu, block != blk) & (0xffffffffu << first);
+            const int len = (other ? __ffs(other) - 1 : 32) - first;
+            segment(first, len, blk, __any_sync(0xffffffffu, lane >= first && lane < first + len && my_place == 0));
+        }
     }
 }
 
@@ -397,25 +462,40 @@ bool fits(const QuantParams& p, int w) {
 
 template <typename T, typename C>
 cudaError_t launch_append(QuantParams p, cudaStream_t s) {
-    // Few tokens: one a CTA, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins one, while that
-    // leaves every SM 16 warps (9350 tokens of 8 heads of 128: 1 / 4 / 8 / 16 tokens a CTA 51 / 22 / 17 / 15.5 us when this was
-    // chosen, 200 of 4 heads 2.8 / 5.6 / 9.5 / 17).  A CTA of many has 80 registers a thread, so that three fit an SM, instead of
-    // two of up to 127 (15.5 instead of 17.0 us); what spills for it costs a few tokens 0.1 to 0.3 us.
-    const int warps = kThreads / 32, units = p.sides * p.hkv;
-    p.tok_per_cta = 1;
-    while (2 * p.tok_per_cta <= std::min(p.block_size, 16) && (int64_t)p.tokens / (2 * p.tok_per_cta) * units >= 148 * 16) p.tok_per_cta *= 2;
-    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), (unsigned)((units + warps - 1) / warps));
-    const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1;
+    // Blocks of more than a warp holds in registers have teams of up to 8 warps (9350 tokens of 8 heads of 128 in blocks of 64 /
+    // 256 / 1024: 17 / 21 / 42 us instead of 21 / 71 / 245, 256 in one block 5.9 instead of 31; a batch's 64 single tokens in
+    // blocks of 64 4.6 instead of 2.4, which the 256 tokens that a CTA looks up cost).
+    const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1, units = p.sides * p.hkv;
     p.row_vecs = p.dim / w;
-    p.row_magic = (65536 + p.row_vecs - 1) / p.row_vecs;     // exact for the 32 lanes and up to 512 vectors
-    p.row_step = 32 / p.row_vecs;
-    p.piece_step = 32 % p.row_vecs;
+    p.team = 1;
+    while (p.team < 8 && 32 * held_of(w) * p.team < (int64_t)p.block_size * p.row_vecs) p.team *= 2;
+    const int at_once = kThreads / 32 / p.team;              // units of a CTA
+    const unsigned groups = (unsigned)((units + at_once - 1) / at_once);
+    // Few tokens: one a CTA and warp of a team, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins
+    // one, with teams 128, while that leaves every SM 16 warps (9350 tokens of 8 heads of 128: 1 / 4 / 8 / 16 tokens a CTA
+    // 51 / 22 / 17 / 15.5 us when this was chosen, 200 of 4 heads 2.8 / 5.6 / 9.5 / 17).  A CTA of many has 80 registers a
+    // thread, so that three fit an SM, instead of two of up to 127 (15.5 instead of 17.0 us); what spills for it costs a few
+    // tokens 0.1 to 0.3 us.
+    p.tok_per_cta = p.team;
+    while (2 * p.tok_per_cta <= std::min(p.block_size, p.team > 1 ? 128 : 16) &&
+           (int64_t)p.tokens / (2 * p.tok_per_cta) * units * p.team >= 148 * 16)
+        p.tok_per_cta *= 2;
+    const dim3 grid((unsigned)((p.tokens + p.tok_per_cta - 1) / p.tok_per_cta), groups);
+    p.row_magic = (65536 + p.row_vecs - 1) / p.row_vecs;     // exact for a team's 256 lanes and up to 512 vectors
+    p.row_step = 32 / p.row_vecs, p.piece_step = 32 % p.row_vecs;
+    p.team_row_step = 32 * p.team / p.row_vecs, p.team_piece_step = 32 * p.team % p.row_vecs;
     const bool even = p.piece_step == 0, few = p.tok_per_cta == 1;
     auto launch = [&](auto kernel) { return ps::launch_dependent(kernel, grid, dim3(kThreads), 0, s, p); };
-    if (w == 16 && even) return few ? launch(quant_append_kernel<T, C, 16, true, 2>) : launch(quant_append_kernel<T, C, 16, true, 3>);
-    if (w == 16) return few ? launch(quant_append_kernel<T, C, 16, false, 2>) : launch(quant_append_kernel<T, C, 16, false, 3>);
-    if (w == 8) return launch(quant_append_kernel<T, C, 8, false, 2>);
-    return launch(quant_append_kernel<T, C, 1, false, 2>);
+    if (p.team > 1) {
+        if (w == 16 && even) return launch(quant_append_kernel<T, C, 16, true, true, 3>);
+        if (w == 16) return launch(quant_append_kernel<T, C, 16, false, true, 3>);
+        if (w == 8) return launch(quant_append_kernel<T, C, 8, false, true, 2>);
+        return launch(quant_append_kernel<T, C, 1, false, true, 2>);
+    }
+    if (w == 16 && even) return few ? launch(quant_append_kernel<T, C, 16, true, false, 2>) : launch(quant_append_kernel<T, C, 16, true, false, 3>);
+    if (w == 16) return few ? launch(quant_append_kernel<T, C, 16, false, false, 2>) : launch(quant_append_kernel<T, C, 16, false, false, 3>);
+    if (w == 8) return launch(quant_append_kernel<T, C, 8, false, false, 2>);
+    return launch(quant_append_kernel<T, C, 1, false, false, 2>);
 }
 template <typename T, typename C>
 cudaError_t launch_read(QuantParams p, cudaStream_t s) {

@@ -747,3 +747,32 @@ def test_a_context_moves_blocks_of_8_bits_with_their_scales():
         check_attn(out, lse, quant_attn_want(*caches[l], q, ids, [c + 1 for c in ctx]))
     assert lib.sync() == B.PS_OK, lib.last_error()
     lib.destroy()
+
+
+# Blocks of more than a warp's registers hold: 4 times 32 vectors of 16 values, 8 of 8 or of one
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+@pytest.mark.parametrize("H,D,S,rows", [
+    (8, 128, 32, [(5, 90), (31, 2), (0, 32)]), (3, 128, 64, [(0, 640), (63, 2), (17, 100), (0, 3)]),
+    (2, 80, 128, [(100, 300), (0, 128), (127, 1)]), (1, 64, 256, [(0, 256), (1, 600), (200, 60), (255, 1)]),
+    (5, 128, 256, [(i % 256, 1) for i in range(0, 900, 7)]), (1, 128, 1024, [(3, 2500), (0, 1024), (1000, 30)]),
+    (8, 128, 64, [(i, 1 + i % 21) for i in range(50)]), (16, 128, 64, [(0, 3001)]), (7, 72, 100, [(0, 255), (99, 257), (50, 20)]),
+    (3, 7, 300, [(2, 700), (0, 40)]), (1, 512, 40, [(39, 90), (0, 7)]), (2, 500, 30, [(29, 90), (0, 70)])])
+def test_append_in_large_blocks(codes, H, D, S, rows):
+    """A row's tokens of a block are dealt to several warps, begin and end anywhere among the 256 that a CTA looks up, and go on
+    behind them; between rows stands padding, a slot behind the pool among it."""
+    rng = np.random.default_rng(H + D + S)
+    nb = sum(-(-(f + n) // S) for f, n in rows) + 3
+    order, slots = rng.permutation(nb).tolist(), []
+    for i, (first, n) in enumerate(rows):
+        ids = [order.pop() for _ in range(-(-(first + n) // S))]
+        slots += [ids[p // S] * S + p % S for p in range(first, first + n)] + ([-1, nb * S] if i % 3 == 1 else [])
+    (kp, ks), (vp, vs) = (make_cache((nb, S, H, D), CODES[codes], gen(D + i), spread=3.0) for i in range(2))
+    mk, mv = CacheModel(kp, ks), CacheModel(vp, vs)
+    for step in range(3):                  # larger, then smaller values
+        k, v = kv_rows(len(slots), H, D, (torch.bfloat16, torch.float16)[step % 2], step + D)
+        k, v = (x * (1.0, 4.0, 0.25)[step] for x in (k, v))
+        append(k, v, (kp, vp, ks, vs), slots, want_status=int(nb * S in slots))
+        mk.append(k, slots)
+        mv.append(v, slots)
+        mk.check(kp, ks)
+        mv.check(vp, vs)
