@@ -7,8 +7,8 @@
 // Bound: memory; a value written is 2 bytes read and 1 written, a value read back 1 and 2.  A scale needs all of its
 // block's new values before the first code can be rounded, so a warp takes one block's tokens of one head ("unit") and holds
 // them in registers between the two: 16 tokens of 128 dims are 4 vectors of 32 bytes a lane.  Larger blocks have several warps.
-// Measured (8 KV heads of 128, bf16): 9350 tokens of prompt chunks appended in 13.6 us, whose bytes would take 8.9; a decode
-// batch's 200 of 4 heads 2.4, one 2.0.  71000 tokens read back in 68.3 us, or 6.4 TB/s, which is what a copy reaches; 300 in 2.3.
+// Measured (8 KV heads of 128, bf16): 9350 tokens of prompt chunks appended in 13.7 us, whose bytes would take 8.9; a decode
+// batch's 200 of 4 heads 2.3, one 2.0.  71000 tokens read back in 68.3 us, or 6.4 TB/s, which is what a copy reaches; 300 in 2.3.
 // What the append spends above its bytes are two rounds and a half of CTAs, in each of which slots, then rows, then the maximum
 // over a warp wait for one another, and a unit's own instructions.  (With the values in shared memory instead of registers, by
 // cp.async, and more warps on an SM: 18.6 us where registers took 15.5.)
@@ -242,13 +242,26 @@ quant_append_kernel(const __grid_constant__ QuantParams p) {
             const float f = __fmul_rn(old, r);
             int q = row0, c = piece0;
             while (q < p.block_size) {
-                Vec<W> x;
-                unsigned char* at = pool + (uint32_t)q * (uint64_t)place_bytes + c * W;
-                x.load(at);
+                // on their way at once: as many as the registers of two CTAs an SM hold (64 blocks of 64 / 256 tokens that
+                // all grow: 8.6 / 26 us with four, 13 / 56 with one)
+                constexpr int kMany = kCtas == 2 ? 4 : 1;
+                Vec<W> x[kMany];
+                unsigned char* at[kMany];
+                bool there[kMany];
 #pragma unroll
-                for (int i = 0; i < (W + 3) / 4; ++i) x.w[i] = C::pack(C::unpack(x.w[i]), f);
-                x.store(at);
-                next(q, c);
+                for (int k = 0; k < kMany; ++k) {
+                    at[k] = pool + (uint32_t)q * (uint64_t)place_bytes + c * W;
+                    there[k] = q < p.block_size;
+                    if (there[k]) x[k].load(at[k]);
+                    next(q, c);
+                }
+#pragma unroll
+                for (int k = 0; k < kMany; ++k) {
+                    if (!there[k]) continue;
+#pragma unroll
+                    for (int i = 0; i < (W + 3) / 4; ++i) x[k].w[i] = C::pack(C::unpack(x[k].w[i]), f);
+                    x[k].store(at[k]);
+                }
             }
             __syncwarp();                    // the new tokens' codes come on top
         }
@@ -462,13 +475,13 @@ bool fits(const QuantParams& p, int w) {
 
 template <typename T, typename C>
 cudaError_t launch_append(QuantParams p, cudaStream_t s) {
-    // Blocks of more than a warp holds in registers have teams of up to 8 warps (9350 tokens of 8 heads of 128 in blocks of 64 /
-    // 256 / 1024: 17 / 21 / 42 us instead of 21 / 71 / 245, 256 in one block 5.9 instead of 31; a batch's 64 single tokens in
-    // blocks of 64 4.6 instead of 2.4, which the 256 tokens that a CTA looks up cost).
+    // Where a block and the call have more tokens than a warp holds in registers, it has a team of up to 8 warps (9350 tokens of 8 heads of 128 in blocks of 64 /
+    // 256 / 1024: 17 / 21 / 43 us instead of 21 / 71 / 245, 256 in one block 5.9 instead of 31; a batch's 64 single tokens in
+    // blocks of 64 4.4 instead of 2.4, which the 256 tokens that a CTA looks up cost).
     const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1, units = p.sides * p.hkv;
     p.row_vecs = p.dim / w;
     p.team = 1;
-    while (p.team < 8 && 32 * held_of(w) * p.team < (int64_t)p.block_size * p.row_vecs) p.team *= 2;
+    while (p.team < 8 && 32 * held_of(w) * p.team < (int64_t)std::min(p.block_size, p.tokens) * p.row_vecs) p.team *= 2;
     const int at_once = kThreads / 32 / p.team;              // units of a CTA
     const unsigned groups = (unsigned)((units + at_once - 1) / at_once);
     // Few tokens: one a CTA and warp of a team, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins
@@ -484,11 +497,11 @@ cudaError_t launch_append(QuantParams p, cudaStream_t s) {
     p.row_magic = (65536 + p.row_vecs - 1) / p.row_vecs;     // exact for a team's 256 lanes and up to 512 vectors
     p.row_step = 32 / p.row_vecs, p.piece_step = 32 % p.row_vecs;
     p.team_row_step = 32 * p.team / p.row_vecs, p.team_piece_step = 32 * p.team % p.row_vecs;
-    const bool even = p.piece_step == 0, few = p.tok_per_cta == 1;
+    const bool even = p.piece_step == 0, few = p.tok_per_cta == p.team;
     auto launch = [&](auto kernel) { return ps::launch_dependent(kernel, grid, dim3(kThreads), 0, s, p); };
     if (p.team > 1) {
-        if (w == 16 && even) return launch(quant_append_kernel<T, C, 16, true, true, 3>);
-        if (w == 16) return launch(quant_append_kernel<T, C, 16, false, true, 3>);
+        if (w == 16 && even) return few ? launch(quant_append_kernel<T, C, 16, true, true, 2>) : launch(quant_append_kernel<T, C, 16, true, true, 3>);
+        if (w == 16) return few ? launch(quant_append_kernel<T, C, 16, false, true, 2>) : launch(quant_append_kernel<T, C, 16, false, true, 3>);
         if (w == 8) return launch(quant_append_kernel<T, C, 8, false, true, 2>);
         return launch(quant_append_kernel<T, C, 1, false, true, 2>);
     }

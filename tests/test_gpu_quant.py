@@ -776,3 +776,23 @@ def test_append_in_large_blocks(codes, H, D, S, rows):
         mv.append(v, slots)
         mk.check(kp, ks)
         mv.check(vp, vs)
+
+
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+@pytest.mark.parametrize("H,D,S,B_", [(8, 128, 256, 5), (8, 128, 256, 64), (3, 80, 64, 300), (2, 72, 200, 40), (1, 7, 90, 33), (8, 128, 16, 400)])
+def test_append_of_single_tokens_that_raise_the_scales_of_blocks_in_use(codes, H, D, S, B_):
+    rng = np.random.default_rng(S + B_)
+    nb = B_ + 2
+    (kp, ks), (vp, vs) = (make_cache((nb, S, H, D), CODES[codes], gen(D + i)) for i in range(2))
+    ks *= 1e-3
+    vs[::2] *= 1e-3                        # some grow, some do not
+    mk, mv = CacheModel(kp, ks), CacheModel(vp, vs)
+    ids = rng.permutation(nb)[:B_]
+    for step in range(2):
+        slots = [int(i) * S + int(p) for i, p in zip(ids, rng.integers(1, S, B_))]
+        k, v = (x * (1 + step) for x in kv_rows(B_, H, D, torch.bfloat16, 9 + step))
+        append(k, v, (kp, vp, ks, vs), slots)
+        mk.append(k, slots)
+        mv.append(v, slots)
+        mk.check(kp, ks)
+        mv.check(vp, vs)
