@@ -475,16 +475,16 @@ bool fits(const QuantParams& p, int w) {
 
 template <typename T, typename C>
 cudaError_t launch_append(QuantParams p, cudaStream_t s) {
-    // Where a block and the call have more tokens than a warp holds in registers, it has a team of up to 8 warps (9350 tokens of 8 heads of 128 in blocks of 64 /
-    // 256 / 1024: 17 / 21 / 43 us instead of 21 / 71 / 245, 256 in one block 5.9 instead of 31; a batch's 64 single tokens in
-    // blocks of 64 4.4 instead of 2.4, which the 256 tokens that a CTA looks up cost).
+    // Where a block and the call have more tokens than a warp holds in registers, it has a team of up to 8 warps (9350 tokens of 8
+    // heads of 128 in blocks of 64 / 256 / 1024: 17 / 21 / 43 us instead of 21 / 71 / 245, 256 in one block 5.9 instead of 31; a
+    // batch's 64 single tokens in blocks of 64 4.4 instead of 2.4, which the 256 tokens that a CTA looks up cost).
     const int w = fits(p, 16) ? 16 : fits(p, 8) ? 8 : 1, units = p.sides * p.hkv;
     p.row_vecs = p.dim / w;
     p.team = 1;
     while (p.team < 8 && 32 * held_of(w) * p.team < (int64_t)std::min(p.block_size, p.tokens) * p.row_vecs) p.team *= 2;
     const int at_once = kThreads / 32 / p.team;              // units of a CTA
     const unsigned groups = (unsigned)((units + at_once - 1) / at_once);
-    // Few tokens: one a CTA and warp of a team, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins
+    // Few tokens: one a CTA and warp, so that they spread over the chip.  Many: 16, of which a block of 16 tokens begins
     // one, with teams 128, while that leaves every SM 16 warps (9350 tokens of 8 heads of 128: 1 / 4 / 8 / 16 tokens a CTA
     // 51 / 22 / 17 / 15.5 us when this was chosen, 200 of 4 heads 2.8 / 5.6 / 9.5 / 17).  A CTA of many has 80 registers a
     // thread, so that three fit an SM, instead of two of up to 127 (15.5 instead of 17.0 us); what spills for it costs a few
