@@ -587,9 +587,9 @@ typedef struct ps_quant_attn_args {
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
  * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^30 floats.  Codes are exact in the products, a
  * query's values are to within 2^-21 of the largest of their head; scores, softmax and sums are in 32 bits.  For the product
- * with V a softmax weight times its token's value scale is an fp16 number, and for results in fp16 the sum of two: relative to
- * the largest weight times the largest value scale that the row has met, 11 bits (22) down to 2^-22 and multiples of 2^-32
- * below.  A query head with a NaN gives NaN, one with an infinite value NaN or infinite results.
+ * with V a softmax weight times its token's value scale is the sum of two fp16 numbers: off by 2^-22 of itself, or by 2^-33 of
+ * the largest weight times the largest value scale that the row has met, whichever is more.  A query head with a NaN gives NaN,
+ * one with an infinite value NaN or infinite results.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
 

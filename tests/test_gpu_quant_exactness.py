@@ -1,0 +1,47 @@
+"""How exact results over a cache of 8 bits are: that of 32-bit arithmetic, rounded once."""
+import numpy as np
+import pytest
+import torch
+
+from device_step_util import DTYPES, HALF_STEP, TINY, attn_want, f64
+from quant_util import CODES, TOP
+from test_gpu_quant import attn_case, run_attn
+
+pytestmark = pytest.mark.gpu
+
+
+def check_rounded_once(got, lse, cache, q, tables, ctx, scale=None):
+    """Results against 64 bits: off by half a step of the value at hand and by what 32-bit arithmetic is off.
+
+    Of the latter attn_want has the part of scores, exp2, sums and the division.  A weight times its value scale is a 32-bit
+    product (2^-24) and held as the sum of two fp16 numbers (half a step of half a step, 2^-22): 2^-21 together.  Below fp16's
+    smallest steps it is off by 2^-25, where largest weights are 2^8 or more and refer to the power of two below the row's
+    largest value scale: 2^-33 of a token's largest possible value, times the tokens."""
+    kp, vp, ks, vs = cache
+    dt = q.dtype
+    K, V = (p.double() * s.double()[:, None, :, None] for p, s in ((kp, ks), (vp, vs)))
+    out, want_lse, tol, tol_lse = attn_want(K, V, q, tables, ctx, 0, scale, weight_error=2.0 ** -21)
+    e = (tol - HALF_STEP[dt] * np.abs(out) - TINY[dt]) / (1 + HALF_STEP[dt])       # attn_want has half of the largest step
+    S, G = kp.shape[1], q.shape[1] // kp.shape[2]
+    for b, n in enumerate(ctx):
+        ids = tables[b][: -(-n // S)]
+        if ids:
+            top = f64(vs)[ids].max(0) * TOP[vp.dtype]
+            e[b] += np.repeat(top, G)[:, None] * (n * 2.0 ** -33)
+    step = HALF_STEP[dt] * np.exp2(np.floor(np.log2(np.maximum(np.abs(out) + e, 2.0 ** -126)))) + TINY[dt]
+    bad = ~(np.abs(f64(got) - out) <= step + e)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} results"
+    fin = np.isfinite(want_lse)
+    assert (np.abs(f64(lse) - want_lse)[fin] <= tol_lse[fin]).all(), np.abs(f64(lse) - want_lse)[fin].max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv,D", [(8, 2, 128), (16, 1, 64)])
+def test_weights_of_few_tokens(dtype, codes, hq, hkv, D):
+    """With few tokens no rounding of a weight is averaged away: each would show in the result."""
+    rng = np.random.default_rng(1)
+    ctx = rng.integers(1, 7, 300).tolist()
+    cache, q, tables = attn_case(rng, ctx, hq, hkv, D, 4, DTYPES[dtype], CODES[codes], spread=2.0)
+    q = q * 0.125                          # scores next to one another
+    check_rounded_once(*run_attn(cache, q, tables, ctx), cache, q, tables, ctx)
