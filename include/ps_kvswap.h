@@ -585,11 +585,11 @@ typedef struct ps_quant_attn_args {
 } ps_quant_attn_args;
 
 /* ps_paged_attn over a cache of 8 bits: the same result, masks, limits, errors and workspace rules, of keys and values code *
- * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^30 floats.  Codes are exact in the products, a
- * query's values are to within 2^-21 of the largest of their head; scores, softmax and sums are in 32 bits.  For the product
- * with V a softmax weight times its token's value scale is the sum of two fp16 numbers: off by 2^-22 of itself, or by 2^-33 of
- * the largest weight times the largest value scale that the row has met, whichever is more.  A query head with a NaN gives NaN,
- * one with an infinite value NaN or infinite results.
+ * scale; blocks lie less than 2^36 bytes apart and their scales less than 2^30 floats.  Codes are exact in the products, and so
+ * are a query's values, but that in bf16 what is below 2^-27 of its head's largest is to within 2^-38 of that; scores, softmax
+ * and sums are in 32 bits.  For the product with V a softmax weight times its token's value scale is the sum of two fp16
+ * numbers: off by 2^-22 of itself, or by 2^-33 of the largest weight times the largest value scale that the row has met,
+ * whichever is more.  A query head with a NaN gives NaN, one with an infinite value NaN or infinite results.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
 

@@ -53,7 +53,7 @@ struct Worker {
     using Stages = R;
     using Type = T;
     using Softmax = State<D, NT>;
-    static constexpr int kDim = D, kColumns = NT, kWarps = 8, kCtas = 1;
+    static constexpr int kDim = D, kColumns = NT, kWarps = 8;
     static constexpr int kSub = R::kTokens / 16;             // groups of 16 tokens in a tile
     const AttnParams& p;
     const int lane, g, c, unit_in_cta, sub;
@@ -260,7 +260,7 @@ struct Worker {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-Tiling tiling_of(int32_t dim, int32_t) { return {dim == 128 ? Ring<128>::kTokens : Ring<64>::kTokens, 8, 1}; }
+Tiling tiling_of(int32_t dim, int32_t) { return {dim == 128 ? Ring<128>::kTokens : Ring<64>::kTokens, 8}; }
 
 template <typename T, int D>
 cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {

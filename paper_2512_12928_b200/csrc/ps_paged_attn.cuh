@@ -7,7 +7,7 @@
 // one vote instead of a maximum over the lanes; weights stay below 2^kSlack and sums in 32 bits lose nothing by it.
 //
 // Work: the rows' tiles form one sequence (with two places more for each row's start and end, which cost about two tiles'
-// time) that is cut into equal shares, one per CTA (one or two an SM), from the lengths each CTA reads itself: no plan is made on the host or
+// time) that is cut into equal shares, one per CTA, from the lengths each CTA reads itself: no plan is made on the host or
 // by another kernel.  A row cut by a share's end leaves partial results (m, sum, accumulators) in the workspace, which a
 // second kernel (paged_join_kernel) combines in order.  The join is a second launch rather than a last-arrival counter in
 // the first: the workspace then needs no initial state, and neither a replayed graph nor a call that shares it in turn can
@@ -251,7 +251,7 @@ __device__ __forceinline__ void slices_meet(const AttnParams& p, int unit_in_cta
 }
 
 template <typename W>
-__global__ void __launch_bounds__(W::kWarps * 32, W::kCtas)
+__global__ void __launch_bounds__(W::kWarps * 32, 1)
 paged_attn_kernel(const __grid_constant__ AttnParams p) {
     constexpr int kMaxWarps = W::kWarps;
     using R = typename W::Stages;
@@ -647,9 +647,9 @@ paged_join_kernel(const __grid_constant__ AttnParams p) {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-// Of a kernel: tokens that a warp takes at a time, most warps of a CTA, and CTAs of an SM.
+// Of a kernel: tokens that a warp takes at a time, and most warps of a CTA.
 struct Tiling {
-    int32_t tile, warps, ctas;
+    int32_t tile, warps;
 };
 // How the heads are dealt to warps.
 struct Layout {
@@ -675,7 +675,7 @@ Layout layout_of(int32_t batch, int32_t hkv, int32_t hq, int32_t dim, TilingOf t
     y.units = (all + y.chunks - 1) / y.chunks;
     for (y.subs = 1; 2 * y.subs * y.units <= tiling.warps; y.subs *= 2) {}
     for (y.step_log2 = 0; (1 << y.step_log2) < tiling.tile * y.subs; ++y.step_log2) {}
-    y.ctas = tiling.ctas * sms;            // as many as the rings leave shared memory for
+    y.ctas = sms;                          // the rings leave no shared memory for more
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t slots = (size_t)y.ctas * 2 * y.units * y.rows;
     y.part_o = 0;
@@ -726,8 +726,7 @@ cudaError_t launch_attn(const AttnParams& p, const Layout& y, bool may_cut, cuda
     if (e == cudaSuccess && may_cut) {
         // Four CTAs of a cut at most, so that all fit the chip at once: those of a second round would begin only when the first
         // has waited for the main kernel.  (64 rows of 4096 tokens and one of 32768, 64 query heads on 8: 179.9 us in 16 bits
-        // and 100.3 in 8, with eight CTAs a cut of three an SM 182.4 and 101.7.  Where the main kernel has two CTAs an SM, two of
-        // a cut instead of four are no better: 62.8 and 63.0 us for 64 rows of 1024 to 4096, but 18.4 and 17.6 for 200 short ones.)
+        // and 100.3 in 8, with eight CTAs a cut of three an SM 182.4 and 101.7.)
         const dim3 grid((unsigned)std::min(4, (y.units * y.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)(y.ctas - 1));
         e = ps::launch_dependent(paged_join_kernel<typename W1::Type, W1::kDim>, grid, dim3(kJoinThreads), (size_t)y.ctas * 2 * sizeof(float), s, p);
     }

@@ -7,11 +7,10 @@
 //
 // Bound: HBM, and next to it the instructions that a code costs: a token and KV head are half the bytes of a 16-bit cache's and
 // as many products and weights.  Measured: 337 MB of cache (64 rows of 1024 to 4096 tokens, 32 query heads on 8 KV heads of 128)
-// 60.5 us in int8 and 58.7 in 8-bit floats (16 bits: 101), about 7 us of which pass before the first tile is there, where rows
-// end and in the join; 1.07 GB (rows of 8192) 168 and 167 us, or 6.4 TB/s, which is what a copy reaches; one row of 500
-// tokens 8.9.  At the board's power limit, after some tenths of a second, the SMs run at 1.5 to 1.7 GHz and the batch takes 67
-// us.  Heads of 64 take 60.5 us for as many bytes; 16 query heads on a KV head of 128 78 and 69 us, of 64 94 and 80.  More
-// than 16 copy the tiles once for every 16, as in 16 bits.
+// 62.7 us in int8 and 60.0 in 8-bit floats (16 bits: 101), about 7 us of which pass before the first tile is there, where rows
+// end and in the join; 1.07 GB (rows of 8192) 175 and 168 us, of which a copy would take 167; one row of 500 tokens 9.1.  Heads
+// of 64 take 63.1 us for as many bytes in int8; 16 query heads on a KV head of 128 85 and 75 us, of 64 98 and 88.  More than 16
+// copy the tiles once for every 16, as in 16 bits.
 //
 // Products: S^T = K Q^T and O^T = V^T P^T as in ps_paged_attn.cu, tokens and then dims as the 16 rows of a product.  A tile of
 // 16 or 32 tokens comes to shared memory as it lies in the pool (cp.async, 16 bytes a lane).  ldmatrix sees pairs of codes as its
@@ -19,11 +18,12 @@
 // two tokens' values.  Which dims and tokens a product's rows and columns stand for is free, so what comes together stays
 // together: of values row g is dim 2g and row g + 8 dim 2g + 1, and queries are laid out as keys come.
 //
-// Values, and keys in 8-bit floats, are widened to fp16 between ldmatrix and the product; every code is exact there.  Queries
-// in bf16 are multiplied by a power of two that puts their head's largest magnitude next to 2^13, and the scores by its inverse.
-// Keys in int8 enter mma.m16n8k32 as they are: a query is a whole number next to 2^20 at its head's largest magnitude, in three
-// digits of 8 bits, whose products are exact whole numbers.  Three such products cost less than widening, an instruction and a
-// quarter a code (the case above 72.3 us with widened keys when it took 66.9 with digits).
+// Codes are widened to fp16 between ldmatrix and the product; every code is exact there.  Queries in fp16 are multiplied as they
+// are.  Those in bf16 are multiplied by a power of two that puts their head's largest magnitude next to 2^13, and the scores by
+// its inverse: what is above 2^-27 of the largest stays exact, and what is below is off by 2^-38 of it at most.
+// (Keys in int8 could enter mma.m16n8k32 as they are, with a query as a whole number in three digits of 8 bits: the case above in
+// 62.0 us, rows of 8192 in 173.  But then a query has 22 bits from its head's largest value on, and with one dim 2^12 times the
+// others, which meets codes near zero, a score lost 3e-4.  A fourth digit spills registers: 70.9 us.)
 //
 // Scales: a_t multiplies a score in 32 bits.  b_t goes into the weight, p_t (b_t / r) with r a power of two next to the
 // largest b that the warp has met, so that weights stay within fp16; sums are multiplied by r where a segment ends.  A weight
@@ -37,7 +37,7 @@ namespace {
 
 // Four codes of a register as two pairs of fp16 numbers.
 struct Int8 {
-    static constexpr bool kDigits = true;                // keys are multiplied as they are
+    static constexpr bool kAlternate = true;             // keys come as codes 0 and 2, 1 and 3
     // a byte b with its top bit turned is k + 128; as the low bits of 0x6400 = 1024 that is 1152 + k, exactly
     static __device__ __forceinline__ uint32_t widen(uint32_t x) {
         uint32_t r;
@@ -48,9 +48,10 @@ struct Int8 {
         lo = widen(x);
         hi = widen(x >> 8);
     }
+    static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) { values(x, lo, hi); }
 };
 struct E4m3 {
-    static constexpr bool kDigits = false;
+    static constexpr bool kAlternate = false;
     static __device__ __forceinline__ void keys(uint32_t x, uint32_t& lo, uint32_t& hi) {        // codes 0 and 1, 2 and 3
         asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(lo), "=r"(hi) : "r"(x));
     }
@@ -58,16 +59,6 @@ struct E4m3 {
 };
 
 // d = a b (first), or d + a b
-__device__ __forceinline__ void mma_s8(bool first, int32_t (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
-    if (first)
-        asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                     : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "r"(0));
-    else
-        asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_f16(bool first, float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
     if (first)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
@@ -78,7 +69,6 @@ __device__ __forceinline__ void mma_f16(bool first, float (&d)[4], const uint4& 
 }
 
 // Tiles of 16 U tokens, and as many bytes on their way for either head size.
-// Warps: of an SM.
 template <int D, int NT, int U, int Warps>
 struct Ring {
     static constexpr int kTokens = 16 * U;                   // of a tile
@@ -96,25 +86,21 @@ struct QuantState : State<D, NT> {
     float inv_ref;                             // 1 / r
 };
 
-// Warps of an SM: 16 of 128 registers a thread for units of up to 8 query heads, 8 for up to 16, which need twice as many.  A warp's
-// instructions wait for one another more than for memory, and four a scheduler fill the gaps (64 rows of 8192 tokens, 32 query
-// heads on 8 of 128: 185 us in int8 with 16 warps and 192 with 8, 177 and 187 in 8-bit floats; of 64 dims and 2048 to 8192
-// tokens 66 and 82.5).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us with 8 warps, 93
-// with 16).
+// Warps of a CTA, of which an SM has one: 16 of 128 registers a thread for units of up to 8 query heads, 8 for up to 16, which need
+// twice as many.  A warp's instructions wait for one another more than for memory, and four a scheduler fill the gaps (64 rows
+// of 1024 to 4096 tokens, 32 query heads on 8 of 128: 62.7 us in int8 with 16 warps and 72.4 with 8, 60.0 and 70.1 in 8-bit
+// floats; of 64 dims and 2048 to 8192 tokens 63.1 and 73.9 in int8).  Short calls pay for it (one row of 300 tokens: 9.1 and 8.0,
+// 200 rows of 10 to 100 19.4 and 17.2).  What 16 warps' registers do not hold costs more than it gives for 16 heads of 64 (88 us
+// with 8 warps, 93 with 16).
 // As two CTAs of 8 warps they do not wait for one another where a row ends, but a row has twice as many parts and what lies
-// next to one another is not read at the same time.  Int8 of 128, whose instructions weigh most, gains (1024 to 4096
-// tokens: 63.0 instead of 64.8 us, 200 rows of 10 to 100: 17.7 instead of 19.5); 8-bit floats lose (65 instead of 59.1), heads of
-// 64 too (65 instead of 62.7).
-template <typename C>
-constexpr int ctas_of(int dim, int nt) { return C::kDigits && nt == 1 && dim == 128 ? 2 : 1; }
-template <typename C>
-constexpr int warps_of(int dim, int nt) { return nt == 1 ? 16 / ctas_of<C>(dim, nt) : 8; }
+// next to one another is not read at the same time (the same in int8: 66.6 us, and 17.6 for the short rows).
+constexpr int warps_of(int nt) { return nt == 1 ? 16 : 8; }
 constexpr int groups_of(int dim, int nt) { return nt == 1 && dim == 128 ? 1 : 2; }     // of 16 tokens, in a tile
 
 template <typename T, typename C, int D, int NT>
 struct Worker {
-    static constexpr int U = groups_of(D, NT), kWarps = warps_of<C>(D, NT), kCtas = ctas_of<C>(D, NT);
-    using Stages = Ring<D, NT, U, kWarps * kCtas>;
+    static constexpr int U = groups_of(D, NT), kWarps = warps_of(NT);
+    using Stages = Ring<D, NT, U, kWarps>;
     using R = Stages;
     using Type = T;
     using Softmax = QuantState<D, NT>;
@@ -131,9 +117,8 @@ struct Worker {
     const uint32_t scale_put;                  // the place of its scale in a stage
     uint32_t put;                              // this lane's place in a stage: row lane / kPieces and, in place, piece lane % kPieces
     uint32_t get;                              // what this lane reads of a stage's half: piece 0 or 1 of its row; piece 2 j + .. is at get ^ 32 j
-    // query head 8 t + g, dims 32 j + 4 c + .. of four and dims 32 j + 16 + 4 c + .. of four: two fp16 numbers a register, or
-    // a digit of all four, digit by digit
-    uint32_t q[NT][D / 32][C::kDigits ? 6 : 4];
+    // query head 8 t + g, dims 32 j + 4 c + .. of four and dims 32 j + 16 + 4 c + .. of four, in the order of the keys' codes
+    uint32_t q[NT][D / 32][4];
     float factor[NT][2];                       // of the scores of heads 8 t + 2 c and 8 t + 2 c + 1, with log2(e) scale in it
     const unsigned char *k_src, *v_src;        // pools at this lane's head and piece
     const float* scale_src;                    // scales of the head: keys', and with one group of tokens the upper lanes' values'
@@ -157,7 +142,7 @@ struct Worker {
     static __device__ __forceinline__ int swap(int token) { return D == 128 ? token & 7 : token >> 1 & 3; }
 
     __device__ __forceinline__ void load_query(int b, int h0, int n) {
-        constexpr bool kScaled = C::kDigits || std::is_same_v<T, __nv_bfloat16>;
+        constexpr bool kScaled = std::is_same_v<T, __nv_bfloat16>;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const T* src = (const T*)p.q + b * p.q_stride + (int64_t)(h0 + 8 * t + g) * D + 4 * c;
@@ -173,37 +158,19 @@ struct Worker {
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 // 2^(top - e) for a magnitude of 2^e, and its inverse: both are normal numbers
-                constexpr int kTop = C::kDigits ? 20 : 13;
+                constexpr int kTop = 13;
                 const uint32_t bits = __float_as_uint(Num<T>::unpack(most).x);
                 const int e = min(max((int)(bits >> 23), kTop + 1), 254);
                 up = __uint_as_float((uint32_t)(254 + kTop - e) << 23);
                 down = __uint_as_float((uint32_t)(e - kTop) << 23);
-                if (C::kDigits && bits >= 0x7f800000u) down = CUDART_NAN_F;      // whole numbers know neither infinity nor NaN
             }
             factor[t][0] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c);
             factor[t][1] = p.scale_log2e * __shfl_sync(0xffffffffu, down, 8 * c + 4);
-            if constexpr (C::kDigits) {
-                // x up as a whole number n, |n| <= 2^21: its digits d, n = d0 + 2^8 d1 + 2^16 d2, d0 and d1 from -128 to 127, are the
-                // bytes of n + 0x208080 less 128, 128 and 32
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
-                    const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
-                    auto whole = [&](float x) { return __float_as_uint(fmaf(x, up, 8388608.f + 0x208080)); };
-                    const uint32_t n0 = whole(a.x), n1 = whole(a.y), n2 = whole(e.x), n3 = whole(e.y);
-                    const uint32_t lo = __byte_perm(n0, n1, 0x5140), lo2 = __byte_perm(n2, n3, 0x5140);      // bytes 0 and 1 of two
-                    uint32_t* to = q[t][j / 2] + j % 2;
-                    to[0] = __byte_perm(lo, lo2, 0x5410) ^ 0x80808080u;
-                    to[2] = __byte_perm(lo, lo2, 0x7632) ^ 0x80808080u;
-                    // a byte of at most 0x41: + 0x60, and the top bit turned is - 0x80
-                    to[4] = (__byte_perm(__byte_perm(n0, n1, 0x0062), __byte_perm(n2, n3, 0x0062), 0x5410) + 0x60606060u) ^ 0x80808080u;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) {
-                    const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
-                    q[t][j / 2][2 * (j % 2)] = N::pack(a.x * up, a.y * up);
-                    q[t][j / 2][2 * (j % 2) + 1] = N::pack(e.x * up, e.y * up);
-                }
+            for (int j = 0; j < D / 16; ++j) {
+                const float2 a = Num<T>::unpack(v[j].x), e = Num<T>::unpack(v[j].y);
+                q[t][j / 2][2 * (j % 2)] = N::pack(a.x * up, (C::kAlternate ? e.x : a.y) * up);
+                q[t][j / 2][2 * (j % 2) + 1] = N::pack((C::kAlternate ? a.y : e.x) * up, e.y * up);
             }
         }
     }
@@ -318,41 +285,21 @@ struct Worker {
     __device__ __forceinline__ void attend(int stage, const Keys& k, uint32_t on, Softmax& st) {
         const uint32_t src = ring + stage * R::kStageBytes;
         float s[U][NT][4];
-        if constexpr (C::kDigits) {
-            // Products of each digit, in whole numbers of at most 2^21
-            int32_t n[3][U][NT][4];
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
+        for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                const uint4 x = k[u][j];       // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
+                uint4 a, b;
+                C::keys(x.x, a.x, a.z);
+                C::keys(x.y, a.y, a.w);
+                C::keys(x.z, b.x, b.z);
+                C::keys(x.w, b.y, b.w);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) mma_f16(j == 0, s[u][t], a, q[t][j][0], q[t][j][1]);
 #pragma unroll
-                        for (int d = 0; d < 3; ++d) mma_s8(j == 0, n[d][u][t], k[u][j], q[t][j][2 * d], q[t][j][2 * d + 1]);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[u][t][i] = fmaf((float)n[2][u][t][i], 65536.f, (float)(n[1][u][t][i] * 256 + n[0][u][t][i]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const uint4 x = k[u][j];   // tokens 0 to 7 and 8 to 15 of 16 dims, then of the next 16
-                    uint4 a, b;
-                    C::keys(x.x, a.x, a.z);
-                    C::keys(x.y, a.y, a.w);
-                    C::keys(x.z, b.x, b.z);
-                    C::keys(x.w, b.y, b.w);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) mma_f16(j == 0, s[u][t], a, q[t][j][0], q[t][j][1]);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][j][2], q[t][j][3]);
-                }
-        }
+                for (int t = 0; t < NT; ++t) N::mma(s[u][t], b, q[t][j][2], q[t][j][3]);
+            }
         uint4 v[U][D / 32];                    // asked for before the softmax
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -477,8 +424,7 @@ struct Worker {
 
 // ---------------------------------------------------------------------------------------------------- host
 
-template <typename C>
-Tiling tiling_of(int32_t dim, int32_t nt) { return {16 * groups_of(dim, nt), warps_of<C>(dim, nt), ctas_of<C>(dim, nt)}; }
+Tiling tiling_of(int32_t dim, int32_t nt) { return {16 * groups_of(dim, nt), warps_of(nt)}; }
 
 template <typename T, typename C, int D>
 cudaError_t launch(const AttnParams& p, const Layout& y, bool may_cut, cudaStream_t s) {
@@ -500,7 +446,7 @@ cudaError_t sms_here(int* sms) {
 }  // namespace
 
 extern "C" int32_t ps_quant_attn_workspace(int32_t num_kv_heads, int32_t num_q_heads, int32_t head_dim, int64_t* bytes) {
-    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of<Int8>, sms_here, bytes);     // 8-bit floats never have more CTAs
+    return workspace_of(num_kv_heads, num_q_heads, head_dim, tiling_of, sms_here, bytes);
 }
 
 extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap) {
@@ -524,8 +470,8 @@ extern "C" int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, c
         if (!on_bytes(c.kpool, c.k_block_stride, 16) || !on_bytes(c.vpool, c.v_block_stride, 16)) return kUneven;
         return nullptr;
     };
-    const int32_t rc = plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks},
-                                 c.codes == PS_CODE_INT8 ? tiling_of<Int8> : tiling_of<E4m3>, sms_here, pools, refuse, &p, &y, &may_cut);
+    const int32_t rc =
+        plan_call(a, {c.num_kv_heads, c.head_dim, c.block_size, c.num_gpu_blocks}, tiling_of, sms_here, pools, refuse, &p, &y, &may_cut);
     if (rc != PS_OK || a.batch == 0) return rc;
     p.kpool = c.kpool, p.vpool = c.vpool, p.k_scale = c.k_scale, p.v_scale = c.v_scale;
     p.k_step = (uint32_t)(c.k_block_stride >> 4), p.v_step = (uint32_t)(c.v_block_stride >> 4);

@@ -45,3 +45,22 @@ def test_weights_of_few_tokens(dtype, codes, hq, hkv, D):
     cache, q, tables = attn_case(rng, ctx, hq, hkv, D, 4, DTYPES[dtype], CODES[codes], spread=2.0)
     q = q * 0.125                          # scores next to one another
     check_rounded_once(*run_attn(cache, q, tables, ctx), cache, q, tables, ctx)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+@pytest.mark.parametrize("hq,hkv,D,up", [(8, 2, 128, 12), (16, 1, 64, 12), (3, 3, 64, 14), (32, 2, 128, 9)])
+def test_a_querys_small_values_next_to_a_large_one(dtype, codes, hq, hkv, D, up):
+    """One dim of every query is 2^up and more times the others and meets codes of zero: the others decide, as in 32 bits."""
+    rng = np.random.default_rng(2)
+    ctx = [1, 300, 40, 900]
+    cache, q, tables = attn_case(rng, ctx, hq, hkv, D, 16, DTYPES[dtype], CODES[codes])
+    q[..., 5] = 2.0 ** up
+    q[..., 6] *= 2.0 ** -8
+    cache[0].view(torch.uint8)[..., 5] = 0
+    check_rounded_once(*run_attn(cache, q, tables, ctx), cache, q, tables, ctx)
+    if dtype == "bf16":                    # and further apart than fp16 reaches
+        q[..., 5] *= 2.0 ** 8
+        q *= 2.0 ** 60
+        cache[2] *= 2.0 ** -60
+        check_rounded_once(*run_attn(cache, q, tables, ctx), cache, q, tables, ctx)
