@@ -545,7 +545,8 @@ typedef struct ps_quant_append_args {
  * Tokens that go to one block stand next to one another in the call, in any order, as ps_build_slots numbers them (the tokens
  * of a row are neighbours); a block that the call comes back to after tokens of others, or after padding, and one that two
  * tokens give the same slot, has undefined contents afterwards.  Pools, scales and inputs must not overlap.
- * head_dim up to 512, up to 1024 KV heads, rows less than 2^31 elements apart, num_gpu_blocks * block_size^2 below 1.8e19.
+ * head_dim up to 512, up to 1024 KV heads, rows less than 2^31 elements apart, block_size below 2^31 - 4096, num_gpu_blocks *
+ * block_size^2 below 1.8e19.
  * Rows of k and v on 32-byte boundaries with blocks on 16-byte boundaries and head_dim a multiple of 16 are read 32 bytes at a
  * time; 16 where halves of these numbers fit, else element by element.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */

@@ -422,6 +422,7 @@ const char* plan(const ps_quant_cache& c, const Given (&given)[2], const int64_t
                  bool rows_written, QuantParams* params) {
     if (tokens < 0 || c.block_size <= 0 || c.num_gpu_blocks <= 0) return "negative count or non-positive size";
     if (tokens > INT32_MAX - 1024) return "too many tokens";   // so that what a warp looks ahead cannot wrap
+    if (c.block_size > INT32_MAX - 4096) return "block_size must be below 2^31 - 4096";    // nor the places that a lane takes at once
     if (c.num_kv_heads <= 0 || c.num_kv_heads > kMaxHeads || c.head_dim <= 0 || c.head_dim > kMaxDim)
         return "num_kv_heads must be from 1 to 1024, head_dim from 1 to 512";
     if (dtype != PS_DTYPE_BF16 && dtype != PS_DTYPE_FP16) return "dtype must be PS_DTYPE_BF16 or PS_DTYPE_FP16";
