@@ -386,8 +386,8 @@ def ps_quant_attn(kpool, vpool, k_scale, v_scale, q, out, block_tables, ctx_lens
                   scale: Optional[float] = None, status_word=None, workspace=None):
     """Decode attention over a cache of 8 bits, from lengths and block tables on the device: (status, error text).
 
-    The other arguments are those of ps_paged_attn; workspace: of ps_quant_attn_workspace bytes.  See ps_quant_attn in the
-    header."""
+    The other arguments are those of ps_paged_attn; workspace: of ps_quant_attn_workspace bytes.  out and lse that lie in the
+    cache are refused.  See ps_quant_attn in the header."""
     return (_tensor_args or _load_tensor_args()).quant_attn(kpool, vpool, k_scale, v_scale, q, out, block_tables, ctx_lens, lse,
                                                             window, scale, status_word, workspace)
 

@@ -20,8 +20,8 @@ LIB_PATH = os.path.join(LIB_DIR, "libps_kvswap.so")
 SOURCES = ["ps_runtime.cu", "ps_swap.cu", "ps_step.cu", "ps_policy.cu", "ps_measure.cu", "ps_copy_kernels.cu",
            "ps_attn_kernels.cu", "ps_static_scratch.cu", "ps_slots.cu", "ps_rope.cu", "ps_paged_attn.cu",
            "ps_quant.cu", "ps_quant_attn.cu"]
-HEADERS = [os.path.join(CSRC, "ps_internal.h"), os.path.join(CSRC, "ps_ctx.h"), os.path.join(CSRC, "ps_paged_attn.cuh"),
-           os.path.join(ROOT, "include", "ps_kvswap.h")]
+HEADERS = [os.path.join(CSRC, "ps_internal.h"), os.path.join(CSRC, "ps_overlap.h"), os.path.join(CSRC, "ps_ctx.h"),
+           os.path.join(CSRC, "ps_paged_attn.cuh"), os.path.join(ROOT, "include", "ps_kvswap.h")]
 
 
 def _nvcc() -> str:
@@ -55,7 +55,7 @@ def build_tensor_args(force: bool = False) -> str:
     if torch.version.cuda is None:
         return ""
     path = tensor_args_path()
-    deps = [TENSOR_ARGS_SOURCE, os.path.join(ROOT, "include", "ps_kvswap.h")]
+    deps = [TENSOR_ARGS_SOURCE, os.path.join(CSRC, "ps_overlap.h"), os.path.join(ROOT, "include", "ps_kvswap.h")]
     if not force and os.path.exists(path) and all(os.path.getmtime(d) <= os.path.getmtime(path) for d in deps):
         return path
     base = os.path.dirname(torch.__file__)

@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "ps_kvswap.h"
+#include "ps_overlap.h"
 
 namespace {
 
@@ -268,9 +269,10 @@ PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // What ps_paged_attn and ps_quant_attn take alike: q, out, block_tables, ctx_lens, lse, window, scale, status_word, workspace.
-template <typename Args, typename Fn, typename Workspace>
-PyObject* attend(Args& p, PyObject* const* a, const at::Tensor& q, const at::Tensor& out, const at::Tensor& tables, const at::Device& dev, Fn fn,
-                 Workspace workspace_of, int32_t hkv, int32_t dim, const char* name) {
+// `check`: of the call's own, once they are in p.
+template <typename Args, typename Check, typename Fn, typename Workspace>
+PyObject* attend(Args& p, PyObject* const* a, const at::Tensor& q, const at::Tensor& out, const at::Tensor& tables, const at::Device& dev, Check check,
+                 Fn fn, Workspace workspace_of, int32_t hkv, int32_t dim, const char* name) {
     const ScalarType dt = q.scalar_type();
     p.q_stride = outer_stride("q", q, q.sizes(), dt, dev);
     p.out_stride = outer_stride("out", out, q.sizes(), dt, dev);
@@ -289,6 +291,7 @@ PyObject* attend(Args& p, PyObject* const* a, const at::Tensor& q, const at::Ten
         p.scale = (float)s;
     }
     p.status_word = vec<int32_t>("status_word", a[7], ScalarType::Int, 1, dev);
+    check();
     at::Tensor scratch;   // kept until the launches are enqueued; then the allocator's order on the stream protects it
     if (a[8] == Py_None) {
         int64_t need = 0;
@@ -335,7 +338,7 @@ PyObject* py_paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.v_block_stride = outer_stride("vpool", vpool, shape, dt, dev);
         p.kpool = kpool.const_data_ptr();
         p.vpool = vpool.const_data_ptr();
-        return attend(p, a + 2, q, out, tables, dev, g_paged_attn, g_workspace, p.num_kv_heads, p.head_dim, "ps_paged_attn");
+        return attend(p, a + 2, q, out, tables, dev, [] {}, g_paged_attn, g_workspace, p.num_kv_heads, p.head_dim, "ps_paged_attn");
     });
 }
 
@@ -435,7 +438,19 @@ PyObject* py_quant_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.cache = quant_cache(a, true, true, dev);
         if (q.size(2) != p.cache.head_dim) throw BadArg{"q: need the pools' dim, " + describe(q)};
         p.table_stride = int_size("block_tables", tables.size(1));
-        return attend(p, a + 4, q, out, tables, dev, g_quant_attn, g_quant_workspace, p.cache.num_kv_heads, p.cache.head_dim, "ps_quant_attn");
+        auto apart = [&] {                   // results lie nowhere in the cache
+            const ps_quant_cache& c = p.cache;
+            const int64_t block = (int64_t)c.block_size * c.num_kv_heads * c.head_dim, width = (int64_t)p.num_q_heads * c.head_dim;
+            for (const ps::RowSet& part : {ps::RowSet{c.kpool, c.k_block_stride, block, 1}, ps::RowSet{c.vpool, c.v_block_stride, block, 1},
+                                           ps::RowSet{c.k_scale, c.k_scale_stride, c.num_kv_heads, 4},
+                                           ps::RowSet{c.v_scale, c.v_scale_stride, c.num_kv_heads, 4}}) {
+                if (p.batch == 0 || c.num_gpu_blocks == 0) return;
+                if (ps::rows_meet(ps::RowSet{p.out, p.out_stride, width}, p.batch, part, c.num_gpu_blocks)) throw BadArg{"out overlaps the cache"};
+                if (p.lse && ps::rows_meet(ps::RowSet{p.lse, 0, (int64_t)p.batch * p.num_q_heads, 4}, 1, part, c.num_gpu_blocks))
+                    throw BadArg{"lse overlaps the cache"};
+            }
+        };
+        return attend(p, a + 4, q, out, tables, dev, apart, g_quant_attn, g_quant_workspace, p.cache.num_kv_heads, p.cache.head_dim, "ps_quant_attn");
     });
 }
 
