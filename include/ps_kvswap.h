@@ -590,7 +590,8 @@ typedef struct ps_quant_attn_args {
  * are a query's values, but that in bf16 what is below 2^-27 of its head's largest is to within 2^-38 of that; scores, softmax
  * and sums are in 32 bits.  For the product with V a softmax weight times its token's value scale is the sum of two fp16
  * numbers: off by 2^-22 of itself, or by 2^-33 of the largest weight times the largest value scale that the row has met,
- * whichever is more.  A query head with a NaN gives NaN, one with an infinite value NaN or infinite results.
+ * whichever is more.  A query head with a NaN gives NaN, one with an infinite value NaN too, or zeros (lse = -inf) where none of
+ * its scores is above -inf.  out and lse must not lie in the cache (binding.py refuses that).
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
 int32_t ps_quant_attn(const ps_quant_attn_args* args, void* stream, char* err_buf, int32_t err_cap);
 

@@ -64,3 +64,36 @@ def test_a_querys_small_values_next_to_a_large_one(dtype, codes, hq, hkv, D, up)
         q *= 2.0 ** 60
         cache[2] *= 2.0 ** -60
         check_rounded_once(*run_attn(cache, q, tables, ctx), cache, q, tables, ctx)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+def test_infinite_queries(codes, dtype):
+    """Scores that are all minus infinity give zeros, as a row without tokens does; any other infinite query gives NaN."""
+    rng = np.random.default_rng(3)
+    ctx = [70, 1, 2000]
+    cache, q, tables = attn_case(rng, ctx, 8, 2, 64, 16, DTYPES[dtype], CODES[codes])
+    codes8 = cache[0].view(torch.uint8)
+    codes8[..., 5] = 0x21                  # positive in every token
+    bad = q.clone()
+    bad[:, 0, 5], bad[:, 3, 5], bad[:, 6, 5] = -float("inf"), float("inf"), -float("inf")
+    bad[:, 6, 9] = float("inf")            # met by codes of either sign
+    codes8[..., 9] |= 1
+    out, lse = run_attn(cache, bad, tables, ctx)
+    K = cache[0].double() * cache[2].double()[:, None, :, None]      # (the odd codes of 8-bit floats have NaN among them)
+    same, same_lse = run_attn(cache, q, tables, ctx)
+    seen = set()
+    for b, n in enumerate(ctx):
+        k = K[torch.tensor(tables[b], device="cuda")].flatten(0, 1)[:n]
+        for h in range(8):
+            scores = k[:, h // 4] @ bad[b, h].double()
+            if torch.isneginf(scores).all():
+                seen.add("zeros")
+                assert not out[b, h].any() and torch.isneginf(lse[b, h])
+            elif not scores.isfinite().all():
+                seen.add("NaN")
+                assert out[b, h].isnan().all() and lse[b, h].isnan()
+            else:
+                seen.add("numbers")
+                assert h not in (0, 3, 6) and torch.equal(out[b, h], same[b, h]) and torch.equal(lse[b, h], same_lse[b, h])
+    assert seen == {"zeros", "NaN", "numbers"}
