@@ -527,7 +527,8 @@ typedef struct ps_quant_append_args {
     const void* k;               /* device [tokens][num_kv_heads][head_dim], rows k_stride apart; NULL if the cache has no keys */
     const void* v;               /* as k */
     const int64_t* slots;        /* device [tokens]: block * block_size + place; negative = padding */
-    int32_t* status_word;        /* 1 = a slot outside the pool (that token is not appended) */
+    int32_t* status_word;        /* 1 = a slot outside the pool: that token is not appended, and a block between whose tokens it
+                                    stands is undefined */
     int64_t k_stride, v_stride;
     int32_t tokens, dtype;       /* ps_dtype of k and v */
 } ps_quant_append_args;
@@ -543,8 +544,9 @@ typedef struct ps_quant_append_args {
  * block that is begun, and all other blocks, keep their bytes.  With an infinite or NaN input its block and head get a NaN
  * scale: all its values then read as NaN until it is begun anew.
  * Tokens that go to one block stand next to one another in the call, in any order, as ps_build_slots numbers them (the tokens
- * of a row are neighbours); a block that the call comes back to after tokens of others, or after padding, and one that two
- * tokens give the same slot, has undefined contents afterwards.  Pools, scales and inputs must not overlap.
+ * of a row are neighbours).  A block that the call comes back to after tokens of others, after padding or after a slot outside
+ * the pool, and one that two tokens give the same slot, has undefined contents and scales afterwards, at all its places and of
+ * what it held before.  Pools, scales and inputs must not overlap.
  * head_dim up to 512, up to 1024 KV heads, rows less than 2^31 elements apart, block_size below 2^31 - 4096, num_gpu_blocks *
  * block_size^2 below 1.8e19.
  * Rows of k and v on 32-byte boundaries with blocks on 16-byte boundaries and head_dim a multiple of 16 are read 32 bytes at a
