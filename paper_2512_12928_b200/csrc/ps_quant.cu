@@ -8,7 +8,8 @@
 // block's new values before the first code can be rounded, so a warp takes one block's tokens of one head ("unit") and holds
 // them in registers between the two: 16 tokens of 128 dims are 4 vectors of 32 bytes a lane.  Larger blocks have several warps.
 // Measured (8 KV heads of 128, bf16): 9350 tokens of prompt chunks appended in 13.7 us, whose bytes would take 8.9; a decode
-// batch's 200 of 4 heads 2.3, one 2.0, where no scale rises (where nearly all do 3 us, 1.2 and 0.7 more).  71000 tokens read back in 68.3 us, or 6.4 TB/s, which is what a copy reaches; 300 in 2.3.
+// batch's 200 of 4 heads 2.3, one 2.0, all where no scale rises (where nearly all do 3, 1.2 and 0.7 us more).  71000 tokens read
+// back in 68.3 us, or 6.4 TB/s, which is what a copy reaches; 300 in 2.3.
 // What the append spends above its bytes are two rounds and a half of CTAs, in each of which slots, then rows, then the maximum
 // over a warp wait for one another, and a unit's own instructions.  (With the values in shared memory instead of registers, by
 // cp.async, and more warps on an SM: 18.6 us where registers took 15.5.)
